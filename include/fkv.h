@@ -336,6 +336,175 @@ int fkv_kmeans_update_noalloc(const fkv_rvq_desc* desc, const uint16_t* x_f16, u
                               const int32_t* stream_book, const uint8_t* symbols, int32_t stage,
                               uint32_t* counts_out, void* stream);
 
+/* ---- paged 8-bit cache ------------------------------------------------------
+ * The live cache between the exact window and the archive: K/V rows of the
+ * tokens that are still attended to, held in 8 bits in pages of a pool.
+ *   - A page holds `page` consecutive tokens of one request, for every KV head:
+ *       keys    k_codes u8 [n_pages][heads][page][d]
+ *       values  v_codes u8 [n_pages][heads][page/16][d][16]  (16-token groups,
+ *               token minor, so that a value channel's tokens are contiguous)
+ *       scales  f32 [n_pages][heads][2]: one for the keys, one for the values
+ *               of that page and head; an element is code * scale
+ *     k_codes and v_codes 16-byte aligned, scales 8-byte aligned.
+ *   - format: FKV_PAGE_INT8, codes -127..127 (largest code q = 127), or
+ *     FKV_PAGE_E4M3, 8-bit floats with 4 exponent and 3 mantissa bits and no
+ *     infinities (q = 448).
+ *   - page: a multiple of 16, 16..256; d: a multiple of 16, 16..256; heads >= 1.
+ *   - A slot is a token's place in the pool, page id * page + offset (int64);
+ *     a request's pages are listed in its row of a block table, in token order.
+ * Rows are FKV_ROW_F16 (binary16) or FKV_ROW_BF16 (bfloat16), with any strides
+ * (in elements, multiples of 8) between tokens and heads and contiguous in d;
+ * their addresses are 16-byte aligned. */
+#define FKV_PAGE_INT8 0
+#define FKV_PAGE_E4M3 1
+#define FKV_ROW_F16 0
+#define FKV_ROW_BF16 1
+
+typedef struct {
+    int64_t n_pages;
+    int32_t page;
+    int32_t heads;
+    int32_t d;
+    int32_t format;
+} fkv_page_desc;
+
+/* How rows lie in memory: row (i, h) of token i, head h starts at element
+ *     (i / group) * stride_group + (i % group) * stride_token + h * stride_head
+ * (group >= 1; a plain [n][heads][d] array has group = n).  Strides are not
+ * negative. */
+typedef struct {
+    int64_t group;
+    int64_t stride_group;
+    int64_t stride_token;
+    int64_t stride_head;
+    int32_t type;
+} fkv_row_desc;
+
+/* Block tables and slot map of one step, from the requests' lengths.  Request r
+ * has kv_len[r] tokens in the cache and brings new_len[r] more (its tokens are
+ * q_start[r] .. q_start[r+1]-1 of the step's rows).  It needs
+ *     need_r = ceil((kv_len + new_len) / page) - ceil(kv_len / page)
+ * further pages.  Requests take pages off the free list in order; with
+ * c_r = need_0 + .. + need_r (refused requests of status 2 and 3 counting none)
+ * request r is served when need_r = 0 or *head + c_r <= n_free, and its j-th
+ * further page is free_pages[*head + c_r - need_r + j].
+ *   kv_len, new_len  device int32 [n_req]
+ *   free_pages       device int32 [n_free] page ids, handed out from *head on
+ *   head             device int32 [1], nullable (0): entries handed out before
+ *                    (a value outside [0, n_free] is taken to the nearer end)
+ *   tables           device int32 [n_req][max_pages], in/out: the entries of the
+ *                    pages taken are written, the others left as they are
+ *   slots            device out int64 [n_tokens]: each row's slot; -1 for the
+ *                    rows of a request that is not served and for rows beyond
+ *                    the last request's
+ *   positions        device out int32 [n_tokens], nullable: each row's position
+ *                    in its request; -1 beyond the last request's
+ *   q_start          device out int32 [n_req + 1], at most n_tokens
+ *   kv_end           device out int32 [n_req]: kv_len + new_len, or kv_len of a
+ *                    request that is not served; neither kv_len nor new_len
+ *   head_out         device out int32 [1]: the largest *head + c_r of the requests
+ *                    served, or *head if none; c_r counts what refused requests
+ *                    asked for, so a value above n_free says that the list was
+ *                    too short for requests before the last one served; not `head`
+ *   next_head        device out int32 [1], nullable: the next step's *head, the
+ *                    list entries handed out by now; not `head`
+ *   status           device out u8 [n_req], nullable: 0 served; 1 the free list
+ *                    is at its end; 2 more than max_pages pages (or 2^31 tokens); 3 a negative
+ *                    length (taken as 0 rows), or rows beyond n_tokens
+ *   n_bad            device u32 counter, += requests not served; nullable
+ * n_req = 0 and n_tokens = 0 are valid. */
+int fkv_page_plan(int32_t page, int64_t n_req, const int32_t* kv_len, const int32_t* new_len,
+                  const int32_t* free_pages, int64_t n_free, const int32_t* head, int32_t* tables,
+                  int64_t max_pages, int64_t n_tokens, int64_t* slots, int32_t* positions,
+                  int32_t* q_start, int32_t* kv_end, int32_t* head_out, int32_t* next_head,
+                  uint8_t* status, uint32_t* n_bad, void* stream);
+
+/* Writes K/V rows into the pages.  Rows i, i+1, .. whose slots follow one
+ * another within a page are one run; a page may be reached by one run of a call
+ * at most (a step's slot map has this form).  For each run, head and K or V:
+ *     a = largest |x| over the run's finite elements
+ *     s = a * (1 / q), or 0 when a < 2^-90
+ *     if the run starts at offset o > 0:  s = max(s, the page's scale), and the
+ *         codes of the page's tokens [0, o) become round(code * (old scale / s))
+ *     code = round(x * (1 / s))   (0 when s = 0), to nearest, ties to even
+ * so the tokens [0, o) of the page stay valid and those after the run are
+ * undefined.  A NaN is stored as 0, an infinity as -q or q.  Rows with a
+ * negative slot are skipped; a slot of no page is skipped too and counted.
+ *   k_rows, v_rows  rows of n_tokens tokens and desc->heads heads, laid out by
+ *                   rows_k and rows_v (types alike)
+ *   slots           device int64 [n_tokens]
+ *   n_bad           device u32 counter, += rows whose slot lies beyond the
+ *                   pool; nullable */
+int fkv_page_store(const fkv_page_desc* desc, const fkv_row_desc* rows_k, const fkv_row_desc* rows_v,
+                   const void* k_rows, const void* v_rows, int64_t n_tokens, const int64_t* slots,
+                   uint8_t* k_codes, uint8_t* v_codes, float* scales, uint32_t* n_bad, void* stream);
+
+/* Reads rows back: code * scale, rounded to the row type (at once or by way of
+ * fp32).  Slots may come in any order and more than once; a slot outside the
+ * pool gives a zero row.  k_rows or v_rows may be null (not read back). */
+int fkv_page_load(const fkv_page_desc* desc, const uint8_t* k_codes, const uint8_t* v_codes,
+                  const float* scales, int64_t n_tokens, const int64_t* slots, const fkv_row_desc* rows_k,
+                  const fkv_row_desc* rows_v, void* k_rows, void* v_rows, void* stream);
+
+/* Attention over the pages.  Request r has kv_len[r] tokens in the cache, the
+ * last n_r = q_start[r+1] - q_start[r] of which are its query tokens (rows
+ * q_start[r] .. of q); the i-th has position pos = kv_len - n_r + i.  Query head
+ * h reads KV head h / (q_heads / heads).  For a visible key j
+ *     x_j = scale * q . k_j
+ *     y_j = softcap * tanh(x_j / softcap)      (x_j when softcap = 0)
+ *     z_j = y_j - slopes[h] * |pos - j|        (y_j without slopes)
+ *     out = sum_j exp(z_j) v_j / sum_j exp(z_j),   lse = log sum_j exp(z_j)
+ * A row that sees no key gives out = 0 and lse = -infinity.  Key j is visible
+ * when j < kv_len and
+ *     causal = 0, or j <= pos, or j < prefix[r]
+ *     window = 0, or j > pos - window, or j < sinks
+ *     j >= first[row]  (the row's document starts there)
+ *   tables          device int32 [n_req][max_pages]; keys of an entry that is
+ *                   no page of the pool are not visible.  kv_len is held to
+ *                   [0, min(max_kv, max_pages * page)]
+ *   n_tokens        rows of q and out (at least q_start[n_req])
+ *   max_new         at least the largest n_r: of a request with more, the rows
+ *                   beyond max_new are left unwritten
+ *   max_kv          at least the largest kv_len; sets the shape of the launch
+ *   q, out          rows [n_tokens][q_heads][d] with the strides given (elements,
+ *                   multiples of 8), 16-byte aligned, of type `type`
+ *   slopes          device f32 [q_heads], nullable
+ *   prefix          device int32 [n_req], nullable
+ *   first           device int32 [n_tokens], nullable
+ *   lse             device out f32 [n_tokens][q_heads], nullable
+ *   workspace       device scratch of fkv_page_attend_workspace() bytes, 16-byte
+ *                   aligned; null when that is 0.  Calls that may run at the
+ *                   same time need one each.
+ * Scores, statistics and sums are fp32; the products run on matrix cores with
+ * the codes and q exact in binary16 (a bfloat16 row is taken times a power of
+ * two) and the weights rounded to binary16.  FKV_ERR_INVALID_ARG also for
+ * q_heads not a multiple of heads; FKV_ERR_SCRATCH_TOO_SMALL for a workspace
+ * that is too small. */
+typedef struct {
+    int64_t n_req;
+    int64_t n_tokens;
+    int64_t max_new;
+    int64_t max_kv;
+    int64_t max_pages;
+    int64_t q_stride_token, q_stride_head;
+    int64_t o_stride_token, o_stride_head;
+    int32_t q_heads;
+    int32_t type;
+    float scale;
+    float softcap;  /* >= 0; 0: none */
+    int32_t causal; /* 0 or 1 */
+    int32_t window; /* >= 0; 0: none */
+    int32_t sinks;  /* >= 0; read with a window only */
+} fkv_attend_desc;
+
+size_t fkv_page_attend_workspace(const fkv_page_desc* desc, const fkv_attend_desc* attend);
+
+int fkv_page_attend(const fkv_page_desc* desc, const fkv_attend_desc* attend, const uint8_t* k_codes,
+                    const uint8_t* v_codes, const float* scales, const void* q, const int32_t* tables,
+                    const int32_t* kv_len, const int32_t* q_start, const float* slopes, const int32_t* prefix,
+                    const int32_t* first, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                    void* stream);
+
 /* ---------------------------------------------------------------------------
  * Measurement aid (not part of the archive path).
  *

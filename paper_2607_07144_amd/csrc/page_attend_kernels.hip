@@ -1,0 +1,879 @@
+// page_attend_kernels.hip -- attention over the paged 8-bit cache, for gfx950.
+//
+// One pass over the keys with the running maximum and sum of a softmax, in base
+// 2: with x the scores times log2 e,
+//     m' = max(m, max x),  l' = l 2^(m-m') + sum 2^(x-m'),
+//     o' = o 2^(m-m') + sum 2^(x-m') v.
+// Both products are formed transposed, S^T = K Q^T and O^T = V^T P^T, on
+// matrix cores: the accumulator of S^T then holds one row's scores per lane
+// (the lane's column), so the statistics are per-lane values, and the weights
+// are already where the second product wants its right operand, with no way
+// through shared memory -- the order in which a product sums over keys is
+// free, so the keys are dealt to the accumulator's rows such that each lane
+// ends up with consecutive ones.
+//
+// int8 codes and 8-bit floats are exact in binary16, and so is q (a bfloat16
+// row is taken times a power of two that brings its largest element near 2^13;
+// elements 2^27 times smaller than that round).  Key scales multiply the fp32
+// scores.  Value scales differ from page to page, so they multiply the fp32
+// weights before those are rounded to binary16: w = p * vs * 2^14 / vr with vr
+// the largest value scale so far, so that w keeps its 11 bits down to p vs / vr
+// = 2^-28; the accumulators carry the factor 2^14 / vr.
+#include "page_common.h"
+
+namespace fkv {
+namespace {
+
+typedef float float4_t __attribute__((ext_vector_type(4)));
+typedef float float16_t __attribute__((ext_vector_type(16)));
+
+constexpr int kThreads = 256;
+constexpr int kWaves = 4;
+constexpr int kTile = 64;          // keys of a tile
+constexpr int kFewRows = 16;       // rows of the kernel for few rows
+constexpr int kTileRows = 128;     // rows of a block of the kernel for many
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+constexpr float kTop = 16384.0f;   // 2^14: the largest weight
+constexpr float kLeast = 0x1p-100f;
+
+struct AttendArgs {
+    const uint8_t* k_codes;
+    const uint8_t* v_codes;
+    const float2* scales;
+    const uint8_t* q;
+    uint8_t* out;
+    float* lse;
+    const int32_t* tables;
+    const int32_t* kv_len;
+    const int32_t* q_start;
+    const float* slopes;
+    const int32_t* prefix;
+    const int32_t* first;
+    float* part;    // [row][split][d] sums of a split's weights times values
+    float2* stat;   // [row][split] its maximum and sum of weights
+    int64_t n_req, n_tokens, max_new, max_kv, max_pages, n_pages;
+    int64_t q_token, q_head, o_token, o_head;
+    int32_t page, heads, group, d, window, sinks;
+    int32_t bf16, causal;
+    int32_t n_splits, split_tiles;
+    uint32_t per_page;     // 16-key groups of a page
+    uint32_t per_page_inv; // and their reciprocal, 2^32 / per_page rounded up (0: one)
+    float scale, softcap;
+};
+
+// A request as a block sees it.
+struct Request {
+    int kv, rows, start, pos0;   // keys; query tokens, the first one's row and position
+};
+
+__device__ __forceinline__ Request request_of(const AttendArgs& a, int64_t r)
+{
+    Request q;
+    const int64_t most = min(a.max_kv, a.max_pages * a.page);
+    q.kv = (int)min((int64_t)max(a.kv_len[r], 0), most);
+    const int64_t b = min(max((int64_t)a.q_start[r], (int64_t)0), a.n_tokens);
+    const int64_t e = min(max((int64_t)a.q_start[r + 1], b), a.n_tokens);
+    q.start = (int)b;
+    q.rows = (int)min(e - b, a.max_new);
+    q.pos0 = q.kv - (int)(e - b);
+    return q;
+}
+
+// What token i of a request sees: keys [lo, hi), of those below wlo only the
+// sinks.
+struct Seen {
+    int lo, hi, wlo;
+};
+
+__device__ __forceinline__ Seen seen_of(const AttendArgs& a, const Request& rq, int64_t r, int i)
+{
+    const int pos = rq.pos0 + i;
+    Seen s;
+    s.lo = a.first ? max(a.first[rq.start + i], 0) : 0;
+    s.hi = rq.kv;
+    if (a.causal) s.hi = min(rq.kv, max(pos + 1, a.prefix ? a.prefix[r] : 0));
+    s.wlo = a.window ? pos - a.window + 1 : 0;
+    return s;
+}
+
+// The tiles that some row of a block sees: s0 .. s0+ns-1 (sinks), then w0 ..,
+// n in all; and what every row sees of all tiles.
+struct Tiles {
+    int s0, ns, w0, n;
+    int lo, hi, wlo;   // a tile in [lo, hi) that lies above wlo or below the sinks needs no mask
+    __device__ __forceinline__ int tile(int e) const { return e < ns ? s0 + e : w0 + e - ns; }
+};
+
+__device__ __forceinline__ Tiles tiles_of(const AttendArgs& a, int lo_min, int lo_max, int hi_min, int hi_max, int wlo_min, int wlo_max)
+{
+    Tiles t;
+    const int end = (hi_max + kTile - 1) / kTile;
+    t.s0 = lo_min / kTile;
+    t.ns = 0;
+    t.w0 = t.s0;
+    if (a.window) {
+        t.w0 = max(lo_min, max(wlo_min, 0)) / kTile;
+        const int s1 = min((int)((min((int64_t)a.sinks, (int64_t)hi_max) + kTile - 1) / kTile), t.w0);
+        t.ns = max(0, s1 - t.s0);
+    }
+    t.n = t.ns + max(0, end - t.w0);
+    t.lo = lo_max;
+    t.hi = hi_min;
+    t.wlo = wlo_max;
+    return t;
+}
+
+__device__ __forceinline__ bool tile_whole(const AttendArgs& a, const Tiles& t, int j0)
+{
+    return j0 >= t.lo && j0 + kTile <= t.hi && (!a.window || j0 >= t.wlo || j0 + kTile <= a.sinks);
+}
+
+__device__ __forceinline__ bool visible(const AttendArgs& a, const Seen& s, int j)
+{
+    return j >= s.lo && j < s.hi && (!a.window || j >= s.wlo || j < a.sinks);
+}
+
+// The page that holds a request's 16-key group, or -1.
+__device__ __forceinline__ int page_of(const AttendArgs& a, const int32_t* table, int kv, int grp)
+{
+    if (grp * 16 >= kv) return -1;
+    const int p = a.per_page_inv ? (int)__umulhi((uint32_t)grp, a.per_page_inv) : grp;
+    const int id = table[p];
+    return (uint32_t)id < (uint64_t)a.n_pages ? id : -1;
+}
+
+// Where a group's codes begin within its page and head, in 16-key groups.
+__device__ __forceinline__ int group_in_page(const AttendArgs& a, int grp)
+{
+    const int p = a.per_page_inv ? (int)__umulhi((uint32_t)grp, a.per_page_inv) : grp;
+    return grp - p * (int)a.per_page;
+}
+
+// 16 codes to binary16, exact.  An int8 code c becomes 1024 + (c + 128) by
+// placing the byte under the exponent of 1024, and 1152 less is c.
+template <bool E4M3>
+__device__ __forceinline__ half2_t codes2(uint32_t w, bool hi)
+{
+    if (E4M3) return hi ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false);
+    const uint32_t u = __builtin_amdgcn_perm(0x64646464u, w ^ 0x80808080u, hi ? 0x04030402u : 0x04010400u);
+    const half2_t bias = {(_Float16)1152.0f, (_Float16)1152.0f};
+    return __builtin_bit_cast(half2_t, u) - bias;
+}
+
+template <bool E4M3>
+__device__ __forceinline__ half8_t codes8(uint32_t a, uint32_t b)
+{
+    const half2_t p = codes2<E4M3>(a, false), q = codes2<E4M3>(a, true);
+    const half2_t r = codes2<E4M3>(b, false), s = codes2<E4M3>(b, true);
+    return half8_t{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
+}
+
+// Keeps the first n bytes of four words.
+__device__ __forceinline__ uint4 first_bytes(uint4 w, int n)
+{
+    auto keep = [&](uint32_t x, int k) { return k >= 4 ? x : k <= 0 ? 0u : x & ((1u << (8 * k)) - 1u); };
+    return make_uint4(keep(w.x, n), keep(w.y, n - 4), keep(w.z, n - 8), keep(w.w, n - 12));
+}
+
+// A bfloat16 row's power of two, from its largest element: largest * 2^e lies
+// in [2^13, 2^14).  0 for a row of zeros and for one with no finite largest.
+__device__ __forceinline__ int row_shift(float largest)
+{
+    const int ex = (int)((__float_as_uint(largest) >> 23) & 0xff);
+    return ex == 0 || ex == 0xff ? 0 : min(max(127 + 13 - ex, -120), 120);
+}
+
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+
+// 8 elements of a q row to binary16.
+__device__ __forceinline__ half8_t q8(uint4 w, bool bf16, float mul)
+{
+    if (!bf16) return __builtin_bit_cast(half8_t, w);
+    half8_t h;
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = (_Float16)(row_to_f32(u[e >> 1], e & 1, true) * mul);
+    return h;
+}
+
+__device__ __forceinline__ float abs_most8(uint4 w)
+{
+    float m = 0.0f;
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(row_to_f32(u[e >> 1], e & 1, true)));
+    return m;
+}
+
+// A score's factors: x = s * mul (no cap), in base 2; capped, s * mul is twice
+// the tanh's argument in base 2, and tanh u = 1 - 2 / (1 + e^2u).
+struct Score {
+    float mul, cap, slope;
+};
+
+__device__ __forceinline__ float capped(float u, float cap)
+{
+    const float e = __builtin_amdgcn_exp2f(u);
+    return cap * (1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + e));
+}
+
+// ------------------------------------------------------------- few rows --
+
+// One KV head of a request and at most 16 rows (query tokens x heads of the
+// group): what bounds it is the reading of the codes, 2 d bytes a key.  A block
+// takes one split of the keys, its four waves every fourth tile of it, each with
+// its own statistics; codes go from memory to registers in the operands' own
+// layout, 16 bytes a lane and load, and the waves' results are joined in LDS.
+// The left operand of S^T takes row t*4+i of key group g as its row 4g+i in
+// product t, so that lane group g ends up with keys 16g .. 16g+15, which are the
+// 16 bytes of a value channel that it loads.  NC: chunks of 64 channels.
+template <bool E4M3, int NC>
+__global__ __launch_bounds__(kThreads) void attend_few_kernel(AttendArgs a)
+{
+    extern __shared__ __align__(16) float lds[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int c16 = lane & 15, g = lane >> 4;
+    const int64_t item = blockIdx.x;
+    const int split = (int)(item % a.n_splits);
+    const int h = (int)(item / a.n_splits % a.heads);
+    const int64_t r = item / a.n_splits / a.heads;
+    const Request rq = request_of(a, r);
+    const int n_rows = rq.rows * a.group;
+    if (n_rows == 0) return;
+    const int d = a.d;
+    const int64_t q_heads = (int64_t)a.heads * a.group;
+
+    // this lane's row, and what the block's rows see
+    const int row = min(c16, n_rows - 1);
+    const int tok = row / a.group;
+    const int head = h * a.group + row % a.group;
+    const Seen mine = seen_of(a, rq, r, tok);
+    int lo_min = 0x7fffffff, lo_max = 0, hi_min = 0x7fffffff, hi_max = 0, wlo_min = 0x7fffffff, wlo_max = 0;
+    for (int i = 0; i < rq.rows; ++i) {
+        const Seen s = seen_of(a, rq, r, i);
+        lo_min = min(lo_min, s.lo), lo_max = max(lo_max, s.lo);
+        hi_min = min(hi_min, s.hi), hi_max = max(hi_max, s.hi);
+        wlo_min = min(wlo_min, s.wlo), wlo_max = max(wlo_max, s.wlo);
+    }
+    const Tiles tl = tiles_of(a, lo_min, lo_max, hi_min, hi_max, wlo_min, wlo_max);
+    const int e0 = split * a.split_tiles;
+    const int e1 = split == a.n_splits - 1 ? tl.n : min(tl.n, e0 + a.split_tiles);
+
+    float m = -__builtin_inff(), l = 0.0f, vref = kLeast;
+    float4_t acc[4 * NC];
+#pragma unroll
+    for (int t = 0; t < 4 * NC; ++t) acc[t] = float4_t{0, 0, 0, 0};
+
+    if (e0 + wave < e1) {
+        // the right operand of S^T: channels 64c + 16g .. + 15 of the row
+        half8_t qf[NC][2];
+        int shift = 0;
+        {
+            const uint8_t* qp = a.q + 2 * ((int64_t)(rq.start + tok) * a.q_token + head * a.q_head);
+            uint4 w[NC][2];
+            float most = 0.0f;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const int e = c * 64 + g * 16;
+                w[c][0] = w[c][1] = make_uint4(0, 0, 0, 0);
+                if (e < d) w[c][0] = *(const uint4*)(qp + 2 * e), w[c][1] = *(const uint4*)(qp + 2 * e + 16);
+                if (a.bf16) most = fmaxf(most, fmaxf(abs_most8(w[c][0]), abs_most8(w[c][1])));
+            }
+            if (a.bf16) {
+                most = fmaxf(most, __shfl_xor(most, 16, 64));
+                most = fmaxf(most, __shfl_xor(most, 32, 64));
+                shift = row_shift(most);
+            }
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                qf[c][0] = q8(w[c][0], a.bf16, pow2(shift));
+                qf[c][1] = q8(w[c][1], a.bf16, pow2(shift));
+            }
+        }
+        const float cap2 = a.softcap * kLog2e;
+        const float mul = pow2(-shift) * (a.softcap > 0.0f ? a.scale * 2.0f * kLog2e / a.softcap : a.scale * kLog2e);
+        const float slope2 = a.slopes ? a.slopes[head] * kLog2e : 0.0f;
+        const int pos = rq.pos0 + tok;
+        const int32_t* table = a.tables + r * a.max_pages;
+        const int64_t per_head = (int64_t)a.page * d;
+        const int gk = c16 >> 2;   // the key group of this lane's left-operand rows
+
+        int j0 = tl.tile(e0 + wave) * kTile;
+        int pk = page_of(a, table, rq.kv, (j0 >> 4) + gk), pv = page_of(a, table, rq.kv, (j0 >> 4) + g);
+        for (int e = e0 + wave; e < e1; e += kWaves) {
+            // codes of the tile
+            uint4 kw[4][NC], vw[4 * NC];
+            const uint8_t* kp = a.k_codes + ((int64_t)pk * a.heads + h) * per_head +
+                                (int64_t)(group_in_page(a, (j0 >> 4) + gk) * 16 + (c16 & 3)) * d + g * 16;
+            const uint8_t* vp = a.v_codes + ((int64_t)pv * a.heads + h) * per_head +
+                                (int64_t)group_in_page(a, (j0 >> 4) + g) * 16 * d + c16 * 16;
+            float2 sc = make_float2(0.0f, 0.0f);
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    kw[t][c] = make_uint4(0, 0, 0, 0);
+                    if (pk >= 0 && c * 64 + g * 16 < d) kw[t][c] = *(const uint4*)(kp + t * 4 * d + c * 64);
+                }
+            if (pv >= 0) sc = a.scales[(int64_t)pv * a.heads + h];
+#pragma unroll
+            for (int t = 0; t < 4 * NC; ++t) {
+                vw[t] = make_uint4(0, 0, 0, 0);
+                if (pv >= 0 && t * 16 < d) vw[t] = *(const uint4*)(vp + t * 256);
+            }
+            const bool mask = !tile_whole(a, tl, j0) || __any(pv < 0);
+            const int j0g = j0 + g * 16;
+            const bool here = pv >= 0;
+            if (e + kWaves < e1) {
+                j0 = tl.tile(e + kWaves) * kTile;
+                pk = page_of(a, table, rq.kv, (j0 >> 4) + gk);
+                pv = page_of(a, table, rq.kv, (j0 >> 4) + g);
+            }
+            // scores of keys j0g .. j0g+15 in turn
+            float4_t s[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                s[t] = float4_t{0, 0, 0, 0};
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(kw[t][c].x, kw[t][c].y), qf[c][0], s[t], 0, 0, 0);
+                    s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(kw[t][c].z, kw[t][c].w), qf[c][1], s[t], 0, 0, 0);
+                }
+            }
+            const float mulk = mul * sc.x;
+            float x[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = s[i >> 2][i & 3] * mulk;
+            if (a.softcap > 0.0f) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] = capped(x[i], cap2);
+            }
+            if (a.slopes) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] -= slope2 * fabsf((float)(j0g + i - pos));
+            }
+            if (mask) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (!here || !visible(a, mine, j0g + i)) x[i] = -__builtin_inff();
+                if (E4M3) {   // codes after the last key may be anything, a NaN among it
+                    const int n = rq.kv - j0g;
+#pragma unroll
+                    for (int t = 0; t < 4 * NC; ++t) vw[t] = first_bytes(vw[t], n);
+                }
+            }
+            float top = x[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+            top = fmaxf(top, __shfl_xor(top, 16, 64));
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            if (__any(top > m || sc.y > vref)) {
+                float vnew = fmaxf(vref, sc.y);
+                vnew = fmaxf(vnew, __shfl_xor(vnew, 16, 64));
+                vnew = fmaxf(vnew, __shfl_xor(vnew, 32, 64));
+                const float mnew = fmaxf(m, top);
+                const float shrink = mnew == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m - mnew);
+                l *= shrink;
+                const float f = shrink * (vref / vnew);
+#pragma unroll
+                for (int t = 0; t < 4 * NC; ++t) acc[t] *= f;
+                m = mnew;
+                vref = vnew;
+            }
+            const float m0 = m == -__builtin_inff() ? 0.0f : m;
+            const float vs = sc.y * (kTop / vref);
+            half8_t p[2];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float w = __builtin_amdgcn_exp2f(x[i] - m0);
+                l += w;
+                p[i >> 3][i & 7] = (_Float16)(w * vs);
+            }
+#pragma unroll
+            for (int t = 0; t < 4 * NC; ++t) {
+                if (t * 16 >= d) continue;
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(vw[t].x, vw[t].y), p[0], acc[t], 0, 0, 0);
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(vw[t].z, vw[t].w), p[1], acc[t], 0, 0, 0);
+            }
+        }
+        l += __shfl_xor(l, 16, 64);
+        l += __shfl_xor(l, 32, 64);
+    }
+
+    // the waves' parts together: [wave][row] maximum and sum, [wave][row][d] sums
+    float* s_m = lds;
+    float* s_l = lds + kWaves * kFewRows;
+    float* s_acc = lds + 2 * kWaves * kFewRows;
+    const int ld = d + 4;
+    if (g == 0) s_m[wave * kFewRows + c16] = m, s_l[wave * kFewRows + c16] = l;
+    const float back = vref * (1.0f / kTop);
+#pragma unroll
+    for (int t = 0; t < 4 * NC; ++t)
+        if (t * 16 < d) *(float4_t*)(s_acc + (wave * kFewRows + c16) * ld + t * 16 + g * 4) = acc[t] * back;
+    __syncthreads();
+    const int quads = d / 4;
+    for (int task = threadIdx.x; task < n_rows * quads; task += kThreads) {
+        const int rw = task / quads, q4 = task % quads;
+        float mm = -__builtin_inff();
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, s_m[w * kFewRows + rw]);
+        const float m0 = mm == -__builtin_inff() ? 0.0f : mm;
+        float ll = 0.0f;
+        float4_t o = {0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float f = __builtin_amdgcn_exp2f(s_m[w * kFewRows + rw] - m0);
+            ll += f * s_l[w * kFewRows + rw];
+            o += f * *(const float4_t*)(s_acc + (w * kFewRows + rw) * ld + 4 * q4);
+        }
+        const int64_t token = rq.start + rw / a.group;
+        const int hq = h * a.group + rw % a.group;
+        if (a.n_splits > 1) {
+            const int64_t at = (token * q_heads + hq) * a.n_splits + split;
+            *(float4_t*)(a.part + at * d + 4 * q4) = o;
+            if (q4 == 0) a.stat[at] = make_float2(mm, ll);
+        } else {
+            const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
+            *(uint2*)(a.out + 2 * (token * a.o_token + hq * a.o_head + 4 * q4)) =
+                make_uint2(f32_to_row2(o[0] * inv, o[1] * inv, a.bf16), f32_to_row2(o[2] * inv, o[3] * inv, a.bf16));
+            if (q4 == 0 && a.lse) a.lse[token * q_heads + hq] = ll == 0.0f ? -__builtin_inff() : kLn2 * (mm + __log2f(ll));
+        }
+    }
+}
+
+// ------------------------------------------------------------ many rows --
+
+// 128 rows of one KV head of a request, 32 a wave: what bounds it is the matrix
+// products.  A tile's codes are widened to binary16 once, into LDS (two buffers:
+// the next tile's codes are on their way from memory meanwhile), and every
+// wave takes its left operands from there.  A value channel's keys lie in LDS
+// in the order 0-3, 8-11, 4-7, 12-15 of each 16, which is the order in which a
+// lane's scores come out of the accumulator.  DP: channels, rounded up.
+template <int DP>
+struct TileLds {
+    static constexpr int kRow = DP + 8;       // of a key: channels
+    static constexpr int vRow = kTile + 8;    // of a channel: keys
+    _Float16 k[2][kTile * kRow];
+    _Float16 v[2][DP * vRow];
+    int lim[kWaves][6];
+};
+
+template <bool E4M3, int DP>
+__global__ __launch_bounds__(kThreads) void attend_tile_kernel(AttendArgs a)
+{
+    typedef TileLds<DP> Lds;
+    extern __shared__ __align__(16) uint8_t raw[];
+    Lds& sh = *(Lds*)raw;
+    constexpr int kChunks = DP / 16;                                          // of a key, 16 codes each
+    constexpr int kLoads = (kTile * kChunks + kThreads - 1) / kThreads;       // a thread's loads of each kind
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int c32 = lane & 31, hf = lane >> 5;
+    const int split = (int)(blockIdx.x % a.n_splits);
+    const int h = (int)(blockIdx.x / a.n_splits);
+    const int64_t r = blockIdx.z;
+    const Request rq = request_of(a, r);
+    const int n_rows = rq.rows * a.group;
+    // the last rows see the most keys: they go first
+    const int n_blocks = (n_rows + kTileRows - 1) / kTileRows;
+    const int block = n_blocks - 1 - (int)blockIdx.y;
+    if (block < 0) return;
+    const int d = a.d;
+    const int64_t q_heads = (int64_t)a.heads * a.group;
+
+    const int row0 = block * kTileRows + wave * 32;
+    const bool used = row0 + c32 < n_rows;
+    const int row = min(row0 + c32, n_rows - 1);
+    const int tok = row / a.group;
+    const int head = h * a.group + row % a.group;
+    const Seen mine = seen_of(a, rq, r, tok);
+    Tiles tl;
+    int wave_lo, wave_hi;   // the keys that some row of the wave sees lie in here
+    {
+        int v[6] = {mine.lo, -mine.lo, mine.hi, -mine.hi, mine.wlo, -mine.wlo};   // minima, and maxima as minima
+#pragma unroll
+        for (int k = 1; k < 32; k <<= 1)
+#pragma unroll
+            for (int i = 0; i < 6; ++i) v[i] = min(v[i], __shfl_xor(v[i], k, 64));
+        if (lane == 0)
+#pragma unroll
+            for (int i = 0; i < 6; ++i) sh.lim[wave][i] = v[i];
+        wave_lo = v[0];
+        wave_hi = row0 < n_rows ? -v[3] : 0;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+            for (int i = 0; i < 6; ++i) v[i] = min(v[i], sh.lim[w][i]);
+        tl = tiles_of(a, v[0], -v[1], v[2], -v[3], v[4], -v[5]);
+    }
+    const int e0 = split * a.split_tiles;
+    const int e1 = split == a.n_splits - 1 ? tl.n : min(tl.n, e0 + a.split_tiles);
+
+    float m = -__builtin_inff(), l = 0.0f, vref = kLeast;
+    float16_t acc[DP / 32];
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[t][i] = 0.0f;
+
+    // the right operand of S^T: channels 16s + 8hf .. + 7 of the row
+    half8_t qf[kChunks];
+    int shift = 0;
+    {
+        const uint8_t* qp = a.q + 2 * ((int64_t)(rq.start + tok) * a.q_token + head * a.q_head);
+        uint4 w[kChunks];
+        float most = 0.0f;
+#pragma unroll
+        for (int s = 0; s < kChunks; ++s) {
+            w[s] = make_uint4(0, 0, 0, 0);
+            if (s * 16 < d) w[s] = *(const uint4*)(qp + 2 * (s * 16 + hf * 8));
+            if (a.bf16) most = fmaxf(most, abs_most8(w[s]));
+        }
+        if (a.bf16) {
+            most = fmaxf(most, __shfl_xor(most, 32, 64));
+            shift = row_shift(most);
+        }
+#pragma unroll
+        for (int s = 0; s < kChunks; ++s) qf[s] = q8(w[s], a.bf16, pow2(shift));
+    }
+    const float cap2 = a.softcap * kLog2e;
+    const float mul = pow2(-shift) * (a.softcap > 0.0f ? a.scale * 2.0f * kLog2e / a.softcap : a.scale * kLog2e);
+    const float slope2 = a.slopes ? a.slopes[head] * kLog2e : 0.0f;
+    const int pos = rq.pos0 + tok;
+    const int32_t* table = a.tables + r * a.max_pages;
+    const int64_t per_head = (int64_t)a.page * d;
+
+    uint4 kw[kLoads], vw[kLoads];
+    float2 sc[4];      // the scales of the tile's four key groups
+    bool whole = true; // and whether all its pages are there
+    auto fetch = [&](int j0) {
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) {
+            const int q = tid + u * kThreads;
+            kw[u] = vw[u] = make_uint4(0, 0, 0, 0);
+            const int key = q / kChunks, c = q % kChunks;
+            if (key < kTile && c * 16 < d) {
+                const int grp = (j0 + key) >> 4, id = page_of(a, table, rq.kv, grp);
+                if (id >= 0)
+                    kw[u] = *(const uint4*)(a.k_codes + ((int64_t)id * a.heads + h) * per_head +
+                                            (int64_t)(group_in_page(a, grp) * 16 + (key & 15)) * d + c * 16);
+            }
+            const int kg = q / DP, ch = q % DP;
+            if (kg < 4 && ch < d) {
+                const int grp = (j0 >> 4) + kg, id = page_of(a, table, rq.kv, grp);
+                if (id >= 0) {
+                    vw[u] = *(const uint4*)(a.v_codes + ((int64_t)id * a.heads + h) * per_head +
+                                            ((int64_t)group_in_page(a, grp) * d + ch) * 16);
+                    if (E4M3 && grp * 16 + 16 > rq.kv) vw[u] = first_bytes(vw[u], rq.kv - grp * 16);
+                }
+            }
+        }
+        whole = true;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int id = page_of(a, table, rq.kv, (j0 >> 4) + k);
+            sc[k] = make_float2(0.0f, -1.0f);
+            if (id >= 0) sc[k] = a.scales[(int64_t)id * a.heads + h];
+            else whole = false;
+        }
+    };
+    if (e0 < e1) fetch(tl.tile(e0) * kTile);
+    for (int e = e0; e < e1; ++e) {
+        const int j0 = tl.tile(e) * kTile;
+        _Float16* ks = sh.k[e & 1];
+        _Float16* vs = sh.v[e & 1];
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) {
+            const int q = tid + u * kThreads;
+            const int key = q / kChunks, c = q % kChunks;
+            if (key < kTile) {
+                *(half8_t*)(ks + key * Lds::kRow + c * 16) = codes8<E4M3>(kw[u].x, kw[u].y);
+                *(half8_t*)(ks + key * Lds::kRow + c * 16 + 8) = codes8<E4M3>(kw[u].z, kw[u].w);
+            }
+            const int kg = q / DP, ch = q % DP;
+            if (kg < 4) {
+                *(half8_t*)(vs + ch * Lds::vRow + kg * 16) = codes8<E4M3>(vw[u].x, vw[u].z);
+                *(half8_t*)(vs + ch * Lds::vRow + kg * 16 + 8) = codes8<E4M3>(vw[u].y, vw[u].w);
+            }
+        }
+        float2 sn[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sn[k] = sc[k];
+        const bool mask = !whole || !tile_whole(a, tl, j0);
+        __syncthreads();
+        if (e + 1 < e1) fetch(tl.tile(e + 1) * kTile);
+        if (j0 >= wave_hi || j0 + kTile <= wave_lo) continue;   // none of the wave's rows
+
+        float x[32];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            float16_t s;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c)
+                s = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8_t*)(ks + (u * 32 + c32) * Lds::kRow + c * 16 + hf * 8), qf[c], s, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[u * 16 + i] = s[i] * (mul * sn[u * 2 + (i >> 3)].x);
+        }
+        // x[u*16+i] is the score of key j0 + 32u + 8(i/4) + 4hf + i%4
+        if (a.softcap > 0.0f) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) x[i] = capped(x[i], cap2);
+        }
+        auto key_of = [&](int i) { return j0 + (i >> 4) * 32 + ((i & 15) >> 2) * 8 + hf * 4 + (i & 3); };
+        if (a.slopes) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) x[i] -= slope2 * fabsf((float)(key_of(i) - pos));
+        }
+        if (mask) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (sn[i >> 3].y < 0.0f || !visible(a, mine, key_of(i))) x[i] = -__builtin_inff();
+        }
+        float top = x[0];
+#pragma unroll
+        for (int i = 1; i < 32; ++i) top = fmaxf(top, x[i]);
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float vtop = fmaxf(fmaxf(sn[0].y, sn[1].y), fmaxf(sn[2].y, sn[3].y));
+        if (__any(top > m || vtop > vref)) {
+            const float mnew = fmaxf(m, top), vnew = fmaxf(vref, vtop);
+            const float shrink = mnew == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m - mnew);
+            l *= shrink;
+            const float f = shrink * (vref / vnew);
+#pragma unroll
+            for (int t = 0; t < DP / 32; ++t) acc[t] *= f;
+            m = mnew;
+            vref = vnew;
+        }
+        const float m0 = m == -__builtin_inff() ? 0.0f : m;
+        const float vmul = kTop / vref;
+        half8_t p[4];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            const float w = __builtin_amdgcn_exp2f(x[i] - m0);
+            l += w;
+            p[i >> 3][i & 7] = (_Float16)(w * (fmaxf(sn[i >> 3].y, 0.0f) * vmul));
+        }
+#pragma unroll
+        for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8_t*)(vs + (t * 32 + c32) * Lds::vRow + k * 16 + hf * 8), p[k], acc[t], 0, 0, 0);
+    }
+    l += __shfl_xor(l, 32, 64);
+    if (!used) return;
+    const int64_t token = rq.start + tok;
+    const float back = vref * (1.0f / kTop);
+    if (a.n_splits > 1) {
+        const int64_t at = (token * q_heads + head) * a.n_splits + split;
+        if (hf == 0) a.stat[at] = make_float2(m, l);
+#pragma unroll
+        for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int ch = t * 32 + i * 8 + hf * 4;
+                if (ch < d)
+                    *(float4_t*)(a.part + at * d + ch) =
+                        float4_t{acc[t][4 * i], acc[t][4 * i + 1], acc[t][4 * i + 2], acc[t][4 * i + 3]} * back;
+            }
+        return;
+    }
+    const float inv = l == 0.0f ? 0.0f : back / l;
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int ch = t * 32 + i * 8 + hf * 4;
+            if (ch < d)
+                *(uint2*)(a.out + 2 * (token * a.o_token + head * a.o_head + ch)) =
+                    make_uint2(f32_to_row2(acc[t][4 * i] * inv, acc[t][4 * i + 1] * inv, a.bf16),
+                               f32_to_row2(acc[t][4 * i + 2] * inv, acc[t][4 * i + 3] * inv, a.bf16));
+        }
+    if (hf == 0 && a.lse) a.lse[token * q_heads + head] = l == 0.0f ? -__builtin_inff() : kLn2 * (m + __log2f(l));
+}
+
+// ----------------------------------------------------------------- join --
+
+// The splits of a row together, a wave each: weights 2^(m_s - max m).
+__global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t q_heads = (int64_t)a.heads * a.group;
+    const int64_t item = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+    if (item >= a.n_req * a.max_new * q_heads) return;
+    const int64_t r = item / (a.max_new * q_heads);
+    const int64_t i = item / q_heads % a.max_new;
+    const int64_t hq = item % q_heads;
+    const Request rq = request_of(a, r);
+    if (i >= rq.rows) return;
+    const int64_t token = rq.start + i;
+    const int64_t at = (token * q_heads + hq) * a.n_splits;
+    float mm = -__builtin_inff();
+    for (int s = lane; s < a.n_splits; s += 64) mm = fmaxf(mm, a.stat[at + s].x);
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) mm = fmaxf(mm, __shfl_xor(mm, k, 64));
+    const float m0 = mm == -__builtin_inff() ? 0.0f : mm;
+    float ll = 0.0f;
+    float4_t o = {0, 0, 0, 0};
+    const int quads = a.d / 4;   // up to 64
+    for (int s = 0; s < a.n_splits; ++s) {
+        const float2 st = a.stat[at + s];
+        if (st.y == 0.0f) continue;   // saw no key
+        const float f = __builtin_amdgcn_exp2f(st.x - m0);
+        ll += f * st.y;
+        if (lane < quads) o += f * *(const float4_t*)(a.part + (at + s) * a.d + 4 * lane);
+    }
+    const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
+    if (lane < quads)
+        *(uint2*)(a.out + 2 * (token * a.o_token + hq * a.o_head + 4 * lane)) =
+            make_uint2(f32_to_row2(o[0] * inv, o[1] * inv, a.bf16), f32_to_row2(o[2] * inv, o[3] * inv, a.bf16));
+    if (lane == 0 && a.lse) a.lse[token * q_heads + hq] = ll == 0.0f ? -__builtin_inff() : kLn2 * (mm + __log2f(ll));
+}
+
+// ------------------------------------------------------------------ host --
+
+struct Shape {
+    bool few;
+    int64_t row_blocks;   // of a request and KV head
+    int n_splits, split_tiles;
+};
+
+// The kernel for few rows where a KV head's rows fit one of its blocks.  The
+// keys are split so that about two thousand blocks of the few-row kernel, or
+// four hundred of the other, are there to fill 256 compute units, with a tile
+// for each wave (four for a block of the tile kernel) at the least.
+Shape shape_of(const fkv_page_desc* p, const fkv_attend_desc* t)
+{
+    Shape s;
+    const int64_t group = t->q_heads / p->heads;
+    const int64_t rows = t->max_new * group;
+    s.few = rows <= kFewRows;
+    s.row_blocks = s.few ? 1 : (rows + kTileRows - 1) / kTileRows;
+    const int64_t kv = min(t->max_kv, t->max_pages * p->page);
+    int64_t tiles = (kv + kTile - 1) / kTile;
+    if (t->window)   // no more than the window's and the sinks' tiles are seen
+        tiles = min(tiles, ((int64_t)t->window + t->max_new + kTile - 1) / kTile + 1 + ((int64_t)t->sinks + kTile - 1) / kTile);
+    const int64_t blocks = max((int64_t)1, t->n_req * p->heads * s.row_blocks);
+    const int64_t want = ((s.few ? 2048 : 400) + blocks - 1) / blocks;
+    const int64_t most = max((int64_t)1, tiles / kWaves);
+    const int64_t n = max((int64_t)1, min(want, most));
+    s.split_tiles = (int)max((int64_t)1, (tiles + n - 1) / n);
+    s.n_splits = (int)max((int64_t)1, (tiles + s.split_tiles - 1) / s.split_tiles);
+    return s;
+}
+
+bool attend_ok(const fkv_page_desc* p, const fkv_attend_desc* t)
+{
+    constexpr int64_t kMost = 1 << 30;
+    return page_desc_ok(p) && t && t->n_req >= 0 && t->n_req <= kMost && t->n_tokens >= 0 && t->n_tokens <= kMost &&
+           t->max_new >= 1 && t->max_new <= kMost && t->max_kv >= 0 && t->max_kv <= kMost && t->max_pages >= 1 &&
+           t->max_pages <= (1 << 26) && stride_ok(t->q_stride_token) && stride_ok(t->q_stride_head) &&
+           stride_ok(t->o_stride_token) && stride_ok(t->o_stride_head) && t->q_heads >= 1 && t->q_heads <= 65535 &&
+           t->q_heads % p->heads == 0 && (t->type == FKV_ROW_F16 || t->type == FKV_ROW_BF16) &&
+           t->scale - t->scale == 0.0f && t->softcap >= 0.0f && t->softcap - t->softcap == 0.0f &&
+           (t->causal == 0 || t->causal == 1) && t->window >= 0 && t->window <= kMost && t->sinks >= 0 && t->sinks <= kMost;
+}
+
+size_t part_bytes(const fkv_page_desc* p, const fkv_attend_desc* t, const Shape& s)
+{
+    return (size_t)t->n_tokens * t->q_heads * s.n_splits * p->d * sizeof(float);
+}
+
+size_t workspace_bytes_of(const fkv_page_desc* p, const fkv_attend_desc* t, const Shape& s)
+{
+    if (s.n_splits == 1) return 0;
+    return part_bytes(p, t, s) + (size_t)t->n_tokens * t->q_heads * s.n_splits * sizeof(float2);
+}
+
+}  // namespace
+}  // namespace fkv
+
+using namespace fkv;
+
+extern "C" size_t fkv_page_attend_workspace(const fkv_page_desc* desc, const fkv_attend_desc* attend)
+{
+    if (!attend_ok(desc, attend)) return 0;
+    return workspace_bytes_of(desc, attend, shape_of(desc, attend));
+}
+
+extern "C" int fkv_page_attend(const fkv_page_desc* desc, const fkv_attend_desc* attend, const uint8_t* k_codes,
+                               const uint8_t* v_codes, const float* scales, const void* q, const int32_t* tables,
+                               const int32_t* kv_len, const int32_t* q_start, const float* slopes,
+                               const int32_t* prefix, const int32_t* first, void* out, float* lse, void* workspace,
+                               size_t workspace_bytes, void* stream)
+{
+    if (!attend_ok(desc, attend)) return FKV_ERR_INVALID_ARG;
+    if (!k_codes || !v_codes || !scales || !aligned(k_codes, 16) || !aligned(v_codes, 16) || !aligned(scales, 8))
+        return FKV_ERR_INVALID_ARG;
+    if (attend->n_req == 0 || attend->n_tokens == 0) return FKV_OK;
+    if (!q || !out || !tables || !kv_len || !q_start || !aligned(q, 16) || !aligned(out, 16) || !aligned(tables, 4) ||
+        !aligned(kv_len, 4) || !aligned(q_start, 4) || !aligned(slopes, 4) || !aligned(prefix, 4) ||
+        !aligned(first, 4) || !aligned(lse, 4) || !aligned(workspace, 16))
+        return FKV_ERR_INVALID_ARG;
+    const Shape s = shape_of(desc, attend);
+    const size_t need = workspace_bytes_of(desc, attend, s);
+    if (need && (!workspace || workspace_bytes < need)) return FKV_ERR_SCRATCH_TOO_SMALL;
+    AttendArgs a = {};
+    a.k_codes = k_codes, a.v_codes = v_codes, a.scales = (const float2*)scales;
+    a.q = (const uint8_t*)q, a.out = (uint8_t*)out, a.lse = lse;
+    a.tables = tables, a.kv_len = kv_len, a.q_start = q_start;
+    a.slopes = slopes, a.prefix = prefix, a.first = first;
+    a.part = (float*)workspace;
+    a.stat = need ? (float2*)((uint8_t*)workspace + part_bytes(desc, attend, s)) : nullptr;
+    a.n_req = attend->n_req, a.n_tokens = attend->n_tokens, a.max_new = attend->max_new, a.max_kv = attend->max_kv;
+    a.max_pages = attend->max_pages, a.n_pages = desc->n_pages;
+    a.q_token = attend->q_stride_token, a.q_head = attend->q_stride_head;
+    a.o_token = attend->o_stride_token, a.o_head = attend->o_stride_head;
+    a.page = desc->page, a.heads = desc->heads, a.group = attend->q_heads / desc->heads, a.d = desc->d;
+    a.window = attend->window, a.sinks = attend->sinks;
+    a.bf16 = attend->type, a.causal = attend->causal;
+    a.n_splits = s.n_splits, a.split_tiles = s.split_tiles;
+    a.per_page = (uint32_t)(desc->page / 16);
+    a.per_page_inv = a.per_page == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + a.per_page - 1) / a.per_page);
+    a.scale = attend->scale, a.softcap = attend->softcap;
+    const hipStream_t st = (hipStream_t)stream;
+    const bool e4m3 = desc->format == FKV_PAGE_E4M3;
+    if (s.few) {
+        const int64_t blocks = a.n_req * a.heads * a.n_splits;
+        if (blocks > 0x7fffff00) return FKV_ERR_UNSUPPORTED;
+        const size_t shm = (2 * kWaves * kFewRows + (size_t)kWaves * kFewRows * (a.d + 4)) * sizeof(float);
+        auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(kThreads), shm, st, a); };
+        if (e4m3)
+            a.d <= 64 ? go(attend_few_kernel<true, 1>) : a.d <= 128 ? go(attend_few_kernel<true, 2>) : go(attend_few_kernel<true, 4>);
+        else
+            a.d <= 64 ? go(attend_few_kernel<false, 1>) : a.d <= 128 ? go(attend_few_kernel<false, 2>) : go(attend_few_kernel<false, 4>);
+    } else {
+        if (s.row_blocks > 65535 || a.n_req > 65535 || (int64_t)a.heads * a.n_splits > 0x7fffff00) return FKV_ERR_UNSUPPORTED;
+        const dim3 grid((unsigned)(a.heads * a.n_splits), (unsigned)s.row_blocks, (unsigned)a.n_req);
+        int status = FKV_OK;
+        auto go = [&](auto kern, size_t shm) {
+            // more LDS than a launch may take unasked
+            if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)shm) != hipSuccess) {
+                status = launch_status();
+                if (status == FKV_OK) status = FKV_ERR_LAUNCH;
+                return;
+            }
+            hipLaunchKernelGGL(kern, grid, dim3(kThreads), shm, st, a);
+        };
+        if (e4m3)
+            a.d <= 64    ? go(attend_tile_kernel<true, 64>, sizeof(TileLds<64>))
+            : a.d <= 96  ? go(attend_tile_kernel<true, 96>, sizeof(TileLds<96>))
+            : a.d <= 128 ? go(attend_tile_kernel<true, 128>, sizeof(TileLds<128>))
+                         : go(attend_tile_kernel<true, 256>, sizeof(TileLds<256>));
+        else
+            a.d <= 64    ? go(attend_tile_kernel<false, 64>, sizeof(TileLds<64>))
+            : a.d <= 96  ? go(attend_tile_kernel<false, 96>, sizeof(TileLds<96>))
+            : a.d <= 128 ? go(attend_tile_kernel<false, 128>, sizeof(TileLds<128>))
+                         : go(attend_tile_kernel<false, 256>, sizeof(TileLds<256>));
+        if (status != FKV_OK) return status;
+    }
+    if (a.n_splits > 1) {
+        const int64_t items = a.n_req * a.max_new * a.heads * a.group;
+        const int64_t blocks = (items + kWaves - 1) / kWaves;
+        if (blocks > 0x7fffff00) return FKV_ERR_UNSUPPORTED;
+        hipLaunchKernelGGL(attend_join_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, st, a);
+    }
+    return launch_status();
+}

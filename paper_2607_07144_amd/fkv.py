@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import NamedTuple
 
 import numpy as np
 
@@ -37,6 +38,29 @@ class fkv_rvq_desc(ctypes.Structure):
                 ("K", ctypes.c_int32), ("n_books", ctypes.c_int32)]
 
 
+FKV_PAGE_INT8, FKV_PAGE_E4M3 = 0, 1
+FKV_ROW_F16, FKV_ROW_BF16 = 0, 1
+
+
+class fkv_page_desc(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int64), ("page", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("d", ctypes.c_int32), ("format", ctypes.c_int32)]
+
+
+class fkv_row_desc(ctypes.Structure):
+    _fields_ = [("group", ctypes.c_int64), ("stride_group", ctypes.c_int64), ("stride_token", ctypes.c_int64),
+                ("stride_head", ctypes.c_int64), ("type", ctypes.c_int32)]
+
+
+class fkv_attend_desc(ctypes.Structure):
+    _fields_ = [("n_req", ctypes.c_int64), ("n_tokens", ctypes.c_int64), ("max_new", ctypes.c_int64),
+                ("max_kv", ctypes.c_int64), ("max_pages", ctypes.c_int64), ("q_stride_token", ctypes.c_int64),
+                ("q_stride_head", ctypes.c_int64), ("o_stride_token", ctypes.c_int64),
+                ("o_stride_head", ctypes.c_int64), ("q_heads", ctypes.c_int32), ("type", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("causal", ctypes.c_int32),
+                ("window", ctypes.c_int32), ("sinks", ctypes.c_int32)]
+
+
 _i32, _i64, _dbl, _p, _sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_double, ctypes.c_void_p, ctypes.c_size_t
 _PC = ctypes.POINTER(fkv_codec)
 _SIGS = {
@@ -63,6 +87,12 @@ _SIGS = {
     "fkv_kmeans_finalize": ([_i32, _i32, _i32, _i32, _i32, _p, _p, _p, _p], ctypes.c_int),
     "fkv_kmeans_update_noalloc": ([ctypes.POINTER(fkv_rvq_desc), _p, _p, _p, _p, _i32, _p, _p], ctypes.c_int),
     "fkv_kmeans_update_noalloc_bytes": ([_i32, _i32, _i32], _sz),
+    "fkv_page_plan": ([_i32, _i64, _p, _p, _p, _i64, _p, _p, _i64, _i64, _p, _p, _p, _p, _p, _p, _p, _p, _p],
+                      ctypes.c_int),
+    "fkv_page_store": ([_p, _p, _p, _p, _p, _i64, _p, _p, _p, _p, _p, _p], ctypes.c_int),
+    "fkv_page_load": ([_p, _p, _p, _p, _i64, _p, _p, _p, _p, _p, _p], ctypes.c_int),
+    "fkv_page_attend_workspace": ([_p, _p], _sz),
+    "fkv_page_attend": ([_p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _sz, _p], ctypes.c_int),
     "fkv_diag_mfma_loop": ([_i32, _i32, _i32, ctypes.c_float, ctypes.c_float, _p, _p], ctypes.c_int),
     "fkv_diag_mfma_loop_flops": ([_i32, _i32], _dbl),
     "fkv_status_string": ([ctypes.c_int], ctypes.c_char_p),
@@ -503,6 +533,202 @@ def fkv_kmeans_update_noalloc(x, books, stream_book, t_begin: int, t_end: int, s
     _check(lib.fkv_kmeans_update_noalloc(ctypes.byref(desc), _ptr(x), _ptr(books), _ptr(stream_book), _ptr(symbols),
                                          stage, _ptr(counts), _stream(stream)), "fkv_kmeans_update_noalloc")
     return books
+
+
+# ------------------------------------------------------------------ paged 8-bit cache
+
+class Pages(NamedTuple):
+    """A pool of pages: k int8 or float8_e4m3fn [n_pages][heads][page][d], v the same type
+    [n_pages][heads][page // 16][d][16], scales f32 [n_pages][heads][2].  Calls take any such triple."""
+    k: object
+    v: object
+    scales: object
+
+
+class PagePlan(NamedTuple):
+    """What fkv_page_plan gives a step: slots i64 [n_tokens], positions i32 [n_tokens], q_start i32 [n_req + 1],
+    kv_end i32 [n_req], head i32 [1] (the free-list entry that the requests served reach up to, refused ones before
+    them counted), next_head i32 [1] (the next step's head: entries handed out by now), status u8 [n_req]."""
+    slots: object
+    positions: object
+    q_start: object
+    kv_end: object
+    head: object
+    next_head: object
+    status: object
+
+
+def fkv_pages(n_pages: int, page: int, heads: int, d: int, dtype=None, device="cuda") -> Pages:
+    """An empty pool of n_pages pages of `page` tokens; dtype torch.int8 (default) or torch.float8_e4m3fn."""
+    torch = _torch()
+    dtype = dtype or torch.int8
+    pages = Pages(torch.zeros((n_pages, heads, page, d), dtype=torch.uint8, device=device).view(dtype),
+                  torch.zeros((n_pages, heads, page // 16, d, 16), dtype=torch.uint8, device=device).view(dtype),
+                  torch.zeros((n_pages, heads, 2), dtype=torch.float32, device=device))
+    _page_desc(pages)
+    return pages
+
+
+def _page_desc(pages) -> fkv_page_desc:
+    torch = _torch()
+    k, v, scales = pages
+    if k.dtype not in (torch.int8, torch.float8_e4m3fn):
+        raise TypeError("pages hold int8 or float8_e4m3fn codes")
+    _need(k, k.dtype, "pages.k")
+    _need(v, k.dtype, "pages.v")
+    _need(scales, torch.float32, "pages.scales")
+    if k.dim() != 4:
+        raise ValueError("pages.k must be [n_pages][heads][page][d]")
+    n, heads, page, d = k.shape
+    if v.shape != (n, heads, page // 16, d, 16) or scales.shape != (n, heads, 2):
+        raise ValueError("shape mismatch between pages.k, pages.v and pages.scales")
+    return fkv_page_desc(n, page, heads, d, FKV_PAGE_INT8 if k.dtype == torch.int8 else FKV_PAGE_E4M3)
+
+
+def _row_type(dtype, name) -> int:
+    torch = _torch()
+    if dtype == torch.float16:
+        return FKV_ROW_F16
+    if dtype == torch.bfloat16:
+        return FKV_ROW_BF16
+    raise TypeError("%s must be float16 or bfloat16" % name)
+
+
+def _rows(t, slots, heads: int, d: int, name) -> fkv_row_desc:
+    """Rows [n][heads][d] of slots [n], or [b][heads][t][d] of slots [b][t]; strided, contiguous in d."""
+    if not t.is_cuda or t.shape[-1] != d or (d > 1 and t.stride(-1) != 1):
+        raise TypeError("%s must be CUDA rows of %d contiguous elements" % (name, d))
+    kind = _row_type(t.dtype, name)
+    if slots.dim() == 1 and t.shape == (slots.shape[0], heads, d):
+        return fkv_row_desc(max(1, t.shape[0]), 0, t.stride(0), t.stride(1), kind)
+    if slots.dim() == 2 and t.shape == (slots.shape[0], heads, slots.shape[1], d):
+        return fkv_row_desc(max(1, t.shape[2]), t.stride(0), t.stride(2), t.stride(1), kind)
+    raise ValueError("%s must be [n][heads][d] for slots [n] or [b][heads][t][d] for slots [b][t]" % name)
+
+
+def fkv_page_plan(page: int, kv_len, new_len, free_pages, head, tables, n_tokens: int, n_bad=None,
+                  stream=None) -> PagePlan:
+    """Block tables and slot map of a step: kv_len, new_len i32 [n_req], free_pages i32 [n_free], head i32 [1] or
+    None, tables i32 [n_req][max_pages] (new entries written in place), n_tokens rows of the step."""
+    torch = _torch()
+    for t, name in ((kv_len, "kv_len"), (new_len, "new_len"), (free_pages, "free_pages"), (tables, "tables")):
+        _need(t, torch.int32, name)
+    if head is not None:
+        _need(head, torch.int32, "head")
+    if n_bad is not None:
+        _need(n_bad, torch.int32, "n_bad")
+    n_req = kv_len.numel()
+    if new_len.numel() != n_req or tables.dim() != 2 or tables.shape[0] != n_req:
+        raise ValueError("shape mismatch between kv_len, new_len and tables")
+    # one allocation for the outputs: int64 slots first, then the int32 arrays, then the bytes
+    words = 2 * n_tokens + n_tokens + n_req + 1 + n_req + 2
+    buf = torch.empty(words + (n_req + 3) // 4, dtype=torch.int32, device=kv_len.device)
+    slots, positions, q_start, kv_end, head_out, next_head, status = buf.split_with_sizes(
+        (2 * n_tokens, n_tokens, n_req + 1, n_req, 1, 1, (n_req + 3) // 4))
+    slots, status = slots.view(torch.int64), status.view(torch.uint8)[:n_req]
+    _check(lib.fkv_page_plan(page, n_req, _ptr(kv_len), _ptr(new_len), _ptr(free_pages), free_pages.numel(),
+                             _ptr(head), _ptr(tables), tables.shape[1], n_tokens, _ptr(slots), _ptr(positions),
+                             _ptr(q_start), _ptr(kv_end), _ptr(head_out), _ptr(next_head), _ptr(status), _ptr(n_bad),
+                             _stream(stream)), "fkv_page_plan")
+    return PagePlan(slots, positions, q_start, kv_end, head_out, next_head, status)
+
+
+def fkv_page_store(pages, k, v, slots, n_bad=None, stream=None):
+    """Writes rows into the pages' slots: k, v f16 or bf16 [n][heads][d] for slots i64 [n], or [b][heads][t][d] for
+    slots [b][t]; any strides, contiguous in d."""
+    torch = _torch()
+    desc = _page_desc(pages)
+    _need(slots, torch.int64, "slots")
+    if n_bad is not None:
+        _need(n_bad, torch.int32, "n_bad")
+    rk, rv = _rows(k, slots, desc.heads, desc.d, "k"), _rows(v, slots, desc.heads, desc.d, "v")
+    _check(lib.fkv_page_store(ctypes.byref(desc), ctypes.byref(rk), ctypes.byref(rv), _ptr(k), _ptr(v), slots.numel(),
+                              _ptr(slots), _ptr(pages[0]), _ptr(pages[1]), _ptr(pages[2]), _ptr(n_bad),
+                              _stream(stream)), "fkv_page_store")
+
+
+def fkv_page_load(pages, slots, dtype=None, k=None, v=None, stream=None):
+    """Reads the slots' rows back: returns (k, v) in f16 or bf16, [n][heads][d] for slots [n] and
+    [b][heads][t][d] for slots [b][t].  With k or v given, those are written (and no other)."""
+    torch = _torch()
+    desc = _page_desc(pages)
+    _need(slots, torch.int64, "slots")
+    if k is None and v is None:
+        shape = ((slots.shape[0], desc.heads, desc.d) if slots.dim() == 1 else
+                 (slots.shape[0], desc.heads, slots.shape[1], desc.d))
+        k, v = torch.empty((2, *shape), dtype=dtype or torch.float16, device=slots.device).unbind(0)
+    rk = _rows(k, slots, desc.heads, desc.d, "k") if k is not None else None
+    rv = _rows(v, slots, desc.heads, desc.d, "v") if v is not None else None
+    _check(lib.fkv_page_load(ctypes.byref(desc), _ptr(pages[0]), _ptr(pages[1]), _ptr(pages[2]), slots.numel(),
+                             _ptr(slots), ctypes.byref(rk) if rk is not None else None,
+                             ctypes.byref(rv) if rv is not None else None, _ptr(k), _ptr(v), _stream(stream)),
+           "fkv_page_load")
+    return k, v
+
+
+def fkv_page_attend(pages, q, tables, kv_len, q_start, max_new: int, max_kv: int, scale=None, softcap: float = 0.0,
+                    causal: bool = True, window: int = 0, sinks: int = 0, slopes=None, prefix=None, first=None,
+                    out=None, lse=None, want_lse: bool = False, workspace=None, stream=None):
+    """Attention of q f16 or bf16 [n_tokens][q_heads][d] (any strides, contiguous in d) over the pages that tables
+    i32 [n_req][max_pages] lists: request r holds kv_len[r] tokens, the last q_start[r+1] - q_start[r] of which are
+    its rows of q.  max_new and max_kv bound the rows and tokens of a request (host values: they set the launch).
+    scale defaults to d ** -0.5; slopes f32 [q_heads], prefix i32 [n_req], first i32 [n_tokens].  Returns
+    (out, lse or None).  workspace: uint8 scratch of fkv_page_attend_workspace bytes, for callers that keep one;
+    without it the call takes its scratch from torch's allocator, on the stream it runs on."""
+    torch = _torch()
+    desc = _page_desc(pages)
+    if not isinstance(q, torch.Tensor) or not q.is_cuda or q.dim() != 3 or q.shape[2] != desc.d or q.stride(2) != 1:
+        raise TypeError("q must be a CUDA tensor [n_tokens][q_heads][d], contiguous in d")
+    n, q_heads, d = q.shape
+    for t, name in ((tables, "tables"), (kv_len, "kv_len"), (q_start, "q_start"), (prefix, "prefix"), (first, "first")):
+        if t is not None:
+            _need(t, torch.int32, name)
+    n_req = kv_len.numel()
+    if tables.dim() != 2 or tables.shape[0] != n_req or q_start.numel() != n_req + 1:
+        raise ValueError("shape mismatch between tables, kv_len and q_start")
+    if (prefix is not None and prefix.numel() != n_req) or (first is not None and first.numel() != n):
+        raise ValueError("prefix must have one entry per request, first one per row of q")
+    if slopes is not None:
+        _need(slopes, torch.float32, "slopes")
+        if slopes.numel() != q_heads:
+            raise ValueError("slopes must have one entry per query head")
+    if out is None:
+        out = torch.empty((n, q_heads, d), dtype=q.dtype, device=q.device)
+    elif not out.is_cuda or out.shape != q.shape or out.dtype != q.dtype or out.stride(2) != 1:
+        raise TypeError("out must be a CUDA tensor of q's shape and type, contiguous in d")
+    if lse is None and want_lse:
+        lse = torch.empty((n, q_heads), dtype=torch.float32, device=q.device)
+    if lse is not None:
+        _need(lse, torch.float32, "lse")
+        if lse.numel() != n * q_heads:
+            raise ValueError("lse has the wrong size")
+    att = fkv_attend_desc(n_req, n, max_new, max_kv, tables.shape[1], q.stride(0), q.stride(1), out.stride(0),
+                          out.stride(1), q_heads, _row_type(q.dtype, "q"), d ** -0.5 if scale is None else scale,
+                          softcap, 1 if causal else 0, window, sinks)
+    need = lib.fkv_page_attend_workspace(ctypes.byref(desc), ctypes.byref(att))
+    if workspace is not None:
+        _need(workspace, torch.uint8, "workspace")
+    elif need:
+        if stream is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        else:
+            with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=q.device)):
+                workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _check(lib.fkv_page_attend(ctypes.byref(desc), ctypes.byref(att), _ptr(pages[0]), _ptr(pages[1]), _ptr(pages[2]),
+                               _ptr(q), _ptr(tables), _ptr(kv_len), _ptr(q_start), _ptr(slopes), _ptr(prefix),
+                               _ptr(first), _ptr(out), _ptr(lse), _ptr(workspace),
+                               0 if workspace is None else workspace.numel(), _stream(stream)), "fkv_page_attend")
+    return out, lse
+
+
+def fkv_page_attend_workspace(pages, q, n_req: int, max_pages: int, max_new: int, max_kv: int, window: int = 0,
+                              sinks: int = 0) -> int:
+    """Bytes of scratch that fkv_page_attend of these shapes takes (0: none)."""
+    desc = _page_desc(pages)
+    n, q_heads, d = q.shape
+    att = fkv_attend_desc(n_req, n, max_new, max_kv, max_pages, 0, 0, 0, 0, q_heads, _row_type(q.dtype, "q"), 1.0, 0.0,
+                          1, window, sinks)
+    return int(lib.fkv_page_attend_workspace(ctypes.byref(desc), ctypes.byref(att)))
 
 
 def fkv_diag_mfma_loop(n_blocks: int, iters: int, out=None, random_operands: bool = False, a: float = 1.0,
