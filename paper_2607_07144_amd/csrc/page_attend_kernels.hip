@@ -21,6 +21,8 @@
 // = 2^-28; the accumulators carry the factor 2^14 / vr.
 #include "page_common.h"
 
+#include <type_traits>
+
 namespace fkv {
 namespace {
 
@@ -206,12 +208,38 @@ __device__ __forceinline__ float abs_most8(uint4 w)
     return m;
 }
 
-// A score's factors: x = s * mul (no cap), in base 2; capped, s * mul is twice
-// the tanh's argument in base 2, and tanh u = 1 - 2 / (1 + e^2u).
-struct Score {
-    float mul, cap, slope;
-};
+// Over the two halves of a wave, and over its four rows of 16 lanes: each
+// lane gets the result of the lanes that share its lower bits.
+__device__ __forceinline__ float halves_max(float a)
+{
+    const uint32_t u = __float_as_uint(a);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
 
+__device__ __forceinline__ float halves_sum(float a)
+{
+    const uint32_t u = __float_as_uint(a);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+__device__ __forceinline__ float rows_max(float a)
+{
+    const uint32_t u = __float_as_uint(a);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return halves_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+
+__device__ __forceinline__ float rows_sum(float a)
+{
+    const uint32_t u = __float_as_uint(a);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return halves_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+// cap * tanh(x / cap) in base 2, u being twice the tanh's argument in base 2:
+// tanh t = 1 - 2 / (1 + e^2t).
 __device__ __forceinline__ float capped(float u, float cap)
 {
     const float e = __builtin_amdgcn_exp2f(u);
@@ -281,9 +309,7 @@ __global__ __launch_bounds__(kThreads) void attend_few_kernel(AttendArgs a)
                 if (a.bf16) most = fmaxf(most, fmaxf(abs_most8(w[c][0]), abs_most8(w[c][1])));
             }
             if (a.bf16) {
-                most = fmaxf(most, __shfl_xor(most, 16, 64));
-                most = fmaxf(most, __shfl_xor(most, 32, 64));
-                shift = row_shift(most);
+                shift = row_shift(rows_max(most));
             }
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
@@ -366,12 +392,9 @@ __global__ __launch_bounds__(kThreads) void attend_few_kernel(AttendArgs a)
             float top = x[0];
 #pragma unroll
             for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
-            top = fmaxf(top, __shfl_xor(top, 16, 64));
-            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            top = rows_max(top);
             if (__any(top > m || sc.y > vref)) {
-                float vnew = fmaxf(vref, sc.y);
-                vnew = fmaxf(vnew, __shfl_xor(vnew, 16, 64));
-                vnew = fmaxf(vnew, __shfl_xor(vnew, 32, 64));
+                const float vnew = rows_max(fmaxf(vref, sc.y));
                 const float mnew = fmaxf(m, top);
                 const float shrink = mnew == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m - mnew);
                 l *= shrink;
@@ -397,8 +420,7 @@ __global__ __launch_bounds__(kThreads) void attend_few_kernel(AttendArgs a)
                 acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(vw[t].z, vw[t].w), p[1], acc[t], 0, 0, 0);
             }
         }
-        l += __shfl_xor(l, 16, 64);
-        l += __shfl_xor(l, 32, 64);
+        l = rows_sum(l);
     }
 
     // the waves' parts together: [wave][row] maximum and sum, [wave][row][d] sums
@@ -459,8 +481,13 @@ struct TileLds {
     int lim[kWaves][6];
 };
 
-template <bool E4M3, int DP>
-__global__ __launch_bounds__(kThreads) void attend_tile_kernel(AttendArgs a)
+// PLAIN: neither cap nor bias; the scores then stay as the product gave them up
+// to the exponential, which takes their factor, the maximum and the value scale
+// in one multiply-add: w = 2^(s c - m + log2 v), v = vs 2^14 / vr, and sum w / v
+// is what l wants.  (v is held at 2^-40 from below: values of such a scale are
+// zeros, or too small for the sum to notice.)
+template <bool E4M3, int DP, bool PLAIN>
+__global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_tile_kernel(AttendArgs a)
 {
     typedef TileLds<DP> Lds;
     extern __shared__ __align__(16) uint8_t raw[];
@@ -531,14 +558,20 @@ __global__ __launch_bounds__(kThreads) void attend_tile_kernel(AttendArgs a)
             if (a.bf16) most = fmaxf(most, abs_most8(w[s]));
         }
         if (a.bf16) {
-            most = fmaxf(most, __shfl_xor(most, 32, 64));
-            shift = row_shift(most);
+            shift = row_shift(halves_max(most));
         }
+        // a negative scale's sign goes into q, so that the factor of a score is not negative
+        const uint32_t sign = a.scale < 0.0f ? 0x80008000u : 0u;
 #pragma unroll
-        for (int s = 0; s < kChunks; ++s) qf[s] = q8(w[s], a.bf16, pow2(shift));
+        for (int s = 0; s < kChunks; ++s) {
+            uint4 u = __builtin_bit_cast(uint4, q8(w[s], a.bf16, pow2(shift)));
+            u.x ^= sign, u.y ^= sign, u.z ^= sign, u.w ^= sign;
+            qf[s] = __builtin_bit_cast(half8_t, u);
+        }
     }
     const float cap2 = a.softcap * kLog2e;
-    const float mul = pow2(-shift) * (a.softcap > 0.0f ? a.scale * 2.0f * kLog2e / a.softcap : a.scale * kLog2e);
+    const float scale = fabsf(a.scale);
+    const float mul = pow2(-shift) * (a.softcap > 0.0f ? scale * 2.0f * kLog2e / a.softcap : scale * kLog2e);
     const float slope2 = a.slopes ? a.slopes[head] * kLog2e : 0.0f;
     const int pos = rq.pos0 + tok;
     const int32_t* table = a.tables + r * a.max_pages;
@@ -605,6 +638,7 @@ __global__ __launch_bounds__(kThreads) void attend_tile_kernel(AttendArgs a)
         if (e + 1 < e1) fetch(tl.tile(e + 1) * kTile);
         if (j0 >= wave_hi || j0 + kTile <= wave_lo) continue;   // none of the wave's rows
 
+        // x[u*16+i] is the score of key j0 + 32u + 8(i/4) + 4hf + i%4
         float x[32];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -615,27 +649,38 @@ __global__ __launch_bounds__(kThreads) void attend_tile_kernel(AttendArgs a)
             for (int c = 0; c < kChunks; ++c)
                 s = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8_t*)(ks + (u * 32 + c32) * Lds::kRow + c * 16 + hf * 8), qf[c], s, 0, 0, 0);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[u * 16 + i] = s[i] * (mul * sn[u * 2 + (i >> 3)].x);
-        }
-        // x[u*16+i] is the score of key j0 + 32u + 8(i/4) + 4hf + i%4
-        if (a.softcap > 0.0f) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) x[i] = capped(x[i], cap2);
+            for (int i = 0; i < 16; ++i) x[u * 16 + i] = s[i];
         }
         auto key_of = [&](int i) { return j0 + (i >> 4) * 32 + ((i & 15) >> 2) * 8 + hf * 4 + (i & 3); };
-        if (a.slopes) {
+        float c[4];   // factors of the four key groups' scores
 #pragma unroll
-            for (int i = 0; i < 32; ++i) x[i] -= slope2 * fabsf((float)(key_of(i) - pos));
+        for (int k = 0; k < 4; ++k) c[k] = PLAIN ? fmaxf(mul * sn[k].x, 0x1p-120f) : mul * sn[k].x;
+        if (!PLAIN) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) x[i] *= c[i >> 3];
+            if (a.softcap > 0.0f) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) x[i] = capped(x[i], cap2);
+            }
+            if (a.slopes) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) x[i] -= slope2 * fabsf((float)(key_of(i) - pos));
+            }
         }
         if (mask) {
 #pragma unroll
             for (int i = 0; i < 32; ++i)
                 if (sn[i >> 3].y < 0.0f || !visible(a, mine, key_of(i))) x[i] = -__builtin_inff();
         }
-        float top = x[0];
+        float top = -__builtin_inff();
 #pragma unroll
-        for (int i = 1; i < 32; ++i) top = fmaxf(top, x[i]);
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        for (int k = 0; k < 4; ++k) {
+            float t = x[8 * k];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) t = fmaxf(t, x[8 * k + i]);
+            top = fmaxf(top, PLAIN ? t * c[k] : t);
+        }
+        top = halves_max(top);
         const float vtop = fmaxf(fmaxf(sn[0].y, sn[1].y), fmaxf(sn[2].y, sn[3].y));
         if (__any(top > m || vtop > vref)) {
             const float mnew = fmaxf(m, top), vnew = fmaxf(vref, vtop);
@@ -651,10 +696,17 @@ __global__ __launch_bounds__(kThreads) void attend_tile_kernel(AttendArgs a)
         const float vmul = kTop / vref;
         half8_t p[4];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            const float w = __builtin_amdgcn_exp2f(x[i] - m0);
-            l += w;
-            p[i >> 3][i & 7] = (_Float16)(w * (fmaxf(sn[i >> 3].y, 0.0f) * vmul));
+        for (int k = 0; k < 4; ++k) {
+            const float v = fmaxf(sn[k].y * vmul, 0x1p-40f);
+            const float b = __builtin_amdgcn_logf(v) - m0;
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float w = __builtin_amdgcn_exp2f(PLAIN ? __builtin_fmaf(x[8 * k + i], c[k], b) : x[8 * k + i] + b);
+                sum += w;
+                p[k][i] = (_Float16)w;
+            }
+            l = __builtin_fmaf(sum, __builtin_amdgcn_rcpf(v), l);
         }
 #pragma unroll
         for (int t = 0; t < DP / 32; ++t)
@@ -662,7 +714,7 @@ __global__ __launch_bounds__(kThreads) void attend_tile_kernel(AttendArgs a)
             for (int k = 0; k < 4; ++k)
                 acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8_t*)(vs + (t * 32 + c32) * Lds::vRow + k * 16 + hf * 8), p[k], acc[t], 0, 0, 0);
     }
-    l += __shfl_xor(l, 32, 64);
+    l = halves_sum(l);
     if (!used) return;
     const int64_t token = rq.start + tok;
     const float back = vref * (1.0f / kTop);
@@ -857,16 +909,18 @@ extern "C" int fkv_page_attend(const fkv_page_desc* desc, const fkv_attend_desc*
             }
             hipLaunchKernelGGL(kern, grid, dim3(kThreads), shm, st, a);
         };
-        if (e4m3)
-            a.d <= 64    ? go(attend_tile_kernel<true, 64>, sizeof(TileLds<64>))
-            : a.d <= 96  ? go(attend_tile_kernel<true, 96>, sizeof(TileLds<96>))
-            : a.d <= 128 ? go(attend_tile_kernel<true, 128>, sizeof(TileLds<128>))
-                         : go(attend_tile_kernel<true, 256>, sizeof(TileLds<256>));
-        else
-            a.d <= 64    ? go(attend_tile_kernel<false, 64>, sizeof(TileLds<64>))
-            : a.d <= 96  ? go(attend_tile_kernel<false, 96>, sizeof(TileLds<96>))
-            : a.d <= 128 ? go(attend_tile_kernel<false, 128>, sizeof(TileLds<128>))
-                         : go(attend_tile_kernel<false, 256>, sizeof(TileLds<256>));
+        auto of_width = [&](auto dp) {
+            constexpr int DP = decltype(dp)::value;
+            const bool plain = !(a.softcap > 0.0f) && !a.slopes;
+            if (e4m3)
+                plain ? go(attend_tile_kernel<true, DP, true>, sizeof(TileLds<DP>)) : go(attend_tile_kernel<true, DP, false>, sizeof(TileLds<DP>));
+            else
+                plain ? go(attend_tile_kernel<false, DP, true>, sizeof(TileLds<DP>)) : go(attend_tile_kernel<false, DP, false>, sizeof(TileLds<DP>));
+        };
+        if (a.d <= 64) of_width(std::integral_constant<int, 64>{});
+        else if (a.d <= 96) of_width(std::integral_constant<int, 96>{});
+        else if (a.d <= 128) of_width(std::integral_constant<int, 128>{});
+        else of_width(std::integral_constant<int, 256>{});
         if (status != FKV_OK) return status;
     }
     if (a.n_splits > 1) {
