@@ -49,6 +49,38 @@ __device__ __forceinline__ uint32_t f32_to_codes(const float (&f)[4])
     return w;
 }
 
+// The same of values that no rounding takes past the largest code.
+template <bool E4M3>
+__device__ __forceinline__ uint32_t near_codes(const float (&f)[4])
+{
+    if (E4M3) {
+        int w = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
+        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], w, true);
+    }
+    // f + 1.5 2^23 has f, rounded to nearest with ties to even, in its low bits
+    uint32_t u[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) u[e] = __float_as_uint(f[e] + 12582912.0f);
+    const uint32_t lo = __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(u[3], u[2], 0x0c0c0400u);
+    return __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+}
+
+// Four codes of a word times a scale, each product rounded once.
+template <bool E4M3>
+__device__ __forceinline__ void scaled_codes(uint32_t w, float s, float* f)
+{
+    if (E4M3) {
+        float c[4];
+        codes_to_f32<true>(w, c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[e] = c[e] * s;
+        return;
+    }
+    w ^= 0x80808080u;   // c + 128, 0..255
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = __builtin_fmaf((float)((w >> (8 * e)) & 0xff), s, -128.0f * s);
+}
+
 // Element e of a packed pair of row elements as fp32, and back (one rounding,
 // to nearest, ties to even; a NaN stays one).
 __device__ __forceinline__ float row_to_f32(uint32_t pair, int e, bool bf16)

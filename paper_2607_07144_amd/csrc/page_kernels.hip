@@ -208,53 +208,105 @@ struct PageArgs {
 struct Rows {
     uint8_t* at;
     int64_t group, stride_group, stride_token, stride_head;
-    __device__ __forceinline__ uint8_t* row(int64_t i, int h) const
+};
+
+// Rows near a first one, with one division for all that lie in its group.
+struct RowsFrom {
+    uint8_t* at;       // of the first row
+    int64_t left;      // rows from it to the end of its group
+    __device__ __forceinline__ RowsFrom(const Rows& r, int64_t i, int h)
     {
-        const int64_t g = group > i ? 0 : i / group;
-        return at + 2 * (g * stride_group + (i - g * group) * stride_token + h * stride_head);
+        const int64_t g = r.group > i ? 0 : (i >> 32 | r.group >> 32) ? i / r.group : (uint32_t)i / (uint32_t)r.group;
+        left = r.group - (i - g * r.group);
+        at = r.at + 2 * (g * r.stride_group + (i - g * r.group) * r.stride_token + h * r.stride_head);
+    }
+    __device__ __forceinline__ uint8_t* row(const Rows& r, int k) const
+    {
+        uint8_t* p = at + 2 * k * r.stride_token;
+        if (k >= left) {   // k - left rows into a later group
+            const int64_t g = 1 + (k - left) / r.group;
+            p += 2 * g * (r.stride_group - r.group * r.stride_token);
+        }
+        return p;
     }
 };
 
-// A run of rows whose slots follow one another within a page is written by one
-// wave for each head and each of K and V.  A lane holds a quad -- the same 8
-// channels of 4 tokens whose offsets are 4q .. 4q+3 -- so that four value codes
-// of a channel, which lie side by side, go out as one word; `page` * d up to 8192
-// elements stay in registers between the largest element and the codes, larger
-// pages are read a second time (from the caches).
-constexpr int kQuads = 4;             // quads of a lane held in registers
-constexpr int kHeld = kQuads * 64;    // quads of a wave
-
-struct Quad {
-    uint4 row[4];
-};
-
-template <bool E4M3>
-__global__ __launch_bounds__(kThreads) void page_store_kernel(PageArgs a, Rows kr, Rows vr, int bf16, int window,
-                                                              uint32_t* n_bad)
+// Both kernels give a lane a column -- 8 channels of a 16-token group -- and
+// four of its tokens: lane 16q + c holds tokens 4q .. 4q+3 of column c, as rows
+// of 16 bytes.  In the values' layout a channel's 16 tokens lie side by side;
+// this is the 4 x 4 exchange between the two, of 32-bit words over the four
+// 16-lane rows of a wave.  Word e of row q goes to word q of row e.
+__device__ __forceinline__ void exchange(uint32_t (&w)[4])
 {
-    const int lane = threadIdx.x & 63;
+    auto swap32 = [](uint32_t& a, uint32_t& b) {
+        const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+        a = r[0], b = r[1];
+    };
+    auto swap16 = [](uint32_t& a, uint32_t& b) {
+        const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+        a = r[0], b = r[1];
+    };
+    swap32(w[0], w[2]);
+    swap32(w[1], w[3]);
+    swap16(w[0], w[1]);
+    swap16(w[2], w[3]);
+}
+
+// Byte e of four words as one word.
+__device__ __forceinline__ uint32_t bytes_of(const uint32_t (&w)[4], int e)
+{
+    const uint32_t sel = 0x0c0c0000u | (uint32_t)(e << 8) | (uint32_t)(4 + e);   // of the second and the first argument
+    const uint32_t lo = __builtin_amdgcn_perm(w[0], w[1], sel);
+    const uint32_t hi = __builtin_amdgcn_perm(w[2], w[3], sel);
+    return __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+}
+
+// A run of rows whose slots follow one another within a page is written by one
+// wave for each head and each of K and V, up to 64 columns of it (a page of 64
+// tokens x 128 channels) held in registers between the largest element and the
+// codes; larger pages are read a second time (from the caches).  What bounds it
+// is memory: rows are read 16 bytes a lane, codes written 8 (keys) and 16
+// (values) bytes a lane.  The largest element is found on the rows' bits, two at
+// a time: without the sign they are in the order of the numbers, and what is
+// not finite comes last; only a run that has such elements looks at each.
+constexpr int kPasses = 4;   // of 16 columns
+
+template <bool E4M3, bool BF16>
+__global__ __launch_bounds__(kThreads, 3) void page_store_kernel(PageArgs a, Rows kr, Rows vr, int window, uint32_t* n_bad)
+{
+    typedef uint16_t ushort2_t __attribute__((ext_vector_type(2)));
+    constexpr uint32_t kInf = BF16 ? 0x7f80 : 0x7c00;
+    constexpr float kLargest = E4M3 ? kLargestE4m3 : kLargestInt8;
+    const int lane = threadIdx.x & 63, c16 = lane & 15, tq = lane >> 4;
     const int64_t n_win = (a.n_tokens + window - 1) / window;
-    const int64_t item = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+    const int64_t item = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (item >= n_win * a.heads * 2) return;
     const bool values = item & 1;
-    const int h = (int)((item >> 1) % a.heads);
-    const int64_t w0 = (item >> 1) / a.heads * window;
-    const int64_t w1 = min(w0 + window, a.n_tokens);
+    const uint32_t hw = (uint32_t)(item >> 1);   // at most 2^31 windows x heads
+    const int h = (int)(hw % (uint32_t)a.heads);
+    const int64_t w0 = (int64_t)(hw / (uint32_t)a.heads) * window;
     const Rows rows = values ? vr : kr;
-    const int chunks = a.d / 8;
+    const uint32_t chunks = a.d / 8;
     const int64_t pool = a.n_pages * a.page;
-    const float largest = E4M3 ? kLargestE4m3 : kLargestInt8;
-    for (int64_t i = w0; i < w1; ++i) {
-        const int64_t slot = a.slots[i];
-        if (slot < 0) continue;
-        if (slot >= pool) {
-            if (n_bad && h == 0 && !values && lane == 0) atomicAdd(n_bad, 1u);
-            continue;
+
+    // the rows of the window that begin a run: at a page's first token, or where the row before does not lead up to them
+    unsigned long long begins;
+    {
+        const int64_t i = w0 + lane;
+        bool first = false;
+        if (lane < window && i < a.n_tokens) {
+            const int64_t slot = a.slots[i], before = i ? a.slots[i - 1] : -2;
+            first = slot >= 0 && slot < pool && ((uint32_t)(slot % a.page) == 0 || before != slot - 1);
+            if (slot >= pool && n_bad && h == 0 && !values) atomicAdd(n_bad, 1u);
         }
+        begins = __ballot(first);
+    }
+    while (begins) {
+        const int64_t i = w0 + __builtin_ctzll(begins);
+        begins &= begins - 1;
+        const int64_t slot = a.slots[i];
         const int64_t page = slot / a.page;
         const int begin = (int)(slot - page * a.page);
-        // its run starts at the page's first token or where the row before it does not lead up to it
-        if (begin && i && a.slots[i - 1] == slot - 1) continue;
         int len = 1;
         {
             const int most = (int)min((int64_t)(a.page - begin), a.n_tokens - i);
@@ -267,39 +319,68 @@ __global__ __launch_bounds__(kThreads) void page_store_kernel(PageArgs a, Rows k
             }
         }
         const int end = begin + len;
-        const int q0 = begin >> 2, n_quads = ((end + 3) >> 2) - q0;   // quads that hold some of the run
-        const int tasks = n_quads * chunks;
-        auto load = [&](int task, Quad& x) {
-            const int q = q0 + task / chunks, c = task % chunks;
+        const int g0 = begin >> 4;
+        const int columns = (((end + 15) >> 4) - g0) * chunks;
+        const RowsFrom from(rows, i, h);
+        // this lane's tokens of a column: offsets first .. first+3 in the page
+        auto place = [&](int col, int& grp, int& chunk) {
+            grp = g0 + (int)((uint32_t)col / chunks);
+            chunk = (int)((uint32_t)col % chunks);
+        };
+        uint4 held[kPasses][4];
+        auto load = [&](int base) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int o = 4 * q + j;
-                x.row[j] = make_uint4(0, 0, 0, 0);
-                if (task < tasks && o >= begin && o < end)
-                    x.row[j] = *(const uint4*)(rows.row(i + (o - begin), h) + 16 * c);
+            for (int u = 0; u < kPasses; ++u) {
+                const int col = base + u * 16 + c16;
+                int grp, chunk;
+                place(col, grp, chunk);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int o = grp * 16 + tq * 4 + j;
+                    held[u][j] = make_uint4(0, 0, 0, 0);
+                    if (col < columns && o >= begin && o < end) held[u][j] = *(const uint4*)(from.row(rows, o - begin) + 16 * chunk);
+                }
             }
         };
-        // the run's largest finite element
-        Quad held[kQuads];
-        float most = 0.0f;
-        for (int base = 0; base < tasks; base += kHeld) {
+        // the largest of the rows' bits, and of those of finite elements
+        ushort2_t top = {0, 0};
+        for (int base = 0; base < columns; base += 16 * kPasses) {
+            load(base);
 #pragma unroll
-            for (int u = 0; u < kQuads; ++u) load(base + u * 64 + lane, held[u]);
+            for (int u = 0; u < kPasses; ++u)
 #pragma unroll
-            for (int u = 0; u < kQuads; ++u)
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t w[4] = {held[u][j].x, held[u][j].y, held[u][j].z, held[u][j].w};
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const uint32_t word = e < 2 ? held[u].row[j].x : e < 4 ? held[u].row[j].y : e < 6 ? held[u].row[j].z : held[u].row[j].w;
-                        const float f = fabsf(row_to_f32(word, e & 1, bf16));
-                        most = fmaxf(most, f < __builtin_inff() ? f : 0.0f);
-                    }
+                    for (int e = 0; e < 4; ++e) top = __builtin_elementwise_max(top, __builtin_bit_cast(ushort2_t, w[e] & 0x7fff7fffu));
+                }
         }
+        uint32_t most = max((uint32_t)top[0], (uint32_t)top[1]);
 #pragma unroll
-        for (int k = 1; k < 64; k <<= 1) most = fmaxf(most, __shfl_xor(most, k, 64));
+        for (int k = 1; k < 64; k <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, k, 64));
+        const bool special = most >= kInf;
+        if (special) {
+            most = 0;
+            for (int base = 0; base < columns; base += 16 * kPasses) {
+                load(base);
+#pragma unroll
+                for (int u = 0; u < kPasses; ++u)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t w[4] = {held[u][j].x, held[u][j].y, held[u][j].z, held[u][j].w};
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const uint32_t b = (w[e >> 1] >> (16 * (e & 1))) & 0x7fff;
+                            most = max(most, b < kInf ? b : 0u);
+                        }
+                    }
+            }
+#pragma unroll
+            for (int k = 1; k < 64; k <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, k, 64));
+        }
+        const float largest = row_to_f32(most, 0, BF16);
         float* sp = (float*)&a.scales[page * a.heads + h] + (values ? 1 : 0);
-        float s = most < 0x1p-90f ? 0.0f : most * (1.0f / largest);
+        float s = largest < 0x1p-90f ? 0.0f : largest * (1.0f / kLargest);
         uint8_t* codes = (values ? a.v_codes : a.k_codes) + (page * a.heads + h) * (int64_t)a.page * a.d;
         if (begin) {
             const float was = *sp;
@@ -307,7 +388,8 @@ __global__ __launch_bounds__(kThreads) void page_store_kernel(PageArgs a, Rows k
             if (s > was) {
                 // the tokens before the run at the new scale; of a quad that the run begins in, only their bytes
                 const float grow = was / s;
-                const int words = values ? q0 * a.d + (begin & 3 ? a.d : 0) : begin * (a.d / 4);
+                const int quads = begin >> 2;
+                const int words = values ? (quads + (begin & 3 ? 1 : 0)) * a.d : begin * (a.d / 4);
                 for (int t = lane; t < words; t += 64) {
                     uint32_t* at;
                     int keep = 4;
@@ -332,52 +414,63 @@ __global__ __launch_bounds__(kThreads) void page_store_kernel(PageArgs a, Rows k
         }
         if (lane == 0) *sp = s;
         const float inv = s > 0.0f ? 1.0f / s : 0.0f;
-        for (int base = 0; base < tasks; base += kHeld) {
-            if (tasks > kHeld) {
+        for (int base = 0; base < columns; base += 16 * kPasses) {
+            if (columns > 16 * kPasses || special) load(base);
 #pragma unroll
-                for (int u = 0; u < kQuads; ++u) load(base + u * 64 + lane, held[u]);
-            }
-#pragma unroll
-            for (int u = 0; u < kQuads; ++u) {
-                const int task = base + u * 64 + lane;
-                if (task >= tasks) continue;
-                const int q = q0 + task / chunks, c = task % chunks;
-                uint32_t code[4][2];   // [token][half of the 8 channels]
+            for (int u = 0; u < kPasses; ++u) {
+                if (base + u * 16 >= columns) break;
+                const int col = base + u * 16 + c16;
+                int grp, chunk;
+                place(col, grp, chunk);
+                const int o0 = grp * 16 + tq * 4;
+                uint32_t code[2][4];   // [half of the 8 channels][token]
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
-                        const uint32_t lo = half ? held[u].row[j].z : held[u].row[j].x;
-                        const uint32_t hi = half ? held[u].row[j].w : held[u].row[j].y;
+                        const uint32_t lo = half ? held[u][j].z : held[u][j].x;
+                        const uint32_t hi = half ? held[u][j].w : held[u][j].y;
                         float f[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float x = row_to_f32(e < 2 ? lo : hi, e & 1, bf16);
-                            f[e] = fabsf(x) < __builtin_inff() ? x * inv : x != x ? 0.0f : copysignf(largest, x);
+                        for (int e = 0; e < 4; ++e) f[e] = row_to_f32(e < 2 ? lo : hi, e & 1, BF16) * inv;
+                        if (special) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const float x = row_to_f32(e < 2 ? lo : hi, e & 1, BF16);
+                                f[e] = fabsf(x) < __builtin_inff() ? f[e] : x != x ? 0.0f : copysignf(kLargest, x);
+                            }
                         }
-                        code[j][half] = f32_to_codes<E4M3>(f);
+                        code[half][j] = near_codes<E4M3>(f);
                     }
-                const bool whole = 4 * q >= begin && 4 * q + 4 <= end;
                 if (!values) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int o = 4 * q + j;
-                        if (o >= begin && o < end)
-                            *(uint2*)(codes + o * a.d + 8 * c) = make_uint2(code[j][0], code[j][1]);
+                    for (int j = 0; j < 4; ++j)
+                        if (col < columns && o0 + j >= begin && o0 + j < end)
+                            *(uint2*)(codes + (o0 + j) * a.d + 8 * chunk) = make_uint2(code[0][j], code[1][j]);
+                    continue;
+                }
+                const bool whole = grp * 16 >= begin && grp * 16 + 16 <= end;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    uint32_t w[4];   // channel e of the half: its four tokens here, then channel tq's sixteen
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = bytes_of(code[half], e);
+                    exchange(w);
+                    if (col >= columns) continue;
+                    uint8_t* at = codes + ((int64_t)grp * a.d + 8 * chunk + 4 * half + tq) * 16;
+                    if (whole) {
+                        *(uint4*)at = make_uint4(w[0], w[1], w[2], w[3]);
+                        continue;
                     }
-                } else {
-                    uint8_t* at = codes + ((int64_t)(q >> 2) * a.d + 8 * c) * 16 + 4 * (q & 3);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        uint32_t word = 0;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) word |= ((code[j][e >> 2] >> (8 * (e & 3))) & 0xff) << (8 * j);
-                        if (whole)
-                            *(uint32_t*)(at + 16 * e) = word;
+                    for (int q = 0; q < 4; ++q) {
+                        const int b = grp * 16 + 4 * q;
+                        if (b >= begin && b + 4 <= end)
+                            *(uint32_t*)(at + 4 * q) = w[q];
                         else
 #pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                if (4 * q + j >= begin && 4 * q + j < end) at[16 * e + j] = (uint8_t)(word >> (8 * j));
+                            for (int e = 0; e < 4; ++e)
+                                if (b + e >= begin && b + e < end) at[4 * q + e] = (uint8_t)(w[q] >> (8 * e));
                     }
                 }
             }
@@ -385,71 +478,88 @@ __global__ __launch_bounds__(kThreads) void page_store_kernel(PageArgs a, Rows k
     }
 }
 
-// Four consecutive rows of the call by 8 channels a lane: where their slots are
-// a quad of a page the value codes come as words, else byte by byte.
-template <bool E4M3>
-__global__ __launch_bounds__(kThreads) void page_load_kernel(PageArgs a, Rows kr, Rows vr, int bf16)
+// 64 rows of the call a wave, of one head and one of K and V.  The rows of one
+// 16-token group that follow one another are a segment; their columns are read
+// 16 at a time, keys 8 bytes a lane and row, values a channel's 16 tokens in 16
+// bytes and then exchanged.  What bounds it is memory.
+template <bool E4M3, bool BF16>
+__global__ __launch_bounds__(kThreads) void page_load_kernel(PageArgs a, Rows kr, Rows vr)
 {
-    const int chunks = a.d / 8;
-    const int64_t n_quads = (a.n_tokens + 3) / 4;
-    const int64_t task = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (task >= n_quads * chunks * a.heads) return;
+    __shared__ uint32_t s_seg[kThreads / 64][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int c16 = lane & 15, tq = lane >> 4;
+    const int64_t n_win = (a.n_tokens + 63) / 64;
+    const int64_t item = (int64_t)blockIdx.x * (kThreads / 64) + wave;
+    if (item >= n_win * a.heads) return;
     const bool values = blockIdx.y ? true : kr.at == nullptr;
     const Rows rows = values ? vr : kr;
-    const int c = (int)(task % chunks);
-    const int h = (int)(task / chunks % a.heads);
-    const int64_t i0 = task / chunks / a.heads * 4;
+    const int h = (int)((uint32_t)item % (uint32_t)a.heads);
+    const int64_t w0 = (int64_t)((uint32_t)item / (uint32_t)a.heads) * 64;
+    const uint32_t chunks = a.d / 8;
     const int64_t pool = a.n_pages * a.page;
-    uint32_t code[4][2];
-    float scale[4];
-    int64_t slot[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        slot[j] = i0 + j < a.n_tokens ? a.slots[i0 + j] : -1;
-        if (slot[j] >= pool) slot[j] = -1;
+    uint32_t* seg = s_seg[wave];
+
+    // segments: first row, and how many
+    const int n = (int)min((int64_t)64, a.n_tokens - w0);
+    int64_t slot = -1;
+    if (lane < n) slot = a.slots[w0 + lane];
+    if (slot >= pool || slot < 0) slot = -1;
+    const int64_t before = __shfl_up(slot, 1, 64);
+    const bool first = lane < n && (lane == 0 || slot < 0 || (slot & 15) == 0 || before != slot - 1);
+    const unsigned long long begins = __ballot(first);
+    if (first) {
+        const unsigned long long later = lane == 63 ? 0 : begins >> (lane + 1);
+        const int len = (later ? __builtin_ctzll(later) + 1 : n - lane);
+        seg[__builtin_popcountll(begins & ((1ull << lane) - 1))] = (uint32_t)lane | (uint32_t)len << 8;
     }
-    const bool quad = slot[0] >= 0 && slot[0] % 4 == 0 && slot[1] == slot[0] + 1 && slot[2] == slot[0] + 2 && slot[3] == slot[0] + 3;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        code[j][0] = code[j][1] = 0;
-        scale[j] = 0.0f;
-        if (slot[j] < 0) continue;
-        const int64_t page = slot[j] / a.page;
-        const int o = (int)(slot[j] - page * a.page);
+    const int columns = __builtin_popcountll(begins) * (int)chunks;
+    const RowsFrom from(rows, w0, h);
+    for (int base = 0; base < columns; base += 16) {
+        const int col = min(base + c16, columns - 1);
+        const uint32_t k = (uint32_t)col / chunks;
+        const int chunk = (int)((uint32_t)col % chunks);
+        const int row0 = seg[k] & 0xff, len = seg[k] >> 8;
+        const int64_t sl = __shfl(slot, row0, 64);
+        const int64_t at = max(sl, (int64_t)0);
+        const int64_t page = (at >> 32) ? at / a.page : (uint32_t)at / (uint32_t)a.page;
+        const int o = (int)(at - page * a.page);
         const float2 sc = a.scales[page * a.heads + h];
-        scale[j] = values ? sc.y : sc.x;
-        const int64_t base = (page * a.heads + h) * (int64_t)a.page * a.d;
-        if (!values) {
-            const uint2 w = *(const uint2*)(a.k_codes + base + o * a.d + 8 * c);
-            code[j][0] = w.x, code[j][1] = w.y;
-        } else if (!quad) {
-            const uint8_t* at = a.v_codes + base + ((int64_t)(o >> 4) * a.d + 8 * c) * 16 + (o & 15);
+        float s = values ? sc.y : sc.x;
+        const int64_t codes = (page * a.heads + h) * (int64_t)a.page * a.d;
+        const int r0 = 4 * tq - (o & 15);   // this lane's first token, as a row of the segment
+        uint32_t code[2][4];                // [half of the 8 channels][token]
+        if (values) {
+            const uint8_t* p = a.v_codes + codes + ((int64_t)(o >> 4) * a.d + 8 * chunk + tq) * 16;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) code[j][e >> 2] |= (uint32_t)at[16 * e] << (8 * (e & 3));
+            for (int half = 0; half < 2; ++half) {
+                const uint4 v = *(const uint4*)(p + 64 * half);
+                uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                exchange(w);   // channel e's tokens 4tq .. 4tq+3
+#pragma unroll
+                for (int j = 0; j < 4; ++j) code[half][j] = bytes_of(w, j);
+            }
+        } else {
+            const uint8_t* p = a.k_codes + codes + (int64_t)((o >> 4) * 16 + 4 * tq) * a.d + 8 * chunk;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint2 v = *(const uint2*)(p + j * a.d);
+                code[0][j] = v.x, code[1][j] = v.y;
+            }
         }
-    }
-    if (values && quad) {
-        const int64_t page = slot[0] / a.page;
-        const int o = (int)(slot[0] - page * a.page);
-        const uint8_t* at = a.v_codes + (page * a.heads + h) * (int64_t)a.page * a.d + ((int64_t)(o >> 4) * a.d + 8 * c) * 16 + (o & 15);
+        if (base + c16 >= columns) continue;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t w = *(const uint32_t*)(at + 16 * e);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) code[j][e >> 2] |= ((w >> (8 * j)) & 0xff) << (8 * (e & 3));
+        for (int j = 0; j < 4; ++j) {
+            if (r0 + j < 0 || r0 + j >= len) continue;
+            uint4 out = make_uint4(0, 0, 0, 0);
+            if (sl >= 0) {
+                float f[8];
+                scaled_codes<E4M3>(code[0][j], s, f);
+                scaled_codes<E4M3>(code[1][j], s, f + 4);
+                out = make_uint4(f32_to_row2(f[0], f[1], BF16), f32_to_row2(f[2], f[3], BF16), f32_to_row2(f[4], f[5], BF16),
+                                 f32_to_row2(f[6], f[7], BF16));
+            }
+            *(uint4*)(from.row(rows, row0 + r0 + j) + 16 * chunk) = out;
         }
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if (i0 + j >= a.n_tokens) break;
-        float f[4], g[4];
-        codes_to_f32<E4M3>(code[j][0], f);
-        codes_to_f32<E4M3>(code[j][1], g);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) f[e] *= scale[j], g[e] *= scale[j];
-        *(uint4*)(rows.row(i0 + j, h) + 16 * c) =
-            make_uint4(f32_to_row2(f[0], f[1], bf16), f32_to_row2(f[2], f[3], bf16), f32_to_row2(g[0], g[1], bf16),
-                       f32_to_row2(g[2], g[3], bf16));
     }
 }
 
@@ -505,13 +615,15 @@ extern "C" int fkv_page_store(const fkv_page_desc* desc, const fkv_row_desc* row
         return FKV_ERR_INVALID_ARG;
     const PageArgs a = {k_codes, v_codes, (float2*)scales, slots, n_tokens, desc->n_pages, desc->page, desc->heads, desc->d};
     // a wave looks at one row, or at 16 where the rows are many
-    const int window = n_tokens <= 1024 ? 1 : 16;
+    const int window = n_tokens * desc->heads <= 32768 ? 1 : 16;
     const int64_t items = (n_tokens + window - 1) / window * desc->heads * 2;
     const int64_t blocks = (items + kThreads / 64 - 1) / (kThreads / 64);
-    if (blocks > kMostBlocks) return FKV_ERR_UNSUPPORTED;
-    auto kern = desc->format == FKV_PAGE_E4M3 ? page_store_kernel<true> : page_store_kernel<false>;
+    if (items > kMostBlocks) return FKV_ERR_UNSUPPORTED;
+    const bool e4m3 = desc->format == FKV_PAGE_E4M3, bf16 = rows_k->type == FKV_ROW_BF16;
+    auto kern = e4m3 ? bf16 ? page_store_kernel<true, true> : page_store_kernel<true, false>
+                     : bf16 ? page_store_kernel<false, true> : page_store_kernel<false, false>;
     hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(kThreads), 0, (hipStream_t)stream, a, rows_of(rows_k, k_rows),
-                       rows_of(rows_v, v_rows), (int)rows_k->type, window, n_bad);
+                       rows_of(rows_v, v_rows), window, n_bad);
     return launch_status();
 }
 
@@ -529,12 +641,13 @@ extern "C" int fkv_page_load(const fkv_page_desc* desc, const uint8_t* k_codes, 
     if (!slots || !aligned(slots, 8)) return FKV_ERR_INVALID_ARG;
     const PageArgs a = {(uint8_t*)k_codes, (uint8_t*)v_codes, (float2*)scales, slots, n_tokens,
                         desc->n_pages, desc->page, desc->heads, desc->d};
-    const int64_t tasks = (n_tokens + 3) / 4 * (desc->d / 8) * desc->heads;
-    const int64_t blocks = (tasks + kThreads - 1) / kThreads;
-    if (blocks > kMostBlocks) return FKV_ERR_UNSUPPORTED;
-    const int type = k_rows ? rows_k->type : rows_v->type;
-    auto kern = desc->format == FKV_PAGE_E4M3 ? page_load_kernel<true> : page_load_kernel<false>;
+    const int64_t items = (n_tokens + 63) / 64 * desc->heads;
+    const int64_t blocks = (items + kThreads / 64 - 1) / (kThreads / 64);
+    if (items > kMostBlocks) return FKV_ERR_UNSUPPORTED;
+    const bool e4m3 = desc->format == FKV_PAGE_E4M3, bf16 = (k_rows ? rows_k : rows_v)->type == FKV_ROW_BF16;
+    auto kern = e4m3 ? bf16 ? page_load_kernel<true, true> : page_load_kernel<true, false>
+                     : bf16 ? page_load_kernel<false, true> : page_load_kernel<false, false>;
     hipLaunchKernelGGL(kern, dim3((unsigned)blocks, k_rows && v_rows ? 2 : 1), dim3(kThreads), 0, (hipStream_t)stream, a,
-                       rows_of(rows_k, k_rows), rows_of(rows_v, v_rows), type);
+                       rows_of(rows_k, k_rows), rows_of(rows_v, v_rows));
     return launch_status();
 }
