@@ -614,8 +614,8 @@ extern "C" int fkv_page_store(const fkv_page_desc* desc, const fkv_row_desc* row
     if (!k_rows || !v_rows || !slots || !aligned(k_rows, 16) || !aligned(v_rows, 16) || !aligned(slots, 8))
         return FKV_ERR_INVALID_ARG;
     const PageArgs a = {k_codes, v_codes, (float2*)scales, slots, n_tokens, desc->n_pages, desc->page, desc->heads, desc->d};
-    // a wave looks at one row, or at 16 where the rows are many
-    const int window = n_tokens * desc->heads <= 32768 ? 1 : 16;
+    // a wave looks at one row, or at a page's worth where the rows are many
+    const int window = n_tokens * desc->heads <= 32768 ? 1 : min(desc->page, 64);
     const int64_t items = (n_tokens + window - 1) / window * desc->heads * 2;
     const int64_t blocks = (items + kThreads / 64 - 1) / (kThreads / 64);
     if (items > kMostBlocks) return FKV_ERR_UNSUPPORTED;
