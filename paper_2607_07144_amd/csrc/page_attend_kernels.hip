@@ -134,7 +134,24 @@ __device__ __forceinline__ bool tile_whole(const AttendArgs& a, const Tiles& t, 
 
 __device__ __forceinline__ bool visible(const AttendArgs& a, const Seen& s, int j)
 {
-    return j >= s.lo && j < s.hi && (!a.window || j >= s.wlo || j < a.sinks);
+    // (no branches: a select for each key)
+    return (j >= s.lo) & (j < s.hi) & ((a.window == 0) | (j >= s.wlo) | (j < a.sinks));
+}
+
+// Loads of addresses that are the same in every lane, through the scalar cache:
+// of arrays that no kernel here writes while it reads them.
+template <typename T>
+__device__ __forceinline__ T scalar_load(const T* p)
+{
+    return *(const __attribute__((address_space(4))) T*)(uintptr_t)p;
+}
+
+// One of four by its number, through selects.
+__device__ __forceinline__ int64_t one_of(int k, int64_t a, int64_t b, int64_t c, int64_t d)
+{
+    const bool odd = k & 1;
+    const int64_t lo = odd ? b : a, hi = odd ? d : c;
+    return k & 2 ? hi : lo;
 }
 
 // Where a request's 16-key group lies: its page and the group within it.  A
@@ -666,6 +683,11 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_tile_kerne
         for (int w = 0; w < kWaves; ++w)
 #pragma unroll
             for (int i = 0; i < 6; ++i) v[i] = min(v[i], sh.lim[w][i]);
+        // the same in all lanes: in scalar registers, and with them all that follows from them
+#pragma unroll
+        for (int i = 0; i < 6; ++i) v[i] = __builtin_amdgcn_readfirstlane(v[i]);
+        wave_lo = __builtin_amdgcn_readfirstlane(wave_lo);
+        wave_hi = __builtin_amdgcn_readfirstlane(wave_hi);
         tl = tiles_of(a, v[0], -v[1], v[2], -v[3], v[4], -v[5]);
     }
     const int e0 = split * a.split_tiles;
@@ -712,8 +734,6 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_tile_kerne
     const int64_t per_head = (int64_t)a.page * d;
 
     uint4 kw[kLoads], vw[kLoads];
-    float2 sc[4];      // the scales of the tile's four key groups
-    bool whole = true; // and whether all its pages are there
     // where a thread's loads lie within a group: channels beyond d come from the last ones
     // (q is zero there, and sums of such channels go nowhere)
     int k_at[kLoads], v_at[kLoads], k_grp[kLoads], v_grp[kLoads];
@@ -730,55 +750,83 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_tile_kerne
     const uint8_t* k_head = a.k_codes + h * per_head;
     const uint8_t* v_head = a.v_codes + h * per_head;
     const int64_t per_id = a.heads * per_head;
-    auto fetch = [&](int j0) {
-        // the four groups' places are the same for all threads
-        Place p[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) p[k] = place_of(a, table, rq.kv, (j0 >> 4) + k);
-        int64_t at[4];
-        whole = true;
+    // The places of a tile's four groups are the same for all threads; they are looked up two tiles
+    // ahead and their scales one, in scalar registers, so that no load of codes waits for another load.
+    Place p1[4];
+    float2 s1[4];
+    bool whole1;
+    auto look_up = [&](int j0) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            check_place(a, p[k]);
-            at[k] = p[k].id * per_id + p[k].in_page * 16 * d;
-            sc[k] = a.scales[(int64_t)p[k].id * a.heads + h];
-            if (!p[k].here) sc[k] = make_float2(0.0f, -1.0f), whole = false;
+            int grp = (j0 >> 4) + k;
+            p1[k].here = grp * 16 < rq.kv;
+            grp = min(grp, (rq.kv - 1) >> 4);
+            const int at = a.per_page_inv ? (int)__umulhi((uint32_t)grp, a.per_page_inv) : grp;
+            p1[k].in_page = grp - at * (int)a.per_page;
+            p1[k].id = scalar_load(table + at);
         }
-        const int64_t at0 = at[0], at1 = at[1], at2 = at[2], at3 = at[3];
-        auto pick = [=](int k) {
-            int64_t v = at0;
-            v = k == 1 ? at1 : v;
-            v = k == 2 ? at2 : v;
-            return k == 3 ? at3 : v;
-        };
+    };
+    auto look_up_scales = [&]() {
+        whole1 = true;
 #pragma unroll
-        for (int u = 0; u < kLoads; ++u) kw[u] = *(const uint4*)(k_head + pick(k_grp[u]) + k_at[u]);
+        for (int k = 0; k < 4; ++k) {
+            check_place(a, p1[k]);
+            const uint64_t two = scalar_load((const uint64_t*)(a.scales + (int64_t)p1[k].id * a.heads + h));
+            s1[k] = __builtin_bit_cast(float2, two);
+            whole1 = whole1 && p1[k].here;
+        }
+    };
+    auto fetch = [&](const Place (&p)[4], bool whole, int j0) {
+        int64_t at[4];
 #pragma unroll
-        for (int u = 0; u < kLoads; ++u) vw[u] = *(const uint4*)(v_head + pick(v_grp[u]) + v_at[u]);
+        for (int k = 0; k < 4; ++k) at[k] = p[k].id * per_id + p[k].in_page * 16 * d;
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) kw[u] = *(const uint4*)(k_head + one_of(k_grp[u], at[0], at[1], at[2], at[3]) + k_at[u]);
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) vw[u] = *(const uint4*)(v_head + one_of(v_grp[u], at[0], at[1], at[2], at[3]) + v_at[u]);
         if (E4M3 && (!whole || j0 + kTile > rq.kv)) {   // codes after the last key may be anything, a NaN among it
+            const uint32_t there = p[0].here | p[1].here << 1 | p[2].here << 2 | p[3].here << 3;
 #pragma unroll
             for (int u = 0; u < kLoads; ++u) {
                 const int k = v_grp[u];
-                const uint32_t there = p[0].here | p[1].here << 1 | p[2].here << 2 | p[3].here << 3;
                 vw[u] = first_bytes(vw[u], (there >> k) & 1 ? rq.kv - j0 - 16 * k : 0);
             }
         }
     };
-    if (e0 < e1) fetch(tl.tile(e0) * kTile);
+    float2 sc[4];      // the scales of the tile's four key groups
+    bool whole = true; // and whether all its pages are there
+    if (e0 < e1) {
+        look_up(tl.tile(e0) * kTile);
+        look_up_scales();
+        fetch(p1, whole1, tl.tile(e0) * kTile);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            sc[k] = s1[k];
+            if (!p1[k].here) sc[k] = make_float2(0.0f, -1.0f);
+        }
+        whole = whole1;
+        look_up(tl.tile(min(e0 + 1, e1 - 1)) * kTile);
+    }
     for (int e = e0; e < e1; ++e) {
         const int j0 = tl.tile(e) * kTile;
         _Float16* ks = sh.k[e & 1];
         _Float16* vs = sh.v[e & 1];
+        look_up_scales();   // of the next tile
+        Place pn[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) pn[k] = p1[k];
+        const bool whole_n = whole1;
+        look_up(tl.tile(min(e + 2, e1 - 1)) * kTile);
 #pragma unroll
         for (int u = 0; u < kLoads; ++u) {
             const int q = tid + u * kThreads;
             const int key = q / kChunks, c = q % kChunks;
-            if (key < kTile) {
+            if (kTile * kChunks % kThreads == 0 || key < kTile) {
                 *(half8_t*)(ks + key * Lds::kRow + c * 16) = codes8<E4M3>(kw[u].x, kw[u].y);
                 *(half8_t*)(ks + key * Lds::kRow + c * 16 + 8) = codes8<E4M3>(kw[u].z, kw[u].w);
             }
             const int kg = q / DP, ch = q % DP;
-            if (kg < 4) {
+            if (kTile * kChunks % kThreads == 0 || kg < 4) {
                 *(half8_t*)(vs + ch * Lds::vRow + kg * 16) = codes8<E4M3>(vw[u].x, vw[u].z);
                 *(half8_t*)(vs + ch * Lds::vRow + kg * 16 + 8) = codes8<E4M3>(vw[u].y, vw[u].w);
             }
@@ -788,7 +836,15 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_tile_kerne
         for (int k = 0; k < 4; ++k) sn[k] = sc[k];
         const bool mask = !whole || !tile_whole(a, tl, j0);
         __syncthreads();
-        if (e + 1 < e1) fetch(tl.tile(e + 1) * kTile);
+        if (e + 1 < e1) {
+            fetch(pn, whole_n, tl.tile(e + 1) * kTile);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                sc[k] = s1[k];
+                if (!pn[k].here) sc[k] = make_float2(0.0f, -1.0f);
+            }
+            whole = whole_n;
+        }
         if (j0 >= wave_hi || j0 + kTile <= wave_lo) continue;   // none of the wave's rows
 
         // x[u*16+i] is the score of key j0 + 32u + 8(i/4) + 4hf + i%4
