@@ -33,7 +33,6 @@ constexpr int kThreads = 256;
 constexpr int kWaves = 4;
 constexpr int kTile = 64;          // keys of a tile
 constexpr int kFewRows = 16;       // rows of the kernel for few rows
-constexpr int kTileRows = 128;     // rows of a block of the kernel for many
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr float kTop = 16384.0f;   // 2^14: the largest weight
@@ -617,32 +616,40 @@ __global__ __launch_bounds__(64 * W, NC <= 2 ? 2 : 1) void attend_few_kernel(Att
 
 // ------------------------------------------------------------ many rows --
 
-// 128 rows of one KV head of a request, 32 a wave: what bounds it is the matrix
+// 32 W rows of one KV head of a request, 32 a wave: what bounds it is the matrix
 // products.  A tile's codes are widened to binary16 once, into LDS (two buffers:
 // the next tile's codes are on their way from memory meanwhile), and every
 // wave takes its left operands from there.  A value channel's keys lie in LDS
 // in the order 0-3, 8-11, 4-7, 12-15 of each 16, which is the order in which a
 // lane's scores come out of the accumulator.  DP: channels, rounded up.
-template <int DP>
+template <int DP, int W>
 struct TileLds {
     static constexpr int kRow = DP + 8;       // of a key: channels
     static constexpr int vRow = kTile + 8;    // of a channel: keys
     _Float16 k[2][kTile * kRow];
     _Float16 v[2][DP * vRow];
-    int lim[kWaves][6];
+    int lim[W][6];
 };
 
 // PLAIN: neither cap nor bias; the scores then stay as the product gave them up
 // to the exponential, which takes their factor, the maximum and the value scale
 // in one multiply-add: w = 2^(s c - m + log2 v), v = vs 2^14 / vr, and sum w / v
 // is what l wants.  (v is held at 2^-40 from below: values of such a scale are
-// zeros, or too small for the sum to notice.)
-template <bool E4M3, int DP, bool PLAIN>
-__global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_tile_kernel(AttendArgs a)
+// zeros, or too small for the sum to notice.)  CAPPED: a cap and no bias; then
+// y = cap (1 - 2 r) with r = 1 / (1 + e^2t), and r stays up to the exponential in
+// the same way: the largest score is that of the smallest r, a masked one has r =
+// infinity.  FULL: anything.
+enum Scores { PLAIN, CAPPED, FULL };
+
+// ONE: pages of a multiple of 64 tokens; a tile then lies in one page, with one scale.
+template <bool E4M3, int DP, Scores SCORES, bool ONE, int W>
+__global__ __launch_bounds__(64 * W, DP <= 128 ? 2 : 1) void attend_tile_kernel(AttendArgs a)
 {
-    typedef TileLds<DP> Lds;
+    typedef TileLds<DP, W> Lds;
+    constexpr int kThreads = 64 * W, kTileRows = 32 * W;
     extern __shared__ __align__(16) uint8_t raw[];
     Lds& sh = *(Lds*)raw;
+    constexpr int G = ONE ? 1 : 4;                                            // parts of a tile that may lie in pages of their own
     constexpr int kChunks = DP / 16;                                          // of a key, 16 codes each
     constexpr int kLoads = (kTile * kChunks + kThreads - 1) / kThreads;       // a thread's loads of each kind
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -680,7 +687,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_tile_kerne
         wave_hi = row0 < n_rows ? -v[3] : 0;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w)
+        for (int w = 0; w < W; ++w)
 #pragma unroll
             for (int i = 0; i < 6; ++i) v[i] = min(v[i], sh.lim[w][i]);
         // the same in all lanes: in scalar registers, and with them all that follows from them
@@ -734,7 +741,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_tile_kerne
     const int64_t per_head = (int64_t)a.page * d;
 
     uint4 kw[kLoads], vw[kLoads];
-    // where a thread's loads lie within a group: channels beyond d come from the last ones
+    // where a thread's loads lie within their part of the tile: channels beyond d come from the last ones
     // (q is zero there, and sums of such channels go nowhere)
     int k_at[kLoads], v_at[kLoads], k_grp[kLoads], v_grp[kLoads];
 #pragma unroll
@@ -743,80 +750,60 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_tile_kerne
         const int key = q / kChunks, kg = q / DP;
         // (a wave's loads are of one group each, but for 96 channels)
         k_grp[u] = DP == 96 ? key >> 4 : __builtin_amdgcn_readfirstlane(key >> 4);
-        k_at[u] = (key & 15) * d + min(q % kChunks * 16, d - 16);
+        k_at[u] = (ONE ? key : key & 15) * d + min(q % kChunks * 16, d - 16);
         v_grp[u] = DP == 96 ? kg : __builtin_amdgcn_readfirstlane(kg);
-        v_at[u] = min(q % DP, d - 1) * 16;
+        v_at[u] = ((ONE ? kg * d : 0) + min(q % DP, d - 1)) * 16;
     }
     const uint8_t* k_head = a.k_codes + h * per_head;
     const uint8_t* v_head = a.v_codes + h * per_head;
     const int64_t per_id = a.heads * per_head;
-    // The places of a tile's four groups are the same for all threads; they are looked up two tiles
-    // ahead and their scales one, in scalar registers, so that no load of codes waits for another load.
-    Place p1[4];
-    float2 s1[4];
-    bool whole1;
+    const float2* scale_head = a.scales + h;
+    // The places of a tile's parts are the same for all threads; they are looked up in scalar registers
+    // before the barrier that the tile before waits at, so that no load of codes waits for another load.
+    Place place[G];
+    float2 scales[G];
+    bool whole;   // all of the tile's pages are there
     auto look_up = [&](int j0) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < G; ++k) {
             int grp = (j0 >> 4) + k;
-            p1[k].here = grp * 16 < rq.kv;
+            place[k].here = grp * 16 < rq.kv;
             grp = min(grp, (rq.kv - 1) >> 4);
             const int at = a.per_page_inv ? (int)__umulhi((uint32_t)grp, a.per_page_inv) : grp;
-            p1[k].in_page = grp - at * (int)a.per_page;
-            p1[k].id = scalar_load(table + at);
+            place[k].in_page = grp - at * (int)a.per_page;
+            place[k].id = scalar_load(table + at);
         }
     };
     auto look_up_scales = [&]() {
-        whole1 = true;
+        whole = true;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            check_place(a, p1[k]);
-            const uint64_t two = scalar_load((const uint64_t*)(a.scales + (int64_t)p1[k].id * a.heads + h));
-            s1[k] = __builtin_bit_cast(float2, two);
-            whole1 = whole1 && p1[k].here;
+        for (int k = 0; k < G; ++k) {
+            check_place(a, place[k]);
+            const uint64_t two = scalar_load((const uint64_t*)(scale_head + (int64_t)place[k].id * a.heads));
+            scales[k] = place[k].here ? __builtin_bit_cast(float2, two) : make_float2(0.0f, -1.0f);
+            whole = whole && place[k].here;
         }
     };
-    auto fetch = [&](const Place (&p)[4], bool whole, int j0) {
+    auto fetch = [&](int j0) {
         int64_t at[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) at[k] = p[k].id * per_id + p[k].in_page * 16 * d;
+        for (int k = 0; k < 4; ++k) at[k] = place[ONE ? 0 : k].id * per_id + place[ONE ? 0 : k].in_page * 16 * d;
 #pragma unroll
-        for (int u = 0; u < kLoads; ++u) kw[u] = *(const uint4*)(k_head + one_of(k_grp[u], at[0], at[1], at[2], at[3]) + k_at[u]);
+        for (int u = 0; u < kLoads; ++u)
+            kw[u] = *(const uint4*)(k_head + (ONE ? at[0] : one_of(k_grp[u], at[0], at[1], at[2], at[3])) + k_at[u]);
 #pragma unroll
-        for (int u = 0; u < kLoads; ++u) vw[u] = *(const uint4*)(v_head + one_of(v_grp[u], at[0], at[1], at[2], at[3]) + v_at[u]);
+        for (int u = 0; u < kLoads; ++u)
+            vw[u] = *(const uint4*)(v_head + (ONE ? at[0] : one_of(v_grp[u], at[0], at[1], at[2], at[3])) + v_at[u]);
         if (E4M3 && (!whole || j0 + kTile > rq.kv)) {   // codes after the last key may be anything, a NaN among it
-            const uint32_t there = p[0].here | p[1].here << 1 | p[2].here << 2 | p[3].here << 3;
+            uint32_t there = 0;
 #pragma unroll
-            for (int u = 0; u < kLoads; ++u) {
-                const int k = v_grp[u];
-                vw[u] = first_bytes(vw[u], (there >> k) & 1 ? rq.kv - j0 - 16 * k : 0);
-            }
+            for (int k = 0; k < 4; ++k) there |= (uint32_t)place[ONE ? 0 : k].here << k;
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u)
+                vw[u] = first_bytes(vw[u], (there >> v_grp[u]) & 1 ? rq.kv - j0 - 16 * v_grp[u] : 0);
         }
     };
-    float2 sc[4];      // the scales of the tile's four key groups
-    bool whole = true; // and whether all its pages are there
-    if (e0 < e1) {
-        look_up(tl.tile(e0) * kTile);
-        look_up_scales();
-        fetch(p1, whole1, tl.tile(e0) * kTile);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            sc[k] = s1[k];
-            if (!p1[k].here) sc[k] = make_float2(0.0f, -1.0f);
-        }
-        whole = whole1;
-        look_up(tl.tile(min(e0 + 1, e1 - 1)) * kTile);
-    }
-    for (int e = e0; e < e1; ++e) {
-        const int j0 = tl.tile(e) * kTile;
-        _Float16* ks = sh.k[e & 1];
-        _Float16* vs = sh.v[e & 1];
-        look_up_scales();   // of the next tile
-        Place pn[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) pn[k] = p1[k];
-        const bool whole_n = whole1;
-        look_up(tl.tile(min(e + 2, e1 - 1)) * kTile);
+    auto widen = [&](_Float16* ks, _Float16* vs) {   // the codes fetched, into a buffer
 #pragma unroll
         for (int u = 0; u < kLoads; ++u) {
             const int q = tid + u * kThreads;
@@ -831,42 +818,66 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_tile_kerne
                 *(half8_t*)(vs + ch * Lds::vRow + kg * 16 + 8) = codes8<E4M3>(vw[u].y, vw[u].w);
             }
         }
-        float2 sn[4];
+    };
+    if (e0 < e1) {
+        look_up(tl.tile(e0) * kTile);
+        look_up_scales();
+        fetch(tl.tile(e0) * kTile);
+        widen(sh.k[e0 & 1], sh.v[e0 & 1]);
+    }
+    for (int e = e0; e < e1; ++e) {
+        const int j0 = tl.tile(e) * kTile;
+        const _Float16* ks = sh.k[e & 1];
+        const _Float16* vs = sh.v[e & 1];
+        float2 sn[G];   // the tile's scales
 #pragma unroll
-        for (int k = 0; k < 4; ++k) sn[k] = sc[k];
-        const bool mask = !whole || !tile_whole(a, tl, j0);
+        for (int k = 0; k < G; ++k) sn[k] = scales[k];
+        const bool all = whole, mask = !all || !tile_whole(a, tl, j0);
+        const int jn = tl.tile(min(e + 1, e1 - 1)) * kTile;
+        look_up(jn);
         __syncthreads();
-        if (e + 1 < e1) {
-            fetch(pn, whole_n, tl.tile(e + 1) * kTile);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                sc[k] = s1[k];
-                if (!pn[k].here) sc[k] = make_float2(0.0f, -1.0f);
-            }
-            whole = whole_n;
-        }
-        if (j0 >= wave_hi || j0 + kTile <= wave_lo) continue;   // none of the wave's rows
+        look_up_scales();
+        fetch(jn);   // (the last tile once more after itself: it goes nowhere)
 
         // x[u*16+i] is the score of key j0 + 32u + 8(i/4) + 4hf + i%4
         float x[32];
+        {
+            half8_t f[kChunks];
+            float16_t s0, s1;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            float16_t s;
+            for (int i = 0; i < 16; ++i) s0[i] = s1[i] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+            for (int c = 0; c < kChunks; ++c) f[c] = *(const half8_t*)(ks + c32 * Lds::kRow + c * 16 + hf * 8);
 #pragma unroll
-            for (int c = 0; c < kChunks; ++c)
-                s = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8_t*)(ks + (u * 32 + c32) * Lds::kRow + c * 16 + hf * 8), qf[c], s, 0, 0, 0);
+            for (int c = 0; c < kChunks; ++c) {
+                s0 = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[c], qf[c], s0, 0, 0, 0);
+                f[c] = *(const half8_t*)(ks + (32 + c32) * Lds::kRow + c * 16 + hf * 8);
+            }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[u * 16 + i] = s[i];
+            for (int c = 0; c < kChunks; ++c) s1 = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[c], qf[c], s1, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = s0[i], x[16 + i] = s1[i];
         }
+        // the values of the first two key groups, on their way during the softmax
+        half8_t g[DP / 32][2];
+#pragma unroll
+        for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) g[t][k] = *(const half8_t*)(vs + (t * 32 + c32) * Lds::vRow + k * 16 + hf * 8);
         auto key_of = [&](int i) { return j0 + (i >> 4) * 32 + ((i & 15) >> 2) * 8 + hf * 4 + (i & 3); };
-        float c[4];   // factors of the four key groups' scores
+        float c[G];   // factors of the scores
 #pragma unroll
-        for (int k = 0; k < 4; ++k) c[k] = PLAIN ? fmaxf(mul * sn[k].x, 0x1p-120f) : mul * sn[k].x;
-        if (!PLAIN) {
+        for (int k = 0; k < G; ++k) c[k] = SCORES == PLAIN ? fmaxf(mul * sn[k].x, 0x1p-120f) : mul * sn[k].x;
+        if (SCORES == CAPPED) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) x[i] *= c[i >> 3];
+            for (int i = 0; i < 32; ++i)
+                x[i] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x[i] * c[ONE ? 0 : i >> 3]));
+#pragma unroll
+            for (int k = 0; k < G; ++k) c[k] = -2.0f * cap2;
+        }
+        if (SCORES == FULL) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) x[i] *= c[ONE ? 0 : i >> 3];
             if (a.softcap > 0.0f) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i) x[i] = capped(x[i], cap2);
@@ -876,21 +887,34 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_tile_kerne
                 for (int i = 0; i < 32; ++i) x[i] -= slope2 * fabsf((float)(key_of(i) - pos));
             }
         }
+        constexpr float kHidden = SCORES == CAPPED ? __builtin_inff() : -__builtin_inff();
         if (mask) {
+            const uint32_t span = (uint32_t)max(mine.hi - mine.lo, 0);
+            const int from = j0 + hf * 4 - mine.lo;
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-                if (sn[i >> 3].y < 0.0f || !visible(a, mine, key_of(i))) x[i] = -__builtin_inff();
+                x[i] = (uint32_t)(from + (i >> 4) * 32 + ((i & 15) >> 2) * 8 + (i & 3)) < span ? x[i] : kHidden;
+            if (a.window) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) x[i] = (key_of(i) >= mine.wlo) | (key_of(i) < a.sinks) ? x[i] : kHidden;
+            }
+            if (!all) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) x[i] = sn[ONE ? 0 : i >> 3].y >= 0.0f ? x[i] : kHidden;
+            }
         }
-        float top = -__builtin_inff();
+        float top = -__builtin_inff(), vtop = -1.0f;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            float t = x[8 * k];
+        for (int k = 0; k < G; ++k) {
+            constexpr int n = 32 / G;
+            float t = x[n * k];
 #pragma unroll
-            for (int i = 1; i < 8; ++i) t = fmaxf(t, x[8 * k + i]);
-            top = fmaxf(top, PLAIN ? t * c[k] : t);
+            for (int i = 1; i < n; ++i)
+                t = SCORES == CAPPED ? __builtin_elementwise_minimum(t, x[n * k + i]) : __builtin_elementwise_maximum(t, x[n * k + i]);
+            top = __builtin_elementwise_maximum(top, SCORES == PLAIN ? t * c[k] : SCORES == CAPPED ? __builtin_fmaf(t, c[k], cap2) : t);
+            vtop = fmaxf(vtop, sn[k].y);
         }
         top = halves_max(top);
-        const float vtop = fmaxf(fmaxf(sn[0].y, sn[1].y), fmaxf(sn[2].y, sn[3].y));
         if (__any(top > m || vtop > vref)) {
             const float mnew = fmaxf(m, top), vnew = fmaxf(vref, vtop);
             const float shrink = mnew == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m - mnew);
@@ -903,25 +927,41 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_tile_kerne
         }
         const float m0 = m == -__builtin_inff() ? 0.0f : m;
         const float vmul = kTop / vref;
-        half8_t p[4];
+        float vb[G], vinv[G];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < G; ++k) {
             const float v = fmaxf(sn[k].y * vmul, 0x1p-40f);
-            const float b = __builtin_amdgcn_logf(v) - m0;
+            vb[k] = __builtin_amdgcn_logf(v) - m0 + (SCORES == CAPPED ? cap2 : 0.0f);
+            vinv[k] = __builtin_amdgcn_rcpf(v);
+        }
+        auto weights = [&](int k) {   // of keys 16k .. 16k+15, this lane's half of them
+            const int part = ONE ? 0 : k;
             float sum = 0.0f;
+            half8_t p;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float w = __builtin_amdgcn_exp2f(PLAIN ? __builtin_fmaf(x[8 * k + i], c[k], b) : x[8 * k + i] + b);
+                const float w = __builtin_amdgcn_exp2f(SCORES != FULL ? __builtin_fmaf(x[8 * k + i], c[part], vb[part]) : x[8 * k + i] + vb[part]);
                 sum += w;
-                p[k][i] = (_Float16)w;
+                p[i] = (_Float16)w;
             }
-            l = __builtin_fmaf(sum, __builtin_amdgcn_rcpf(v), l);
+            l = __builtin_fmaf(sum, vinv[part], l);
+            return p;
+        };
+        const half8_t p0 = weights(0), p1 = weights(1);
+#pragma unroll
+        for (int t = 0; t < DP / 32; ++t) {
+            acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(g[t][0], p0, acc[t], 0, 0, 0);
+            g[t][0] = *(const half8_t*)(vs + (t * 32 + c32) * Lds::vRow + 2 * 16 + hf * 8);
+            acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(g[t][1], p1, acc[t], 0, 0, 0);
+            g[t][1] = *(const half8_t*)(vs + (t * 32 + c32) * Lds::vRow + 3 * 16 + hf * 8);
         }
+        const half8_t p2 = weights(2), p3 = weights(3);
 #pragma unroll
-        for (int t = 0; t < DP / 32; ++t)
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8_t*)(vs + (t * 32 + c32) * Lds::vRow + k * 16 + hf * 8), p[k], acc[t], 0, 0, 0);
+        for (int t = 0; t < DP / 32; ++t) {
+            acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(g[t][0], p2, acc[t], 0, 0, 0);
+            acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(g[t][1], p3, acc[t], 0, 0, 0);
+        }
+        widen(sh.k[(e + 1) & 1], sh.v[(e + 1) & 1]);
     }
     l = halves_sum(l);
     if (!used) return;
@@ -1024,7 +1064,8 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a)
 
 struct Shape {
     bool few;
-    int64_t row_blocks;   // of a request and KV head
+    int tile_waves;       // of the kernel for many rows, 32 rows each,
+    int64_t row_blocks;   // and its blocks of a request and KV head
     int64_t blocks;       // of the kernel for few rows,
     int few_waves;        // and their waves
     int n_splits, split_tiles;
@@ -1044,7 +1085,14 @@ Shape shape_of(const fkv_page_desc* p, const fkv_attend_desc* t)
     const int64_t group = t->q_heads / p->heads;
     const int64_t rows = t->max_new * group;
     s.few = rows <= kFewRows;
-    s.row_blocks = s.few ? 1 : (rows + kTileRows - 1) / kTileRows;
+    // Eight waves share a tile's widening, four make finer blocks, two of which fill a compute unit with
+    // phases of their own.  Measured with 4 and 8 (us): 4096 rows x 4 heads over 32,768 keys, d = 128 2207
+    // and 2064, capped 2810 and 2683; one prompt of 4096 183 and 164, 16 of 2048 770 and 748; 8 of 500 to 2000
+    // rows over 2000 to 8000 keys 885 and 923, capped 1137 and 1297; 40 rows x 4 heads over 8192 keys 95 and
+    // 103; d = 96 296 and 285; d = 64, 16,384 rows 589 and 700.
+    const bool even = 4 * t->n_tokens >= 3 * t->n_req * t->max_new;   // the requests' rows are about as many
+    s.tile_waves = p->d > 64 && p->d <= 128 && rows >= 4096 && even ? 8 : 4;
+    s.row_blocks = s.few ? 1 : (rows + 32 * s.tile_waves - 1) / (32 * s.tile_waves);
     const int64_t kv = min(t->max_kv, t->max_pages * p->page);
     int64_t tiles = (kv + kTile - 1) / kTile;
     if (t->window)   // no more than the window's and the sinks' tiles are seen
@@ -1175,22 +1223,34 @@ extern "C" int fkv_page_attend(const fkv_page_desc* desc, const fkv_attend_desc*
         if (s.row_blocks > 65535 || a.n_req > 65535 || (int64_t)a.heads * a.n_splits > 0x7fffff00) return FKV_ERR_UNSUPPORTED;
         const dim3 grid((unsigned)(a.heads * a.n_splits), (unsigned)s.row_blocks, (unsigned)a.n_req);
         int status = FKV_OK;
-        auto go = [&](auto kern, size_t shm) {
+        auto go = [&](auto kern, size_t shm, int w) {
             // more LDS than a launch may take unasked
             if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)shm) != hipSuccess) {
                 status = launch_status();
                 if (status == FKV_OK) status = FKV_ERR_LAUNCH;
                 return;
             }
-            hipLaunchKernelGGL(kern, grid, dim3(kThreads), shm, st, a);
+            hipLaunchKernelGGL(kern, grid, dim3(64 * w), shm, st, a);
+        };
+        auto of_waves = [&](auto dp, auto waves) {
+            constexpr int DP = decltype(dp)::value, W = decltype(waves)::value;
+            constexpr size_t shm = sizeof(TileLds<DP, W>);
+            auto of_scores = [&](auto scores) {
+                constexpr Scores S = decltype(scores)::value;
+                if (a.page % kTile == 0)
+                    e4m3 ? go(attend_tile_kernel<true, DP, S, true, W>, shm, W) : go(attend_tile_kernel<false, DP, S, true, W>, shm, W);
+                else
+                    e4m3 ? go(attend_tile_kernel<true, DP, S, false, W>, shm, W) : go(attend_tile_kernel<false, DP, S, false, W>, shm, W);
+            };
+            if (a.slopes) of_scores(std::integral_constant<Scores, FULL>{});
+            else if (a.softcap > 0.0f) of_scores(std::integral_constant<Scores, CAPPED>{});
+            else of_scores(std::integral_constant<Scores, PLAIN>{});
         };
         auto of_width = [&](auto dp) {
-            constexpr int DP = decltype(dp)::value;
-            const bool plain = !(a.softcap > 0.0f) && !a.slopes;
-            if (e4m3)
-                plain ? go(attend_tile_kernel<true, DP, true>, sizeof(TileLds<DP>)) : go(attend_tile_kernel<true, DP, false>, sizeof(TileLds<DP>));
-            else
-                plain ? go(attend_tile_kernel<false, DP, true>, sizeof(TileLds<DP>)) : go(attend_tile_kernel<false, DP, false>, sizeof(TileLds<DP>));
+            if constexpr (decltype(dp)::value == 96 || decltype(dp)::value == 128) {
+                if (s.tile_waves == 8) return of_waves(dp, std::integral_constant<int, 8>{});
+            }
+            of_waves(dp, std::integral_constant<int, 4>{});
         };
         if (a.d <= 64) of_width(std::integral_constant<int, 64>{});
         else if (a.d <= 96) of_width(std::integral_constant<int, 96>{});
