@@ -138,16 +138,22 @@ def _ptr(t):
 def _stream(stream):
     if stream is not None:
         return int(stream)
-    torch = _torch()
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    torch = _TORCH or _torch()
+    C = torch._C
+    raw = getattr(C, "_cuda_getCurrentRawStream", None)
     if raw is None:
         return torch.cuda.current_stream().cuda_stream
-    return raw(torch.cuda.current_device())
+    device = getattr(C, "_cuda_getDevice", None)
+    return raw(device() if device is not None else torch.cuda.current_device())
 
 
 def _need(t, dtype, name):
-    if not isinstance(t, _torch().Tensor) or not t.is_cuda or t.dtype != dtype or not t.is_contiguous():
-        raise TypeError("%s must be a contiguous CUDA tensor of %s" % (name, dtype))
+    try:
+        if t.is_cuda and t.dtype is dtype and t.is_contiguous():
+            return
+    except AttributeError:   # no tensor
+        pass
+    raise TypeError("%s must be a contiguous CUDA tensor of %s" % (name, dtype))
 
 
 # ------------------------------------------------------------------ codec
@@ -570,39 +576,45 @@ def fkv_pages(n_pages: int, page: int, heads: int, d: int, dtype=None, device="c
 
 
 def _page_desc(pages) -> fkv_page_desc:
-    torch = _torch()
+    torch = _TORCH or _torch()
     k, v, scales = pages
-    if k.dtype not in (torch.int8, torch.float8_e4m3fn):
+    code = k.dtype
+    if code is torch.int8:
+        kind = FKV_PAGE_INT8
+    elif code is torch.float8_e4m3fn:
+        kind = FKV_PAGE_E4M3
+    else:
         raise TypeError("pages hold int8 or float8_e4m3fn codes")
-    _need(k, k.dtype, "pages.k")
-    _need(v, k.dtype, "pages.v")
+    _need(k, code, "pages.k")
+    _need(v, code, "pages.v")
     _need(scales, torch.float32, "pages.scales")
     if k.dim() != 4:
         raise ValueError("pages.k must be [n_pages][heads][page][d]")
     n, heads, page, d = k.shape
     if v.shape != (n, heads, page // 16, d, 16) or scales.shape != (n, heads, 2):
         raise ValueError("shape mismatch between pages.k, pages.v and pages.scales")
-    return fkv_page_desc(n, page, heads, d, FKV_PAGE_INT8 if k.dtype == torch.int8 else FKV_PAGE_E4M3)
+    return fkv_page_desc(n, page, heads, d, kind)
 
 
 def _row_type(dtype, name) -> int:
-    torch = _torch()
-    if dtype == torch.float16:
+    torch = _TORCH or _torch()
+    if dtype is torch.float16:
         return FKV_ROW_F16
-    if dtype == torch.bfloat16:
+    if dtype is torch.bfloat16:
         return FKV_ROW_BF16
     raise TypeError("%s must be float16 or bfloat16" % name)
 
 
 def _rows(t, slots, heads: int, d: int, name) -> fkv_row_desc:
     """Rows [n][heads][d] of slots [n], or [b][heads][t][d] of slots [b][t]; strided, contiguous in d."""
-    if not t.is_cuda or t.shape[-1] != d or (d > 1 and t.stride(-1) != 1):
+    shape, stride = t.shape, t.stride()
+    if not t.is_cuda or stride[-1] != 1:
         raise TypeError("%s must be CUDA rows of %d contiguous elements" % (name, d))
-    kind = _row_type(t.dtype, name)
-    if slots.dim() == 1 and t.shape == (slots.shape[0], heads, d):
-        return fkv_row_desc(max(1, t.shape[0]), 0, t.stride(0), t.stride(1), kind)
-    if slots.dim() == 2 and t.shape == (slots.shape[0], heads, slots.shape[1], d):
-        return fkv_row_desc(max(1, t.shape[2]), t.stride(0), t.stride(2), t.stride(1), kind)
+    kind, at = _row_type(t.dtype, name), slots.shape
+    if len(at) == 1 and shape == (at[0], heads, d):
+        return fkv_row_desc(shape[0] or 1, 0, stride[0], stride[1], kind)
+    if len(at) == 2 and shape == (at[0], heads, at[1], d):
+        return fkv_row_desc(shape[2] or 1, stride[0], stride[2], stride[1], kind)
     raise ValueError("%s must be [n][heads][d] for slots [n] or [b][heads][t][d] for slots [b][t]" % name)
 
 
@@ -610,59 +622,75 @@ def fkv_page_plan(page: int, kv_len, new_len, free_pages, head, tables, n_tokens
                   stream=None) -> PagePlan:
     """Block tables and slot map of a step: kv_len, new_len i32 [n_req], free_pages i32 [n_free], head i32 [1] or
     None, tables i32 [n_req][max_pages] (new entries written in place), n_tokens rows of the step."""
-    torch = _torch()
-    for t, name in ((kv_len, "kv_len"), (new_len, "new_len"), (free_pages, "free_pages"), (tables, "tables")):
-        _need(t, torch.int32, name)
+    torch = _TORCH or _torch()
+    i32 = torch.int32
+    _need(kv_len, i32, "kv_len")
+    _need(new_len, i32, "new_len")
+    _need(free_pages, i32, "free_pages")
+    _need(tables, i32, "tables")
     if head is not None:
-        _need(head, torch.int32, "head")
+        _need(head, i32, "head")
     if n_bad is not None:
-        _need(n_bad, torch.int32, "n_bad")
-    n_req = kv_len.numel()
-    if new_len.numel() != n_req or tables.dim() != 2 or tables.shape[0] != n_req:
+        _need(n_bad, i32, "n_bad")
+    n_req, width = kv_len.numel(), tables.shape
+    if new_len.numel() != n_req or len(width) != 2 or width[0] != n_req:
         raise ValueError("shape mismatch between kv_len, new_len and tables")
-    # one allocation for the outputs: int64 slots first, then the int32 arrays, then the bytes
-    words = 2 * n_tokens + n_tokens + n_req + 1 + n_req + 2
-    buf = torch.empty(words + (n_req + 3) // 4, dtype=torch.int32, device=kv_len.device)
-    slots, positions, q_start, kv_end, head_out, next_head, status = buf.split_with_sizes(
-        (2 * n_tokens, n_tokens, n_req + 1, n_req, 1, 1, (n_req + 3) // 4))
-    slots, status = slots.view(torch.int64), status.view(torch.uint8)[:n_req]
-    _check(lib.fkv_page_plan(page, n_req, _ptr(kv_len), _ptr(new_len), _ptr(free_pages), free_pages.numel(),
-                             _ptr(head), _ptr(tables), tables.shape[1], n_tokens, _ptr(slots), _ptr(positions),
-                             _ptr(q_start), _ptr(kv_end), _ptr(head_out), _ptr(next_head), _ptr(status), _ptr(n_bad),
+    # one allocation for the outputs: int64 slots first, then the int32 arrays, then the bytes; the addresses go to
+    # the call as offsets, and the tensors are made while the kernel runs
+    r4 = (n_req + 3) // 4
+    sizes = (2 * n_tokens, n_tokens, n_req + 1, n_req, 1, 1, r4)
+    buf = torch.empty(3 * n_tokens + 2 * n_req + 3 + r4, dtype=i32, device=kv_len.device)
+    at = buf.data_ptr()
+    rows = at + 12 * n_tokens          # q_start
+    ends = rows + 4 * n_req + 4        # kv_end
+    marks = ends + 4 * n_req           # head, next_head, status
+    _check(lib.fkv_page_plan(page, n_req, kv_len.data_ptr(), new_len.data_ptr(), free_pages.data_ptr(),
+                             free_pages.numel(), _ptr(head), tables.data_ptr(), width[1], n_tokens, at,
+                             at + 8 * n_tokens, rows, ends, marks, marks + 4, marks + 8, _ptr(n_bad),
                              _stream(stream)), "fkv_page_plan")
-    return PagePlan(slots, positions, q_start, kv_end, head_out, next_head, status)
+    slots, positions, q_start, kv_end, head_out, next_head, status = buf.split_with_sizes(sizes)
+    status = status.view(torch.uint8)
+    return PagePlan(slots.view(torch.int64), positions, q_start, kv_end, head_out, next_head,
+                    status if n_req == 4 * r4 else status[:n_req])
 
 
 def fkv_page_store(pages, k, v, slots, n_bad=None, stream=None):
     """Writes rows into the pages' slots: k, v f16 or bf16 [n][heads][d] for slots i64 [n], or [b][heads][t][d] for
     slots [b][t]; any strides, contiguous in d."""
-    torch = _torch()
+    torch = _TORCH or _torch()
     desc = _page_desc(pages)
     _need(slots, torch.int64, "slots")
     if n_bad is not None:
         _need(n_bad, torch.int32, "n_bad")
-    rk, rv = _rows(k, slots, desc.heads, desc.d, "k"), _rows(v, slots, desc.heads, desc.d, "v")
-    _check(lib.fkv_page_store(ctypes.byref(desc), ctypes.byref(rk), ctypes.byref(rv), _ptr(k), _ptr(v), slots.numel(),
-                              _ptr(slots), _ptr(pages[0]), _ptr(pages[1]), _ptr(pages[2]), _ptr(n_bad),
-                              _stream(stream)), "fkv_page_store")
+    heads, d = desc.heads, desc.d
+    rk, rv = _rows(k, slots, heads, d, "k"), _rows(v, slots, heads, d, "v")
+    ref = ctypes.byref
+    _check(lib.fkv_page_store(ref(desc), ref(rk), ref(rv), k.data_ptr(), v.data_ptr(), slots.numel(),
+                              slots.data_ptr(), pages[0].data_ptr(), pages[1].data_ptr(), pages[2].data_ptr(),
+                              _ptr(n_bad), _stream(stream)), "fkv_page_store")
 
 
 def fkv_page_load(pages, slots, dtype=None, k=None, v=None, stream=None):
     """Reads the slots' rows back: returns (k, v) in f16 or bf16, [n][heads][d] for slots [n] and
     [b][heads][t][d] for slots [b][t].  With k or v given, those are written (and no other)."""
-    torch = _torch()
+    torch = _TORCH or _torch()
     desc = _page_desc(pages)
     _need(slots, torch.int64, "slots")
+    heads, d = desc.heads, desc.d
     if k is None and v is None:
-        shape = ((slots.shape[0], desc.heads, desc.d) if slots.dim() == 1 else
-                 (slots.shape[0], desc.heads, slots.shape[1], desc.d))
-        k, v = torch.empty((2, *shape), dtype=dtype or torch.float16, device=slots.device).unbind(0)
-    rk = _rows(k, slots, desc.heads, desc.d, "k") if k is not None else None
-    rv = _rows(v, slots, desc.heads, desc.d, "v") if v is not None else None
-    _check(lib.fkv_page_load(ctypes.byref(desc), _ptr(pages[0]), _ptr(pages[1]), _ptr(pages[2]), slots.numel(),
-                             _ptr(slots), ctypes.byref(rk) if rk is not None else None,
-                             ctypes.byref(rv) if rv is not None else None, _ptr(k), _ptr(v), _stream(stream)),
-           "fkv_page_load")
+        at = slots.shape
+        shape = (at[0], heads, d) if len(at) == 1 else (at[0], heads, at[1], d)
+        dtype = dtype or torch.float16
+        k = torch.empty(shape, dtype=dtype, device=slots.device)
+        v = torch.empty(shape, dtype=dtype, device=slots.device)
+        rk = rv = _rows(k, slots, heads, d, "k")
+    else:
+        rk = _rows(k, slots, heads, d, "k") if k is not None else None
+        rv = _rows(v, slots, heads, d, "v") if v is not None else None
+    ref = ctypes.byref
+    _check(lib.fkv_page_load(ref(desc), pages[0].data_ptr(), pages[1].data_ptr(), pages[2].data_ptr(), slots.numel(),
+                             slots.data_ptr(), None if rk is None else ref(rk), None if rv is None else ref(rv),
+                             _ptr(k), _ptr(v), _stream(stream)), "fkv_page_load")
     return k, v
 
 
@@ -675,48 +703,61 @@ def fkv_page_attend(pages, q, tables, kv_len, q_start, max_new: int, max_kv: int
     scale defaults to d ** -0.5; slopes f32 [q_heads], prefix i32 [n_req], first i32 [n_tokens].  Returns
     (out, lse or None).  workspace: uint8 scratch of fkv_page_attend_workspace bytes, for callers that keep one;
     without it the call takes its scratch from torch's allocator, on the stream it runs on."""
-    torch = _torch()
+    torch = _TORCH or _torch()
     desc = _page_desc(pages)
-    if not isinstance(q, torch.Tensor) or not q.is_cuda or q.dim() != 3 or q.shape[2] != desc.d or q.stride(2) != 1:
-        raise TypeError("q must be a CUDA tensor [n_tokens][q_heads][d], contiguous in d")
-    n, q_heads, d = q.shape
-    for t, name in ((tables, "tables"), (kv_len, "kv_len"), (q_start, "q_start"), (prefix, "prefix"), (first, "first")):
-        if t is not None:
-            _need(t, torch.int32, name)
-    n_req = kv_len.numel()
-    if tables.dim() != 2 or tables.shape[0] != n_req or q_start.numel() != n_req + 1:
+    if not isinstance(q, torch.Tensor) or not q.is_cuda or q.dim() != 3:
+        raise TypeError("q must be a CUDA tensor [n_tokens][q_heads][d]")
+    (n, q_heads, d), q_stride = q.shape, q.stride()
+    if d != desc.d or q_stride[2] != 1:
+        raise TypeError("q must have rows of %d contiguous elements" % desc.d)
+    i32, kind = torch.int32, _row_type(q.dtype, "q")
+    _need(tables, i32, "tables")
+    _need(kv_len, i32, "kv_len")
+    _need(q_start, i32, "q_start")
+    n_req, width = kv_len.numel(), tables.shape
+    if len(width) != 2 or width[0] != n_req or q_start.numel() != n_req + 1:
         raise ValueError("shape mismatch between tables, kv_len and q_start")
-    if (prefix is not None and prefix.numel() != n_req) or (first is not None and first.numel() != n):
-        raise ValueError("prefix must have one entry per request, first one per row of q")
+    if prefix is not None:
+        _need(prefix, i32, "prefix")
+        if prefix.numel() != n_req:
+            raise ValueError("prefix must have one entry per request")
+    if first is not None:
+        _need(first, i32, "first")
+        if first.numel() != n:
+            raise ValueError("first must have one entry per row of q")
     if slopes is not None:
         _need(slopes, torch.float32, "slopes")
         if slopes.numel() != q_heads:
             raise ValueError("slopes must have one entry per query head")
     if out is None:
         out = torch.empty((n, q_heads, d), dtype=q.dtype, device=q.device)
-    elif not out.is_cuda or out.shape != q.shape or out.dtype != q.dtype or out.stride(2) != 1:
-        raise TypeError("out must be a CUDA tensor of q's shape and type, contiguous in d")
-    if lse is None and want_lse:
-        lse = torch.empty((n, q_heads), dtype=torch.float32, device=q.device)
+        o_stride = (q_heads * d, d)
+    else:
+        if not out.is_cuda or out.shape != q.shape or out.dtype is not q.dtype or out.stride(2) != 1:
+            raise TypeError("out must be a CUDA tensor of q's shape and type, contiguous in d")
+        o_stride = out.stride()
     if lse is not None:
         _need(lse, torch.float32, "lse")
         if lse.numel() != n * q_heads:
             raise ValueError("lse has the wrong size")
-    att = fkv_attend_desc(n_req, n, max_new, max_kv, tables.shape[1], q.stride(0), q.stride(1), out.stride(0),
-                          out.stride(1), q_heads, _row_type(q.dtype, "q"), d ** -0.5 if scale is None else scale,
-                          softcap, 1 if causal else 0, window, sinks)
-    need = lib.fkv_page_attend_workspace(ctypes.byref(desc), ctypes.byref(att))
+    elif want_lse:
+        lse = torch.empty((n, q_heads), dtype=torch.float32, device=q.device)
+    att = fkv_attend_desc(n_req, n, max_new, max_kv, width[1], q_stride[0], q_stride[1], o_stride[0], o_stride[1],
+                          q_heads, kind, d ** -0.5 if scale is None else scale, softcap, 1 if causal else 0, window,
+                          sinks)
+    ref = ctypes.byref
     if workspace is not None:
         _need(workspace, torch.uint8, "workspace")
-    elif need:
-        if stream is None:
+    else:
+        need = lib.fkv_page_attend_workspace(ref(desc), ref(att))
+        if need and stream is None:
             workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-        else:
+        elif need:
             with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=q.device)):
                 workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-    _check(lib.fkv_page_attend(ctypes.byref(desc), ctypes.byref(att), _ptr(pages[0]), _ptr(pages[1]), _ptr(pages[2]),
-                               _ptr(q), _ptr(tables), _ptr(kv_len), _ptr(q_start), _ptr(slopes), _ptr(prefix),
-                               _ptr(first), _ptr(out), _ptr(lse), _ptr(workspace),
+    _check(lib.fkv_page_attend(ref(desc), ref(att), pages[0].data_ptr(), pages[1].data_ptr(), pages[2].data_ptr(),
+                               q.data_ptr(), tables.data_ptr(), kv_len.data_ptr(), q_start.data_ptr(), _ptr(slopes),
+                               _ptr(prefix), _ptr(first), out.data_ptr(), _ptr(lse), _ptr(workspace),
                                0 if workspace is None else workspace.numel(), _stream(stream)), "fkv_page_attend")
     return out, lse
 
