@@ -275,17 +275,9 @@ __device__ __forceinline__ float capped(float u, float cap)
 // ------------------------------------------------------------- few rows --
 
 // One KV head of a request and at most 16 rows (query tokens x heads of the
-// group): what bounds it is the reading of the codes, 2 d bytes a key.  The tiles
-// of all requests and heads stand in one line, request by request and head by
-// head, and every block takes an equal piece of it, so that a batch of any
-// lengths keeps the whole chip busy to the end; where a piece ends inside a
-// head's keys its sums go to the workspace and are joined by a second kernel.
-// The line's length is only known on the device: each block forms the sum of
-// the requests' tiles for itself.  Where the line is short (n_splits = 1) a block takes
-// one head's keys whole.  A block's four waves take every fourth tile of its piece,
-// each with its own statistics; codes go from memory to registers in the operands'
-// own layout, 16 bytes a lane and load, the next tile's keys while a tile's
-// softmax runs, and the waves' results are joined in LDS.
+// group): what bounds it is the reading of the codes, 2 d bytes a key.  Codes go
+// from memory to registers in the operands' own layout, 16 bytes a lane and
+// load, the next tile's keys while a tile's softmax runs.
 // The left operand of S^T takes row t*4+i of key group g as its row 4g+i in
 // product t, so that lane group g ends up with keys 16g .. 16g+15, which are the
 // 16 bytes of a value channel that it loads.  NC: chunks of 64 channels.
@@ -301,10 +293,253 @@ __device__ __forceinline__ Tiles few_tiles(const AttendArgs& a, const Request& r
     return tiles_of(a, lo_min, lo_max, hi_min, hi_max, wlo_min, wlo_max);
 }
 
+// A wave's rows: this lane's is number row of the block's, token tok of the
+// request, query head head.
+struct FewRow {
+    int row, tok, head;
+};
+
+__device__ __forceinline__ FewRow few_row(const AttendArgs& a, const Request& rq, int h)
+{
+    FewRow w;
+    w.row = min((int)threadIdx.x & 15, rq.rows * a.group - 1);
+    w.tok = w.row / a.group;
+    w.head = h * a.group + w.row % a.group;
+    return w;
+}
+
+// Statistics and sums of a wave: lane 16g + c holds channels 16t + 4g .. + 3 of
+// row c in acc[t], times 2^14 / vref.
+template <int NC>
+struct FewSums {
+    float m, l, vref;
+    float4_t acc[4 * NC];
+    __device__ __forceinline__ FewSums() : m(-__builtin_inff()), l(0.0f), vref(kLeast)
+    {
+#pragma unroll
+        for (int t = 0; t < 4 * NC; ++t) acc[t] = float4_t{0, 0, 0, 0};
+    }
+};
+
+// A wave over tiles e0, e0 + step, .. below e1 (one at least).
+template <bool E4M3, int NC>
+__device__ __forceinline__ void few_keys(const AttendArgs& a, const Request& rq, int64_t r, int h, const Tiles& tl, const FewRow& fr,
+                                         int e0, int step, int e1, FewSums<NC>& st)
+{
+    const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
+    const int d = a.d, tok = fr.tok, head = fr.head;
+    const int64_t per_head = (int64_t)a.page * d;
+    const Seen mine = seen_of(a, rq, r, tok);
+    const int32_t* table = a.tables + r * a.max_pages;
+    const int gk = c16 >> 2;   // the key group of this lane's left-operand rows
+    // channels beyond d are loaded from the last ones: q is zero there, and their sums go nowhere
+    int kc[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) kc[c] = (c16 & 3) * d + min(c * 64 + g * 16, d - 16);
+    const uint8_t* k_head = a.k_codes + h * per_head;
+    const uint8_t* v_head = a.v_codes + h * per_head + c16 * 16;
+    const int64_t per_id = a.heads * per_head;
+    const float2* scale_head = a.scales + h;
+    uint4 kw[4][NC];
+    float2 sc, sc_next;
+    auto load_keys = [&](const Place& p) {
+        const uint8_t* kp = k_head + p.id * per_id + p.in_page * 16 * d;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) kw[t][c] = *(const uint4*)(kp + kc[c] + t * 4 * d);
+    };
+    int j0 = tl.tile(e0) * kTile;
+    Place pk = place_of(a, table, rq.kv, (j0 >> 4) + gk), pv = place_of(a, table, rq.kv, (j0 >> 4) + g);
+    int j1 = tl.tile(min(e0 + step, e1 - 1)) * kTile;
+    Place pk1 = place_of(a, table, rq.kv, (j1 >> 4) + gk), pv1 = place_of(a, table, rq.kv, (j1 >> 4) + g);
+    check_place(a, pk);
+    check_place(a, pv);
+    load_keys(pk);
+    sc = scale_head[(int64_t)pv.id * a.heads];
+
+    // the right operand of S^T: channels 64c + 16g .. + 15 of the row
+    half8_t qf[NC][2];
+    int shift = 0;
+    {
+        const uint8_t* qp = a.q + 2 * ((int64_t)(rq.start + tok) * a.q_token + head * a.q_head);
+        uint4 w[NC][2];
+        float most = 0.0f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int e = c * 64 + g * 16;
+            w[c][0] = w[c][1] = make_uint4(0, 0, 0, 0);
+            if (e < d) w[c][0] = *(const uint4*)(qp + 2 * e), w[c][1] = *(const uint4*)(qp + 2 * e + 16);
+            if (a.bf16) most = fmaxf(most, fmaxf(abs_most8(w[c][0]), abs_most8(w[c][1])));
+        }
+        if (a.bf16) shift = row_shift(rows_max(most));
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            qf[c][0] = q8(w[c][0], a.bf16, pow2(shift));
+            qf[c][1] = q8(w[c][1], a.bf16, pow2(shift));
+        }
+    }
+    const float cap2 = a.softcap * kLog2e;
+    const float mul = pow2(-shift) * (a.softcap > 0.0f ? a.scale * 2.0f * kLog2e / a.softcap : a.scale * kLog2e);
+    const float slope2 = a.slopes ? a.slopes[head] * kLog2e : 0.0f;
+    const int pos = rq.pos0 + tok;
+
+    for (int e = e0; e < e1; e += step) {
+        // the tile's values, on their way while its scores are formed
+        uint4 vw[4 * NC];
+        const uint8_t* vp = v_head + pv.id * per_id + pv.in_page * 16 * d;
+#pragma unroll
+        for (int t = 0; t < 4 * NC; ++t) vw[t] = *(const uint4*)(vp + min(t * 16, d - 16) * 16);
+        const bool here = pv.here;
+        const bool mask = !tile_whole(a, tl, j0) || __any(!here);
+        if (!here) sc = make_float2(0.0f, 0.0f);
+        const int j0g = j0 + g * 16;
+        // scores of keys j0g .. j0g+15 in turn
+        float4_t s[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            s[t] = float4_t{0, 0, 0, 0};
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(kw[t][c].x, kw[t][c].y), qf[c][0], s[t], 0, 0, 0);
+                s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(kw[t][c].z, kw[t][c].w), qf[c][1], s[t], 0, 0, 0);
+            }
+        }
+        // the next tile's keys, and the pages of the one after
+        if (e + step < e1) {
+            check_place(a, pk1);
+            check_place(a, pv1);
+            load_keys(pk1);
+            sc_next = scale_head[(int64_t)pv1.id * a.heads];
+            j0 = j1, pv = pv1;
+            j1 = tl.tile(min(e + 2 * step, e1 - 1)) * kTile;
+            pk1 = place_of(a, table, rq.kv, (j1 >> 4) + gk);
+            pv1 = place_of(a, table, rq.kv, (j1 >> 4) + g);
+        }
+        const float mulk = mul * sc.x;
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = s[i >> 2][i & 3] * mulk;
+        if (a.softcap > 0.0f) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = capped(x[i], cap2);
+        }
+        if (a.slopes) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] -= slope2 * fabsf((float)(j0g + i - pos));
+        }
+        if (mask) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (!here || !visible(a, mine, j0g + i)) x[i] = -__builtin_inff();
+            if (E4M3) {   // codes after the last key may be anything, a NaN among it
+                const int n = here ? rq.kv - j0g : 0;
+#pragma unroll
+                for (int t = 0; t < 4 * NC; ++t) vw[t] = first_bytes(vw[t], n);
+            }
+        }
+        float top = x[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+        top = rows_max(top);
+        if (__any(top > st.m || sc.y > st.vref)) {
+            const float vnew = rows_max(fmaxf(st.vref, sc.y));
+            const float mnew = fmaxf(st.m, top);
+            const float shrink = mnew == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(st.m - mnew);
+            st.l *= shrink;
+            const float k = shrink * (st.vref / vnew);
+#pragma unroll
+            for (int t = 0; t < 4 * NC; ++t) st.acc[t] *= k;
+            st.m = mnew;
+            st.vref = vnew;
+        }
+        const float m0 = st.m == -__builtin_inff() ? 0.0f : st.m;
+        const float vs = sc.y * (kTop / st.vref);
+        half8_t p[2];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float w = __builtin_amdgcn_exp2f(x[i] - m0);
+            st.l += w;
+            p[i >> 3][i & 7] = (_Float16)(w * vs);
+        }
+#pragma unroll
+        for (int t = 0; t < 4 * NC; ++t) {
+            st.acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(vw[t].x, vw[t].y), p[0], st.acc[t], 0, 0, 0);
+            st.acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(vw[t].z, vw[t].w), p[1], st.acc[t], 0, 0, 0);
+        }
+        sc = sc_next;
+    }
+    st.l = rows_sum(st.l);
+}
+
+// A block a KV head and request, its W waves every W-th tile each, their
+// results joined in LDS: for contexts too short to be split.
+template <bool E4M3, int NC, int W>
+__global__ __launch_bounds__(64 * W, NC <= 2 ? 2 : 1) void attend_few_kernel(AttendArgs a)
+{
+    extern __shared__ __align__(16) float lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c16 = lane & 15, g = lane >> 4;
+    const int d = a.d;
+    const int64_t q_heads = (int64_t)a.heads * a.group;
+    const int64_t r = blockIdx.x / a.heads;
+    const int h = (int)(blockIdx.x % a.heads);
+    const Request rq = request_of(a, r);
+    if (rq.rows == 0) return;
+    const int n_rows = rq.rows * a.group;
+    const Tiles tl = few_tiles(a, rq, r);
+    FewSums<NC> st;
+    if (wave < tl.n) few_keys<E4M3, NC>(a, rq, r, h, tl, few_row(a, rq, h), wave, W, tl.n, st);
+
+    // the waves' parts together: [wave][row] maximum and sum, [wave][row][d] sums
+    float* s_m = lds;
+    float* s_l = lds + W * kFewRows;
+    float* s_acc = lds + 2 * W * kFewRows;
+    const int ld = d + 4;
+    if (g == 0) s_m[wave * kFewRows + c16] = st.m, s_l[wave * kFewRows + c16] = st.l;
+    const float back = st.vref * (1.0f / kTop);
+    if (c16 < n_rows) {
+#pragma unroll
+        for (int t = 0; t < 4 * NC; ++t)
+            if (t * 16 < d) *(float4_t*)(s_acc + (wave * kFewRows + c16) * ld + t * 16 + g * 4) = st.acc[t] * back;
+    }
+    __syncthreads();
+    const int quads = d / 4;
+    for (int task = tid; task < n_rows * quads; task += 64 * W) {
+        const int rw = task / quads, q4 = task % quads;
+        float mm = -__builtin_inff();
+#pragma unroll
+        for (int w = 0; w < W; ++w) mm = fmaxf(mm, s_m[w * kFewRows + rw]);
+        const float m0 = mm == -__builtin_inff() ? 0.0f : mm;
+        float ll = 0.0f;
+        float4_t o = {0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const float k = __builtin_amdgcn_exp2f(s_m[w * kFewRows + rw] - m0);
+            ll += k * s_l[w * kFewRows + rw];
+            o += k * *(const float4_t*)(s_acc + (w * kFewRows + rw) * ld + 4 * q4);
+        }
+        const int64_t token = rq.start + rw / a.group;
+        const int hq = h * a.group + rw % a.group;
+        const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
+        *(uint2*)(a.out + 2 * (token * a.o_token + hq * a.o_head + 4 * q4)) =
+            make_uint2(f32_to_row2(o[0] * inv, o[1] * inv, a.bf16), f32_to_row2(o[2] * inv, o[3] * inv, a.bf16));
+        if (q4 == 0 && a.lse) a.lse[token * q_heads + hq] = ll == 0.0f ? -__builtin_inff() : kLn2 * (mm + __log2f(ll));
+    }
+}
+
+// Longer contexts.  The tiles of all requests and heads stand in one line,
+// request by request and head by head, and every wave takes an equal piece of
+// it, so that a batch of any lengths keeps the whole chip busy to the end;
+// where a piece ends inside a head's keys its sums go to the workspace and are
+// joined by a second kernel.  The line's length is only known on the device:
+// each block forms the sum of the requests' tiles for itself.
+//
 // A request's tiles in the line: none without rows, else one at least, so that
 // a row that sees no key is written too.  Before each head's tiles stand kBegin
 // places that hold none: what beginning a head costs, in tiles.
-constexpr int kBegin = 5;
+constexpr int kBegin = 3;
+constexpr int kLeastPiece = 2;   // tiles
 
 __device__ __forceinline__ int line_tiles(const AttendArgs& a, int64_t r)
 {
@@ -319,29 +554,21 @@ __device__ __forceinline__ int64_t uniform(int64_t v)
     return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
-template <bool E4M3, int NC, int W, bool LINE>
-__global__ __launch_bounds__(64 * W, NC <= 2 ? 2 : 1) void attend_few_kernel(AttendArgs a)
+template <bool E4M3, int NC>
+__global__ __launch_bounds__(kThreads, NC <= 2 ? 2 : 1) void attend_line_kernel(AttendArgs a)
 {
-    extern __shared__ __align__(16) float lds[];
-    __shared__ int64_t s_sum[64 * W];
-    __shared__ int64_t s_part[W];
-    __shared__ int32_t s_most[W];
+    __shared__ int64_t s_sum[kThreads];
+    __shared__ int64_t s_part[kWaves];
+    __shared__ int32_t s_most[kWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c16 = lane & 15, g = lane >> 4;
     const int d = a.d;
     const int64_t q_heads = (int64_t)a.heads * a.group;
-    const int64_t per_head = (int64_t)a.page * d;
 
-    // this block's piece [f, f1) of the line, the request r that it begins in
-    // and a head's places before r
-    int64_t f, f1, r, before, piece;
-    int tiles = 0, places = 0;
-    if (!LINE) {
-        r = blockIdx.x / a.heads;
-        before = f = 0;
-        f1 = piece = 1;
-    } else {
-        const int64_t per = (a.n_req + 64 * W - 1) / 64 * W;   // requests of a thread
+    // places of the requests before each thread's
+    const int64_t per = (a.n_req + kThreads - 1) / kThreads;   // requests of a thread
+    int64_t piece, total;
+    {
         const int64_t b = min(tid * per, a.n_req), e = min(b + per, a.n_req);
         int64_t sum = 0;
         int most = 0;
@@ -359,9 +586,9 @@ __global__ __launch_bounds__(64 * W, NC <= 2 ? 2 : 1) void attend_few_kernel(Att
         }
         if (lane == 63) s_part[wave] = upto, s_most[wave] = most;
         __syncthreads();
-        int64_t total = 0;
+        total = 0;
 #pragma unroll
-        for (int w = 0; w < W; ++w) {
+        for (int w = 0; w < kWaves; ++w) {
             if (w < wave) upto += s_part[w];
             total += s_part[w];
             most = max(most, s_most[w]);
@@ -369,248 +596,68 @@ __global__ __launch_bounds__(64 * W, NC <= 2 ? 2 : 1) void attend_few_kernel(Att
         s_sum[tid] = upto - sum;
         __syncthreads();
         // equal pieces, as long as it takes for no head to be in more than n_splits of them
-        piece = max((total * a.heads + gridDim.x - 1) / gridDim.x, (int64_t)(most - 1 + a.n_splits - 2) / (a.n_splits - 1));
-        piece = max(piece, (int64_t)(kBegin + W));
-        piece = uniform(piece);
-        f = blockIdx.x * piece;
-        f1 = uniform(min(f + piece, total * a.heads));
-        if (f >= f1) return;
-        int lo = 0, hi = 64 * W;   // the last thread whose requests begin at or before f
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (s_sum[mid] * a.heads <= f) lo = mid;
-            else hi = mid;
-        }
-        r = uniform(lo * per);
-        before = uniform(s_sum[lo]);
-        tiles = line_tiles(a, r), places = tiles ? tiles + kBegin : 0;
+        const int64_t waves = (int64_t)gridDim.x * kWaves;
+        total *= a.heads;
+        piece = max((total + waves - 1) / waves, (int64_t)(most - 1 + a.n_splits - 2) / (a.n_splits - 1));
+        piece = uniform(max(piece, (int64_t)(kBegin + kLeastPiece)));
     }
-
+    // this wave's piece [f, f1) of the line, the request r that it begins in and a head's places before r
+    // (neighbouring pieces in different blocks: a short line is spread over all compute units)
+    int64_t f = ((int64_t)wave * gridDim.x + blockIdx.x) * piece;
+    const int64_t f1 = uniform(min(f + piece, total));
+    if (f >= f1) return;
+    int lo = 0, hi = kThreads;   // the last thread whose requests begin at or before f
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (s_sum[mid] * a.heads <= f) lo = mid;
+        else hi = mid;
+    }
+    int64_t r = uniform(lo * per), before = uniform(s_sum[lo]);
+    int tiles = line_tiles(a, r), places = tiles ? tiles + kBegin : 0;
     while (f < f1) {
-        int h = 0, e0 = 0, e1 = 0x7fffffff, split = 0, n_split = 1;
-        if (!LINE) {
-            h = blockIdx.x % a.heads;
-            f = f1;
-        } else {
-            while (f >= (before + places) * a.heads) {
-                before += places;
-                tiles = line_tiles(a, ++r);
-                places = tiles ? tiles + kBegin : 0;
-            }
-            const int64_t in_r = f - before * a.heads;
-            h = (int)(in_r / places);
-            const int from = (int)(in_r - (int64_t)h * places);
-            const int len = (int)min((int64_t)(places - from), f1 - f);
-            const int64_t tile0 = f - from + kBegin;   // where the head's tiles begin in the line
-            f += len;
-            if (from + len <= kBegin) continue;   // no tile of the head is in the piece
-            e0 = max(from - kBegin, 0);
-            e1 = from + len - kBegin;
-            split = (int)((tile0 + e0) / piece - tile0 / piece);
-            n_split = (int)((tile0 + tiles - 1) / piece - tile0 / piece) + 1;
+        while (f >= (before + places) * a.heads) {
+            before += places;
+            tiles = line_tiles(a, ++r);
+            places = tiles ? tiles + kBegin : 0;
         }
+        const int64_t in_r = f - before * a.heads;
+        const int h = (int)(in_r / places);
+        const int from = (int)(in_r - (int64_t)h * places);
+        const int len = (int)min((int64_t)(places - from), f1 - f);
+        const int64_t tile0 = f - from + kBegin;   // where the head's tiles begin in the line
+        f += len;
+        if (from + len <= kBegin) continue;   // no tile of the head is in the piece
+        const int e0 = max(from - kBegin, 0);
+        const int split = (int)((tile0 + e0) / piece - tile0 / piece);
+        const int n_split = (int)((tile0 + tiles - 1) / piece - tile0 / piece) + 1;
 
         const Request rq = request_of(a, r);
-        const int n_rows = rq.rows * a.group;
-        if (n_rows == 0) return;   // (a line holds no such request)
         const Tiles tl = few_tiles(a, rq, r);
-        e1 = min(e1, tl.n);
-        const int row = min(c16, n_rows - 1);   // this lane's row
-        const int tok = row / a.group;
-        const int head = h * a.group + row % a.group;
-        const Seen mine = seen_of(a, rq, r, tok);
-
-        float m = -__builtin_inff(), l = 0.0f, vref = kLeast;
-        float4_t acc[4 * NC];
-#pragma unroll
-        for (int t = 0; t < 4 * NC; ++t) acc[t] = float4_t{0, 0, 0, 0};
-
-        if (e0 + wave < e1) {
-            const int32_t* table = a.tables + r * a.max_pages;
-            const int gk = c16 >> 2;   // the key group of this lane's left-operand rows
-            // channels beyond d are loaded from the last ones: q is zero there, and their sums go nowhere
-            int kc[NC];
-#pragma unroll
-            for (int c = 0; c < NC; ++c) kc[c] = (c16 & 3) * d + min(c * 64 + g * 16, d - 16);
-            const uint8_t* k_head = a.k_codes + h * per_head;
-            const uint8_t* v_head = a.v_codes + h * per_head + c16 * 16;
-            const int64_t per_id = a.heads * per_head;
-            const float2* scale_head = a.scales + h;
-            uint4 kw[4][NC];
-            float2 sc, sc_next;
-            auto load_keys = [&](const Place& p) {
-                const uint8_t* kp = k_head + p.id * per_id + p.in_page * 16 * d;
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int c = 0; c < NC; ++c) kw[t][c] = *(const uint4*)(kp + kc[c] + t * 4 * d);
-            };
-            int j0 = tl.tile(e0 + wave) * kTile;
-            Place pk = place_of(a, table, rq.kv, (j0 >> 4) + gk), pv = place_of(a, table, rq.kv, (j0 >> 4) + g);
-            int j1 = tl.tile(min(e0 + wave + W, e1 - 1)) * kTile;
-            Place pk1 = place_of(a, table, rq.kv, (j1 >> 4) + gk), pv1 = place_of(a, table, rq.kv, (j1 >> 4) + g);
-            check_place(a, pk);
-            check_place(a, pv);
-            load_keys(pk);
-            sc = scale_head[(int64_t)pv.id * a.heads];
-
-            // the right operand of S^T: channels 64c + 16g .. + 15 of the row
-            half8_t qf[NC][2];
-            int shift = 0;
-            {
-                const uint8_t* qp = a.q + 2 * ((int64_t)(rq.start + tok) * a.q_token + head * a.q_head);
-                uint4 w[NC][2];
-                float most = 0.0f;
-#pragma unroll
-                for (int c = 0; c < NC; ++c) {
-                    const int e = c * 64 + g * 16;
-                    w[c][0] = w[c][1] = make_uint4(0, 0, 0, 0);
-                    if (e < d) w[c][0] = *(const uint4*)(qp + 2 * e), w[c][1] = *(const uint4*)(qp + 2 * e + 16);
-                    if (a.bf16) most = fmaxf(most, fmaxf(abs_most8(w[c][0]), abs_most8(w[c][1])));
-                }
-                if (a.bf16) shift = row_shift(rows_max(most));
-#pragma unroll
-                for (int c = 0; c < NC; ++c) {
-                    qf[c][0] = q8(w[c][0], a.bf16, pow2(shift));
-                    qf[c][1] = q8(w[c][1], a.bf16, pow2(shift));
-                }
-            }
-            const float cap2 = a.softcap * kLog2e;
-            const float mul = pow2(-shift) * (a.softcap > 0.0f ? a.scale * 2.0f * kLog2e / a.softcap : a.scale * kLog2e);
-            const float slope2 = a.slopes ? a.slopes[head] * kLog2e : 0.0f;
-            const int pos = rq.pos0 + tok;
-
-            for (int e = e0 + wave; e < e1; e += W) {
-                // the tile's values, on their way while its scores are formed
-                uint4 vw[4 * NC];
-                const uint8_t* vp = v_head + pv.id * per_id + pv.in_page * 16 * d;
-#pragma unroll
-                for (int t = 0; t < 4 * NC; ++t) vw[t] = *(const uint4*)(vp + min(t * 16, d - 16) * 16);
-                const bool here = pv.here;
-                const bool mask = !tile_whole(a, tl, j0) || __any(!here);
-                if (!here) sc = make_float2(0.0f, 0.0f);
-                const int j0g = j0 + g * 16;
-                // scores of keys j0g .. j0g+15 in turn
-                float4_t s[4];
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    s[t] = float4_t{0, 0, 0, 0};
-#pragma unroll
-                    for (int c = 0; c < NC; ++c) {
-                        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(kw[t][c].x, kw[t][c].y), qf[c][0], s[t], 0, 0, 0);
-                        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(kw[t][c].z, kw[t][c].w), qf[c][1], s[t], 0, 0, 0);
-                    }
-                }
-                // the next tile's keys, and the pages of the one after
-                if (e + W < e1) {
-                    check_place(a, pk1);
-                    check_place(a, pv1);
-                    load_keys(pk1);
-                    sc_next = scale_head[(int64_t)pv1.id * a.heads];
-                    j0 = j1, pv = pv1;
-                    j1 = tl.tile(min(e + 2 * W, e1 - 1)) * kTile;
-                    pk1 = place_of(a, table, rq.kv, (j1 >> 4) + gk);
-                    pv1 = place_of(a, table, rq.kv, (j1 >> 4) + g);
-                }
-                const float mulk = mul * sc.x;
-                float x[16];
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[i] = s[i >> 2][i & 3] * mulk;
-                if (a.softcap > 0.0f) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) x[i] = capped(x[i], cap2);
-                }
-                if (a.slopes) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) x[i] -= slope2 * fabsf((float)(j0g + i - pos));
-                }
-                if (mask) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (!here || !visible(a, mine, j0g + i)) x[i] = -__builtin_inff();
-                    if (E4M3) {   // codes after the last key may be anything, a NaN among it
-                        const int n = here ? rq.kv - j0g : 0;
-#pragma unroll
-                        for (int t = 0; t < 4 * NC; ++t) vw[t] = first_bytes(vw[t], n);
-                    }
-                }
-                float top = x[0];
-#pragma unroll
-                for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
-                top = rows_max(top);
-                if (__any(top > m || sc.y > vref)) {
-                    const float vnew = rows_max(fmaxf(vref, sc.y));
-                    const float mnew = fmaxf(m, top);
-                    const float shrink = mnew == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m - mnew);
-                    l *= shrink;
-                    const float k = shrink * (vref / vnew);
-#pragma unroll
-                    for (int t = 0; t < 4 * NC; ++t) acc[t] *= k;
-                    m = mnew;
-                    vref = vnew;
-                }
-                const float m0 = m == -__builtin_inff() ? 0.0f : m;
-                const float vs = sc.y * (kTop / vref);
-                half8_t p[2];
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float w = __builtin_amdgcn_exp2f(x[i] - m0);
-                    l += w;
-                    p[i >> 3][i & 7] = (_Float16)(w * vs);
-                }
-#pragma unroll
-                for (int t = 0; t < 4 * NC; ++t) {
-                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(vw[t].x, vw[t].y), p[0], acc[t], 0, 0, 0);
-                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(vw[t].z, vw[t].w), p[1], acc[t], 0, 0, 0);
-                }
-                sc = sc_next;
-            }
-            l = rows_sum(l);
-        }
-
-        // the waves' parts together: [wave][row] maximum and sum, [wave][row][d] sums
-        float* s_m = lds;
-        float* s_l = lds + W * kFewRows;
-        float* s_acc = lds + 2 * W * kFewRows;
-        const int ld = d + 4;
-        if (g == 0) s_m[wave * kFewRows + c16] = m, s_l[wave * kFewRows + c16] = l;
-        const float back = vref * (1.0f / kTop);
-        if (c16 < n_rows) {
+        const int e1 = min(from + len - kBegin, tl.n);
+        const FewRow fr = few_row(a, rq, h);
+        FewSums<NC> st;
+        if (e0 < e1) few_keys<E4M3, NC>(a, rq, r, h, tl, fr, e0, 1, e1, st);
+        if (split == 0 && lane == 0) a.pieces[r * a.heads + h] = n_split;
+        if (c16 >= rq.rows * a.group) continue;
+        const int64_t token = rq.start + fr.tok;
+        if (n_split > 1) {
+            const float back = st.vref * (1.0f / kTop);
+            const int64_t at = (token * q_heads + fr.head) * a.n_splits + split;
 #pragma unroll
             for (int t = 0; t < 4 * NC; ++t)
-                if (t * 16 < d) *(float4_t*)(s_acc + (wave * kFewRows + c16) * ld + t * 16 + g * 4) = acc[t] * back;
-        }
-        __syncthreads();
-        const int quads = d / 4;
-        for (int task = tid; task < n_rows * quads; task += 64 * W) {
-            const int rw = task / quads, q4 = task % quads;
-            float mm = -__builtin_inff();
+                if (t * 16 < d) *(float4_t*)(a.part + at * d + t * 16 + g * 4) = st.acc[t] * back;
+            if (g == 0) a.stat[at] = make_float2(st.m, st.l);
+        } else {
+            const float inv = st.l == 0.0f ? 0.0f : st.vref * (1.0f / kTop) / st.l;
 #pragma unroll
-            for (int w = 0; w < W; ++w) mm = fmaxf(mm, s_m[w * kFewRows + rw]);
-            const float m0 = mm == -__builtin_inff() ? 0.0f : mm;
-            float ll = 0.0f;
-            float4_t o = {0, 0, 0, 0};
-#pragma unroll
-            for (int w = 0; w < W; ++w) {
-                const float k = __builtin_amdgcn_exp2f(s_m[w * kFewRows + rw] - m0);
-                ll += k * s_l[w * kFewRows + rw];
-                o += k * *(const float4_t*)(s_acc + (w * kFewRows + rw) * ld + 4 * q4);
+            for (int t = 0; t < 4 * NC; ++t) {
+                const float4_t o = st.acc[t] * inv;
+                if (t * 16 < d)
+                    *(uint2*)(a.out + 2 * (token * a.o_token + fr.head * a.o_head + t * 16 + g * 4)) =
+                        make_uint2(f32_to_row2(o[0], o[1], a.bf16), f32_to_row2(o[2], o[3], a.bf16));
             }
-            const int64_t token = rq.start + rw / a.group;
-            const int hq = h * a.group + rw % a.group;
-            if (n_split > 1) {
-                const int64_t at = (token * q_heads + hq) * a.n_splits + split;
-                *(float4_t*)(a.part + at * d + 4 * q4) = o;
-                if (q4 == 0) a.stat[at] = make_float2(mm, ll);
-            } else {
-                const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
-                *(uint2*)(a.out + 2 * (token * a.o_token + hq * a.o_head + 4 * q4)) =
-                    make_uint2(f32_to_row2(o[0] * inv, o[1] * inv, a.bf16), f32_to_row2(o[2] * inv, o[3] * inv, a.bf16));
-                if (q4 == 0 && a.lse) a.lse[token * q_heads + hq] = ll == 0.0f ? -__builtin_inff() : kLn2 * (mm + __log2f(ll));
-            }
+            if (g == 0 && a.lse) a.lse[token * q_heads + fr.head] = st.l == 0.0f ? -__builtin_inff() : kLn2 * (st.m + __log2f(st.l));
         }
-        if (LINE && split == 0 && tid == 0) a.pieces[r * a.heads + h] = n_split;
-        __syncthreads();
     }
 }
 
@@ -997,16 +1044,21 @@ __global__ __launch_bounds__(64 * W, DP <= 128 ? 2 : 1) void attend_tile_kernel(
 
 // ----------------------------------------------------------------- join --
 
-// The splits of a row together, a wave each: weights 2^(m_s - max m).  A lane
-// holds four channels of every second split (of each, where d > 128), and the
-// sums of kJoin splits are on their way at a time.
+// The splits of a row together: weights 2^(m_s - max m).  R waves of a block
+// take one row's splits in turn (R = 1: a row each); a lane holds four channels
+// of every second split of its wave (of each, where d > 128), and the sums of
+// kJoin splits are on their way at a time.
 constexpr int kJoin = 4;
+constexpr int kManySplits = 32;   // from which on a block takes one row
 
+template <int R>
 __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a)
 {
-    const int lane = threadIdx.x & 63;
+    __shared__ float4_t s_o[kWaves][64];
+    __shared__ float s_l[kWaves];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t q_heads = (int64_t)a.heads * a.group;
-    const int64_t item = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+    const int64_t item = R == 1 ? (int64_t)blockIdx.x * kWaves + wave : blockIdx.x;
     if (item >= a.n_req * a.max_new * q_heads) return;
     const int64_t r = item / (a.max_new * q_heads);
     const int64_t i = item / q_heads % a.max_new;
@@ -1026,14 +1078,15 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a)
     const bool wide = a.d > 128;
     const int sub = wide ? 0 : lane >> 5, subs = wide ? 1 : 2, q4 = wide ? lane : lane & 31;
     const bool has = 4 * q4 < a.d;
+    const int first = (R == 1 ? 0 : wave * subs) + sub, step = R * subs;
     float ll = 0.0f;
     float4_t o = {0, 0, 0, 0};
-    for (int s0 = sub; s0 < n; s0 += kJoin * subs) {
+    for (int s0 = first; s0 < n; s0 += kJoin * step) {
         float4_t p[kJoin];
         float2 st[kJoin];
 #pragma unroll
         for (int k = 0; k < kJoin; ++k) {
-            const int s = s0 + k * subs;
+            const int s = s0 + k * step;
             st[k] = make_float2(-__builtin_inff(), 0.0f);
             p[k] = float4_t{0, 0, 0, 0};
             if (s < n) {
@@ -1052,6 +1105,14 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a)
         ll = halves_sum(ll);
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] = halves_sum(o[e]);
+    }
+    if (R > 1) {
+        s_o[wave][lane] = o;
+        if (lane == 0) s_l[wave] = ll;
+        __syncthreads();
+        if (wave) return;
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) o += s_o[w][lane], ll += s_l[w];
     }
     const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
     if (has && sub == 0)
@@ -1106,7 +1167,7 @@ Shape shape_of(const fkv_page_desc* p, const fkv_attend_desc* t)
             s.blocks = heads;
             if (p->d <= 128 && heads <= kFewBlocks / 2 && tiles > kWaves) s.few_waves = 8;
         } else {
-            s.n_splits = (int)min((tiles + kWaves - 1) / kWaves + 1, max((int64_t)4, min((int64_t)128, 16 * kFewBlocks / heads)));
+            s.n_splits = (int)min((tiles + kLeastPiece - 1) / kLeastPiece + 1, max((int64_t)4, min((int64_t)512, 32 * kFewBlocks / heads)));
             s.blocks = kFewBlocks;
         }
         return s;
@@ -1205,16 +1266,17 @@ extern "C" int fkv_page_attend(const fkv_page_desc* desc, const fkv_attend_desc*
         auto of_width = [&](auto nc) {
             constexpr int NC = decltype(nc)::value;
             if (s.n_splits > 1) {
-                e4m3 ? go(attend_few_kernel<true, NC, 4, true>, 4) : go(attend_few_kernel<false, NC, 4, true>, 4);
+                auto kern = e4m3 ? attend_line_kernel<true, NC> : attend_line_kernel<false, NC>;
+                hipLaunchKernelGGL(kern, dim3((unsigned)s.blocks), dim3(kThreads), 0, st, a);
                 return;
             }
             if constexpr (NC <= 2) {
                 if (s.few_waves == 8) {
-                    e4m3 ? go(attend_few_kernel<true, NC, 8, false>, 8) : go(attend_few_kernel<false, NC, 8, false>, 8);
+                    e4m3 ? go(attend_few_kernel<true, NC, 8>, 8) : go(attend_few_kernel<false, NC, 8>, 8);
                     return;
                 }
             }
-            e4m3 ? go(attend_few_kernel<true, NC, 4, false>, 4) : go(attend_few_kernel<false, NC, 4, false>, 4);
+            e4m3 ? go(attend_few_kernel<true, NC, 4>, 4) : go(attend_few_kernel<false, NC, 4>, 4);
         };
         if (a.d <= 64) of_width(std::integral_constant<int, 1>{});
         else if (a.d <= 128) of_width(std::integral_constant<int, 2>{});
@@ -1260,9 +1322,10 @@ extern "C" int fkv_page_attend(const fkv_page_desc* desc, const fkv_attend_desc*
     }
     if (a.n_splits > 1) {
         const int64_t items = a.n_req * a.max_new * a.heads * a.group;
-        const int64_t blocks = (items + kWaves - 1) / kWaves;
+        const bool many = a.n_splits >= kManySplits;
+        const int64_t blocks = many ? items : (items + kWaves - 1) / kWaves;
         if (blocks > 0x7fffff00) return FKV_ERR_UNSUPPORTED;
-        hipLaunchKernelGGL(attend_join_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, st, a);
+        hipLaunchKernelGGL(many ? attend_join_kernel<kWaves> : attend_join_kernel<1>, dim3((unsigned)blocks), dim3(kThreads), 0, st, a);
     }
     return launch_status();
 }
