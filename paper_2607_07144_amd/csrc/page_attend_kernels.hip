@@ -669,6 +669,22 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 2 : 1) void attend_line_kernel(
 // wave takes its left operands from there.  A value channel's keys lie in LDS
 // in the order 0-3, 8-11, 4-7, 12-15 of each 16, which is the order in which a
 // lane's scores come out of the accumulator.  DP: channels, rounded up.
+//
+// Blocks go out request by request, the longest context first, so that no long
+// one is left for the end: of up to 64 requests, the one with z longer ones.
+__device__ __forceinline__ int64_t by_length(const AttendArgs& a, int z)
+{
+    if (a.n_req == 1 || a.n_req > 64) return z;
+    const int n = (int)a.n_req, lane = threadIdx.x & 63;
+    const int mine = lane < n ? a.kv_len[lane] : -1;
+    int longer = 0;
+    for (int j = 0; j < n; ++j) {
+        const int other = __builtin_amdgcn_readlane(mine, j);
+        longer += (other > mine) | ((other == mine) & (j < lane));
+    }
+    return __builtin_ctzll(__ballot(lane < n && longer == z));
+}
+
 template <int DP, int W>
 struct TileLds {
     static constexpr int kRow = DP + 8;       // of a key: channels
@@ -690,7 +706,7 @@ enum Scores { PLAIN, CAPPED, FULL };
 
 // ONE: pages of a multiple of 64 tokens; a tile then lies in one page, with one scale.
 template <bool E4M3, int DP, Scores SCORES, bool ONE, int W>
-__global__ __launch_bounds__(64 * W, DP <= 128 ? 2 : 1) void attend_tile_kernel(AttendArgs a)
+__global__ __launch_bounds__(64 * W, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) void attend_tile_kernel(AttendArgs a)
 {
     typedef TileLds<DP, W> Lds;
     constexpr int kThreads = 64 * W, kTileRows = 32 * W;
@@ -703,7 +719,7 @@ __global__ __launch_bounds__(64 * W, DP <= 128 ? 2 : 1) void attend_tile_kernel(
     const int c32 = lane & 31, hf = lane >> 5;
     const int split = (int)(blockIdx.x % a.n_splits);
     const int h = (int)(blockIdx.x / a.n_splits);
-    const int64_t r = blockIdx.z;
+    const int64_t r = by_length(a, blockIdx.z);
     const Request rq = request_of(a, r);
     const int n_rows = rq.rows * a.group;
     // the last rows see the most keys: they go first
