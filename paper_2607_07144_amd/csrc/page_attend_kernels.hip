@@ -16,9 +16,11 @@
 // row is taken times a power of two that brings its largest element near 2^13;
 // elements 2^27 times smaller than that round).  Key scales multiply the fp32
 // scores.  Value scales differ from page to page, so they multiply the fp32
-// weights before those are rounded to binary16: w = p * vs * 2^14 / vr with vr
+// weights before those are rounded to binary16: w = p * vs * 2^8 / vr with vr
 // the largest value scale so far, so that w keeps its 11 bits down to p vs / vr
-// = 2^-28; the accumulators carry the factor 2^14 / vr.
+// = 2^-22; the accumulators carry the factor 2^8 / vr.  m need not be the maximum
+// itself: it moves, and the accumulators with it, only when a score passes it by
+// more than 6, where w would near binary16's end.
 #include "page_common.h"
 
 #include <type_traits>
@@ -35,7 +37,8 @@ constexpr int kTile = 64;          // keys of a tile
 constexpr int kFewRows = 16;       // rows of the kernel for few rows
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
-constexpr float kTop = 16384.0f;   // 2^14: the largest weight
+constexpr float kTop = 256.0f;     // the weight of a key at the reference maximum, and
+constexpr float kSlack = 6.0f;     // how far scores may pass that before it moves: weights stay below 2^14
 constexpr float kLeast = 0x1p-100f;
 
 struct AttendArgs {
@@ -309,7 +312,7 @@ __device__ __forceinline__ FewRow few_row(const AttendArgs& a, const Request& rq
 }
 
 // Statistics and sums of a wave: lane 16g + c holds channels 16t + 4g .. + 3 of
-// row c in acc[t], times 2^14 / vref.
+// row c in acc[t], times 2^8 / vref.
 template <int NC>
 struct FewSums {
     float m, l, vref;
@@ -442,7 +445,7 @@ __device__ __forceinline__ void few_keys(const AttendArgs& a, const Request& rq,
 #pragma unroll
         for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
         top = rows_max(top);
-        if (__any(top > st.m || sc.y > st.vref)) {
+        if (__any(top > st.m + kSlack || sc.y > st.vref)) {
             const float vnew = rows_max(fmaxf(st.vref, sc.y));
             const float mnew = fmaxf(st.m, top);
             const float shrink = mnew == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(st.m - mnew);
@@ -696,7 +699,7 @@ struct TileLds {
 
 // PLAIN: neither cap nor bias; the scores then stay as the product gave them up
 // to the exponential, which takes their factor, the maximum and the value scale
-// in one multiply-add: w = 2^(s c - m + log2 v), v = vs 2^14 / vr, and sum w / v
+// in one multiply-add: w = 2^(s c - m + log2 v), v = vs 2^8 / vr, and sum w / v
 // is what l wants.  (v is held at 2^-40 from below: values of such a scale are
 // zeros, or too small for the sum to notice.)  CAPPED: a cap and no bias; then
 // y = cap (1 - 2 r) with r = 1 / (1 + e^2t), and r stays up to the exponential in
@@ -978,7 +981,7 @@ __global__ __launch_bounds__(64 * W, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) void atte
             vtop = fmaxf(vtop, sn[k].y);
         }
         top = halves_max(top);
-        if (__any(top > m || vtop > vref)) {
+        if (__any(top > m + kSlack || vtop > vref)) {
             const float mnew = fmaxf(m, top), vnew = fmaxf(vref, vtop);
             const float shrink = mnew == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m - mnew);
             l *= shrink;
