@@ -54,14 +54,15 @@ struct AttendArgs {
     const float* slopes;
     const int32_t* prefix;
     const int32_t* first;
-    float* part;    // [row][split][d] sums of a split's weights times values
-    float2* stat;   // [row][split] its maximum and sum of weights
-    int32_t* pieces; // [request][KV head] splits that the kernel for few rows made
+    float* part;    // [row][split][d] sums of a split's weights times values, or [piece][2][row][d]
+    float2* stat;   // likewise: their maximum and sum of weights
+    int2* pieces;   // [request][KV head] how many pieces of the line its tiles lie in, and the first
     int64_t n_req, n_tokens, max_new, max_kv, max_pages, n_pages;
     int64_t q_token, q_head, o_token, o_head;
     int32_t page, heads, group, d, window, sinks;
     int32_t bf16, causal;
     int32_t n_splits, split_tiles;
+    int32_t piece_rows;    // of a KV head: max_new x group
     uint32_t per_page;     // 16-key groups of a page
     uint32_t per_page_inv; // and their reciprocal, 2^32 / per_page rounded up (0: one)
     float scale, softcap;
@@ -97,7 +98,7 @@ __device__ __forceinline__ Seen seen_of(const AttendArgs& a, const Request& rq, 
     Seen s;
     s.lo = a.first ? max(a.first[rq.start + i], 0) : 0;
     s.hi = rq.kv;
-    if (a.causal) s.hi = min(rq.kv, max(pos + 1, a.prefix ? a.prefix[r] : 0));
+    if (a.causal) s.hi = min(rq.kv, max(pos + 1, a.prefix ? max(a.prefix[r], 0) : 0));
     s.wlo = a.window ? pos - a.window + 1 : 0;
     return s;
 }
@@ -535,14 +536,18 @@ __global__ __launch_bounds__(64 * W, NC <= 2 ? 2 : 1) void attend_few_kernel(Att
 // request by request and head by head, and every wave takes an equal piece of
 // it, so that a batch of any lengths keeps the whole chip busy to the end;
 // where a piece ends inside a head's keys its sums go to the workspace and are
-// joined by a second kernel.  The line's length is only known on the device:
-// each block forms the sum of the requests' tiles for itself.
+// joined by a second kernel.  A piece has two places there, one for the head that
+// began before it and one for the head that goes on behind it, so that the
+// workspace does not grow with the batch and heads may have any number of pieces.
+// The line's length is only known on the device: each block forms the sum of the
+// requests' tiles for itself.
 //
 // A request's tiles in the line: none without rows, else one at least, so that
 // a row that sees no key is written too.  Before each head's tiles stand kBegin
 // places that hold none: what beginning a head costs, in tiles.
 constexpr int kBegin = 3;
 constexpr int kLeastPiece = 2;   // tiles
+constexpr int kMostPieces = 512; // of a head
 
 __device__ __forceinline__ int line_tiles(const AttendArgs& a, int64_t r)
 {
@@ -598,15 +603,16 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 2 : 1) void attend_line_kernel(
         }
         s_sum[tid] = upto - sum;
         __syncthreads();
-        // equal pieces, as long as it takes for no head to be in more than n_splits of them
+        // equal pieces, as long as it takes for no head to be in more than kMostPieces of them
         const int64_t waves = (int64_t)gridDim.x * kWaves;
         total *= a.heads;
-        piece = max((total + waves - 1) / waves, (int64_t)(most - 1 + a.n_splits - 2) / (a.n_splits - 1));
+        piece = max((total + waves - 1) / waves, (int64_t)(most - 1 + kMostPieces - 2) / (kMostPieces - 1));
         piece = uniform(max(piece, (int64_t)(kBegin + kLeastPiece)));
     }
     // this wave's piece [f, f1) of the line, the request r that it begins in and a head's places before r
     // (neighbouring pieces in different blocks: a short line is spread over all compute units)
-    int64_t f = ((int64_t)wave * gridDim.x + blockIdx.x) * piece;
+    const int64_t number = (int64_t)wave * gridDim.x + blockIdx.x;
+    int64_t f = number * piece;
     const int64_t f1 = uniform(min(f + piece, total));
     if (f >= f1) return;
     int lo = 0, hi = kThreads;   // the last thread whose requests begin at or before f
@@ -640,12 +646,12 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 2 : 1) void attend_line_kernel(
         const FewRow fr = few_row(a, rq, h);
         FewSums<NC> st;
         if (e0 < e1) few_keys<E4M3, NC>(a, rq, r, h, tl, fr, e0, 1, e1, st);
-        if (split == 0 && lane == 0) a.pieces[r * a.heads + h] = n_split;
+        if (split == 0 && lane == 0) a.pieces[r * a.heads + h] = make_int2(n_split, (int)number);
         if (c16 >= rq.rows * a.group) continue;
         const int64_t token = rq.start + fr.tok;
         if (n_split > 1) {
             const float back = st.vref * (1.0f / kTop);
-            const int64_t at = (token * q_heads + fr.head) * a.n_splits + split;
+            const int64_t at = (2 * number + (split == 0)) * a.piece_rows + fr.row;
 #pragma unroll
             for (int t = 0; t < 4 * NC; ++t)
                 if (t * 16 < d) *(float4_t*)(a.part + at * d + t * 16 + g * 4) = st.acc[t] * back;
@@ -1084,12 +1090,16 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a)
     const int64_t hq = item % q_heads;
     const Request rq = request_of(a, r);
     if (i >= rq.rows) return;
-    const int n = a.pieces ? a.pieces[r * a.heads + hq / a.group] : a.n_splits;
+    const int2 piece = a.pieces ? a.pieces[r * a.heads + hq / a.group] : make_int2(a.n_splits, 0);
+    const int n = piece.x;
     if (a.pieces && n == 1) return;   // written already
     const int64_t token = rq.start + i;
-    const int64_t at = (token * q_heads + hq) * a.n_splits;
+    // where split s lies: the first piece's sums in its second place, the others' in their first
+    const int64_t at = a.pieces ? 2 * (int64_t)piece.y * a.piece_rows + i * a.group + hq % a.group : (token * q_heads + hq) * a.n_splits;
+    const int64_t per_split = a.pieces ? 2 * a.piece_rows : 1, of_first = a.pieces ? a.piece_rows : 0;
+    auto place = [&](int s) { return at + s * per_split + (s ? 0 : of_first); };
     float mm = -__builtin_inff();
-    for (int s = lane; s < n; s += 64) mm = fmaxf(mm, a.stat[at + s].x);
+    for (int s = lane; s < n; s += 64) mm = fmaxf(mm, a.stat[place(s)].x);
     mm = halves_max(mm);
 #pragma unroll
     for (int k = 1; k < 32; k <<= 1) mm = fmaxf(mm, __shfl_xor(mm, k, 64));
@@ -1109,8 +1119,8 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a)
             st[k] = make_float2(-__builtin_inff(), 0.0f);
             p[k] = float4_t{0, 0, 0, 0};
             if (s < n) {
-                st[k] = a.stat[at + s];
-                if (has) p[k] = *(const float4_t*)(a.part + (at + s) * a.d + 4 * q4);
+                st[k] = a.stat[place(s)];
+                if (has) p[k] = *(const float4_t*)(a.part + place(s) * a.d + 4 * q4);
             }
         }
 #pragma unroll
@@ -1148,15 +1158,16 @@ struct Shape {
     int64_t row_blocks;   // and its blocks of a request and KV head
     int64_t blocks;       // of the kernel for few rows,
     int few_waves;        // and their waves
-    int n_splits, split_tiles;
+    int n_splits, split_tiles;   // (few rows: 1, or more than 1 for the line)
+    bool join_blocks;     // a block joins a row's splits, not a wave
 };
 
 constexpr int64_t kFewBlocks = 512;   // two on each compute unit
 
 // The kernel for few rows where a KV head's rows fit one of its blocks.  Its
 // keys are split where the heads alone leave compute units idle or the longest
-// request may hold up the rest; how the tiles are dealt is settled on the device,
-// with at most n_splits splits of a head.  The other kernel's keys are split so
+// request may hold up the rest; how the tiles are dealt is settled on the device.
+// The other kernel's keys are split so
 // that about four hundred blocks are there, with four tiles for a block at the
 // least.
 Shape shape_of(const fkv_page_desc* p, const fkv_attend_desc* t)
@@ -1186,8 +1197,9 @@ Shape shape_of(const fkv_page_desc* p, const fkv_attend_desc* t)
             s.blocks = heads;
             if (p->d <= 128 && heads <= kFewBlocks / 2 && tiles > kWaves) s.few_waves = 8;
         } else {
-            s.n_splits = (int)min((tiles + kLeastPiece - 1) / kLeastPiece + 1, max((int64_t)4, min((int64_t)512, 32 * kFewBlocks / heads)));
+            s.n_splits = 2;
             s.blocks = kFewBlocks;
+            s.join_blocks = heads <= kFewBlocks && tiles >= kManySplits * kLeastPiece;
         }
         return s;
     }
@@ -1196,6 +1208,7 @@ Shape shape_of(const fkv_page_desc* p, const fkv_attend_desc* t)
     const int64_t n = max((int64_t)1, min(want, most));
     s.split_tiles = (int)((tiles + n - 1) / n);
     s.n_splits = (int)((tiles + s.split_tiles - 1) / s.split_tiles);
+    s.join_blocks = s.n_splits >= kManySplits;
     return s;
 }
 
@@ -1211,7 +1224,7 @@ bool attend_ok(const fkv_page_desc* p, const fkv_attend_desc* t)
            (t->causal == 0 || t->causal == 1) && t->window >= 0 && t->window <= kMost && t->sinks >= 0 && t->sinks <= kMost;
 }
 
-// The workspace: sums, then maxima and sums of weights, then the few-row kernel's counts.
+// The workspace: sums, then maxima and sums of weights, then the heads' pieces of the line.
 struct Workspace {
     size_t stat, pieces, bytes;
 };
@@ -1219,11 +1232,12 @@ struct Workspace {
 Workspace workspace_of(const fkv_page_desc* p, const fkv_attend_desc* t, const Shape& s)
 {
     if (s.n_splits == 1) return Workspace{0, 0, 0};
-    const size_t rows = (size_t)t->n_tokens * t->q_heads * s.n_splits;
+    const size_t rows = s.few ? (size_t)s.blocks * kWaves * 2 * (t->max_new * (t->q_heads / p->heads))
+                              : (size_t)t->n_tokens * t->q_heads * s.n_splits;
     Workspace w;
     w.stat = rows * p->d * sizeof(float);
     w.pieces = w.stat + rows * sizeof(float2);
-    w.bytes = w.pieces + (s.few ? (size_t)t->n_req * p->heads * sizeof(int32_t) : 0);
+    w.bytes = w.pieces + (s.few ? (size_t)t->n_req * p->heads * sizeof(int2) : 0);
     return w;
 }
 
@@ -1262,7 +1276,7 @@ extern "C" int fkv_page_attend(const fkv_page_desc* desc, const fkv_attend_desc*
     a.slopes = slopes, a.prefix = prefix, a.first = first;
     a.part = (float*)workspace;
     a.stat = (float2*)((uint8_t*)workspace + ws.stat);
-    a.pieces = ws.bytes && s.few ? (int32_t*)((uint8_t*)workspace + ws.pieces) : nullptr;
+    a.pieces = ws.bytes && s.few ? (int2*)((uint8_t*)workspace + ws.pieces) : nullptr;
     a.n_req = attend->n_req, a.n_tokens = attend->n_tokens, a.max_new = attend->max_new, a.max_kv = attend->max_kv;
     a.max_pages = attend->max_pages, a.n_pages = desc->n_pages;
     a.q_token = attend->q_stride_token, a.q_head = attend->q_stride_head;
@@ -1271,6 +1285,7 @@ extern "C" int fkv_page_attend(const fkv_page_desc* desc, const fkv_attend_desc*
     a.window = attend->window, a.sinks = attend->sinks;
     a.bf16 = attend->type, a.causal = attend->causal;
     a.n_splits = s.n_splits, a.split_tiles = s.split_tiles;
+    a.piece_rows = s.few ? (int32_t)(attend->max_new * a.group) : 0;
     a.per_page = (uint32_t)(desc->page / 16);
     a.per_page_inv = a.per_page == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + a.per_page - 1) / a.per_page);
     a.scale = attend->scale, a.softcap = attend->softcap;
@@ -1341,10 +1356,9 @@ extern "C" int fkv_page_attend(const fkv_page_desc* desc, const fkv_attend_desc*
     }
     if (a.n_splits > 1) {
         const int64_t items = a.n_req * a.max_new * a.heads * a.group;
-        const bool many = a.n_splits >= kManySplits;
-        const int64_t blocks = many ? items : (items + kWaves - 1) / kWaves;
+        const int64_t blocks = s.join_blocks ? items : (items + kWaves - 1) / kWaves;
         if (blocks > 0x7fffff00) return FKV_ERR_UNSUPPORTED;
-        hipLaunchKernelGGL(many ? attend_join_kernel<kWaves> : attend_join_kernel<1>, dim3((unsigned)blocks), dim3(kThreads), 0, st, a);
+        hipLaunchKernelGGL(s.join_blocks ? attend_join_kernel<kWaves> : attend_join_kernel<1>, dim3((unsigned)blocks), dim3(kThreads), 0, st, a);
     }
     return launch_status();
 }
