@@ -526,30 +526,31 @@ __global__ __launch_bounds__(kThreads, 3) void page_store_kernel(PageArgs a, Row
     }
 }
 
-// 64 rows of the call a wave, of one head and one of K and V.  The rows of one
+// 64 rows of the call a wave (`window`: 16 where rows are few, so that a wave's
+// columns do not wait for one another), of one head and one of K and V.  The rows of one
 // 16-token group that follow one another are a segment; their columns are read
 // 16 at a time, keys 8 bytes a lane and row, values a channel's 16 tokens in 16
 // bytes and then exchanged.  What bounds it is memory: four contexts of 32,732
 // tokens, 8 heads of 128, 162 us (805 MB, 5.0 TB/s, the rate of a copy).
 template <bool E4M3, bool BF16>
-__global__ __launch_bounds__(kThreads) void page_load_kernel(PageArgs a, Rows kr, Rows vr)
+__global__ __launch_bounds__(kThreads) void page_load_kernel(PageArgs a, Rows kr, Rows vr, int window)
 {
     __shared__ uint32_t s_seg[kThreads / 64][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c16 = lane & 15, tq = lane >> 4;
-    const int64_t n_win = (a.n_tokens + 63) / 64;
+    const int64_t n_win = (a.n_tokens + window - 1) / window;
     const int64_t item = (int64_t)blockIdx.x * (kThreads / 64) + wave;
     if (item >= n_win * a.heads) return;
     const bool values = blockIdx.y ? true : kr.at == nullptr;
     const Rows rows = values ? vr : kr;
     const int h = (int)((uint32_t)item % (uint32_t)a.heads);
-    const int64_t w0 = (int64_t)((uint32_t)item / (uint32_t)a.heads) * 64;
+    const int64_t w0 = (int64_t)((uint32_t)item / (uint32_t)a.heads) * window;
     const uint32_t chunks = a.d / 8;
     const int64_t pool = a.n_pages * a.page;
     uint32_t* seg = s_seg[wave];
 
     // segments: first row, and how many
-    const int n = (int)min((int64_t)64, a.n_tokens - w0);
+    const int n = (int)min((int64_t)window, a.n_tokens - w0);
     int64_t slot = -1;
     if (lane < n) slot = a.slots[w0 + lane];
     if (slot >= pool || slot < 0) slot = -1;
@@ -692,13 +693,16 @@ extern "C" int fkv_page_load(const fkv_page_desc* desc, const uint8_t* k_codes, 
     if (!slots || !aligned(slots, 8)) return FKV_ERR_INVALID_ARG;
     const PageArgs a = {(uint8_t*)k_codes, (uint8_t*)v_codes, (float2*)scales, slots, n_tokens,
                         desc->n_pages, desc->page, desc->heads, desc->d};
-    const int64_t items = (n_tokens + 63) / 64 * desc->heads;
+    // with 16 and 64 rows a wave (us): 1024 tokens x 12 heads of 64 4.6 and 6.5, 2730 7.2 and 8.0, 5461 11.5 and 9.6;
+    // 1024 x 8 of 128 5.5 and 8.8, 2730 8.3 and 10.5, 5461 12.5 and 14.4, 8192 17.6 and 14.1
+    const int window = n_tokens * desc->heads <= 32768 ? 16 : 64;
+    const int64_t items = (n_tokens + window - 1) / window * desc->heads;
     const int64_t blocks = (items + kThreads / 64 - 1) / (kThreads / 64);
     if (items > kMostBlocks) return FKV_ERR_UNSUPPORTED;
     const bool e4m3 = desc->format == FKV_PAGE_E4M3, bf16 = (k_rows ? rows_k : rows_v)->type == FKV_ROW_BF16;
     auto kern = e4m3 ? bf16 ? page_load_kernel<true, true> : page_load_kernel<true, false>
                      : bf16 ? page_load_kernel<false, true> : page_load_kernel<false, false>;
     hipLaunchKernelGGL(kern, dim3((unsigned)blocks, k_rows && v_rows ? 2 : 1), dim3(kThreads), 0, (hipStream_t)stream, a,
-                       rows_of(rows_k, k_rows), rows_of(rows_v, v_rows));
+                       rows_of(rows_k, k_rows), rows_of(rows_v, v_rows), window);
     return launch_status();
 }
