@@ -12,6 +12,16 @@ typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
 constexpr float kLargestInt8 = 127.0f;
 constexpr float kLargestE4m3 = 448.0f;
 
+// Orders what the lanes of a wave wrote before it, in LDS or memory, before what
+// any of them reads after it.  (A wave's operations are performed in order: it
+// keeps the compiler to that order and costs no instruction.)
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // Four codes of a 32-bit word as fp32.
 template <bool E4M3>
 __device__ __forceinline__ void codes_to_f32(uint32_t w, float (&f)[4])

@@ -460,6 +460,7 @@ __global__ __launch_bounds__(kThreads, 3) void page_store_kernel(PageArgs a, Row
                 }
             }
         }
+        wave_sync();   // every lane has read the scale, and words of which others write bytes
         if (lane == 0) *sp = s;
         const float inv = s > 0.0f ? 1.0f / s : 0.0f;
         for (int base = 0; base < columns; base += 16 * kPasses) {
@@ -562,6 +563,7 @@ __global__ __launch_bounds__(kThreads) void page_load_kernel(PageArgs a, Rows kr
         const int len = (later ? __builtin_ctzll(later) + 1 : n - lane);
         seg[__builtin_popcountll(begins & ((1ull << lane) - 1))] = (uint32_t)lane | (uint32_t)len << 8;
     }
+    wave_sync();   // the segments' lanes wrote, every lane reads
     const int columns = __builtin_popcountll(begins) * (int)chunks;
     const RowsFrom from(rows, w0, h);
     for (int base = 0; base < columns; base += 16) {
