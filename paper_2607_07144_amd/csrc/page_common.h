@@ -75,20 +75,16 @@ __device__ __forceinline__ uint32_t near_codes(const float (&f)[4])
     return __builtin_amdgcn_perm(hi, lo, 0x05040100u);
 }
 
-// Four codes of a word times a scale, each product rounded once.
+// Four codes of a word times a scale, each product rounded once.  (An int8 code is
+// taken as what it is: through a bias of 128, 128 times the scale of the largest
+// bfloat16 rows is beyond fp32 where code times scale is not.)
 template <bool E4M3>
 __device__ __forceinline__ void scaled_codes(uint32_t w, float s, float* f)
 {
-    if (E4M3) {
-        float c[4];
-        codes_to_f32<true>(w, c);
+    float c[4];
+    codes_to_f32<E4M3>(w, c);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) f[e] = c[e] * s;
-        return;
-    }
-    w ^= 0x80808080u;   // c + 128, 0..255
-#pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] = __builtin_fmaf((float)((w >> (8 * e)) & 0xff), s, -128.0f * s);
+    for (int e = 0; e < 4; ++e) f[e] = c[e] * s;
 }
 
 // Element e of a packed pair of row elements as fp32, and back (one rounding,

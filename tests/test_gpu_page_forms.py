@@ -39,3 +39,25 @@ def test_load_of_many_rows_in_no_order(fkv, codes, rows):
     slots[[5, 64, 1000]] = -1, 135 * 16, -7
     assert 2101 * 16 > 32768
     check_load(fkv, pool, slots, rows)
+
+
+@pytest.mark.parametrize("codes", [INT8, E4M3])
+def test_the_largest_bfloat16_rows_come_back(fkv, codes):
+    """Pages whose largest element is the largest bfloat16 number, its negative or the one below it: code * scale is
+    finite for every code, and so is what is read back, beside zeros and small elements too."""
+    top = torch.finfo(torch.bfloat16).max
+    below = torch.tensor([0x7f7e], dtype=torch.int16).view(torch.bfloat16).float().item()
+    x = torch.zeros((64, 2, 16), dtype=torch.bfloat16)
+    x[0, :, 0], x[1, :, 1], x[2, :, 2:9], x[3, 0] = top, -top, 1.0, torch.linspace(-top, top, 16).bfloat16()
+    x[16, :, 3], x[17] = below, 7.0e37
+    x[32, :, 3], x[33] = -top, -1.7e38
+    x[48:] = top
+    for n in (64, 1):      # the second with a row a page
+        pages = fkv.fkv_pages(4, 16, 2, 16, codes)
+        slots = torch.arange(64) if n == 64 else torch.arange(4) * 16
+        rows = x[slots]
+        fkv.fkv_page_store(pages, rows.cuda(), rows.flip(2).contiguous().cuda(), slots.cuda())
+        for got, every in zip(fkv.fkv_page_load(pages, slots.cuda(), torch.bfloat16), ref.values(*(t.cpu() for t in pages))):
+            want = every[slots // 16, :, slots % 16]
+            assert got.isfinite().all()
+            assert ((got.cpu().double() - want).abs() <= want.abs() * (2.0 ** -8 + 2.0 ** -23)).all()
