@@ -40,6 +40,9 @@ constexpr float kLn2 = 0.69314718055994530942f;
 constexpr float kTop = 256.0f;     // the weight of a key at the reference maximum, and
 constexpr float kSlack = 6.0f;     // how far scores may pass that before it moves: weights stay below 2^14
 constexpr float kLeast = 0x1p-100f;
+// Sums of weights times values that are to be joined with others are kept times 2^-30: bfloat16 values may be near
+// fp32's end, where a sum of a few of them is beyond it and their mean is not (2^24 keys of weights up to 2^6).
+constexpr float kPart = 0x1p-30f;
 
 struct AttendArgs {
     const uint8_t* k_codes;
@@ -54,7 +57,7 @@ struct AttendArgs {
     const float* slopes;
     const int32_t* prefix;
     const int32_t* first;
-    float* part;    // [row][split][d] sums of a split's weights times values, or [piece][2][row][d]
+    float* part;    // [row][split][d] sums of a split's weights times values, times kPart, or [piece][2][row][d]
     float2* stat;   // likewise: their maximum and sum of weights
     int2* pieces;   // [request][KV head] how many pieces of the line its tiles lie in, and the first
     int64_t n_req, n_tokens, max_new, max_kv, max_pages, n_pages;
@@ -502,11 +505,10 @@ __global__ __launch_bounds__(64 * W, NC <= 2 ? 2 : 1) void attend_few_kernel(Att
     float* s_acc = lds + 2 * W * kFewRows;
     const int ld = d + 4;
     if (g == 0) s_m[wave * kFewRows + c16] = st.m, s_l[wave * kFewRows + c16] = st.l;
-    const float back = st.vref * (1.0f / kTop);
     if (c16 < n_rows) {
 #pragma unroll
         for (int t = 0; t < 4 * NC; ++t)
-            if (t * 16 < d) *(float4_t*)(s_acc + (wave * kFewRows + c16) * ld + t * 16 + g * 4) = st.acc[t] * back;
+            if (t * 16 < d) *(float4_t*)(s_acc + (wave * kFewRows + c16) * ld + t * 16 + g * 4) = st.acc[t] * (kPart / kTop) * st.vref;
     }
     __syncthreads();
     const int quads = d / 4;
@@ -526,7 +528,7 @@ __global__ __launch_bounds__(64 * W, NC <= 2 ? 2 : 1) void attend_few_kernel(Att
         }
         const int64_t token = rq.start + rw / a.group;
         const int hq = h * a.group + rw % a.group;
-        const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
+        const float inv = ll == 0.0f ? 0.0f : (1.0f / kPart) / ll;
         *(uint2*)(a.out + 2 * (token * a.o_token + hq * a.o_head + 4 * q4)) =
             make_uint2(f32_to_row2(o[0] * inv, o[1] * inv, a.bf16), f32_to_row2(o[2] * inv, o[3] * inv, a.bf16));
         if (q4 == 0 && a.lse) a.lse[token * q_heads + hq] = ll == 0.0f ? -__builtin_inff() : kLn2 * (mm + __log2f(ll));
@@ -654,11 +656,10 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 2 : 1) void attend_line_kernel(
         if (c16 >= rq.rows * a.group) continue;
         const int64_t token = rq.start + fr.tok;
         if (n_split > 1) {
-            const float back = st.vref * (1.0f / kTop);
             const int64_t at = (2 * number + (split == 0)) * a.piece_rows + fr.row;
 #pragma unroll
             for (int t = 0; t < 4 * NC; ++t)
-                if (t * 16 < d) *(float4_t*)(a.part + at * d + t * 16 + g * 4) = st.acc[t] * back;
+                if (t * 16 < d) *(float4_t*)(a.part + at * d + t * 16 + g * 4) = st.acc[t] * (kPart / kTop) * st.vref;
             if (g == 0) a.stat[at] = make_float2(st.m, st.l);
         } else {
             const float inv = st.l == 0.0f ? 0.0f : st.vref * (1.0f / kTop) / st.l;
@@ -1044,7 +1045,6 @@ __global__ __launch_bounds__(64 * W, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) void atte
     l = halves_sum(l);
     if (!used) return;
     const int64_t token = rq.start + tok;
-    const float back = vref * (1.0f / kTop);
     if (a.n_splits > 1) {
         const int64_t at = (token * q_heads + head) * a.n_splits + split;
         if (hf == 0) a.stat[at] = make_float2(m, l);
@@ -1055,11 +1055,11 @@ __global__ __launch_bounds__(64 * W, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) void atte
                 const int ch = t * 32 + i * 8 + hf * 4;
                 if (ch < d)
                     *(float4_t*)(a.part + at * d + ch) =
-                        float4_t{acc[t][4 * i], acc[t][4 * i + 1], acc[t][4 * i + 2], acc[t][4 * i + 3]} * back;
+                        float4_t{acc[t][4 * i], acc[t][4 * i + 1], acc[t][4 * i + 2], acc[t][4 * i + 3]} * (kPart / kTop) * vref;
             }
         return;
     }
-    const float inv = l == 0.0f ? 0.0f : back / l;
+    const float inv = l == 0.0f ? 0.0f : vref * (1.0f / kTop) / l;
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t)
 #pragma unroll
@@ -1150,7 +1150,7 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a)
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) o += s_o[w][lane], ll += s_l[w];
     }
-    const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
+    const float inv = ll == 0.0f ? 0.0f : (1.0f / kPart) / ll;
     if (has && sub == 0)
         *(uint2*)(a.out + 2 * (token * a.o_token + hq * a.o_head + 4 * q4)) =
             make_uint2(f32_to_row2(o[0] * inv, o[1] * inv, a.bf16), f32_to_row2(o[2] * inv, o[3] * inv, a.bf16));

@@ -1,4 +1,6 @@
 """The paged 8-bit cache at the sizes where its calls take another form: many rows, many requests, long and wide rows."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -61,3 +63,34 @@ def test_the_largest_bfloat16_rows_come_back(fkv, codes):
             want = every[slots // 16, :, slots % 16]
             assert got.isfinite().all()
             assert ((got.cpu().double() - want).abs() <= want.abs() * (2.0 ** -8 + 2.0 ** -23)).all()
+
+
+def check_pool(fkv, pool, q, tables, kv, q_start, max_new, max_kv, bound=None, **opt):
+    """fkv_page_attend of a CPU pool against 64 bits, within the reference's bounds."""
+    k, v, scales = pool
+    want, lse, off, loff = ref.attend(k, v, scales, q, tables, kv, q_start, q.shape[2] ** -0.5, **opt)
+    dopt = {name: (x.cuda() if isinstance(x, torch.Tensor) else x) for name, x in opt.items()}
+    got, glse = fkv.fkv_page_attend(fkv.Pages(k.cuda(), v.cuda(), scales.cuda()), q.cuda(), tables.cuda(), kv.cuda(),
+                                    q_start.cuda(), max_new, max_kv, want_lse=True, **dopt)
+    got, glse = got.cpu().double(), glse.cpu().double()
+    u = 2.0 ** -11 if q.dtype == torch.float16 else 2.0 ** -8
+    empty = lse == -math.inf
+    assert torch.equal(glse == -math.inf, empty) and not got[empty].any()
+    worst = ((got - want).abs() / (off + u * (want.abs() + off) + 2.0 ** -24)).max()
+    assert worst <= 1, float(worst)
+    assert ((glse - lse).abs()[~empty] <= loff[~empty]).all()
+
+
+@pytest.mark.parametrize("codes", [INT8, E4M3])
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("kv,new", [(200, 1), (1000, 1), (3000, 2), (9000, 1), (200, 40), (9000, 40)])
+def test_attend_values_near_the_end_of_bfloat16(fkv, codes, page, kv, new):
+    """Values of 1e38: a sum of a few of them is beyond fp32, their weighted mean is not, however the keys are split."""
+    n_pages = -(-kv // page)
+    k, v, scales = random_pages(n_pages, page, 2, 64, codes, 3)
+    v = (v.float().abs() + (20 if codes == INT8 else 16)).clamp(max=ref.LARGEST[codes]).to(codes)
+    scales[:, :, 1] = 2.6e38 / ref.LARGEST[codes] * (0.3 + 0.7 * torch.rand((n_pages, 2)))
+    q = torch.randn((new, 4, 64), generator=torch.Generator().manual_seed(4)).to(torch.bfloat16) * 0.02
+    tables = torch.randperm(n_pages, generator=torch.Generator().manual_seed(5)).int()[None]
+    check_pool(fkv, (k, v, scales), q, tables, torch.tensor([kv], dtype=torch.int32), torch.tensor([0, new], dtype=torch.int32),
+               new, kv)
