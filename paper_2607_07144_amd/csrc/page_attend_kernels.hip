@@ -17,8 +17,8 @@
 // elements 2^27 times smaller than that round).  Key scales multiply the fp32
 // scores.  Value scales differ from page to page, so they multiply the fp32
 // weights before those are rounded to binary16: w = p * vs * 2^8 / vr with vr
-// the largest value scale so far, so that w keeps its 11 bits down to p vs / vr
-// = 2^-22; the accumulators carry the factor 2^8 / vr.  m need not be the maximum
+// the largest value scale so far of what the row sees, so that w keeps its 11
+// bits down to p vs / vr = 2^-22; the accumulators carry the factor 2^8 / vr.  m need not be the maximum
 // itself: it moves, and the accumulators with it, only when a score passes it by
 // more than 6, where w would near binary16's end.
 #include "page_common.h"
@@ -448,9 +448,10 @@ __device__ __forceinline__ void few_keys(const AttendArgs& a, const Request& rq,
         float top = x[0];
 #pragma unroll
         for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+        const float vtop = top > -__builtin_inff() ? sc.y : 0.0f;   // of a group of which the row sees a key
         top = rows_max(top);
-        if (__any(top > st.m + kSlack || sc.y > st.vref)) {
-            const float vnew = rows_max(fmaxf(st.vref, sc.y));
+        if (__any(top > st.m + kSlack || vtop > st.vref)) {
+            const float vnew = rows_max(fmaxf(st.vref, vtop));
             const float mnew = fmaxf(st.m, top);
             const float shrink = mnew == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(st.m - mnew);
             st.l *= shrink;
@@ -461,7 +462,7 @@ __device__ __forceinline__ void few_keys(const AttendArgs& a, const Request& rq,
             st.vref = vnew;
         }
         const float m0 = st.m == -__builtin_inff() ? 0.0f : st.m;
-        const float vs = sc.y * (kTop / st.vref);
+        const float vs = fminf(sc.y * (kTop / st.vref), kTop);   // (beyond that only where all weights are 0)
         half8_t p[2];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -983,6 +984,7 @@ __global__ __launch_bounds__(64 * W, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) void atte
             }
         }
         float top = -__builtin_inff(), vtop = -1.0f;
+        float tops[G];
 #pragma unroll
         for (int k = 0; k < G; ++k) {
             constexpr int n = 32 / G;
@@ -992,8 +994,15 @@ __global__ __launch_bounds__(64 * W, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) void atte
                 t = SCORES == CAPPED ? __builtin_elementwise_minimum(t, x[n * k + i]) : __builtin_elementwise_maximum(t, x[n * k + i]);
             top = __builtin_elementwise_maximum(top, SCORES == PLAIN ? t * c[k] : SCORES == CAPPED ? __builtin_fmaf(t, c[k], cap2) : t);
             vtop = fmaxf(vtop, sn[k].y);
+            tops[k] = t;
         }
         top = halves_max(top);
+        if (mask) {   // only of parts of which the row sees a key
+            vtop = -1.0f;
+#pragma unroll
+            for (int k = 0; k < G; ++k) vtop = fmaxf(vtop, tops[k] != kHidden ? sn[k].y : -1.0f);
+            vtop = halves_max(vtop);
+        }
         if (__any(top > m + kSlack || vtop > vref)) {
             const float mnew = fmaxf(m, top), vnew = fmaxf(vref, vtop);
             const float shrink = mnew == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m - mnew);
@@ -1009,7 +1018,7 @@ __global__ __launch_bounds__(64 * W, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) void atte
         float vb[G], vinv[G];
 #pragma unroll
         for (int k = 0; k < G; ++k) {
-            const float v = fmaxf(sn[k].y * vmul, 0x1p-40f);
+            const float v = __builtin_amdgcn_fmed3f(sn[k].y * vmul, 0x1p-40f, kTop);   // (more only where nothing is seen)
             vb[k] = __builtin_amdgcn_logf(v) - m0 + (SCORES == CAPPED ? cap2 : 0.0f);
             vinv[k] = __builtin_amdgcn_rcpf(v);
         }

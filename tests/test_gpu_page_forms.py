@@ -94,3 +94,32 @@ def test_attend_values_near_the_end_of_bfloat16(fkv, codes, page, kv, new):
     tables = torch.randperm(n_pages, generator=torch.Generator().manual_seed(5)).int()[None]
     check_pool(fkv, (k, v, scales), q, tables, torch.tensor([kv], dtype=torch.int32), torch.tensor([0, new], dtype=torch.int32),
                new, kv)
+
+
+@pytest.mark.parametrize("codes,rows", [(INT8, torch.float16), (E4M3, torch.bfloat16)])
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("opt", [{}, dict(softcap=30.0), dict(slopes=True)])
+@pytest.mark.parametrize("new", [1, 4, 300])
+def test_attend_large_values_behind_a_mask(fkv, codes, rows, page, opt, new):
+    """A row's result has the same bits of accuracy whatever the values that its mask hides: documents of values 2^25 times
+    those of the next or more, and a last one, which the rows before it do not see yet."""
+    kv, n_pages = 448, 448 // page
+    k, v, scales = random_pages(n_pages, page, 2, 64, codes, 6)
+    # (binary16 results of both kinds of documents have to stay within its range)
+    large, small = (2.0 ** 11, 2.0 ** -14) if new == 300 and rows == torch.float16 else (2.0 ** 40, 2.0 ** -9)
+    size = torch.full((448,), small)
+    cut = 208 if page == 16 else 192                  # (inside a tile of 64 keys where a page may end there)
+    size[:cut], size[384:] = large, large     # tokens of the first document, and of the last
+    scales[:, :, 1] *= size[::page, None]
+    tables = torch.arange(n_pages, dtype=torch.int32)[None]
+    last = kv if new == 300 else 384 - 9              # (few rows: none of the last document's)
+    pos = torch.arange(last - new, last)
+    first = torch.where(pos < cut, 0, torch.where(pos < 384, cut, 384)).int()
+    q = torch.randn((new, 4, 64), generator=torch.Generator().manual_seed(7)).to(rows) * 0.1
+    opt = dict(opt)
+    if opt.pop("slopes", False):
+        opt["slopes"] = torch.tensor([0.001, 0.01, 0.02, 0.1])
+    check_pool(fkv, (k, v, scales), q, tables, torch.tensor([last], dtype=torch.int32), torch.tensor([0, new], dtype=torch.int32),
+               new, last, first=first, **opt)
+    check_pool(fkv, (k, v, scales), q, tables, torch.tensor([last], dtype=torch.int32), torch.tensor([0, new], dtype=torch.int32),
+               new, last, window=100, **opt)
