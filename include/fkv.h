@@ -475,7 +475,8 @@ int fkv_page_load(const fkv_page_desc* desc, const uint8_t* k_codes, const uint8
  *   workspace       device scratch of fkv_page_attend_workspace() bytes, 16-byte
  *                   aligned; null when that is 0.  Calls that may run at the
  *                   same time need one each.
- * Scores, statistics and sums are fp32; the products run on matrix cores with
+ * Scores, statistics and sums are fp32, with the cap within 2^-21 of softcap (of
+ * 128 at most) or 2^-20 of y (beyond); the products run on matrix cores with
  * the codes and q exact in binary16 (a bfloat16 row is taken times a power of
  * two) and the weights rounded to binary16.  FKV_ERR_INVALID_ARG also for
  * q_heads not a multiple of heads; FKV_ERR_SCRATCH_TOO_SMALL for a workspace

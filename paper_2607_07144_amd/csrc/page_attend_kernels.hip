@@ -272,11 +272,28 @@ __device__ __forceinline__ float rows_sum(float a)
 }
 
 // cap * tanh(x / cap) in base 2, u being twice the tanh's argument in base 2:
-// tanh t = 1 - 2 / (1 + e^2t).
+// tanh t = 1 - 2 / (1 + e^2t).  For small t that is the difference of two numbers
+// near 1, so the error is of the size of the cap, about 2^-23 of it: a score's is
+// about 2^-16 for the caps up to kSmallCap that take this form.
+constexpr float kSmallCap = 128.0f;
+
 __device__ __forceinline__ float capped(float u, float cap)
 {
     const float e = __builtin_amdgcn_exp2f(u);
     return cap * (1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + e));
+}
+
+// The same of a larger cap, x being the score in base 2: below |t| = 0.4 the series
+// x (1 - t^2 / 3 + 2 t^4 / 15 - ..) to t^10, which ends within 2^-24 of itself, and the
+// form above beyond, where its error is 2^-21 of the result.
+__device__ __forceinline__ float capped_large(float x, float cap, float inv_cap)
+{
+    const float t = x * inv_cap, q = t * t;
+    float p = __builtin_fmaf(q, -1382.0f / 155925.0f, 62.0f / 2835.0f);
+    p = __builtin_fmaf(q, p, -17.0f / 315.0f);
+    p = __builtin_fmaf(q, p, 2.0f / 15.0f);
+    p = __builtin_fmaf(q, p, -1.0f / 3.0f);
+    return fabsf(t) < 0.4f ? __builtin_fmaf(x * q, p, x) : capped(t * (2.0f * kLog2e), cap);
 }
 
 // ------------------------------------------------------------- few rows --
@@ -387,7 +404,8 @@ __device__ __forceinline__ void few_keys(const AttendArgs& a, const Request& rq,
         }
     }
     const float cap2 = a.softcap * kLog2e;
-    const float mul = pow2(-shift) * (a.softcap > 0.0f ? a.scale * 2.0f * kLog2e / a.softcap : a.scale * kLog2e);
+    const bool large_cap = a.softcap > kSmallCap;
+    const float mul = pow2(-shift) * (a.softcap > 0.0f && !large_cap ? a.scale * 2.0f * kLog2e / a.softcap : a.scale * kLog2e);
     const float slope2 = a.slopes ? a.slopes[head] * kLog2e : 0.0f;
     const int pos = rq.pos0 + tok;
 
@@ -427,7 +445,11 @@ __device__ __forceinline__ void few_keys(const AttendArgs& a, const Request& rq,
         float x[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] = s[i >> 2][i & 3] * mulk;
-        if (a.softcap > 0.0f) {
+        if (large_cap) {
+            const float inv = 1.0f / cap2;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = capped_large(x[i], cap2, inv);
+        } else if (a.softcap > 0.0f) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[i] = capped(x[i], cap2);
         }
@@ -715,11 +737,13 @@ struct TileLds {
 // to the exponential, which takes their factor, the maximum and the value scale
 // in one multiply-add: w = 2^(s c - m + log2 v), v = vs 2^8 / vr, and sum w / v
 // is what l wants.  (v is held at 2^-40 from below: values of such a scale are
-// zeros, or too small for the sum to notice.)  CAPPED: a cap and no bias; then
+// zeros, or too small for the sum to notice.)  CAPPED: a small cap and no bias; then
 // y = cap (1 - 2 r) with r = 1 / (1 + e^2t), and r stays up to the exponential in
 // the same way: the largest score is that of the smallest r, a masked one has r =
-// infinity.  FULL: anything.
-enum Scores { PLAIN, CAPPED, FULL };
+// infinity.  FULL: a bias, with or without a small cap.  LARGE: a larger cap, with
+// or without a bias; as a branch of FULL it took 3 to 10% of the calls without one
+// (registers), and it has no instance for pages of whole tiles.
+enum Scores { PLAIN, CAPPED, FULL, LARGE };
 
 // ONE: pages of a multiple of 64 tokens; a tile then lies in one page, with one scale.
 template <bool E4M3, int DP, Scores SCORES, bool ONE, int W>
@@ -814,7 +838,7 @@ __global__ __launch_bounds__(64 * W, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) void atte
     }
     const float cap2 = a.softcap * kLog2e;
     const float scale = fabsf(a.scale);
-    const float mul = pow2(-shift) * (a.softcap > 0.0f ? scale * 2.0f * kLog2e / a.softcap : scale * kLog2e);
+    const float mul = pow2(-shift) * (SCORES != LARGE && a.softcap > 0.0f ? scale * 2.0f * kLog2e / a.softcap : scale * kLog2e);
     const float slope2 = a.slopes ? a.slopes[head] * kLog2e : 0.0f;
     const int pos = rq.pos0 + tok;
     const int32_t* table = a.tables + r * a.max_pages;
@@ -955,10 +979,14 @@ __global__ __launch_bounds__(64 * W, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) void atte
 #pragma unroll
             for (int k = 0; k < G; ++k) c[k] = -2.0f * cap2;
         }
-        if (SCORES == FULL) {
+        if (SCORES == FULL || SCORES == LARGE) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) x[i] *= c[ONE ? 0 : i >> 3];
-            if (a.softcap > 0.0f) {
+            if (SCORES == LARGE) {
+                const float inv = 1.0f / cap2;
+#pragma unroll
+                for (int i = 0; i < 32; ++i) x[i] = capped_large(x[i], cap2, inv);
+            } else if (a.softcap > 0.0f) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i) x[i] = capped(x[i], cap2);
             }
@@ -1028,7 +1056,7 @@ __global__ __launch_bounds__(64 * W, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) void atte
             half8_t p;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float w = __builtin_amdgcn_exp2f(SCORES != FULL ? __builtin_fmaf(x[8 * k + i], c[part], vb[part]) : x[8 * k + i] + vb[part]);
+                const float w = __builtin_amdgcn_exp2f(SCORES == PLAIN || SCORES == CAPPED ? __builtin_fmaf(x[8 * k + i], c[part], vb[part]) : x[8 * k + i] + vb[part]);
                 sum += w;
                 p[i] = (_Float16)w;
             }
@@ -1349,12 +1377,16 @@ extern "C" int fkv_page_attend(const fkv_page_desc* desc, const fkv_attend_desc*
             constexpr size_t shm = sizeof(TileLds<DP, W>);
             auto of_scores = [&](auto scores) {
                 constexpr Scores S = decltype(scores)::value;
-                if (a.page % kTile == 0)
-                    e4m3 ? go(attend_tile_kernel<true, DP, S, true, W>, shm, W) : go(attend_tile_kernel<false, DP, S, true, W>, shm, W);
-                else
-                    e4m3 ? go(attend_tile_kernel<true, DP, S, false, W>, shm, W) : go(attend_tile_kernel<false, DP, S, false, W>, shm, W);
+                if constexpr (S != LARGE) {
+                    if (a.page % kTile == 0) {
+                        e4m3 ? go(attend_tile_kernel<true, DP, S, true, W>, shm, W) : go(attend_tile_kernel<false, DP, S, true, W>, shm, W);
+                        return;
+                    }
+                }
+                e4m3 ? go(attend_tile_kernel<true, DP, S, false, W>, shm, W) : go(attend_tile_kernel<false, DP, S, false, W>, shm, W);
             };
-            if (a.slopes) of_scores(std::integral_constant<Scores, FULL>{});
+            if (a.softcap > kSmallCap) of_scores(std::integral_constant<Scores, LARGE>{});
+            else if (a.slopes) of_scores(std::integral_constant<Scores, FULL>{});
             else if (a.softcap > 0.0f) of_scores(std::integral_constant<Scores, CAPPED>{});
             else of_scores(std::integral_constant<Scores, PLAIN>{});
         };

@@ -123,3 +123,42 @@ def test_attend_large_values_behind_a_mask(fkv, codes, rows, page, opt, new):
                new, last, first=first, **opt)
     check_pool(fkv, (k, v, scales), q, tables, torch.tensor([last], dtype=torch.int32), torch.tensor([0, new], dtype=torch.int32),
                new, last, window=100, **opt)
+
+
+@pytest.mark.parametrize("cap", [30.0, 128.0, 129.0, 1e3, 1e4, 1e6, 1e30])
+@pytest.mark.parametrize("slopes", [False, True])
+@pytest.mark.parametrize("kv,new", [(200, 1), (3000, 1), (700, 40), (700, 130)])
+def test_attend_large_caps(fkv, cap, slopes, kv, new):
+    """cap * tanh(x / cap) for caps far above the scores, where tanh is nearly its argument.  The scores are bound to
+    2^-21 of a cap of at most 128, and to 2^-20 of their own size for a larger one, beside the dot product's
+    (d + 8) 2^-24 sum |q k|."""
+    page, heads, group, d = 16, 2, 2, 64
+    n_pages = -(-kv // page)
+    k, v, scales = random_pages(n_pages, page, heads, d, INT8, 8)
+    scales[:, :, 0] = 2.0 ** -5
+    tables = torch.randperm(n_pages, generator=torch.Generator().manual_seed(9)).int()
+    q = torch.randn((new, heads * group, d), generator=torch.Generator().manual_seed(10)).to(torch.float16)
+    kk, vv = (t[tables.long()].transpose(0, 1).reshape(heads, -1, d)[:, :kv].repeat_interleave(group, 0) for t in ref.values(k, v, scales))
+    x = torch.stack([q[:, h].double() @ kk[h].t() for h in range(4)]) * d ** -0.5          # [head][row][key]
+    size = torch.stack([q[:, h].double().abs() @ kk[h].abs().t() for h in range(4)]) * d ** -0.5
+    z = cap * torch.tanh(x / cap)
+    off = size * (d + 8) * 2.0 ** -24 + z.abs() * 2.0 ** -20 + (cap * 2.0 ** -21 if cap <= 128 else 0.0)
+    slope = torch.tensor([0.5, 0.1, 0.03, 0.002])
+    pos, j = torch.arange(kv - new, kv), torch.arange(kv)
+    far = (pos[:, None] - j).abs()
+    if slopes:
+        z = z - slope.double()[:, None, None] * far
+        off = off + slope.double()[:, None, None] * far * 2.0 ** -21 + z.abs() * 2.0 ** -21
+    z = torch.where(j <= pos[:, None], z, -math.inf)
+    lse = z.logsumexp(2)
+    w = torch.exp(z - lse[:, :, None])
+    big = torch.where(w > 2.0 ** -30, off, 0.0).amax(2)
+    assert big.max() < 0.02
+    got, glse = fkv.fkv_page_attend(fkv.Pages(k.cuda(), v.cuda(), scales.cuda()), q.cuda(), tables[None].cuda(),
+                                    dev([kv], torch.int32), dev([0, new], torch.int32), new, kv, softcap=cap,
+                                    slopes=slope.cuda() if slopes else None, want_lse=True)
+    err = (glse.cpu().double().t() - lse).abs()
+    assert (err <= 2 * big + lse.abs() * 2.0 ** -20 + 2.0 ** -18).all(), float(err.max())
+    out = (w @ vv).transpose(0, 1)
+    most = (2.0 ** -11 + 4 * big.t()[:, :, None] + 2.0 ** -18) * (w @ vv.abs()).transpose(0, 1)
+    assert ((got.cpu().double() - out).abs() <= most + 2.0 ** -11 * (out.abs() + most) + 2.0 ** -24).all()
