@@ -1247,7 +1247,8 @@ Shape shape_of(const fkv_page_desc* p, const fkv_attend_desc* t)
         }
         return s;
     }
-    const int64_t want = (400 + heads * s.row_blocks - 1) / (heads * s.row_blocks);
+    // (the two may be any numbers: their product only where it is small)
+    const int64_t want = heads >= 400 || s.row_blocks >= 400 ? 1 : (400 + heads * s.row_blocks - 1) / (heads * s.row_blocks);
     const int64_t most = max((int64_t)1, tiles / kWaves);
     const int64_t n = max((int64_t)1, min(want, most));
     s.split_tiles = (int)((tiles + n - 1) / n);
@@ -1335,8 +1336,11 @@ extern "C" int fkv_page_attend(const fkv_page_desc* desc, const fkv_attend_desc*
     a.scale = attend->scale, a.softcap = attend->softcap;
     const hipStream_t st = (hipStream_t)stream;
     const bool e4m3 = desc->format == FKV_PAGE_E4M3;
+    // what a launch cannot hold is refused before the first
+    const int64_t items = s.n_splits > 1 ? a.n_req * a.max_new * a.heads * a.group : 0;   // rows to be joined
+    const int64_t joins = s.join_blocks ? items : (items + kWaves - 1) / kWaves;
+    if (joins > 0x7fffff00 || s.blocks > 0x7fffff00) return FKV_ERR_UNSUPPORTED;
     if (s.few) {
-        if (s.blocks > 0x7fffff00) return FKV_ERR_UNSUPPORTED;
         auto go = [&](auto kern, int w) {
             const size_t shm = (2 * w * kFewRows + (size_t)w * kFewRows * (a.d + 4)) * sizeof(float);
             hipLaunchKernelGGL(kern, dim3((unsigned)s.blocks), dim3(64 * w), shm, st, a);
@@ -1402,11 +1406,7 @@ extern "C" int fkv_page_attend(const fkv_page_desc* desc, const fkv_attend_desc*
         else of_width(std::integral_constant<int, 256>{});
         if (status != FKV_OK) return status;
     }
-    if (a.n_splits > 1) {
-        const int64_t items = a.n_req * a.max_new * a.heads * a.group;
-        const int64_t blocks = s.join_blocks ? items : (items + kWaves - 1) / kWaves;
-        if (blocks > 0x7fffff00) return FKV_ERR_UNSUPPORTED;
-        hipLaunchKernelGGL(s.join_blocks ? attend_join_kernel<kWaves> : attend_join_kernel<1>, dim3((unsigned)blocks), dim3(kThreads), 0, st, a);
-    }
+    if (a.n_splits > 1)
+        hipLaunchKernelGGL(s.join_blocks ? attend_join_kernel<kWaves> : attend_join_kernel<1>, dim3((unsigned)joins), dim3(kThreads), 0, st, a);
     return launch_status();
 }

@@ -622,6 +622,7 @@ Rows rows_of(const fkv_row_desc* r, const void* at)
 }
 
 constexpr int64_t kMostBlocks = 0x7fffff00;
+constexpr int64_t kMostRows = (int64_t)1 << 40;   // beyond any memory; times the heads it is a number of 64 bits
 
 }  // namespace
 }  // namespace fkv
@@ -659,7 +660,8 @@ extern "C" int fkv_page_store(const fkv_page_desc* desc, const fkv_row_desc* row
                               const void* k_rows, const void* v_rows, int64_t n_tokens, const int64_t* slots,
                               uint8_t* k_codes, uint8_t* v_codes, float* scales, uint32_t* n_bad, void* stream)
 {
-    if (!page_desc_ok(desc) || !row_desc_ok(rows_k) || !row_desc_ok(rows_v) || rows_k->type != rows_v->type || n_tokens < 0)
+    if (!page_desc_ok(desc) || !row_desc_ok(rows_k) || !row_desc_ok(rows_v) || rows_k->type != rows_v->type || n_tokens < 0 ||
+        n_tokens > kMostRows)
         return FKV_ERR_INVALID_ARG;
     if (!k_codes || !v_codes || !scales || !aligned(k_codes, 16) || !aligned(v_codes, 16) || !aligned(scales, 8) ||
         !aligned(n_bad, 4))
@@ -685,7 +687,7 @@ extern "C" int fkv_page_load(const fkv_page_desc* desc, const uint8_t* k_codes, 
                              const float* scales, int64_t n_tokens, const int64_t* slots, const fkv_row_desc* rows_k,
                              const fkv_row_desc* rows_v, void* k_rows, void* v_rows, void* stream)
 {
-    if (!page_desc_ok(desc) || n_tokens < 0 || (k_rows && !row_desc_ok(rows_k)) || (v_rows && !row_desc_ok(rows_v)) ||
+    if (!page_desc_ok(desc) || n_tokens < 0 || n_tokens > kMostRows || (k_rows && !row_desc_ok(rows_k)) || (v_rows && !row_desc_ok(rows_v)) ||
         (k_rows && v_rows && rows_k->type != rows_v->type))
         return FKV_ERR_INVALID_ARG;
     if (!k_codes || !v_codes || !scales || !aligned(k_codes, 16) || !aligned(v_codes, 16) || !aligned(scales, 8) ||
