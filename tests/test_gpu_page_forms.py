@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import pages_reference as ref
-from test_gpu_pages import E4M3, INT8, dev
+from test_gpu_pages import E4M3, INT8, _slopes, bits, check_attend, dev, make_pool, make_rows, slot_map
 
 pytestmark = pytest.mark.gpu
 
@@ -65,7 +65,7 @@ def test_the_largest_bfloat16_rows_come_back(fkv, codes):
             assert ((got.cpu().double() - want).abs() <= want.abs() * (2.0 ** -8 + 2.0 ** -23)).all()
 
 
-def check_pool(fkv, pool, q, tables, kv, q_start, max_new, max_kv, bound=None, **opt):
+def check_pool(fkv, pool, q, tables, kv, q_start, max_new, max_kv, **opt):
     """fkv_page_attend of a CPU pool against 64 bits, within the reference's bounds."""
     k, v, scales = pool
     want, lse, off, loff = ref.attend(k, v, scales, q, tables, kv, q_start, q.shape[2] ** -0.5, **opt)
@@ -162,3 +162,162 @@ def test_attend_large_caps(fkv, cap, slopes, kv, new):
     out = (w @ vv).transpose(0, 1)
     most = (2.0 ** -11 + 4 * big.t()[:, :, None] + 2.0 ** -18) * (w @ vv.abs()).transpose(0, 1)
     assert ((got.cpu().double() - out).abs() <= most + 2.0 ** -11 * (out.abs() + most) + 2.0 ** -24).all()
+
+
+# ---------------------------------------------------------------- forms that the sizes of a call choose
+
+MANY = [
+    # page, heads, d, code type, row type, (before, new) of each request: more than 32,768 rows x heads
+    (16, 16, 32, INT8, torch.float16, [(0, 1000), (5, 333), (15, 1), (3, 9), (0, 16), (16, 747)]),
+    (48, 16, 48, E4M3, torch.bfloat16, [(47, 2), (1, 46), (0, 48), (13, 1999)] + [(7, 3)] * 20),
+    (64, 24, 80, INT8, torch.bfloat16, [(0, 1301), (63, 1), (20, 60), (0, 5)]),
+    (256, 24, 16, INT8, torch.float16, [(0, 700), (100, 90), (255, 2), (3, 600), (30, 70)]),
+    (128, 24, 128, E4M3, torch.float16, [(9, 120), (0, 128), (127, 3), (0, 1150)]),
+    (16, 40, 16, E4M3, torch.float16, [(k % 16, 1) for k in range(823)]),
+    (32, 12, 64, INT8, torch.bfloat16, [(30, 5)] * 560),
+]
+
+
+@pytest.mark.parametrize("page,heads,d,codes,rows,lengths", MANY)
+@pytest.mark.parametrize("special", [False, True])
+def test_store_of_many_rows(fkv, page, heads, d, codes, rows, lengths, special):
+    """A wave looks at a page's worth of rows: several runs in it, runs that begin before and end after it, and rows
+    of no page between them."""
+    n_pages = sum(-(-(kv + new) // page) for kv, new in lengths) + 2
+    slots, _ = slot_map(lengths, page, n_pages, d)
+    n = len(slots)
+    gaps = np.flatnonzero(np.diff(slots) != 1) + 1                         # between requests, and pages apart
+    sent = np.insert(slots, [gaps[0], gaps[0], gaps[-1], n], [-1, n_pages * page + 3, -2 ** 40, n_pages * page])
+    assert len(sent) * heads > 32768 and len(sent) % min(page, 64)
+    k, v, scales = random_pages(n_pages, page, heads, d, codes, 11)
+    rk, rv = make_rows(len(sent), heads, d, rows, 12, special), make_rows(len(sent), heads, d, rows, 13, special)
+    pages = fkv.Pages(k.cuda(), v.cuda(), scales.cuda())
+    bad = torch.zeros(1, dtype=torch.int32, device="cuda")
+    fkv.fkv_page_store(pages, rk.cuda(), rv.cuda(), dev(sent), n_bad=bad)
+    torch.cuda.synchronize()
+    assert int(bad) == 2
+    was = k.clone()
+    ref.store(k, v, scales, rk, rv, sent)
+    seen = torch.zeros((n_pages, page), dtype=torch.bool)
+    for i, m in ref.runs(slots, page):
+        p, o = divmod(int(slots[i]), page)
+        seen[p, :o + m] = True
+    assert torch.equal(bits(pages.scales), bits(scales))
+    valid = seen[:, None, :, None]
+    for got, want in ((pages.k.cpu(), k), (pages.v.cpu(), v)):
+        got, want = (x.view(torch.uint8) if x.dim() == 4 else x.view(torch.uint8).transpose(-1, -2).reshape(k.shape) for x in (got, want))
+        assert torch.equal(torch.where(valid, got, 0), torch.where(valid, want, 0))
+    untouched = ~seen.any(1)
+    assert untouched.any() and torch.equal(bits(pages.k)[untouched], bits(was)[untouched])
+
+
+@pytest.mark.parametrize("page,heads,d,codes", [(16, 16, 64, INT8), (48, 24, 80, E4M3), (64, 16, 128, INT8), (256, 40, 16, E4M3),
+                                               (32, 17, 256, INT8)])
+@pytest.mark.parametrize("rows", [torch.float16, torch.bfloat16])
+def test_load_of_many_rows(fkv, page, heads, d, codes, rows):
+    """64 rows a wave: contexts in order from any offset, and rows in no order with some of no page."""
+    n_pages = -(-2200 // page)
+    pool = random_pages(n_pages, page, heads, d, codes, 14)
+    rng = np.random.default_rng(15)
+    whole = (rng.permutation(n_pages)[:, None] * page + np.arange(page)).reshape(-1)
+    mixed = rng.integers(-2, n_pages * page + 2, 2103)
+    for slots in (whole[7:2190], mixed):
+        assert len(slots) * heads > 32768 and len(slots) % 64
+        check_load(fkv, pool, slots, rows)
+    # and head-major streams, the second of K only
+    pages = fkv.Pages(*(t.cuda() for t in pool))
+    slots = dev(whole[3:3 + 3 * 711].reshape(3, 711))
+    x = torch.empty((2, 3, heads, 711, d), dtype=rows, device="cuda")
+    fkv.fkv_page_load(pages, slots, k=x[0], v=x[1])
+    k, v = fkv.fkv_page_load(pages, slots.view(-1), rows)
+    assert torch.equal(x[0].transpose(1, 2).reshape(k.shape), k) and torch.equal(x[1].transpose(1, 2).reshape(v.shape), v)
+    only = torch.zeros_like(x[0])
+    fkv.fkv_page_load(pages, slots, k=only)
+    assert torch.equal(only, x[0])
+
+
+def check_sample(fkv, lengths, new, page, heads, group, d, codes, rows, seed, most=40, **opt):
+    """A causal call checked at some of its rows, each taken as a request of one row that ends at its position."""
+    k, v, scales, tables = make_pool(lengths, page, heads, d, codes, seed)
+    n = sum(new)
+    q = torch.randn((n, heads * group, d), generator=torch.Generator().manual_seed(seed + 1)).to(rows)
+    start = np.concatenate(([0], np.cumsum(new)))
+    got, glse = fkv.fkv_page_attend(fkv.Pages(k.cuda(), v.cuda(), scales.cuda()), q.cuda(), tables.cuda(), dev(lengths, torch.int32),
+                                    dev(start, torch.int32), max(new), max(lengths), want_lse=True,
+                                    **{name: (x.cuda() if isinstance(x, torch.Tensor) else x) for name, x in opt.items()})
+    got, glse = got.cpu().double(), glse.cpu().double()
+    assert got.isfinite().all()
+    rng = np.random.default_rng(seed)
+    pick = np.unique(np.concatenate((start[:-1], start[1:] - 1, rng.integers(0, n, most))))      # first and last ones too
+    r = np.searchsorted(start, pick, side="right") - 1
+    kv = np.maximum(np.array(lengths)[r] - np.array(new)[r] + pick - start[r] + 1, 0)
+    if codes == E4M3:      # a product with a NaN code that no row sees would be one
+        for c in (k, v):
+            b = c.view(torch.uint8)
+            b[b == 0x7f] = 0
+    want, lse, off, loff = ref.attend(k, v, torch.nan_to_num(scales), q[pick], tables[r], torch.from_numpy(kv),
+                                      np.arange(len(pick) + 1), d ** -0.5, **opt)
+    u = 2.0 ** -11 if rows == torch.float16 else 2.0 ** -8
+    empty = lse == -math.inf
+    assert torch.equal(glse[pick] == -math.inf, empty) and not got[pick][empty].any()
+    worst = ((got[pick] - want).abs() / (off + u * (want.abs() + off) + 2.0 ** -24)).max()
+    assert worst <= 1, float(worst)
+    assert ((glse[pick] - lse).abs()[~empty] <= loff[~empty]).all()
+
+
+@pytest.mark.parametrize("opt", [{}, dict(softcap=30.0), dict(slopes=True), dict(softcap=500.0, slopes=True), dict(window=150, sinks=5)])
+@pytest.mark.parametrize("page", [48, 64])
+@pytest.mark.parametrize("d", [80, 96, 112, 128])
+@pytest.mark.parametrize("codes,rows", [(INT8, torch.float16), (E4M3, torch.bfloat16)])
+def test_attend_blocks_of_256_rows(fkv, codes, rows, d, page, opt):
+    """At least 4096 rows of a KV head, even requests, 64 < d <= 128: eight waves a block, the last block part full; the
+    keys in one piece, and (fewer rows of more keys) in two or more that are joined."""
+    opt = dict(opt)
+    if opt.pop("slopes", False):
+        opt["slopes"] = _slopes(32)
+    for lengths, new in (([300, 131], [130, 131]), ([1100], [131])):
+        assert max(new) * 32 >= 4096 and 4 * sum(new) >= 3 * len(new) * max(new) and (max(new) * 32) % 256
+        check_sample(fkv, lengths, new, page, 1, 32, d, codes, rows, d + page, most=8, **opt)
+
+
+@pytest.mark.parametrize("opt", [{}, dict(softcap=30.0, slopes=True), dict(softcap=500.0), dict(window=70, sinks=3)])
+@pytest.mark.parametrize("d,page", [(144, 16), (256, 64), (192, 256)])
+@pytest.mark.parametrize("codes,rows", [(INT8, torch.float16), (E4M3, torch.bfloat16)])
+def test_attend_few_rows_of_more_than_128_channels(fkv, codes, rows, d, page, opt):
+    """At most 1024 keys: a block a head; more: the line of tiles, joined by a block a row; many rows: 64-key tiles."""
+    opt = dict(opt)
+    if opt.pop("slopes", False):
+        opt["slopes"] = _slopes(8)
+    check_attend(fkv, [1000, 17, 0, 260], [1, 1, 1, 1], page, 2, 4, d, codes, rows, seed=d, **opt)
+    check_attend(fkv, [700, 64], [2, 2], page, 1, 8, d, codes, rows, seed=d + 1, **opt)
+    check_attend(fkv, [9000, 40], [1, 1], page, 1, 8, d, codes, rows, seed=d + 2, **opt)
+    check_sample(fkv, [5000], [40], page, 1, 8, d, codes, rows, d + 3, most=4, **opt)
+
+
+@pytest.mark.parametrize("codes,rows", [(INT8, torch.bfloat16), (E4M3, torch.float16)])
+def test_attend_of_more_requests_than_a_block_has_threads(fkv, codes, rows):
+    """The line of tiles of 257 and 700 requests, long ones first, among and last, some empty and some without rows."""
+    for n in (257, 700):
+        rng = np.random.default_rng(n)
+        lengths = rng.integers(0, 200, n)
+        lengths[[0, n // 2, n - 1]] = 1500, 2100, 1100
+        new = (rng.random(n) < 0.8).astype(int)
+        new[[0, n // 2, n - 1]] = 1
+        check_attend(fkv, lengths.tolist(), new.tolist(), 16, 2, 4, 32, codes, rows, seed=n)
+
+
+@pytest.mark.parametrize("n", [64, 65, 90])
+def test_attend_prompts_of_more_than_64_requests(fkv, n):
+    """Up to 64 requests go out by length, more in order; both with lengths alike, empty ones and none of the rows."""
+    rng = np.random.default_rng(n)
+    lengths = rng.integers(0, 150, n)
+    lengths[5:12] = 77
+    new = np.minimum(rng.integers(0, 31, n), lengths)
+    new[3], lengths[3] = 30, 400
+    check_attend(fkv, lengths.tolist(), new.tolist(), 32, 1, 2, 32, INT8, torch.float16, seed=n)
+
+
+@pytest.mark.parametrize("codes", [INT8, E4M3])
+def test_attend_one_head_of_many_tiles(fkv, codes):
+    """A head of 1600 tiles in more pieces than any other test's, the join taking several rounds of its splits."""
+    check_sample(fkv, [102_400 - 7], [3], 256, 1, 2, 64, codes, torch.float16, 21, most=1)
