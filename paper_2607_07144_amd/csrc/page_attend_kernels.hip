@@ -943,139 +943,145 @@ __global__ __launch_bounds__(64 * W, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) void atte
         look_up_scales();
         fetch(jn);   // (the last tile once more after itself: it goes nowhere)
 
-        // x[u*16+i] is the score of key j0 + 32u + 8(i/4) + 4hf + i%4
-        float x[32];
-        {
-            half8_t f[kChunks];
-            float16_t s0, s1;
+        // A wave none of whose rows sees a key of the tile leaves it to the others.  Without and with (us), eight prompts
+        // of 500 to 2000 rows over 2000 to 8000 keys: d = 128 1110 and 1057, capped with a prefix 1345 and 1298, with a bias
+        // 1289 and 1252; d = 256 1783 and 1666, with a bias 1917 and 1961.  Not at d <= 64, where the widening below then
+        // waits for the products: 16 prompts of 1024 rows 82.0 and 83.5, packed documents 64 and 67.
+        if (DP <= 64 || (j0 < wave_hi && j0 + kTile > wave_lo)) {
+            // x[u*16+i] is the score of key j0 + 32u + 8(i/4) + 4hf + i%4
+            float x[32];
+            {
+                half8_t f[kChunks];
+                float16_t s0, s1;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s0[i] = s1[i] = 0.0f;
+                for (int i = 0; i < 16; ++i) s0[i] = s1[i] = 0.0f;
 #pragma unroll
-            for (int c = 0; c < kChunks; ++c) f[c] = *(const half8_t*)(ks + c32 * Lds::kRow + c * 16 + hf * 8);
+                for (int c = 0; c < kChunks; ++c) f[c] = *(const half8_t*)(ks + c32 * Lds::kRow + c * 16 + hf * 8);
 #pragma unroll
-            for (int c = 0; c < kChunks; ++c) {
-                s0 = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[c], qf[c], s0, 0, 0, 0);
-                f[c] = *(const half8_t*)(ks + (32 + c32) * Lds::kRow + c * 16 + hf * 8);
+                for (int c = 0; c < kChunks; ++c) {
+                    s0 = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[c], qf[c], s0, 0, 0, 0);
+                    f[c] = *(const half8_t*)(ks + (32 + c32) * Lds::kRow + c * 16 + hf * 8);
+                }
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c) s1 = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[c], qf[c], s1, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] = s0[i], x[16 + i] = s1[i];
             }
+            // the values of the first two key groups, on their way during the softmax
+            half8_t g[DP / 32][2];
 #pragma unroll
-            for (int c = 0; c < kChunks; ++c) s1 = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[c], qf[c], s1, 0, 0, 0);
+            for (int t = 0; t < DP / 32; ++t)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = s0[i], x[16 + i] = s1[i];
-        }
-        // the values of the first two key groups, on their way during the softmax
-        half8_t g[DP / 32][2];
+                for (int k = 0; k < 2; ++k) g[t][k] = *(const half8_t*)(vs + (t * 32 + c32) * Lds::vRow + k * 16 + hf * 8);
+            auto key_of = [&](int i) { return j0 + (i >> 4) * 32 + ((i & 15) >> 2) * 8 + hf * 4 + (i & 3); };
+            float c[G];   // factors of the scores
 #pragma unroll
-        for (int t = 0; t < DP / 32; ++t)
+            for (int k = 0; k < G; ++k) c[k] = SCORES == PLAIN ? fmaxf(mul * sn[k].x, 0x1p-120f) : mul * sn[k].x;
+            if (SCORES == CAPPED) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) g[t][k] = *(const half8_t*)(vs + (t * 32 + c32) * Lds::vRow + k * 16 + hf * 8);
-        auto key_of = [&](int i) { return j0 + (i >> 4) * 32 + ((i & 15) >> 2) * 8 + hf * 4 + (i & 3); };
-        float c[G];   // factors of the scores
+                for (int i = 0; i < 32; ++i)
+                    x[i] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x[i] * c[ONE ? 0 : i >> 3]));
 #pragma unroll
-        for (int k = 0; k < G; ++k) c[k] = SCORES == PLAIN ? fmaxf(mul * sn[k].x, 0x1p-120f) : mul * sn[k].x;
-        if (SCORES == CAPPED) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                x[i] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x[i] * c[ONE ? 0 : i >> 3]));
-#pragma unroll
-            for (int k = 0; k < G; ++k) c[k] = -2.0f * cap2;
-        }
-        if (SCORES == FULL || SCORES == LARGE) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) x[i] *= c[ONE ? 0 : i >> 3];
-            if (SCORES == LARGE) {
-                const float inv = 1.0f / cap2;
-#pragma unroll
-                for (int i = 0; i < 32; ++i) x[i] = capped_large(x[i], cap2, inv);
-            } else if (a.softcap > 0.0f) {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) x[i] = capped(x[i], cap2);
+                for (int k = 0; k < G; ++k) c[k] = -2.0f * cap2;
             }
-            if (a.slopes) {
+            if (SCORES == FULL || SCORES == LARGE) {
 #pragma unroll
-                for (int i = 0; i < 32; ++i) x[i] -= slope2 * fabsf((float)(key_of(i) - pos));
+                for (int i = 0; i < 32; ++i) x[i] *= c[ONE ? 0 : i >> 3];
+                if (SCORES == LARGE) {
+                    const float inv = 1.0f / cap2;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) x[i] = capped_large(x[i], cap2, inv);
+                } else if (a.softcap > 0.0f) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) x[i] = capped(x[i], cap2);
+                }
+                if (a.slopes) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) x[i] -= slope2 * fabsf((float)(key_of(i) - pos));
+                }
             }
-        }
-        constexpr float kHidden = SCORES == CAPPED ? __builtin_inff() : -__builtin_inff();
-        if (mask) {
-            const uint32_t span = (uint32_t)max(mine.hi - mine.lo, 0);
-            const int from = j0 + hf * 4 - mine.lo;
+            constexpr float kHidden = SCORES == CAPPED ? __builtin_inff() : -__builtin_inff();
+            if (mask) {
+                const uint32_t span = (uint32_t)max(mine.hi - mine.lo, 0);
+                const int from = j0 + hf * 4 - mine.lo;
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-                x[i] = (uint32_t)(from + (i >> 4) * 32 + ((i & 15) >> 2) * 8 + (i & 3)) < span ? x[i] : kHidden;
-            if (a.window) {
+                for (int i = 0; i < 32; ++i)
+                    x[i] = (uint32_t)(from + (i >> 4) * 32 + ((i & 15) >> 2) * 8 + (i & 3)) < span ? x[i] : kHidden;
+                if (a.window) {
 #pragma unroll
-                for (int i = 0; i < 32; ++i) x[i] = (key_of(i) >= mine.wlo) | (key_of(i) < a.sinks) ? x[i] : kHidden;
+                    for (int i = 0; i < 32; ++i) x[i] = (key_of(i) >= mine.wlo) | (key_of(i) < a.sinks) ? x[i] : kHidden;
+                }
+                if (!all) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) x[i] = sn[ONE ? 0 : i >> 3].y >= 0.0f ? x[i] : kHidden;
+                }
             }
-            if (!all) {
+            float top = -__builtin_inff(), vtop = -1.0f;
+            float tops[G];
 #pragma unroll
-                for (int i = 0; i < 32; ++i) x[i] = sn[ONE ? 0 : i >> 3].y >= 0.0f ? x[i] : kHidden;
+            for (int k = 0; k < G; ++k) {
+                constexpr int n = 32 / G;
+                float t = x[n * k];
+#pragma unroll
+                for (int i = 1; i < n; ++i)
+                    t = SCORES == CAPPED ? __builtin_elementwise_minimum(t, x[n * k + i]) : __builtin_elementwise_maximum(t, x[n * k + i]);
+                top = __builtin_elementwise_maximum(top, SCORES == PLAIN ? t * c[k] : SCORES == CAPPED ? __builtin_fmaf(t, c[k], cap2) : t);
+                vtop = fmaxf(vtop, sn[k].y);
+                tops[k] = t;
             }
-        }
-        float top = -__builtin_inff(), vtop = -1.0f;
-        float tops[G];
+            top = halves_max(top);
+            if (mask) {   // only of parts of which the row sees a key
+                vtop = -1.0f;
 #pragma unroll
-        for (int k = 0; k < G; ++k) {
-            constexpr int n = 32 / G;
-            float t = x[n * k];
-#pragma unroll
-            for (int i = 1; i < n; ++i)
-                t = SCORES == CAPPED ? __builtin_elementwise_minimum(t, x[n * k + i]) : __builtin_elementwise_maximum(t, x[n * k + i]);
-            top = __builtin_elementwise_maximum(top, SCORES == PLAIN ? t * c[k] : SCORES == CAPPED ? __builtin_fmaf(t, c[k], cap2) : t);
-            vtop = fmaxf(vtop, sn[k].y);
-            tops[k] = t;
-        }
-        top = halves_max(top);
-        if (mask) {   // only of parts of which the row sees a key
-            vtop = -1.0f;
-#pragma unroll
-            for (int k = 0; k < G; ++k) vtop = fmaxf(vtop, tops[k] != kHidden ? sn[k].y : -1.0f);
-            vtop = halves_max(vtop);
-        }
-        if (__any(top > m + kSlack || vtop > vref)) {
-            const float mnew = fmaxf(m, top), vnew = fmaxf(vref, vtop);
-            const float shrink = mnew == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m - mnew);
-            l *= shrink;
-            const float f = shrink * (vref / vnew);
-#pragma unroll
-            for (int t = 0; t < DP / 32; ++t) acc[t] *= f;
-            m = mnew;
-            vref = vnew;
-        }
-        const float m0 = m == -__builtin_inff() ? 0.0f : m;
-        const float vmul = kTop / vref;
-        float vb[G], vinv[G];
-#pragma unroll
-        for (int k = 0; k < G; ++k) {
-            const float v = __builtin_amdgcn_fmed3f(sn[k].y * vmul, 0x1p-40f, kTop);   // (more only where nothing is seen)
-            vb[k] = __builtin_amdgcn_logf(v) - m0 + (SCORES == CAPPED ? cap2 : 0.0f);
-            vinv[k] = __builtin_amdgcn_rcpf(v);
-        }
-        auto weights = [&](int k) {   // of keys 16k .. 16k+15, this lane's half of them
-            const int part = ONE ? 0 : k;
-            float sum = 0.0f;
-            half8_t p;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float w = __builtin_amdgcn_exp2f(SCORES == PLAIN || SCORES == CAPPED ? __builtin_fmaf(x[8 * k + i], c[part], vb[part]) : x[8 * k + i] + vb[part]);
-                sum += w;
-                p[i] = (_Float16)w;
+                for (int k = 0; k < G; ++k) vtop = fmaxf(vtop, tops[k] != kHidden ? sn[k].y : -1.0f);
+                vtop = halves_max(vtop);
             }
-            l = __builtin_fmaf(sum, vinv[part], l);
-            return p;
-        };
-        const half8_t p0 = weights(0), p1 = weights(1);
+            if (__any(top > m + kSlack || vtop > vref)) {
+                const float mnew = fmaxf(m, top), vnew = fmaxf(vref, vtop);
+                const float shrink = mnew == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m - mnew);
+                l *= shrink;
+                const float f = shrink * (vref / vnew);
 #pragma unroll
-        for (int t = 0; t < DP / 32; ++t) {
-            acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(g[t][0], p0, acc[t], 0, 0, 0);
-            g[t][0] = *(const half8_t*)(vs + (t * 32 + c32) * Lds::vRow + 2 * 16 + hf * 8);
-            acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(g[t][1], p1, acc[t], 0, 0, 0);
-            g[t][1] = *(const half8_t*)(vs + (t * 32 + c32) * Lds::vRow + 3 * 16 + hf * 8);
-        }
-        const half8_t p2 = weights(2), p3 = weights(3);
+                for (int t = 0; t < DP / 32; ++t) acc[t] *= f;
+                m = mnew;
+                vref = vnew;
+            }
+            const float m0 = m == -__builtin_inff() ? 0.0f : m;
+            const float vmul = kTop / vref;
+            float vb[G], vinv[G];
 #pragma unroll
-        for (int t = 0; t < DP / 32; ++t) {
-            acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(g[t][0], p2, acc[t], 0, 0, 0);
-            acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(g[t][1], p3, acc[t], 0, 0, 0);
+            for (int k = 0; k < G; ++k) {
+                const float v = __builtin_amdgcn_fmed3f(sn[k].y * vmul, 0x1p-40f, kTop);   // (more only where nothing is seen)
+                vb[k] = __builtin_amdgcn_logf(v) - m0 + (SCORES == CAPPED ? cap2 : 0.0f);
+                vinv[k] = __builtin_amdgcn_rcpf(v);
+            }
+            auto weights = [&](int k) {   // of keys 16k .. 16k+15, this lane's half of them
+                const int part = ONE ? 0 : k;
+                float sum = 0.0f;
+                half8_t p;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float w = __builtin_amdgcn_exp2f(SCORES == PLAIN || SCORES == CAPPED ? __builtin_fmaf(x[8 * k + i], c[part], vb[part]) : x[8 * k + i] + vb[part]);
+                    sum += w;
+                    p[i] = (_Float16)w;
+                }
+                l = __builtin_fmaf(sum, vinv[part], l);
+                return p;
+            };
+            const half8_t p0 = weights(0), p1 = weights(1);
+#pragma unroll
+            for (int t = 0; t < DP / 32; ++t) {
+                acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(g[t][0], p0, acc[t], 0, 0, 0);
+                g[t][0] = *(const half8_t*)(vs + (t * 32 + c32) * Lds::vRow + 2 * 16 + hf * 8);
+                acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(g[t][1], p1, acc[t], 0, 0, 0);
+                g[t][1] = *(const half8_t*)(vs + (t * 32 + c32) * Lds::vRow + 3 * 16 + hf * 8);
+            }
+            const half8_t p2 = weights(2), p3 = weights(3);
+#pragma unroll
+            for (int t = 0; t < DP / 32; ++t) {
+                acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(g[t][0], p2, acc[t], 0, 0, 0);
+                acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(g[t][1], p3, acc[t], 0, 0, 0);
+            }
         }
         widen(sh.k[(e + 1) & 1], sh.v[(e + 1) & 1]);
     }
