@@ -564,7 +564,7 @@ __global__ __launch_bounds__(64 * W, NC <= 2 ? 2 : 1) void attend_few_kernel(Att
 // where a piece ends inside a head's keys its sums go to the workspace and are
 // joined by a second kernel.  A piece has two places there, one for the head that
 // began before it and one for the head that goes on behind it, so that the
-// workspace does not grow with the batch and heads may have any number of pieces.
+// workspace does not grow with the batch.
 // The line's length is only known on the device: each block forms the sum of the
 // requests' tiles for itself.  Single tokens, 8 KV heads of 128, groups of four:
 // four contexts of 32,768 tokens 48 us (5.6 TB/s) and the join 5; 64 ragged ones of
@@ -576,7 +576,9 @@ __global__ __launch_bounds__(64 * W, NC <= 2 ? 2 : 1) void attend_few_kernel(Att
 // places that hold none: what beginning a head costs, in tiles.
 constexpr int kBegin = 3;
 constexpr int kLeastPiece = 2;   // tiles
-constexpr int kMostPieces = 512; // of a head
+// Pieces of a head at the most: beyond, the join loses more than the pieces save (one KV head of 128, groups of eight,
+// with the bound and without, us: a context of 1,048,576 tokens 85 and 104; two heads, 262,144 tokens 53 and 58).
+constexpr int kMostPieces = 512;
 
 __device__ __forceinline__ int line_tiles(const AttendArgs& a, int64_t r)
 {
@@ -1372,16 +1374,8 @@ extern "C" int fkv_page_attend(const fkv_page_desc* desc, const fkv_attend_desc*
     } else {
         if (s.row_blocks > 65535 || a.n_req > 65535 || (int64_t)a.heads * a.n_splits > 0x7fffff00) return FKV_ERR_UNSUPPORTED;
         const dim3 grid((unsigned)(a.heads * a.n_splits), (unsigned)s.row_blocks, (unsigned)a.n_req);
-        int status = FKV_OK;
-        auto go = [&](auto kern, size_t shm, int w) {
-            // more LDS than a launch may take unasked
-            if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)shm) != hipSuccess) {
-                status = launch_status();
-                if (status == FKV_OK) status = FKV_ERR_LAUNCH;
-                return;
-            }
-            hipLaunchKernelGGL(kern, grid, dim3(64 * w), shm, st, a);
-        };
+        // (a launch may take all of a block's 160 KB of LDS; the widest tiles take 141)
+        auto go = [&](auto kern, size_t shm, int w) { hipLaunchKernelGGL(kern, grid, dim3(64 * w), shm, st, a); };
         auto of_waves = [&](auto dp, auto waves) {
             constexpr int DP = decltype(dp)::value, W = decltype(waves)::value;
             constexpr size_t shm = sizeof(TileLds<DP, W>);
@@ -1410,7 +1404,6 @@ extern "C" int fkv_page_attend(const fkv_page_desc* desc, const fkv_attend_desc*
         else if (a.d <= 96) of_width(std::integral_constant<int, 96>{});
         else if (a.d <= 128) of_width(std::integral_constant<int, 128>{});
         else of_width(std::integral_constant<int, 256>{});
-        if (status != FKV_OK) return status;
     }
     if (a.n_splits > 1)
         hipLaunchKernelGGL(s.join_blocks ? attend_join_kernel<kWaves> : attend_join_kernel<1>, dim3((unsigned)joins), dim3(kThreads), 0, st, a);
