@@ -405,13 +405,18 @@ typedef struct {
  *   head_out         device out int32 [1]: the largest *head + c_r of the requests
  *                    served, or *head if none; c_r counts what refused requests
  *                    asked for, so a value above n_free says that the list was
- *                    too short for requests before the last one served; not `head`
+ *                    too short for requests before the last one served; not the
+ *                    next step's *head, which is next_head; not `head`
  *   next_head        device out int32 [1], nullable: the next step's *head, the
  *                    list entries handed out by now; not `head`
  *   status           device out u8 [n_req], nullable: 0 served; 1 the free list
  *                    is at its end; 2 more than max_pages pages (or 2^31 tokens); 3 a negative
  *                    length (taken as 0 rows), or rows beyond n_tokens
  *   n_bad            device u32 counter, += requests not served; nullable
+ * The rows of a request that is not served stay between its entries of q_start.
+ * Nothing is stored for them (their slots are -1), but fkv_page_attend over
+ * q_start and kv_end takes them for the last tokens that the cache holds of the
+ * request and gives them results: a caller leaves those out by status.
  * n_req = 0 and n_tokens = 0 are valid. */
 int fkv_page_plan(int32_t page, int64_t n_req, const int32_t* kv_len, const int32_t* new_len,
                   const int32_t* free_pages, int64_t n_free, const int32_t* head, int32_t* tables,
@@ -475,12 +480,17 @@ int fkv_page_load(const fkv_page_desc* desc, const uint8_t* k_codes, const uint8
  *   workspace       device scratch of fkv_page_attend_workspace() bytes, 16-byte
  *                   aligned; null when that is 0.  Calls that may run at the
  *                   same time need one each.
- * Scores, statistics and sums are fp32, with the cap within 2^-21 of softcap (of
- * 128 at most) or 2^-20 of y (beyond); the products run on matrix cores with
- * the codes and q exact in binary16 (a bfloat16 row is taken times a power of
- * two) and the weights rounded to binary16.  FKV_ERR_INVALID_ARG also for
+ * Scores, statistics and sums are fp32 (exp and log by the hardware's
+ * instructions, a few units of fp32's last place), with the cap within 2^-21 of
+ * softcap (of 128 at most) or 2^-20 of y (beyond).  The products run on matrix
+ * cores with the codes and q exact in binary16 (a bfloat16 row is taken times a
+ * power of two; elements 2^27 below its largest round).  A weight is rounded to
+ * binary16 with its page's value scale multiplied in: it keeps 11 bits where that
+ * product is above 2^-22 of the largest value scale that the row sees.  FKV_ERR_INVALID_ARG also for
  * q_heads not a multiple of heads; FKV_ERR_SCRATCH_TOO_SMALL for a workspace
- * that is too small. */
+ * that is too small; FKV_ERR_UNSUPPORTED for more than 65,535 requests or
+ * 8,388,480 rows of a KV head (max_new * q_heads / heads) where a KV head may have
+ * more than 16 rows, and beyond 2^31 blocks otherwise. */
 typedef struct {
     int64_t n_req;
     int64_t n_tokens;

@@ -18,9 +18,13 @@
 // scores.  Value scales differ from page to page, so they multiply the fp32
 // weights before those are rounded to binary16: w = p * vs * 2^8 / vr with vr
 // the largest value scale so far of what the row sees, so that w keeps its 11
-// bits down to p vs / vr = 2^-22; the accumulators carry the factor 2^8 / vr.  m need not be the maximum
-// itself: it moves, and the accumulators with it, only when a score passes it by
-// more than 6, where w would near binary16's end.
+// bits down to p vs / vr = 2^-22; the accumulators carry the factor 2^8 / vr.  m
+// need not be the maximum itself: it moves, and the accumulators with it, only
+// when a score passes it by more than 6, where w would near binary16's end.  Powers
+// of two, logarithms and the
+// reciprocals in a cap and in a value scale's share of the sum are the hardware's
+// instructions, within about one unit of fp32's last place: far below the weights'
+// 2^-11.
 #include "page_common.h"
 
 #include <type_traits>
@@ -504,7 +508,7 @@ __device__ __forceinline__ void few_keys(const AttendArgs& a, const Request& rq,
 
 // A block a KV head and request, its W waves every W-th tile each, their
 // results joined in LDS: for contexts too short to be split.  One sequence of 1024
-// tokens, 12 heads of 64: 8.0 us, two tiles a wave in sequence.
+// tokens, 12 heads of 64: 8.2 us, two tiles a wave in sequence.
 template <bool E4M3, int NC, int W>
 __global__ __launch_bounds__(64 * W, NC <= 2 ? 2 : 1) void attend_few_kernel(AttendArgs a)
 {
@@ -567,9 +571,9 @@ __global__ __launch_bounds__(64 * W, NC <= 2 ? 2 : 1) void attend_few_kernel(Att
 // workspace does not grow with the batch.
 // The line's length is only known on the device: each block forms the sum of the
 // requests' tiles for itself.  Single tokens, 8 KV heads of 128, groups of four:
-// four contexts of 32,768 tokens 48 us (5.6 TB/s) and the join 5; 64 ragged ones of
-// 1 to 32,768, capped, with a bias, 74 us (4.6 TB/s) and 7 (80 while a head had at
-// most 32 pieces).
+// four contexts of 32,768 tokens 59 us (4.6 TB/s; 48 where a part of the codes is
+// still in the caches) and the join 5; 64 ragged ones of 1 to 32,768, capped, with a
+// bias, 76 us (4.6 TB/s) and 6.
 //
 // A request's tiles in the line: none without rows, else one at least, so that
 // a row that sees no key is written too.  Before each head's tiles stand kBegin
@@ -709,7 +713,9 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 2 : 1) void attend_line_kernel(
 // in the order 0-3, 8-11, 4-7, 12-15 of each 16, which is the order in which a
 // lane's scores come out of the accumulator.  DP: channels, rounded up.  4096 rows x
 // 32 heads of 128 over 32,768 keys 2.0 ms (1.0 PFLOP/s); eight prompts of 500 to
-// 2000 rows over 2000 to 8000 keys, capped, 1.36 ms (0.74 PFLOP/s: vector issue).
+// 2000 rows over 2000 to 8000 keys, capped, 1.30 ms (0.77 PFLOP/s; the vector unit
+// busy 57% of the time and the matrix cores 31%, since a wave has a tile's products,
+// caps and weights in turn and the waves of a SIMD overlap them only in part).
 //
 // Blocks go out request by request, the longest context first, so that no long
 // one is left for the end: of up to 64 requests, the one with z longer ones.
@@ -1229,10 +1235,11 @@ Shape shape_of(const fkv_page_desc* p, const fkv_attend_desc* t)
     const int64_t rows = t->max_new * group;
     s.few = rows <= kFewRows;
     // Eight waves share a tile's widening, four make finer blocks, two of which fill a compute unit with
-    // phases of their own.  Measured with 4 and 8 (us): 4096 rows x 4 heads over 32,768 keys, d = 128 2207
-    // and 2064, capped 2810 and 2683; one prompt of 4096 183 and 164, 16 of 2048 770 and 748; 8 of 500 to 2000
-    // rows over 2000 to 8000 keys 885 and 923, capped 1137 and 1297; 40 rows x 4 heads over 8192 keys 95 and
-    // 103; d = 96 296 and 285; d = 64, 16,384 rows 589 and 700.
+    // phases of their own.  Measured with 4 and 8 (us), 8 KV heads of 128: a 4096-token chunk over 32,768 keys, groups
+    // of four, 2207 and 2036; one prompt of 4096 169 and 165; eight of 500 to 2000 rows over 2000 to 8000 keys 1088 and
+    // 1075, with a bias 1302 and 1281, capped 1278 and 1308.  Fewer rows: 40 x 4 heads over 8192 keys 19.6 and 20.9,
+    // 16 prompts of 2048 with one query head a KV head 216 and 255.  Uneven: 16 of 100 to 4096 rows 264 and 275.
+    // d = 64, 16,384 rows 589 and 700.
     const bool even = 4 * t->n_tokens >= 3 * t->n_req * t->max_new;   // the requests' rows are about as many
     s.tile_waves = p->d > 64 && p->d <= 128 && rows >= 4096 && even ? 8 : 4;
     s.row_blocks = s.few ? 1 : (rows + 32 * s.tile_waves - 1) / (32 * s.tile_waves);

@@ -48,7 +48,8 @@ __device__ __forceinline__ uint32_t block_sum_before(uint32_t v, uint32_t* part,
 // by two 64-way probes of the sums, and the others mostly are that request's too.
 // A row's page is read from the old table entries or straight from the free
 // list, so nothing waits for the new entries.  16 requests, 16 rows 5.4 us; 2048
-// requests, 551,557 rows 15.3.
+// requests, 551,557 rows 16: waves wait two thirds of the time, for the sums, the
+// search, a look-up a row, and a second round of turns for the last 5% of the rows.
 constexpr int kPlanPer = 8;                         // requests of a thread
 constexpr int kPlanTile = kThreads * kPlanPer;
 constexpr int kPlanTurns = 4;
@@ -316,7 +317,7 @@ __device__ __forceinline__ uint32_t bytes_of(const uint32_t (&w)[4], int e)
 // (values) bytes a lane.  The largest element is found on the rows' bits, two at
 // a time: without the sign they are in the order of the numbers, and what is
 // not finite comes last; only a run that has such elements looks at each.  32,768
-// tokens, 8 heads of 128: 48 us (201 MB, 4.1 TB/s).
+// tokens, 8 heads of 128: 56 us (201 MB, 3.6 TB/s; 48 with the rows in the caches).
 constexpr int kPasses = 4;   // of 16 columns
 
 template <bool E4M3, bool BF16>

@@ -554,7 +554,9 @@ class Pages(NamedTuple):
 class PagePlan(NamedTuple):
     """What fkv_page_plan gives a step: slots i64 [n_tokens], positions i32 [n_tokens], q_start i32 [n_req + 1],
     kv_end i32 [n_req], head i32 [1] (the free-list entry that the requests served reach up to, refused ones before
-    them counted), next_head i32 [1] (the next step's head: entries handed out by now), status u8 [n_req]."""
+    them counted; not the next step's head), next_head i32 [1] (the next step's head: entries handed out by now),
+    status u8 [n_req] (0: served).  A refused request's rows keep their place in q_start, with slots of -1: attention
+    takes them for the last tokens that the cache holds of it, so leave its results out by status."""
     slots: object
     positions: object
     q_start: object
