@@ -444,6 +444,53 @@ int fkv_page_store(const fkv_page_desc* desc, const fkv_row_desc* rows_k, const 
                    const void* k_rows, const void* v_rows, int64_t n_tokens, const int64_t* slots,
                    uint8_t* k_codes, uint8_t* v_codes, float* scales, uint32_t* n_bad, void* stream);
 
+/* Rows on their way into the pages: fkv_page_store of a step's K/V rows with the
+ * rotation by position applied to the key rows, and to the step's query rows, and
+ * with the pages' boxes kept up to date; one launch.
+ * The first `rot` channels of a row at position p turn in pairs (a, b),
+ *     a' = a * c - b * s,  b' = b * c + a * s,  (c, s) = table[p][i],
+ * each product and sum rounded to fp32.  Pair i is channels (i, i + rot/2) with
+ * FKV_ROTATE_HALVES, (2i, 2i + 1) with FKV_ROTATE_PAIRS.  Key rows are not rounded
+ * to their type in between: scales and codes are those that fkv_page_store forms,
+ * of the fp32 values.  Query rows are rounded once, to nearest, ties to even.
+ *   rotate          nullable: no rotation and no query rows.  rot: a multiple of
+ *                   16, 0..d; n_pos: the table's rows (up to 2^31); q_heads: read
+ *                   with query rows only
+ *   q_rows, q_out   query rows of n_tokens tokens and q_heads heads, laid out by
+ *                   rows_q and rows_q_out, of the K/V rows' type; both null: none.
+ *                   They may be the same rows (same address and layout), and do not
+ *                   overlap otherwise
+ *   positions       device int32 [n_tokens]; null with rot = 0.  A position outside
+ *                   the table is taken to its nearer end and counted, but for rows
+ *                   with a negative position and a negative slot: they are no rows
+ *                   of a request (fkv_page_plan's beyond the last one), and their
+ *                   q_out rows are left as they were
+ *   table           device f32 [n_pos][rot/2][2], cosines and sines, 16-byte
+ *                   aligned; null with rot = 0
+ *   boxes           device [n_pages][heads][2][d] codes in the pages' format,
+ *                   16-byte aligned, nullable: of each page that a row is written
+ *                   to, the smallest and the largest code of every key channel over
+ *                   its tokens up to the row.  A page is to have been written with
+ *                   its boxes from its first token on
+ *   n_bad           device u32 counter, += rows whose slot lies beyond the pool or
+ *                   whose position lies outside the table; nullable
+ * The other arguments, and what they may hold, are fkv_page_store's. */
+#define FKV_ROTATE_HALVES 0
+#define FKV_ROTATE_PAIRS 1
+
+typedef struct {
+    int64_t n_pos;
+    int32_t rot;
+    int32_t pairing;
+    int32_t q_heads;
+} fkv_rotate_desc;
+
+int fkv_page_append(const fkv_page_desc* desc, const fkv_rotate_desc* rotate, const fkv_row_desc* rows_q,
+                    const fkv_row_desc* rows_q_out, const fkv_row_desc* rows_k, const fkv_row_desc* rows_v,
+                    const void* q_rows, void* q_out, const void* k_rows, const void* v_rows, int64_t n_tokens,
+                    const int64_t* slots, const int32_t* positions, const float* table, uint8_t* k_codes,
+                    uint8_t* v_codes, float* scales, uint8_t* boxes, uint32_t* n_bad, void* stream);
+
 /* Reads rows back: code * scale, rounded to the row type (at once or by way of
  * fp32).  Slots may come in any order and more than once; a slot outside the
  * pool gives a zero row.  k_rows or v_rows may be null (not read back). */

@@ -1,0 +1,385 @@
+// page_append_kernels.hip -- rows on their way into the paged cache, for gfx950:
+// query and key rows rotated by their positions, K/V rows written into pages, and
+// the boxes of the pages' keys kept up to date, in one launch.
+//
+// A rotation turns pairs of channels (a, b) of a row by the angle of its position
+// and pair:  a' = a c - b s,  b' = b c + a s,  with (c, s) from a table, each
+// product and sum rounded to fp32.  Keys are never rounded to their type in
+// between: their scale and codes come from the fp32 values.
+//
+// A page's box is the smallest and the largest code of each key channel over its
+// tokens.  Rounding to codes is monotone, so the box of re-scaled codes is the
+// re-scaled box, and a box is brought up to date from itself and the new rows.
+#include "page_rows_device.h"
+
+namespace fkv {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = 4;
+constexpr float kInf = __builtin_inff();
+
+struct AppendArgs {
+    Rows q, q_out, k, v;
+    const int32_t* positions;
+    const float4* table;   // two pairs' (c, s) at a time
+    uint8_t* boxes;
+    uint32_t* n_bad;
+    int64_t n_pos;
+    int64_t store_items;   // windows x heads x (K, V): a wave each
+    int64_t q_lanes;       // tokens x groups of query heads x units: a lane each
+    int32_t window, q_heads, q_groups;
+    int32_t rot;
+    bool pairs;
+};
+
+// Channels are taken in units of 16, two chunks of 8 that hold eight pairs: of
+// rotated channels c and c + rot/2 the unit's chunks lie rot/2 apart, else they are
+// neighbours.  The table's entries of unit u are 8u .. 8u+7 either way.
+struct Unit {
+    int c0, c1;     // chunks
+    bool turned;
+};
+
+__device__ __forceinline__ Unit unit_of(const AppendArgs& p, int u)
+{
+    const int half = p.rot >> 4;
+    const bool apart = !p.pairs && u < half;
+    return Unit{apart ? u : 2 * u, apart ? u + half : 2 * u + 1, u < half};
+}
+
+__device__ __forceinline__ int table_row(const AppendArgs& p, int64_t i)
+{
+    return (int)min(max((int64_t)p.positions[i], (int64_t)0), p.n_pos - 1);
+}
+
+// 16 elements of a unit in fp32, turned by the table's eight entries.
+template <bool BF16>
+__device__ __forceinline__ void turn(uint4 lo, uint4 hi, const float4 (&cs)[4], bool turned, bool pairs, float (&f)[16])
+{
+    const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+    for (int e = 0; e < 16; ++e) f[e] = row_to_f32(w[e >> 1], e & 1, BF16);
+    if (!turned) return;
+    if (pairs) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float c = e & 1 ? cs[e >> 1].z : cs[e >> 1].x, s = e & 1 ? cs[e >> 1].w : cs[e >> 1].y;
+            const float a = f[2 * e], b = f[2 * e + 1];
+            f[2 * e] = a * c - b * s;
+            f[2 * e + 1] = b * c + a * s;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float c = e & 1 ? cs[e >> 1].z : cs[e >> 1].x, s = e & 1 ? cs[e >> 1].w : cs[e >> 1].y;
+            const float a = f[e], b = f[8 + e];
+            f[e] = a * c - b * s;
+            f[8 + e] = b * c + a * s;
+        }
+    }
+}
+
+// A wave writes a run of one head's keys, as store_run does, turned on the way.
+// Lane 16q + c has unit c % units of tokens 4q .. 4q+3 of every 16-token group whose
+// turn is c / units; kHeld turns (64 tokens of 128 channels) are held in registers
+// between the largest element and the codes.
+constexpr int kHeld = 2;
+
+template <bool E4M3, bool BF16>
+__device__ __forceinline__ void append_keys(const PageArgs& a, const AppendArgs& p, float* s_box, int64_t i, int h, int64_t page,
+                                            int begin, int len)
+{
+    constexpr float kLargest = E4M3 ? kLargestE4m3 : kLargestInt8;
+    const int lane = threadIdx.x & 63, c16 = lane & 15, tq = lane >> 4;
+    const int d = a.d, units = d >> 4, end = begin + len;
+    const int turns = 16 / units;                    // 16-token groups at a time
+    const int turn_of = c16 / units, u = c16 - turn_of * units;
+    const bool used = turn_of < turns;
+    const Unit unit = unit_of(p, u);
+    const int g0 = begin >> 4;
+    const int n_pass = (((end + 15) >> 4) - g0 + turns - 1) / turns;
+    const RowsFrom from(p.k, i, h);
+    auto first_token = [&](int pass) { return (g0 + pass * turns + turn_of) * 16 + tq * 4; };
+    auto load = [&](int pass, float (&f)[4][16]) {
+        const int o0 = first_token(pass);
+        uint4 lo[4], hi[4];
+        int row[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            lo[j] = hi[j] = make_uint4(0, 0, 0, 0);
+            row[j] = 0;
+            if (used && o0 + j >= begin && o0 + j < end) {
+                const int64_t k = o0 + j - begin;
+                const uint8_t* at = from.row(p.k, (int)k);
+                lo[j] = *(const uint4*)(at + 16 * unit.c0);
+                hi[j] = *(const uint4*)(at + 16 * unit.c1);
+                if (unit.turned) row[j] = table_row(p, i + k);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float4 cs[4];
+            if (unit.turned) {
+                const float4* t = p.table + (int64_t)row[j] * (p.rot >> 2) + 4 * u;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) cs[e] = t[e];
+            }
+            turn<BF16>(lo[j], hi[j], cs, unit.turned, p.pairs, f[j]);
+        }
+    };
+    float held[kHeld][4][16];
+    // the largest of the values' bits without the sign, which are in the order of the numbers, and of the finite ones'
+    uint32_t most = 0;
+    auto look = [&](bool finite) {
+        for (int p0 = 0; p0 < n_pass; p0 += kHeld) {
+#pragma unroll
+            for (int t = 0; t < kHeld; ++t) {
+                if (p0 + t >= n_pass) break;
+                load(p0 + t, held[t]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const uint32_t b = __float_as_uint(held[t][j][e]) & 0x7fffffffu;
+                        most = max(most, finite && b >= 0x7f800000u ? 0u : b);
+                    }
+            }
+        }
+#pragma unroll
+        for (int k = 1; k < 64; k <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, k, 64));
+    };
+    look(false);
+    const bool special = most >= 0x7f800000u;
+    if (special) {
+        most = 0;
+        look(true);
+    }
+    const float largest = __uint_as_float(most);
+    float* sp = (float*)&a.scales[page * a.heads + h];
+    float s = largest < 0x1p-90f ? 0.0f : largest * (1.0f / kLargest);
+    uint8_t* codes = a.k_codes + (page * a.heads + h) * (int64_t)a.page * d;
+    float grow = 1.0f;
+    if (begin) {
+        const float was = *sp;
+        s = fmaxf(s, was);
+        if (s > was) {
+            grow = was / s;
+            rescale_before<E4M3>(codes, d, false, begin, grow);
+        }
+    }
+    wave_sync();   // every lane has read the scale
+    if (lane == 0) *sp = s;
+    const float inv = s > 0.0f ? 1.0f / s : 0.0f;
+    float low[16], high[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) low[e] = kInf, high[e] = -kInf;
+    for (int p0 = 0; p0 < n_pass; p0 += kHeld) {
+#pragma unroll
+        for (int t = 0; t < kHeld; ++t) {
+            if (p0 + t >= n_pass) break;
+            if (n_pass > kHeld) load(p0 + t, held[t]);
+            const int o0 = first_token(p0 + t);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float (&f)[16] = held[t][j];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float x = f[e];
+                    f[e] = x * inv;
+                    if (special) f[e] = fabsf(x) < kInf ? f[e] : x != x ? 0.0f : copysignf(kLargest, x);
+                }
+                const bool there = used && o0 + j >= begin && o0 + j < end;
+                if (p.boxes) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        low[e] = fminf(low[e], there ? f[e] : kInf);
+                        high[e] = fmaxf(high[e], there ? f[e] : -kInf);
+                    }
+                }
+                uint32_t w[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float four[4] = {f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]};
+                    w[k] = near_codes<E4M3>(four);
+                }
+                if (there) {
+                    uint8_t* at = codes + (o0 + j) * d;
+                    *(uint2*)(at + 8 * unit.c0) = make_uint2(w[0], w[1]);
+                    *(uint2*)(at + 8 * unit.c1) = make_uint2(w[2], w[3]);
+                }
+            }
+        }
+    }
+    if (!p.boxes) return;
+    // The lanes of a unit together, and with the page's box before the run: a lane four channels.
+    wave_sync();   // (of the run before)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s_box[e * 64 + lane] = low[e], s_box[(16 + e) * 64 + lane] = high[e];
+    wave_sync();
+    if (4 * lane >= d) return;
+    const int chunk = lane >> 1, half = p.rot >> 4;
+    const bool apart = !p.pairs && chunk < 2 * half;
+    const int of = apart ? (chunk >= half ? chunk - half : chunk) : chunk >> 1;
+    const int e0 = 8 * (apart ? chunk >= half : chunk & 1) + 4 * (lane & 1);
+    uint32_t* box = (uint32_t*)(p.boxes + (page * a.heads + h) * 2 * (int64_t)d) + lane;
+    float lo[4], hi[4];
+    if (begin) {
+        codes_to_f32<E4M3>(box[0], lo);
+        codes_to_f32<E4M3>(box[d / 4], hi);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) lo[e] *= grow, hi[e] *= grow;
+        codes_to_f32<E4M3>(f32_to_codes<E4M3>(lo), lo);
+        codes_to_f32<E4M3>(f32_to_codes<E4M3>(hi), hi);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) lo[e] = kInf, hi[e] = -kInf;
+    }
+    for (int t = 0; t < turns; ++t)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int from_lane = 16 * q + t * units + of;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                lo[e] = fminf(lo[e], s_box[(e0 + e) * 64 + from_lane]);
+                hi[e] = fmaxf(hi[e], s_box[(16 + e0 + e) * 64 + from_lane]);
+            }
+        }
+    box[0] = f32_to_codes<E4M3>(lo);
+    box[d / 4] = f32_to_codes<E4M3>(hi);
+}
+
+// Query rows: a lane one unit of kQHeads heads of a token, whose table entries it
+// reads once.
+constexpr int kQHeads = 4;
+
+template <bool BF16>
+__device__ __forceinline__ void turn_queries(const PageArgs& a, const AppendArgs& p, int64_t item)
+{
+    const int64_t at = item * 64 + (threadIdx.x & 63);
+    if (at >= p.q_lanes) return;
+    const uint32_t units = a.d >> 4;
+    const int64_t tg = (at >> 32) ? at / units : (uint32_t)at / units;
+    const int u = (int)(at - tg * units);
+    const int64_t i = (tg >> 32) ? tg / p.q_groups : (uint32_t)tg / (uint32_t)p.q_groups;
+    const int h0 = (int)(tg - i * p.q_groups) * kQHeads;
+    if (p.rot && p.positions[i] < 0 && a.slots[i] < 0) return;   // no row of a request
+    const Unit unit = unit_of(p, u);
+    float4 cs[4];
+    if (unit.turned) {
+        const float4* t = p.table + (int64_t)table_row(p, i) * (p.rot >> 2) + 4 * u;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) cs[e] = t[e];
+    }
+    const uint8_t* in = RowsFrom(p.q, i, 0).at;
+    uint8_t* out = RowsFrom(p.q_out, i, 0).at;
+    uint4 lo[kQHeads], hi[kQHeads];
+#pragma unroll
+    for (int k = 0; k < kQHeads; ++k) {
+        const uint8_t* row = in + 2 * (int64_t)min(h0 + k, p.q_heads - 1) * p.q.stride_head;
+        lo[k] = *(const uint4*)(row + 16 * unit.c0);
+        hi[k] = *(const uint4*)(row + 16 * unit.c1);
+    }
+#pragma unroll
+    for (int k = 0; k < kQHeads; ++k) {
+        if (h0 + k >= p.q_heads) break;
+        float f[16];
+        turn<BF16>(lo[k], hi[k], cs, unit.turned, p.pairs, f);
+        uint8_t* row = out + 2 * (int64_t)(h0 + k) * p.q_out.stride_head;
+        uint32_t w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = f32_to_row2(f[2 * e], f[2 * e + 1], BF16);
+        *(uint4*)(row + 16 * unit.c0) = make_uint4(w[0], w[1], w[2], w[3]);
+        *(uint4*)(row + 16 * unit.c1) = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+}
+
+// A wave a run and head of K or of V, then waves for the query rows.
+template <bool E4M3, bool BF16>
+__global__ __launch_bounds__(kThreads, 2) void page_append_kernel(PageArgs a, AppendArgs p)
+{
+    __shared__ float s_box[kWaves][32 * 64];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t item = (int64_t)blockIdx.x * kWaves + wave;
+    if (item >= p.store_items) {
+        if (p.q_lanes) turn_queries<BF16>(a, p, item - p.store_items);
+        return;
+    }
+    const bool values = item & 1;
+    const uint32_t hw = (uint32_t)(item >> 1);   // at most 2^31 windows x heads
+    const int h = (int)(hw % (uint32_t)a.heads);
+    const int64_t w0 = (int64_t)(hw / (uint32_t)a.heads) * p.window;
+    const int64_t pool = a.n_pages * a.page;
+    unsigned long long begins = run_begins(a, w0, p.window, [&](int64_t i, int64_t slot) {
+        if (!p.n_bad || h || values) return;
+        const int64_t pos = p.rot ? p.positions[i] : 0;
+        if (slot >= pool || (p.rot && (pos >= p.n_pos || (pos < 0 && slot >= 0)))) atomicAdd(p.n_bad, 1u);
+    });
+    while (begins) {
+        const int64_t i = w0 + __builtin_ctzll(begins);
+        begins &= begins - 1;
+        const int64_t slot = a.slots[i];
+        const int64_t page = slot / a.page;
+        const int begin = (int)(slot - page * a.page);
+        const int len = run_length(a, i, slot, begin);
+        if (values)
+            store_run<E4M3, BF16>(a, p.v, true, i, h, page, begin, len);
+        else
+            append_keys<E4M3, BF16>(a, p, s_box[wave], i, h, page, begin, len);
+    }
+}
+
+}  // namespace
+}  // namespace fkv
+
+using namespace fkv;
+
+extern "C" int fkv_page_append(const fkv_page_desc* desc, const fkv_rotate_desc* rotate, const fkv_row_desc* rows_q,
+                               const fkv_row_desc* rows_q_out, const fkv_row_desc* rows_k, const fkv_row_desc* rows_v,
+                               const void* q_rows, void* q_out, const void* k_rows, const void* v_rows, int64_t n_tokens,
+                               const int64_t* slots, const int32_t* positions, const float* table, uint8_t* k_codes,
+                               uint8_t* v_codes, float* scales, uint8_t* boxes, uint32_t* n_bad, void* stream)
+{
+    if (!page_desc_ok(desc) || !row_desc_ok(rows_k) || !row_desc_ok(rows_v) || rows_k->type != rows_v->type || n_tokens < 0 ||
+        n_tokens > kMostRows)
+        return FKV_ERR_INVALID_ARG;
+    const int32_t rot = rotate ? rotate->rot : 0;
+    if (rotate && (rot < 0 || rot > desc->d || rot % 16 || (rotate->pairing != FKV_ROTATE_HALVES && rotate->pairing != FKV_ROTATE_PAIRS) ||
+                   (rot && (rotate->n_pos < 1 || rotate->n_pos > ((int64_t)1 << 31) || !table || !aligned(table, 16)))))
+        return FKV_ERR_INVALID_ARG;
+    const bool with_q = q_rows != nullptr;
+    if (with_q != (q_out != nullptr)) return FKV_ERR_INVALID_ARG;
+    if (with_q && (!rotate || rotate->q_heads < 1 || rotate->q_heads > 65535 || !row_desc_ok(rows_q) || !row_desc_ok(rows_q_out) ||
+                   rows_q->type != rows_k->type || rows_q_out->type != rows_k->type || !aligned(q_rows, 16) || !aligned(q_out, 16)))
+        return FKV_ERR_INVALID_ARG;
+    if (!k_codes || !v_codes || !scales || !aligned(k_codes, 16) || !aligned(v_codes, 16) || !aligned(scales, 8) ||
+        !aligned(boxes, 16) || !aligned(n_bad, 4))
+        return FKV_ERR_INVALID_ARG;
+    if (n_tokens == 0) return FKV_OK;
+    if (!k_rows || !v_rows || !slots || !aligned(k_rows, 16) || !aligned(v_rows, 16) || !aligned(slots, 8) ||
+        (rot && (!positions || !aligned(positions, 4))))
+        return FKV_ERR_INVALID_ARG;
+    const PageArgs a = {k_codes, v_codes, (float2*)scales, slots, n_tokens, desc->n_pages, desc->page, desc->heads, desc->d};
+    AppendArgs p = {};
+    p.q = rows_of(rows_q, q_rows), p.q_out = rows_of(rows_q_out, q_out);
+    p.k = rows_of(rows_k, k_rows), p.v = rows_of(rows_v, v_rows);
+    p.positions = positions, p.table = (const float4*)table, p.boxes = boxes, p.n_bad = n_bad;
+    p.n_pos = rotate ? rotate->n_pos : 0;
+    p.rot = rot;
+    p.pairs = rotate && rotate->pairing == FKV_ROTATE_PAIRS;
+    // a wave looks at one row, or at a page's worth where the rows are many
+    p.window = n_tokens * desc->heads <= 32768 ? 1 : min(desc->page, 64);
+    p.store_items = (n_tokens + p.window - 1) / p.window * desc->heads * 2;
+    if (with_q) {
+        p.q_heads = rotate->q_heads;
+        p.q_groups = (p.q_heads + kQHeads - 1) / kQHeads;
+        p.q_lanes = n_tokens * p.q_groups * (desc->d / 16);
+    }
+    const int64_t items = p.store_items + (p.q_lanes + 63) / 64;
+    if (p.store_items > kMostBlocks || (items + kWaves - 1) / kWaves > kMostBlocks) return FKV_ERR_UNSUPPORTED;
+    const bool e4m3 = desc->format == FKV_PAGE_E4M3, bf16 = rows_k->type == FKV_ROW_BF16;
+    auto kern = e4m3 ? bf16 ? page_append_kernel<true, true> : page_append_kernel<true, false>
+                     : bf16 ? page_append_kernel<false, true> : page_append_kernel<false, false>;
+    hipLaunchKernelGGL(kern, dim3((unsigned)((items + kWaves - 1) / kWaves)), dim3(kThreads), 0, (hipStream_t)stream, a, p);
+    return launch_status();
+}

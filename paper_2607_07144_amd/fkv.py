@@ -40,6 +40,7 @@ class fkv_rvq_desc(ctypes.Structure):
 
 FKV_PAGE_INT8, FKV_PAGE_E4M3 = 0, 1
 FKV_ROW_F16, FKV_ROW_BF16 = 0, 1
+FKV_ROTATE_HALVES, FKV_ROTATE_PAIRS = 0, 1
 
 
 class fkv_page_desc(ctypes.Structure):
@@ -50,6 +51,11 @@ class fkv_page_desc(ctypes.Structure):
 class fkv_row_desc(ctypes.Structure):
     _fields_ = [("group", ctypes.c_int64), ("stride_group", ctypes.c_int64), ("stride_token", ctypes.c_int64),
                 ("stride_head", ctypes.c_int64), ("type", ctypes.c_int32)]
+
+
+class fkv_rotate_desc(ctypes.Structure):
+    _fields_ = [("n_pos", ctypes.c_int64), ("rot", ctypes.c_int32), ("pairing", ctypes.c_int32),
+                ("q_heads", ctypes.c_int32)]
 
 
 class fkv_attend_desc(ctypes.Structure):
@@ -90,6 +96,7 @@ _SIGS = {
     "fkv_page_plan": ([_i32, _i64, _p, _p, _p, _i64, _p, _p, _i64, _i64, _p, _p, _p, _p, _p, _p, _p, _p, _p],
                       ctypes.c_int),
     "fkv_page_store": ([_p, _p, _p, _p, _p, _i64, _p, _p, _p, _p, _p, _p], ctypes.c_int),
+    "fkv_page_append": ([_p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _i64, _p, _p, _p, _p, _p, _p, _p, _p, _p], ctypes.c_int),
     "fkv_page_load": ([_p, _p, _p, _p, _i64, _p, _p, _p, _p, _p, _p], ctypes.c_int),
     "fkv_page_attend_workspace": ([_p, _p], _sz),
     "fkv_page_attend": ([_p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _sz, _p], ctypes.c_int),
@@ -670,6 +677,80 @@ def fkv_page_store(pages, k, v, slots, n_bad=None, stream=None):
     _check(lib.fkv_page_store(ref(desc), ref(rk), ref(rv), k.data_ptr(), v.data_ptr(), slots.numel(),
                               slots.data_ptr(), pages[0].data_ptr(), pages[1].data_ptr(), pages[2].data_ptr(),
                               _ptr(n_bad), _stream(stream)), "fkv_page_store")
+
+
+def fkv_boxes(pages):
+    """Boxes of a pool's pages, for fkv_page_append and fkv_page_select: codes of the pages' type
+    [n_pages][heads][2][d], the smallest and largest of each key channel."""
+    torch = _TORCH or _torch()
+    n, heads, _, d = pages[0].shape
+    return torch.zeros((n, heads, 2, d), dtype=torch.uint8, device=pages[0].device).view(pages[0].dtype)
+
+
+def fkv_rotation_table(n_pos: int, rot: int, base: float = 10000.0, device="cuda"):
+    """A table for fkv_page_append, f32 [n_pos][rot // 2][2]: cosines and sines of the angles p * base ** (-2 i / rot),
+    formed in 64 bits.  Tables of other frequencies, or with a factor, are made the same way."""
+    torch = _TORCH or _torch()
+    freq = base ** (-torch.arange(0, rot, 2, dtype=torch.float64, device=device) / rot)
+    angle = torch.arange(n_pos, dtype=torch.float64, device=device)[:, None] * freq
+    return torch.stack((angle.cos(), angle.sin()), -1).float()
+
+
+def _need_boxes(boxes, pages) -> None:
+    k = pages[0]
+    _need(boxes, k.dtype, "boxes")
+    n, heads, _, d = k.shape
+    if boxes.shape != (n, heads, 2, d):
+        raise ValueError("boxes must be [n_pages][heads][2][d]")
+
+
+def fkv_page_append(pages, k, v, slots, positions=None, table=None, q=None, q_out=None, pairs: bool = False,
+                    boxes=None, n_bad=None, stream=None):
+    """Writes rows into the pages' slots as fkv_page_store does, the key rows turned by their positions on the way, and
+    turns the query rows: k, v, q f16 or bf16 [n][heads][d] for slots i64 [n] and positions i32 [n], or [b][heads][t][d]
+    for [b][t]; table f32 [n_pos][rot // 2][2] (fkv_rotation_table), None for no rotation; channels (i, i + rot // 2) are
+    turned together, or (2i, 2i + 1) with pairs.  boxes (fkv_boxes) of the pages written are kept up to date.  Returns
+    the query rows (q_out, which may be q; by default new ones), or None without q."""
+    torch = _TORCH or _torch()
+    desc = _page_desc(pages)
+    _need(slots, torch.int64, "slots")
+    if n_bad is not None:
+        _need(n_bad, torch.int32, "n_bad")
+    heads, d = desc.heads, desc.d
+    rk, rv = _rows(k, slots, heads, d, "k"), _rows(v, slots, heads, d, "v")
+    rotate = rq = ro = None
+    n_pos = rot = q_heads = 0
+    if table is not None:
+        _need(table, torch.float32, "table")
+        if table.dim() != 3 or table.shape[2] != 2:
+            raise ValueError("table must be [n_pos][rot // 2][2]")
+        n_pos, rot = table.shape[0], 2 * table.shape[1]
+        if positions is None:
+            raise TypeError("a rotation needs positions")
+        _need(positions, torch.int32, "positions")
+        if positions.shape != slots.shape:
+            raise ValueError("positions and slots differ in shape")
+    if q is not None:
+        if q.dim() != len(slots.shape) + 2:
+            raise ValueError("q must be [n][q_heads][d] for slots [n] or [b][q_heads][t][d] for slots [b][t]")
+        q_heads = q.shape[1]
+        rq = _rows(q, slots, q_heads, d, "q")
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        ro = _rows(q_out, slots, q_heads, d, "q_out")
+    elif q_out is not None:
+        raise TypeError("q_out without q")
+    if boxes is not None:
+        _need_boxes(boxes, pages)
+    ref = ctypes.byref
+    if rot or rq is not None:
+        rotate = ref(fkv_rotate_desc(n_pos, rot, FKV_ROTATE_PAIRS if pairs else FKV_ROTATE_HALVES, q_heads))
+    _check(lib.fkv_page_append(ref(desc), rotate, None if rq is None else ref(rq), None if ro is None else ref(ro),
+                               ref(rk), ref(rv), _ptr(q), _ptr(q_out), k.data_ptr(), v.data_ptr(), slots.numel(),
+                               slots.data_ptr(), _ptr(positions) if rot else None, _ptr(table) if rot else None,
+                               pages[0].data_ptr(), pages[1].data_ptr(), pages[2].data_ptr(), _ptr(boxes), _ptr(n_bad),
+                               _stream(stream)), "fkv_page_append")
+    return q_out
 
 
 def fkv_page_load(pages, slots, dtype=None, k=None, v=None, stream=None):
