@@ -563,6 +563,73 @@ int fkv_page_attend(const fkv_page_desc* desc, const fkv_attend_desc* attend, co
                     const int32_t* first, void* out, float* lse, void* workspace, size_t workspace_bytes,
                     void* stream);
 
+/* The pages of long contexts that are worth attending to: for each query token and
+ * KV head, n_select of the pages that the token sees.  The token (row) i of request r,
+ * as of fkv_page_attend, sees the pages 0 .. P-1 of its block table, with
+ *     P = ceil(kv_len / page), or with causal = 1 ceil(min(pos + 1, kv_len) / page).
+ * With P <= n_select all are selected.  Otherwise the first keep_first and the last
+ * keep_last are, and of the others those with the largest scores, of equal ones the
+ * first.  A page's score is a bound on its keys' products with q, in units of its own:
+ *     w_c = round(q_c * 2^e), to nearest, ties to even, held to -127 .. 127, with 2^e
+ *           bringing the row's largest finite |q_c| to [64, 128) (e at most 126; a row
+ *           with none above 2^-126 has e = 0); a NaN counts as 0
+ *     S = sum_c max(w_c * lo_c, w_c * hi_c)                          (whole numbers)
+ *     score = the largest, over the query heads of the KV head, of
+ *             ((float)S * scale) * 2^-e                    (two products in fp32)
+ * with lo and hi the page's box: its codes (int8), or floor(code / 4) and
+ * ceil(code / 4) (8-bit floats), and scale its key scale.  A product that is a NaN, and
+ * any of a table entry that is no page of the pool, counts as -infinity.
+ *   boxes      device [n_pages][heads][2][d] codes, 16-byte aligned, as
+ *              fkv_page_append keeps them; scales: the pages'
+ *   q          rows [n_tokens][q_heads][d] with the strides given, 16-byte aligned
+ *   tables, kv_len, q_start, max_new, max_kv, max_pages   as for fkv_page_attend
+ *   selected   device out int32 [n_tokens][heads][n_select]: columns of the token's
+ *              block table, ascending; -1 after the last.  Rows that fkv_page_attend
+ *              leaves unwritten are left as they were
+ *   workspace  device scratch of fkv_page_select_workspace() bytes, 16-byte aligned;
+ *              null when that is 0.  Calls that may run at the same time need one each
+ * n_select: 1 .. 2^20, keep_first + keep_last at most n_select.  FKV_ERR_UNSUPPORTED
+ * for more blocks than a launch holds (n_req * max_new * heads beyond 2^31). */
+typedef struct {
+    int64_t n_req;
+    int64_t n_tokens;
+    int64_t max_new;
+    int64_t max_kv;
+    int64_t max_pages;
+    int64_t q_stride_token, q_stride_head;
+    int32_t q_heads;
+    int32_t type;
+    int32_t causal; /* 0 or 1 */
+    int32_t n_select;
+    int32_t keep_first;
+    int32_t keep_last;
+} fkv_select_desc;
+
+size_t fkv_page_select_workspace(const fkv_page_desc* desc, const fkv_select_desc* select);
+
+int fkv_page_select(const fkv_page_desc* desc, const fkv_select_desc* select, const uint8_t* boxes, const float* scales,
+                    const void* q, const int32_t* tables, const int32_t* kv_len, const int32_t* q_start,
+                    int32_t* selected, void* workspace, size_t workspace_bytes, void* stream);
+
+/* fkv_page_attend over lists of pages: key j of a request is visible to a row and KV
+ * head when it is to fkv_page_attend's and its page is listed for them.
+ *   selected    device int32 [n_tokens][heads][n_selected] columns of the token's block
+ *               table, in any order (fkv_page_select's form); an entry that is none of
+ *               the request's columns (-1) lists nothing, and the keys of a page listed
+ *               more than once count as often
+ *   n_selected  1 .. 2^20
+ *   workspace   of fkv_page_attend_selected_workspace() bytes
+ * The other arguments, accuracy and errors are fkv_page_attend's, but for its limits
+ * on rows: FKV_ERR_UNSUPPORTED for more blocks than a launch holds (n_req * max_new *
+ * heads beyond 2^31). */
+size_t fkv_page_attend_selected_workspace(const fkv_page_desc* desc, const fkv_attend_desc* attend, int64_t n_selected);
+
+int fkv_page_attend_selected(const fkv_page_desc* desc, const fkv_attend_desc* attend, int64_t n_selected,
+                             const int32_t* selected, const uint8_t* k_codes, const uint8_t* v_codes,
+                             const float* scales, const void* q, const int32_t* tables, const int32_t* kv_len,
+                             const int32_t* q_start, const float* slopes, const int32_t* prefix, const int32_t* first,
+                             void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---------------------------------------------------------------------------
  * Measurement aid (not part of the archive path).
  *

@@ -18,7 +18,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libfkv.so")
 
 SOURCES = ["fkv_codec.cpp", "cgr_kernels.hip", "rvq_kernels.hip", "archive_kernels.hip", "kmeans_kernels.hip",
-           "page_kernels.hip", "page_append_kernels.hip", "page_attend_kernels.hip", "diag_kernels.hip"]
+           "page_kernels.hip", "page_append_kernels.hip", "page_attend_kernels.hip", "page_select_kernels.hip",
+           "diag_kernels.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

@@ -1,0 +1,753 @@
+// page_select_kernels.hip -- attention to a few pages of a long context, for
+// gfx950: a bound on the scores of each page's keys, the pages with the largest
+// bounds for each query token and KV head, and attention over lists of pages.
+//
+// A page's box holds the smallest and largest code of every key channel, lo and hi,
+// so that no key of the page has a product with q above
+//     sum_c max(q_c lo_c, q_c hi_c) = sum_c q+_c hi_c + q-_c lo_c,
+// with q+ and q- the positive and negative parts of q: a matrix product of twice the
+// keys' width.  It is formed of whole numbers, q being rounded to 8 bits with a power
+// of two for each row, so that it is exact in any order: which pages are selected does
+// not depend on how the work is dealt out.
+#include "page_attend_device.h"
+
+#include <algorithm>
+
+namespace fkv {
+namespace {
+
+typedef int int4_t __attribute__((ext_vector_type(4)));
+
+struct SelectArgs : AttendArgs {
+    const uint8_t* boxes;
+    float* scores;      // [token][KV head][score_stride]
+    int32_t* selected;  // [token][KV head][n_select]
+    int64_t score_stride;
+    int64_t row_groups;   // of the scoring kernel: row tiles of a request, R a wave
+    int32_t n_select, keep_first, keep_last;
+    int32_t tile_chunks;  // and its blocks along the pages, of wave_tiles tiles of 16 pages a wave
+    int32_t wave_tiles;
+    int32_t lanes_log;    // a token's rows of a tile: a power of two of them
+};
+
+__device__ __forceinline__ int pages_of(const AttendArgs& a, int tokens)   // tokens >= 0
+{
+    const uint32_t groups = (uint32_t)((int64_t)tokens + 15) >> 4;
+    if (groups == 0) return 0;
+    return (int)(a.per_page_inv ? __umulhi(groups - 1, a.per_page_inv) : groups - 1) + 1;
+}
+
+// The pages that token i of a request may select from.
+__device__ __forceinline__ int pages_seen(const AttendArgs& a, const Request& rq, int i)
+{
+    const int end = a.causal ? min(rq.pos0 + i + 1, rq.kv) : rq.kv;
+    return pages_of(a, max(end, 0));
+}
+
+// ---------------------------------------------------------------- scores --
+
+// Four codes of a box as 8-bit whole numbers: int8 codes as they are, 8-bit floats
+// in units of 4, rounded away from the box's inside (HIGH: up).
+template <bool E4M3, bool HIGH>
+__device__ __forceinline__ uint32_t whole4(uint32_t w)
+{
+    if (!E4M3) return w;
+    float f[4];
+    codes_to_f32<true>(w, f);
+    uint32_t u[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) u[e] = (uint32_t)(int)(HIGH ? ceilf(f[e] * 0.25f) : floorf(f[e] * 0.25f));
+    const uint32_t lo = __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(u[3], u[2], 0x0c0c0400u);
+    return __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+}
+
+template <bool E4M3, bool HIGH>
+__device__ __forceinline__ int4_t whole16(uint4 w)
+{
+    return int4_t{(int)whole4<E4M3, HIGH>(w.x), (int)whole4<E4M3, HIGH>(w.y), (int)whole4<E4M3, HIGH>(w.z), (int)whole4<E4M3, HIGH>(w.w)};
+}
+
+// The largest of the lanes that share all bits of their number but the lowest `log`
+// (up to four).
+__device__ __forceinline__ float lanes_max(float v, int log)
+{
+    auto with = [&](auto ctrl) {
+        const int u = __builtin_bit_cast(int, v);
+        v = fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(u, u, decltype(ctrl)::value, 0xf, 0xf, false)));
+    };
+    if (log > 0) with(std::integral_constant<int, 0xb1>{});    // with the neighbour,
+    if (log > 1) with(std::integral_constant<int, 0x4e>{});    // the other pair of four,
+    if (log > 2) with(std::integral_constant<int, 0x141>{});   // the other four of eight,
+    if (log > 3) with(std::integral_constant<int, 0x140>{});   // the other eight
+    return v;
+}
+
+// Sixteen rows -- a few tokens' heads of one KV head, or 16 of one token's -- as whole
+// numbers: the right operand of the product, positive and negative parts.
+template <int NC>
+struct RowTile {
+    int4_t plus[NC], minus[NC];
+    float mul;   // 2^-e
+};
+
+template <int NC>
+__device__ __forceinline__ RowTile<NC> row_tile(const SelectArgs& a, const Request& rq, int tok, int head)
+{
+    const int g = (threadIdx.x & 63) >> 4;
+    const uint8_t* qp = a.q + 2 * ((int64_t)(rq.start + tok) * a.q_token + head * a.q_head);
+    uint4 w[NC][2];
+    float most = 0.0f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        const int e = c * 64 + g * 16;
+        w[c][0] = w[c][1] = make_uint4(0, 0, 0, 0);
+        if (e < a.d) w[c][0] = *(const uint4*)(qp + 2 * e), w[c][1] = *(const uint4*)(qp + 2 * e + 16);
+    }
+    auto each = [&](auto f) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                const uint4 u = w[c][k >> 3];
+                const uint32_t pair[4] = {u.x, u.y, u.z, u.w};
+                f(c, k, row_to_f32(pair[(k >> 1) & 3], k & 1, a.bf16));
+            }
+    };
+    each([&](int, int, float x) { most = fmaxf(most, fabsf(x) < __builtin_inff() ? fabsf(x) : 0.0f); });
+    most = rows_max(most);
+    const int ex = (int)(__float_as_uint(most) >> 23);
+    const int e = ex == 0 ? 0 : min(133 - ex, 126);
+    const float mul = pow2(e);
+    RowTile<NC> t;
+    t.mul = pow2(-e);
+    uint32_t plus[NC][4], minus[NC][4];
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) plus[c][k] = minus[c][k] = 0;
+    each([&](int c, int k, float x) {
+        const float y = rintf(fminf(fmaxf(x == x ? x * mul : 0.0f, -127.0f), 127.0f));
+        const int v = (int)y;
+        plus[c][k >> 2] |= (uint32_t)max(v, 0) << (8 * (k & 3));
+        minus[c][k >> 2] |= (uint32_t)(min(v, 0) & 0xff) << (8 * (k & 3));
+    });
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        t.plus[c] = int4_t{(int)plus[c][0], (int)plus[c][1], (int)plus[c][2], (int)plus[c][3]};
+        t.minus[c] = int4_t{(int)minus[c][0], (int)minus[c][1], (int)minus[c][2], (int)minus[c][3]};
+    }
+    return t;
+}
+
+// A wave: R tiles of 16 rows of one KV head of a request against wave_tiles tiles of
+// 16 pages.  The left operand takes a page's box as one of its rows, so that lane
+// 16g + c ends up with row c's sums of pages 4g .. 4g+3.
+template <bool E4M3, int NC, int R>
+__global__ __launch_bounds__(kThreads) void page_score_kernel(SelectArgs a)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int c16 = lane & 15, g = lane >> 4;
+    uint32_t b = blockIdx.x;
+    const int h = (int)(b % (uint32_t)a.heads);
+    b /= (uint32_t)a.heads;
+    const int chunk = (int)(b % (uint32_t)a.tile_chunks);
+    b /= (uint32_t)a.tile_chunks;
+    const int64_t r = b / (uint32_t)a.row_groups;
+    const int rg = (int)(b - (uint32_t)r * (uint32_t)a.row_groups);
+    const Request rq = request_of(a, r);
+    // tokens of a tile, of the wave, and this lane's in its first tile
+    const int per_tile = 16 >> a.lanes_log;
+    const int tok0 = rg * R * per_tile;
+    if (tok0 >= rq.rows) return;
+    const int most_seen = pages_seen(a, rq, min(tok0 + R * per_tile, rq.rows) - 1);   // (later tokens see no fewer)
+    if (most_seen <= a.n_select) return;   // every page of theirs is selected
+    const int tiles = (most_seen + 15) >> 4;
+    const int first = chunk * a.wave_tiles * kWaves + wave;
+    if (first >= tiles) return;
+    const int n_tiles = min(a.wave_tiles, (tiles - first + kWaves - 1) / kWaves);
+
+    const int32_t* table = a.tables + r * a.max_pages;
+    int kc[NC];   // channels beyond d are taken from the last ones: q is zero there
+#pragma unroll
+    for (int c = 0; c < NC; ++c) kc[c] = min(c * 64 + g * 16, a.d - 16);
+    struct Pages {
+        uint4 lo[NC], hi[NC];
+        float scale;   // of page c16; a NaN where there is none
+    };
+    auto id_of = [&](int k) { return table[min((first + k * kWaves) * 16 + c16, most_seen - 1)]; };
+    auto load = [&](int id) {
+        Pages p;
+        const bool here = (uint32_t)id < (uint64_t)a.n_pages;
+        const int64_t at = (here ? id : 0) * (int64_t)a.heads + h;
+        p.scale = here ? a.scales[at].x : __builtin_nanf("");
+        const uint8_t* box = a.boxes + at * 2 * a.d;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) p.lo[c] = *(const uint4*)(box + kc[c]), p.hi[c] = *(const uint4*)(box + a.d + kc[c]);
+        return p;
+    };
+    int id1 = id_of(min(1, n_tiles - 1));
+    Pages next = load(id_of(0));
+    const int chunks = (a.group + 15) >> 4;   // of a token's heads, 16 a tile
+    auto tile_at = [&](int t, int c) {
+        const int tok = min(tok0 + t * per_tile + (c16 >> a.lanes_log), rq.rows - 1);
+        const int in_group = min(c * 16 + (c16 & ((1 << a.lanes_log) - 1)), a.group - 1);
+        return row_tile<NC>(a, rq, tok, h * a.group + in_group);
+    };
+    RowTile<NC> rows[R];
+#pragma unroll
+    for (int t = 0; t < R; ++t) rows[t] = tile_at(t, 0);
+    for (int k = 0; k < n_tiles; ++k) {
+        const Pages now = next;
+        if (k + 1 < n_tiles) {
+            next = load(id1);
+            id1 = id_of(min(k + 2, n_tiles - 1));
+        }
+        int4_t lo[NC], hi[NC];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) lo[c] = whole16<E4M3, false>(now.lo[c]), hi[c] = whole16<E4M3, true>(now.hi[c]);
+        float scale[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) scale[i] = __shfl(now.scale, 4 * g + i, 64);
+        const int tile = first + k * kWaves;
+#pragma unroll
+        for (int t = 0; t < R; ++t) {
+            float x[4];
+            auto score = [&](const RowTile<NC>& row, bool again) {
+                int4_t sum = {0, 0, 0, 0};
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(hi[c], row.plus[c], sum, 0, 0, 0);
+                    sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(lo[c], row.minus[c], sum, 0, 0, 0);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float y = ((float)sum[i] * scale[i]) * row.mul;
+                    const float z = y == y ? y : -__builtin_inff();
+                    x[i] = again ? fmaxf(x[i], z) : z;
+                }
+            };
+            score(rows[t], false);
+            for (int c = 1; c < chunks; ++c) score(tile_at(t, c), true);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = lanes_max(x[i], a.lanes_log);
+            const int tok = tok0 + t * per_tile + (c16 >> a.lanes_log);
+            if ((c16 & ((1 << a.lanes_log) - 1)) == 0 && tok < rq.rows)
+                *(float4_t*)(a.scores + ((rq.start + tok) * (int64_t)a.heads + h) * a.score_stride + tile * 16 + g * 4) =
+                    float4_t{x[0], x[1], x[2], x[3]};
+        }
+    }
+}
+
+// ------------------------------------------------------------- selection --
+
+// Scores as whole numbers in their order, none of them 0.
+__device__ __forceinline__ uint32_t order_of(float x)
+{
+    const uint32_t u = __float_as_uint(x + 0.0f);   // (-0 is 0)
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// A row of the lists: token, KV head, and how many pages the token sees.
+struct SelectRow {
+    int64_t at;   // token * heads + h
+    int seen;
+    bool any;
+};
+
+__device__ __forceinline__ SelectRow select_row(const SelectArgs& a, int64_t item)
+{
+    SelectRow s = {0, 0, false};
+    if (item >= a.n_req * a.max_new * a.heads) return s;
+    const int h = (int)(item % a.heads);
+    const int64_t ri = item / a.heads;
+    const int64_t r = ri / a.max_new;
+    const int i = (int)(ri - r * a.max_new);
+    const Request rq = request_of(a, r);
+    if (i >= rq.rows) return s;
+    s.at = (rq.start + i) * (int64_t)a.heads + h;
+    s.seen = pages_seen(a, rq, i);
+    s.any = true;
+    return s;
+}
+
+// A wave a row, its scores in registers: page 64 n + lane in key[n].  The smallest
+// score selected is found bit by bit from the first that the scores differ in; each
+// step counts those above by ballots, and the search ends when the count fits.
+template <int N>
+__global__ __launch_bounds__(kThreads) void page_select_kernel(SelectArgs a)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const SelectRow row = select_row(a, (int64_t)blockIdx.x * kWaves + wave);
+    if (!row.any) return;
+    int32_t* out = a.selected + row.at * a.n_select;
+    if (row.seen <= a.n_select) {
+        for (int j = lane; j < a.n_select; j += 64) out[j] = j < row.seen ? j : -1;
+        return;
+    }
+    // (more pages than are selected: those always kept are apart from each other)
+    const int from = a.keep_first, to = row.seen - a.keep_last, want = a.n_select - a.keep_first - a.keep_last;
+    const float* scores = a.scores + row.at * a.score_stride;
+    uint32_t key[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const int p = 64 * n + lane;
+        key[n] = 0;
+        if (p >= from && p < to) key[n] = order_of(scores[p]);
+    }
+    uint32_t top = 0, low = 0xffffffffu;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        top = max(top, key[n]);
+        low = min(low, key[n] ? key[n] : 0xffffffffu);
+    }
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) {
+        top = max(top, (uint32_t)__shfl_xor((int)top, k, 64));
+        low = min(low, (uint32_t)__shfl_xor((int)low, k, 64));
+    }
+    auto count = [&](uint32_t least) {
+        int c = 0;
+#pragma unroll
+        for (int n = 0; n < N; ++n) c += __builtin_popcountll(__ballot(key[n] >= least));
+        return c;
+    };
+    // the largest t of which `want` scores or more are not below
+    uint32_t t = 0xffffffffu;
+    int ties = 0;   // of those equal to t so many are taken, the first ones
+    if (want) {
+        const uint32_t differ = top ^ low;
+        int bit = differ ? 31 - __builtin_clz(differ) : -1;
+        t = bit < 0 ? top : top & ~((2u << bit) - 1u);
+        bool fits = false;
+        for (; bit >= 0 && !fits; --bit) {
+            const uint32_t c = t | 1u << bit;
+            const int n = count(c);
+            if (n >= want) t = c;
+            fits = n == want;
+        }
+        ties = fits ? 0x7fffffff : want - (t == 0xffffffffu ? 0 : count(t + 1));
+    }
+    int at = 0;
+    const unsigned long long below = (1ull << lane) - 1;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const int p = 64 * n + lane;
+        if (64 * n >= row.seen) break;
+        const unsigned long long same = __ballot(want && key[n] == t);
+        const bool kept = p < row.seen && (p < from || p >= to);
+        const bool take = kept || (want && key[n] > t) || (want && key[n] == t && __builtin_popcountll(same & below) < ties);
+        ties -= min(ties, (int)__builtin_popcountll(same));
+        const unsigned long long m = __ballot(take);
+        if (take) out[at + __builtin_popcountll(m & below)] = p;
+        at += __builtin_popcountll(m);
+    }
+}
+
+// A block a row, for more pages than a wave holds: digits of 8 bits from the first
+// bit that the scores differ in, each from a histogram of those that share the digits
+// before.
+constexpr int kWideThreads = 1024;
+
+__global__ __launch_bounds__(kWideThreads) void page_select_wide_kernel(SelectArgs a)
+{
+    constexpr int kWideWaves = kWideThreads / 64;
+    __shared__ uint32_t s_count[256];
+    __shared__ uint32_t s_top[kWideWaves], s_low[kWideWaves];
+    __shared__ int s_before[kWideWaves], s_same[kWideWaves];
+    __shared__ uint32_t s_digit, s_left;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const SelectRow row = select_row(a, blockIdx.x);
+    if (!row.any) return;
+    int32_t* out = a.selected + row.at * a.n_select;
+    if (row.seen <= a.n_select) {
+        for (int j = tid; j < a.n_select; j += kWideThreads) out[j] = j < row.seen ? j : -1;
+        return;
+    }
+    const int from = a.keep_first, to = row.seen - a.keep_last, want = a.n_select - a.keep_first - a.keep_last;
+    const float* scores = a.scores + row.at * a.score_stride;
+    auto key_of = [&](int p) { return p >= from && p < to ? order_of(scores[p]) : 0u; };
+    uint32_t top = 0, low = 0xffffffffu;
+    for (int p = tid; p < row.seen; p += kWideThreads) {
+        const uint32_t k = key_of(p);
+        top = max(top, k);
+        low = min(low, k ? k : 0xffffffffu);
+    }
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) {
+        top = max(top, (uint32_t)__shfl_xor((int)top, k, 64));
+        low = min(low, (uint32_t)__shfl_xor((int)low, k, 64));
+    }
+    if (lane == 0) s_top[wave] = top, s_low[wave] = low;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWideWaves; ++w) top = max(top, s_top[w]), low = min(low, s_low[w]);
+
+    uint32_t t = 0xffffffffu;
+    int ties = 0;
+    if (want) {
+        const uint32_t differ = top ^ low;
+        int bits = differ ? 32 - __builtin_clz(differ) : 0;   // still open
+        t = bits == 32 ? 0 : top >> bits << bits;
+        int left = want;                                      // wanted of those that share the bits settled
+        while (bits > 0) {
+            const int shift = max(bits - 8, 0), n_digits = 1 << (bits - shift);
+            if (tid < 256) s_count[tid] = 0;
+            __syncthreads();
+            for (int p = tid; p < row.seen; p += kWideThreads) {
+                const uint32_t k = key_of(p);
+                if (k && ((k ^ t) >> 1 >> (bits - 1)) == 0) atomicAdd(&s_count[(k >> shift) & (uint32_t)(n_digits - 1)], 1u);
+            }
+            __syncthreads();
+            if (wave == 0) {
+                // four digits a lane, the largest first; the sum over larger ones says where `left` is reached
+                uint32_t c[4], sum = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    c[e] = s_count[255 - (4 * lane + e)];
+                    sum += c[e];
+                }
+                uint32_t upto = sum;
+#pragma unroll
+                for (int k = 1; k < 64; k <<= 1) {
+                    const uint32_t u = __shfl_up(upto, k, 64);
+                    if (lane >= k) upto += u;
+                }
+                uint32_t before = upto - sum;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (before < (uint32_t)left && before + c[e] >= (uint32_t)left) {
+                        s_digit = 255 - (4 * lane + e);
+                        s_left = (uint32_t)left - before;
+                    }
+                    before += c[e];
+                }
+            }
+            __syncthreads();
+            t |= s_digit << shift;
+            left = (int)s_left;
+            bits = shift;
+            __syncthreads();
+        }
+        ties = left;
+    }
+    // the list, 1024 pages at a time
+    int at = 0, same_before = 0;
+    const unsigned long long below = (1ull << lane) - 1;
+    for (int p0 = 0; p0 < row.seen; p0 += kWideThreads) {
+        const int p = p0 + tid;
+        const uint32_t k = key_of(p);
+        const unsigned long long same = __ballot(want && k == t);
+        if (lane == 0) s_same[wave] = __builtin_popcountll(same);
+        __syncthreads();
+        int rank = same_before + __builtin_popcountll(same & below);
+#pragma unroll
+        for (int w = 0; w < kWideWaves; ++w) {
+            if (w < wave) rank += s_same[w];
+            same_before += s_same[w];
+        }
+        const bool kept = p < row.seen && (p < from || p >= to);
+        const bool take = kept || (want && k > t) || (want && k == t && rank < ties);
+        const unsigned long long m = __ballot(take);
+        if (lane == 0) s_before[wave] = __builtin_popcountll(m);
+        __syncthreads();
+        int mine = at + __builtin_popcountll(m & below);
+#pragma unroll
+        for (int w = 0; w < kWideWaves; ++w) {
+            if (w < wave) mine += s_before[w];
+            at += s_before[w];
+        }
+        if (take) out[mine] = p;
+    }
+}
+
+// ----------------------------------------------------- attention to lists --
+
+// W waves an item -- a token, a KV head and up to 16 of its query heads -- that take
+// the list's tiles in turn, with those of the item's other splits; their sums joined
+// in LDS, and the splits' by a second kernel.
+template <bool E4M3, int NC, int W>
+__global__ __launch_bounds__(kThreads, NC <= 2 ? 2 : 1) void attend_listed_kernel(AttendArgs a)
+{
+    extern __shared__ __align__(16) float lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c16 = lane & 15, g = lane >> 4;
+    const int d = a.d;
+    const int64_t q_heads = (int64_t)a.heads * a.group;
+    const int split = (int)(blockIdx.x % (uint32_t)a.n_splits);
+    const int64_t block = blockIdx.x / (uint32_t)a.n_splits;
+    const int64_t item = W == 1 ? block * kWaves + wave : block;
+    const int chunks = (a.group + kFewRows - 1) / kFewRows;
+    if (item >= a.n_req * a.max_new * chunks * a.heads) return;
+    const int h = (int)(item % a.heads);
+    const int64_t of_token = item / a.heads;
+    const int chunk = (int)(of_token % chunks);
+    const int64_t r = of_token / chunks / a.max_new;
+    const int i = (int)(of_token / chunks - r * a.max_new);
+    const Request rq = request_of(a, r);
+    if (i >= rq.rows) return;
+    const int64_t token = rq.start + i;
+    const int32_t* list = a.listed + (token * a.heads + h) * a.n_listed;
+    int n = 0;   // entries up to the last that names a page
+    if (rq.kv > 0)
+        for (int j0 = 0; j0 < a.n_listed; j0 += 64) {
+            const unsigned long long m = __ballot(j0 + lane < a.n_listed && list[min((int64_t)(j0 + lane), a.n_listed - 1)] >= 0);
+            if (m) n = j0 + 64 - __builtin_clzll(m);
+        }
+    const int places = n * (int)a.per_page, tiles = (places + 3) >> 2;
+    const int n_rows = min(a.group - chunk * kFewRows, kFewRows);
+    const FewRow fr = {min(c16, n_rows - 1), i, h * a.group + chunk * kFewRows + min(c16, n_rows - 1)};
+    FewSums<NC> st;
+    const int e0 = split * W + (W == 1 ? 0 : wave);
+    if (e0 < tiles) few_keys<E4M3, NC, true>(a, rq, r, h, Tiles{}, fr, e0, a.n_splits * W, tiles, st, list, places);
+
+    if (W == 1) {
+        if (c16 >= n_rows) return;
+        const float inv = st.l == 0.0f ? 0.0f : st.vref * (1.0f / kTop) / st.l;
+#pragma unroll
+        for (int t = 0; t < 4 * NC; ++t) {
+            const float4_t o = st.acc[t] * inv;
+            if (t * 16 < d)
+                *(uint2*)(a.out + 2 * (token * a.o_token + fr.head * a.o_head + t * 16 + g * 4)) =
+                    make_uint2(f32_to_row2(o[0], o[1], a.bf16), f32_to_row2(o[2], o[3], a.bf16));
+        }
+        if (g == 0 && a.lse) a.lse[token * q_heads + fr.head] = st.l == 0.0f ? -__builtin_inff() : kLn2 * (st.m + __log2f(st.l));
+        return;
+    }
+    // the waves' parts together: [wave][row] maximum and sum, [wave][row][d] sums
+    float* s_m = lds;
+    float* s_l = lds + W * kFewRows;
+    float* s_acc = lds + 2 * W * kFewRows;
+    const int ld = d + 4;
+    if (g == 0) s_m[wave * kFewRows + c16] = st.m, s_l[wave * kFewRows + c16] = st.l;
+    if (c16 < n_rows) {
+#pragma unroll
+        for (int t = 0; t < 4 * NC; ++t)
+            if (t * 16 < d) *(float4_t*)(s_acc + (wave * kFewRows + c16) * ld + t * 16 + g * 4) = st.acc[t] * (kPart / kTop) * st.vref;
+    }
+    __syncthreads();
+    const int quads = d / 4;
+    for (int task = tid; task < n_rows * quads; task += 64 * W) {
+        const int rw = task / quads, q4 = task % quads;
+        float mm = -__builtin_inff();
+#pragma unroll
+        for (int w = 0; w < W; ++w) mm = fmaxf(mm, s_m[w * kFewRows + rw]);
+        const float m0 = mm == -__builtin_inff() ? 0.0f : mm;
+        float ll = 0.0f;
+        float4_t o = {0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const float k = __builtin_amdgcn_exp2f(s_m[w * kFewRows + rw] - m0);
+            ll += k * s_l[w * kFewRows + rw];
+            o += k * *(const float4_t*)(s_acc + (w * kFewRows + rw) * ld + 4 * q4);
+        }
+        const int64_t hq = h * a.group + chunk * kFewRows + rw;
+        if (a.n_splits > 1) {
+            const int64_t at = (token * q_heads + hq) * a.n_splits + split;
+            *(float4_t*)(a.part + at * d + 4 * q4) = o;
+            if (q4 == 0) a.stat[at] = make_float2(mm, ll);
+            continue;
+        }
+        const float inv = ll == 0.0f ? 0.0f : (1.0f / kPart) / ll;
+        *(uint2*)(a.out + 2 * (token * a.o_token + hq * a.o_head + 4 * q4)) =
+            make_uint2(f32_to_row2(o[0] * inv, o[1] * inv, a.bf16), f32_to_row2(o[2] * inv, o[3] * inv, a.bf16));
+        if (q4 == 0 && a.lse) a.lse[token * q_heads + hq] = ll == 0.0f ? -__builtin_inff() : kLn2 * (mm + __log2f(ll));
+    }
+}
+
+// ------------------------------------------------------------------ host --
+
+constexpr int64_t kMostBlocks = 0x7fffff00;
+constexpr int64_t kMostListed = 1 << 20;
+
+bool select_ok(const fkv_page_desc* p, const fkv_select_desc* t)
+{
+    constexpr int64_t kMost = 1 << 30;
+    return page_desc_ok(p) && t && t->n_req >= 0 && t->n_req <= kMost && t->n_tokens >= 0 && t->n_tokens <= kMost &&
+           t->max_new >= 1 && t->max_new <= kMost && t->max_kv >= 0 && t->max_kv <= kMost && t->max_pages >= 1 &&
+           t->max_pages <= (1 << 26) && stride_ok(t->q_stride_token) && stride_ok(t->q_stride_head) && t->q_heads >= 1 &&
+           t->q_heads <= 65535 && t->q_heads % p->heads == 0 && (t->type == FKV_ROW_F16 || t->type == FKV_ROW_BF16) &&
+           (t->causal == 0 || t->causal == 1) && t->n_select >= 1 && t->n_select <= kMostListed && t->keep_first >= 0 &&
+           t->keep_last >= 0 && (int64_t)t->keep_first + t->keep_last <= t->n_select;
+}
+
+// Pages that a request may have, and a row of scores: none where every page is selected.
+int64_t most_pages(const fkv_page_desc* p, const fkv_select_desc* t)
+{
+    return std::min((t->max_kv + p->page - 1) / p->page, t->max_pages);
+}
+
+int64_t score_stride(const fkv_page_desc* p, const fkv_select_desc* t)
+{
+    const int64_t n = most_pages(p, t);
+    return n <= t->n_select ? 0 : (n + 15) / 16 * 16;
+}
+
+// a * b, or the largest size there is: of sizes beyond any memory.
+size_t bytes_or_most(size_t a, size_t b)
+{
+    size_t n;
+    return __builtin_mul_overflow(a, b, &n) ? ~(size_t)0 : n;
+}
+
+constexpr int kHeldPages = 2048;   // that a wave of the selection holds
+
+// How the splits of an item's list are chosen: see fkv_page_attend_selected.
+struct ListedShape {
+    int waves;       // of an item in a block
+    int n_splits;
+    int64_t items;
+    bool join_blocks;
+};
+
+ListedShape listed_shape(const fkv_page_desc* p, const fkv_attend_desc* t, int64_t n_listed)
+{
+    ListedShape s;
+    const int64_t group = t->q_heads / p->heads;
+    const int64_t of_token = p->heads * ((group + kFewRows - 1) / kFewRows);
+    s.items = std::min(t->n_req * t->max_new, (int64_t)1 << 34) * of_token;   // (2^34 are too many, whatever the heads)
+    const int64_t tiles = (n_listed * (p->page / 16) + 3) / 4;
+    s.n_splits = 1;
+    s.waves = s.items >= 2048 || tiles <= 1 ? 1 : kWaves;
+    if (s.waves == kWaves && s.items < 256) {
+        const int64_t want = (512 + s.items - 1) / std::max((int64_t)1, s.items), most = std::max((int64_t)1, tiles / (2 * kWaves));
+        s.n_splits = (int)std::min(want, most);
+    }
+    s.join_blocks = s.n_splits >= kManySplits;
+    return s;
+}
+
+Workspace listed_workspace(const fkv_page_desc* p, const fkv_attend_desc* t, const ListedShape& s)
+{
+    if (s.n_splits == 1) return Workspace{0, 0, 0};
+    const size_t rows = (size_t)(t->n_tokens * t->q_heads) * (size_t)s.n_splits;
+    Workspace w;
+    w.stat = rows * p->d * sizeof(float);
+    w.pieces = w.bytes = bytes_or_most(rows, p->d * sizeof(float) + sizeof(float2));
+    return w;
+}
+
+}  // namespace
+}  // namespace fkv
+
+using namespace fkv;
+
+extern "C" size_t fkv_page_select_workspace(const fkv_page_desc* desc, const fkv_select_desc* select)
+{
+    if (!select_ok(desc, select)) return 0;
+    return bytes_or_most((size_t)(select->n_tokens * desc->heads), (size_t)score_stride(desc, select) * sizeof(float));
+}
+
+extern "C" int fkv_page_select(const fkv_page_desc* desc, const fkv_select_desc* select, const uint8_t* boxes, const float* scales,
+                               const void* q, const int32_t* tables, const int32_t* kv_len, const int32_t* q_start,
+                               int32_t* selected, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!select_ok(desc, select)) return FKV_ERR_INVALID_ARG;
+    if (!boxes || !scales || !aligned(boxes, 16) || !aligned(scales, 8)) return FKV_ERR_INVALID_ARG;
+    if (select->n_req == 0 || select->n_tokens == 0) return FKV_OK;
+    if (!q || !tables || !kv_len || !q_start || !selected || !aligned(q, 16) || !aligned(tables, 4) || !aligned(kv_len, 4) ||
+        !aligned(q_start, 4) || !aligned(selected, 4) || !aligned(workspace, 16))
+        return FKV_ERR_INVALID_ARG;
+    const size_t need = fkv_page_select_workspace(desc, select);
+    if (need && (!workspace || workspace_bytes < need)) return FKV_ERR_SCRATCH_TOO_SMALL;
+    fkv_attend_desc t = {};
+    t.n_req = select->n_req, t.n_tokens = select->n_tokens, t.max_new = select->max_new, t.max_kv = select->max_kv;
+    t.max_pages = select->max_pages, t.q_stride_token = select->q_stride_token, t.q_stride_head = select->q_stride_head;
+    t.q_heads = select->q_heads, t.type = select->type, t.causal = select->causal;
+    SelectArgs a = {};
+    (AttendArgs&)a = attend_args(desc, &t, nullptr, nullptr, scales, q, tables, kv_len, q_start, nullptr, nullptr, nullptr, nullptr, nullptr);
+    a.boxes = boxes, a.scores = (float*)workspace, a.selected = selected;
+    a.score_stride = score_stride(desc, select);
+    a.n_select = select->n_select, a.keep_first = select->keep_first, a.keep_last = select->keep_last;
+    const int64_t pages = most_pages(desc, select);
+    const hipStream_t st = (hipStream_t)stream;
+    if (a.n_req > kMostBlocks / a.max_new || a.n_req * a.max_new > kMostBlocks / a.heads) return FKV_ERR_UNSUPPORTED;
+    const int64_t rows = a.n_req * a.max_new * a.heads;
+    if (need) {
+        a.lanes_log = 0;
+        while (a.lanes_log < 4 && (1 << a.lanes_log) < a.group) ++a.lanes_log;
+        const int64_t row_tiles = (a.max_new + (16 >> a.lanes_log) - 1) / (16 >> a.lanes_log);
+        const bool many = row_tiles >= 4 && a.d <= 128;   // four row tiles a wave
+        a.row_groups = many ? (row_tiles + 3) / 4 : row_tiles;
+        const int64_t tiles = (pages + 15) / 16;
+        // as many page tiles a wave as leave the chip two thousand waves
+        int64_t wave_tiles = std::min(tiles * a.row_groups, (int64_t)1 << 30) * std::min(a.n_req * a.heads, (int64_t)1 << 30) / 2048;
+        wave_tiles = std::min((int64_t)8, std::max((int64_t)1, wave_tiles));
+        a.wave_tiles = (int32_t)wave_tiles;
+        a.tile_chunks = (int32_t)((tiles + wave_tiles * kWaves - 1) / (wave_tiles * kWaves));
+        const int64_t blocks = a.n_req * a.heads * a.row_groups;   // (row groups are no more than max_new)
+        if (blocks > kMostBlocks / a.tile_chunks) return FKV_ERR_UNSUPPORTED;
+        const bool e4m3 = desc->format == FKV_PAGE_E4M3;
+        auto go = [&](auto kern) {
+            hipLaunchKernelGGL(kern, dim3((unsigned)(blocks * a.tile_chunks)), dim3(kThreads), 0, st, a);
+        };
+        auto of_width = [&](auto nc) {
+            constexpr int NC = decltype(nc)::value;
+            if constexpr (NC <= 2) {
+                if (many) return e4m3 ? go(page_score_kernel<true, NC, 4>) : go(page_score_kernel<false, NC, 4>);
+            }
+            e4m3 ? go(page_score_kernel<true, NC, 1>) : go(page_score_kernel<false, NC, 1>);
+        };
+        if (a.d <= 64) of_width(std::integral_constant<int, 1>{});
+        else if (a.d <= 128) of_width(std::integral_constant<int, 2>{});
+        else of_width(std::integral_constant<int, 4>{});
+    }
+    if (need && pages > kHeldPages) {
+        hipLaunchKernelGGL(page_select_wide_kernel, dim3((unsigned)rows), dim3(kWideThreads), 0, st, a);
+    } else {
+        auto kern = !need || pages <= 256 ? page_select_kernel<4> : pages <= 512 ? page_select_kernel<8> : pages <= 1024 ? page_select_kernel<16> : page_select_kernel<32>;
+        hipLaunchKernelGGL(kern, dim3((unsigned)((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, st, a);
+    }
+    return launch_status();
+}
+
+extern "C" size_t fkv_page_attend_selected_workspace(const fkv_page_desc* desc, const fkv_attend_desc* attend, int64_t n_selected)
+{
+    if (!attend_ok(desc, attend) || n_selected < 1 || n_selected > kMostListed) return 0;
+    return listed_workspace(desc, attend, listed_shape(desc, attend, n_selected)).bytes;
+}
+
+extern "C" int fkv_page_attend_selected(const fkv_page_desc* desc, const fkv_attend_desc* attend, int64_t n_selected,
+                                        const int32_t* selected, const uint8_t* k_codes, const uint8_t* v_codes,
+                                        const float* scales, const void* q, const int32_t* tables, const int32_t* kv_len,
+                                        const int32_t* q_start, const float* slopes, const int32_t* prefix, const int32_t* first,
+                                        void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!attend_ok(desc, attend) || n_selected < 1 || n_selected > kMostListed) return FKV_ERR_INVALID_ARG;
+    if (!k_codes || !v_codes || !scales || !aligned(k_codes, 16) || !aligned(v_codes, 16) || !aligned(scales, 8))
+        return FKV_ERR_INVALID_ARG;
+    if (attend->n_req == 0 || attend->n_tokens == 0) return FKV_OK;
+    if (!q || !out || !tables || !kv_len || !q_start || !selected || !aligned(q, 16) || !aligned(out, 16) || !aligned(tables, 4) ||
+        !aligned(kv_len, 4) || !aligned(q_start, 4) || !aligned(selected, 4) || !aligned(slopes, 4) || !aligned(prefix, 4) ||
+        !aligned(first, 4) || !aligned(lse, 4) || !aligned(workspace, 16))
+        return FKV_ERR_INVALID_ARG;
+    const ListedShape s = listed_shape(desc, attend, n_selected);
+    const Workspace ws = listed_workspace(desc, attend, s);
+    if (ws.bytes && (!workspace || workspace_bytes < ws.bytes)) return FKV_ERR_SCRATCH_TOO_SMALL;
+    const int64_t blocks = s.waves == 1 ? (s.items + kWaves - 1) / kWaves : s.items;
+    if (blocks > kMostBlocks / s.n_splits) return FKV_ERR_UNSUPPORTED;
+    AttendArgs a = attend_args(desc, attend, k_codes, v_codes, scales, q, tables, kv_len, q_start, slopes, prefix, first, out, lse);
+    a.listed = selected, a.n_listed = n_selected;
+    a.part = (float*)workspace;
+    a.stat = (float2*)((uint8_t*)workspace + ws.stat);
+    a.n_splits = s.n_splits;
+    const int64_t items = s.n_splits > 1 ? a.n_req * a.max_new * a.heads * a.group : 0;   // rows to be joined
+    const int64_t joins = s.join_blocks ? items : (items + kWaves - 1) / kWaves;
+    if (joins > kMostBlocks) return FKV_ERR_UNSUPPORTED;
+    const hipStream_t st = (hipStream_t)stream;
+    const bool e4m3 = desc->format == FKV_PAGE_E4M3;
+    auto of_width = [&](auto nc) {
+        constexpr int NC = decltype(nc)::value;
+        auto go = [&](auto kern, size_t shm) {
+            hipLaunchKernelGGL(kern, dim3((unsigned)(blocks * s.n_splits)), dim3(kThreads), shm, st, a);
+        };
+        if (s.waves == 1) return e4m3 ? go(attend_listed_kernel<true, NC, 1>, 0) : go(attend_listed_kernel<false, NC, 1>, 0);
+        const size_t shm = (2 * kWaves * kFewRows + (size_t)kWaves * kFewRows * (a.d + 4)) * sizeof(float);
+        e4m3 ? go(attend_listed_kernel<true, NC, kWaves>, shm) : go(attend_listed_kernel<false, NC, kWaves>, shm);
+    };
+    if (a.d <= 64) of_width(std::integral_constant<int, 1>{});
+    else if (a.d <= 128) of_width(std::integral_constant<int, 2>{});
+    else of_width(std::integral_constant<int, 4>{});
+    if (a.n_splits > 1)
+        hipLaunchKernelGGL(s.join_blocks ? attend_join_kernel<kWaves> : attend_join_kernel<1>, dim3((unsigned)joins), dim3(kThreads), 0, st, a);
+    return launch_status();
+}

@@ -67,6 +67,14 @@ class fkv_attend_desc(ctypes.Structure):
                 ("window", ctypes.c_int32), ("sinks", ctypes.c_int32)]
 
 
+class fkv_select_desc(ctypes.Structure):
+    _fields_ = [("n_req", ctypes.c_int64), ("n_tokens", ctypes.c_int64), ("max_new", ctypes.c_int64),
+                ("max_kv", ctypes.c_int64), ("max_pages", ctypes.c_int64), ("q_stride_token", ctypes.c_int64),
+                ("q_stride_head", ctypes.c_int64), ("q_heads", ctypes.c_int32), ("type", ctypes.c_int32),
+                ("causal", ctypes.c_int32), ("n_select", ctypes.c_int32), ("keep_first", ctypes.c_int32),
+                ("keep_last", ctypes.c_int32)]
+
+
 _i32, _i64, _dbl, _p, _sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_double, ctypes.c_void_p, ctypes.c_size_t
 _PC = ctypes.POINTER(fkv_codec)
 _SIGS = {
@@ -100,6 +108,11 @@ _SIGS = {
     "fkv_page_load": ([_p, _p, _p, _p, _i64, _p, _p, _p, _p, _p, _p], ctypes.c_int),
     "fkv_page_attend_workspace": ([_p, _p], _sz),
     "fkv_page_attend": ([_p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _sz, _p], ctypes.c_int),
+    "fkv_page_select_workspace": ([_p, _p], _sz),
+    "fkv_page_select": ([_p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _sz, _p], ctypes.c_int),
+    "fkv_page_attend_selected_workspace": ([_p, _p, _i64], _sz),
+    "fkv_page_attend_selected": ([_p, _p, _i64, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _sz, _p],
+                                 ctypes.c_int),
     "fkv_diag_mfma_loop": ([_i32, _i32, _i32, ctypes.c_float, ctypes.c_float, _p, _p], ctypes.c_int),
     "fkv_diag_mfma_loop_flops": ([_i32, _i32], _dbl),
     "fkv_status_string": ([ctypes.c_int], ctypes.c_char_p),
@@ -776,22 +789,13 @@ def fkv_page_load(pages, slots, dtype=None, k=None, v=None, stream=None):
                              _ptr(k), _ptr(v), _stream(stream)), "fkv_page_load")
     return k, v
 
-
-def fkv_page_attend(pages, q, tables, kv_len, q_start, max_new: int, max_kv: int, scale=None, softcap: float = 0.0,
-                    causal: bool = True, window: int = 0, sinks: int = 0, slopes=None, prefix=None, first=None,
-                    out=None, lse=None, want_lse: bool = False, workspace=None, stream=None):
-    """Attention of q f16 or bf16 [n_tokens][q_heads][d] (any strides, contiguous in d) over the pages that tables
-    i32 [n_req][max_pages] lists: request r holds kv_len[r] tokens, the last q_start[r+1] - q_start[r] of which are
-    its rows of q.  max_new and max_kv bound the rows and tokens of a request (host values: they set the launch).
-    scale defaults to d ** -0.5; slopes f32 [q_heads], prefix i32 [n_req], first i32 [n_tokens].  Returns
-    (out, lse or None).  workspace: uint8 scratch of fkv_page_attend_workspace bytes, for callers that keep one;
-    without it the call takes its scratch from torch's allocator, on the stream it runs on."""
+def _q_rows(pages, q, tables, kv_len, q_start):
+    """The checks that calls over requests' query rows share: (page desc, row type, requests, columns of a table)."""
     torch = _TORCH or _torch()
     desc = _page_desc(pages)
     if not isinstance(q, torch.Tensor) or not q.is_cuda or q.dim() != 3:
         raise TypeError("q must be a CUDA tensor [n_tokens][q_heads][d]")
-    (n, q_heads, d), q_stride = q.shape, q.stride()
-    if d != desc.d or q_stride[2] != 1:
+    if q.shape[2] != desc.d or q.stride(2) != 1:
         raise TypeError("q must have rows of %d contiguous elements" % desc.d)
     i32, kind = torch.int32, _row_type(q.dtype, "q")
     _need(tables, i32, "tables")
@@ -800,6 +804,25 @@ def fkv_page_attend(pages, q, tables, kv_len, q_start, max_new: int, max_kv: int
     n_req, width = kv_len.numel(), tables.shape
     if len(width) != 2 or width[0] != n_req or q_start.numel() != n_req + 1:
         raise ValueError("shape mismatch between tables, kv_len and q_start")
+    return desc, kind, n_req, width[1]
+
+
+def _scratch(need: int, device, stream):
+    """uint8 scratch from torch's allocator, of the stream that the call runs on; None for none."""
+    torch = _TORCH or _torch()
+    if not need:
+        return None
+    if stream is None:
+        return torch.empty(need, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device)):
+        return torch.empty(need, dtype=torch.uint8, device=device)
+
+
+def _attention(desc, kind: int, n_req: int, width: int, q, max_new: int, max_kv: int, scale, softcap: float, causal: bool,
+               window: int, sinks: int, slopes, prefix, first, out, lse, want_lse: bool):
+    """The further arguments of the attention calls checked: (attend desc, out, lse)."""
+    torch = _TORCH or _torch()
+    (n, q_heads, d), q_stride, i32 = q.shape, q.stride(), torch.int32
     if prefix is not None:
         _need(prefix, i32, "prefix")
         if prefix.numel() != n_req:
@@ -825,19 +848,104 @@ def fkv_page_attend(pages, q, tables, kv_len, q_start, max_new: int, max_kv: int
             raise ValueError("lse has the wrong size")
     elif want_lse:
         lse = torch.empty((n, q_heads), dtype=torch.float32, device=q.device)
-    att = fkv_attend_desc(n_req, n, max_new, max_kv, width[1], q_stride[0], q_stride[1], o_stride[0], o_stride[1],
-                          q_heads, kind, d ** -0.5 if scale is None else scale, softcap, 1 if causal else 0, window,
-                          sinks)
+    return fkv_attend_desc(n_req, n, max_new, max_kv, width, q_stride[0], q_stride[1], o_stride[0], o_stride[1], q_heads, kind,
+                           d ** -0.5 if scale is None else scale, softcap, 1 if causal else 0, window, sinks), out, lse
+
+
+def fkv_page_select(pages, boxes, q, tables, kv_len, q_start, max_new: int, max_kv: int, n_select: int, keep_first: int = 1,
+                    keep_last: int = 1, causal: bool = True, selected=None, workspace=None, stream=None):
+    """The pages that each query token is to attend to: of those that it sees, the first keep_first, the last keep_last
+    and the n_select - keep_first - keep_last others with the largest bounds on their keys' scores (all, where there are
+    no more).  boxes (fkv_boxes, kept by fkv_page_append); q, tables, kv_len, q_start, max_new, max_kv as for
+    fkv_page_attend.  Returns i32 [n_tokens][heads][n_select]: columns of the token's row of tables, ascending, -1 after
+    the last; rows of no request are left as they were.  workspace: uint8 scratch of fkv_page_select_workspace bytes, for
+    callers that keep one."""
+    torch = _TORCH or _torch()
+    desc, kind, n_req, width = _q_rows(pages, q, tables, kv_len, q_start)
+    _need_boxes(boxes, pages)
+    (n, q_heads, _), q_stride = q.shape, q.stride()
+    sel = fkv_select_desc(n_req, n, max_new, max_kv, width, q_stride[0], q_stride[1], q_heads, kind, 1 if causal else 0,
+                          n_select, keep_first, keep_last)
+    if selected is None:
+        selected = torch.empty((n, desc.heads, max(n_select, 1)), dtype=torch.int32, device=q.device)
+    else:
+        _need(selected, torch.int32, "selected")
+        if selected.shape != (n, desc.heads, n_select):
+            raise ValueError("selected must be [n_tokens][heads][n_select]")
     ref = ctypes.byref
     if workspace is not None:
         _need(workspace, torch.uint8, "workspace")
     else:
-        need = lib.fkv_page_attend_workspace(ref(desc), ref(att))
-        if need and stream is None:
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-        elif need:
-            with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=q.device)):
-                workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        workspace = _scratch(lib.fkv_page_select_workspace(ref(desc), ref(sel)), q.device, stream)
+    _check(lib.fkv_page_select(ref(desc), ref(sel), boxes.data_ptr(), pages[2].data_ptr(), q.data_ptr(), tables.data_ptr(),
+                               kv_len.data_ptr(), q_start.data_ptr(), selected.data_ptr(), _ptr(workspace),
+                               0 if workspace is None else workspace.numel(), _stream(stream)), "fkv_page_select")
+    return selected
+
+
+def fkv_page_select_workspace(pages, q, n_req: int, max_pages: int, max_new: int, max_kv: int, n_select: int) -> int:
+    """Bytes of scratch that fkv_page_select of these shapes takes (0: none)."""
+    desc = _page_desc(pages)
+    sel = fkv_select_desc(n_req, q.shape[0], max_new, max_kv, max_pages, 0, 0, q.shape[1], _row_type(q.dtype, "q"), 1, n_select,
+                          0, 0)
+    return int(lib.fkv_page_select_workspace(ctypes.byref(desc), ctypes.byref(sel)))
+
+
+def fkv_page_attend_selected(pages, q, tables, kv_len, q_start, selected, max_new: int, max_kv: int, scale=None,
+                             softcap: float = 0.0, causal: bool = True, window: int = 0, sinks: int = 0, slopes=None,
+                             prefix=None, first=None, out=None, lse=None, want_lse: bool = False, workspace=None,
+                             stream=None):
+    """fkv_page_attend over the pages that selected i32 [n_tokens][heads][n] lists for each query token and KV head
+    (fkv_page_select's result; columns of the token's row of tables in any order, an entry that is none lists nothing).
+    Returns (out, lse or None).  workspace: uint8 scratch of fkv_page_attend_selected_workspace bytes."""
+    torch = _TORCH or _torch()
+    desc, kind, n_req, width = _q_rows(pages, q, tables, kv_len, q_start)
+    _need(selected, torch.int32, "selected")
+    at = selected.shape
+    if len(at) != 3 or at[0] != q.shape[0] or at[1] != desc.heads:
+        raise ValueError("selected must be [n_tokens][heads][n]")
+    att, out, lse = _attention(desc, kind, n_req, width, q, max_new, max_kv, scale, softcap, causal, window, sinks, slopes,
+                               prefix, first, out, lse, want_lse)
+    ref = ctypes.byref
+    if workspace is not None:
+        _need(workspace, torch.uint8, "workspace")
+    else:
+        workspace = _scratch(lib.fkv_page_attend_selected_workspace(ref(desc), ref(att), at[2]), q.device, stream)
+    _check(lib.fkv_page_attend_selected(ref(desc), ref(att), at[2], selected.data_ptr(), pages[0].data_ptr(),
+                                        pages[1].data_ptr(), pages[2].data_ptr(), q.data_ptr(), tables.data_ptr(),
+                                        kv_len.data_ptr(), q_start.data_ptr(), _ptr(slopes), _ptr(prefix), _ptr(first),
+                                        out.data_ptr(), _ptr(lse), _ptr(workspace),
+                                        0 if workspace is None else workspace.numel(), _stream(stream)),
+           "fkv_page_attend_selected")
+    return out, lse
+
+
+def fkv_page_attend_selected_workspace(pages, q, n_req: int, max_pages: int, max_new: int, max_kv: int, n_selected: int) -> int:
+    """Bytes of scratch that fkv_page_attend_selected of these shapes takes (0: none)."""
+    desc = _page_desc(pages)
+    n, q_heads, d = q.shape
+    att = fkv_attend_desc(n_req, n, max_new, max_kv, max_pages, 0, 0, 0, 0, q_heads, _row_type(q.dtype, "q"), 1.0, 0.0, 1, 0, 0)
+    return int(lib.fkv_page_attend_selected_workspace(ctypes.byref(desc), ctypes.byref(att), n_selected))
+
+
+def fkv_page_attend(pages, q, tables, kv_len, q_start, max_new: int, max_kv: int, scale=None, softcap: float = 0.0,
+                    causal: bool = True, window: int = 0, sinks: int = 0, slopes=None, prefix=None, first=None,
+                    out=None, lse=None, want_lse: bool = False, workspace=None, stream=None):
+    """Attention of q f16 or bf16 [n_tokens][q_heads][d] (any strides, contiguous in d) over the pages that tables
+    i32 [n_req][max_pages] lists: request r holds kv_len[r] tokens, the last q_start[r+1] - q_start[r] of which are
+    its rows of q.  max_new and max_kv bound the rows and tokens of a request (host values: they set the launch).
+    scale defaults to d ** -0.5; slopes f32 [q_heads], prefix i32 [n_req], first i32 [n_tokens].  Returns
+    (out, lse or None).  workspace: uint8 scratch of fkv_page_attend_workspace bytes, for callers that keep one;
+    without it the call takes its scratch from torch's allocator, on the stream it runs on."""
+    torch = _TORCH or _torch()
+    desc, kind, n_req, width = _q_rows(pages, q, tables, kv_len, q_start)
+    att, out, lse = _attention(desc, kind, n_req, width, q, max_new, max_kv, scale, softcap, causal, window, sinks, slopes,
+                               prefix, first, out, lse, want_lse)
+    ref = ctypes.byref
+    if workspace is not None:
+        _need(workspace, torch.uint8, "workspace")
+    else:
+        workspace = _scratch(lib.fkv_page_attend_workspace(ref(desc), ref(att)), q.device, stream)
     _check(lib.fkv_page_attend(ref(desc), ref(att), pages[0].data_ptr(), pages[1].data_ptr(), pages[2].data_ptr(),
                                q.data_ptr(), tables.data_ptr(), kv_len.data_ptr(), q_start.data_ptr(), _ptr(slopes),
                                _ptr(prefix), _ptr(first), out.data_ptr(), _ptr(lse), _ptr(workspace),

@@ -47,3 +47,89 @@ def test_append_arguments(F):
     assert append(n=0, t=None, q=None, out=None, rq=None, ro=None, tab=None, pos=None) == 0
     assert append(n=1 << 40) == F.FKV_ERR_UNSUPPORTED
     assert append(n=1 << 40, t=T(100, 64, 0, 65535)) == F.FKV_ERR_UNSUPPORTED
+
+
+def select_desc(F, **kw):
+    base = dict(n_req=2, n_tokens=4, max_new=2, max_kv=64, max_pages=4, q_stride_token=256, q_stride_head=64, q_heads=4, type=0,
+                causal=1, n_select=2, keep_first=1, keep_last=1)
+    return F.fkv_select_desc(**{**base, **kw})
+
+
+def test_select_arguments(F):
+    E = F.FKV_ERR_INVALID_ARG
+    desc = F.fkv_page_desc(8, 16, 2, 64, 0)
+
+    def select(d=desc, box=g, sc=g, q=g, tab=g, kv=g, qs=g, sel=g, ws=g, nws=1 << 20, **kw):
+        t = select_desc(F, **kw)
+        return F.lib.fkv_page_select(ref(d), ref(t), box, sc, q, tab, kv, qs, sel, ws, nws, None)
+
+    for kw in (dict(d=None), dict(d=F.fkv_page_desc(8, 24, 2, 64, 0)), dict(box=None), dict(box=half), dict(sc=None), dict(sc=P(0x10004)),
+               dict(q=None), dict(q=half), dict(tab=None), dict(tab=odd), dict(kv=None), dict(kv=odd), dict(qs=None), dict(qs=odd),
+               dict(sel=None), dict(sel=odd), dict(ws=half), dict(q_heads=3), dict(q_heads=0), dict(type=2), dict(causal=2), dict(max_new=0),
+               dict(max_kv=-1), dict(max_pages=0), dict(n_req=-1), dict(n_tokens=-1), dict(q_stride_token=4), dict(q_stride_head=-8),
+               dict(n_select=0), dict(n_select=(1 << 20) + 1), dict(keep_first=-1), dict(keep_last=-1), dict(keep_first=2)):
+        assert select(**kw) == E, kw
+    assert select(n_req=0, q=None, sel=None) == 0 and select(n_tokens=0, q=None) == 0
+    assert F.lib.fkv_page_select(ref(desc), None, g, g, g, g, g, g, g, g, 1 << 20, None) == E
+    assert select(ws=None) == select(nws=2 * 4 * 16 * 4 - 1) == F.FKV_ERR_SCRATCH_TOO_SMALL
+
+
+def test_select_scratch(F):
+    """A score a row, KV head and page, rows of 16 pages; none where all pages are selected."""
+    desc = F.fkv_page_desc(8, 16, 2, 64, 0)
+    need = lambda **kw: F.lib.fkv_page_select_workspace(ref(desc), ref(select_desc(F, **kw)))     # noqa: E731
+    assert need() == 2 * 4 * 16 * 4
+    assert need(max_kv=300, max_pages=40) == 2 * 4 * 32 * 4
+    assert need(n_select=4) == 0 and need(max_kv=32) == 0 and need(max_pages=2) == 0
+    assert need(n_select=0) == 0 and F.lib.fkv_page_select_workspace(None, ref(select_desc(F))) == 0
+    wide = F.fkv_page_desc(8, 16, 65535, 64, 0)
+    assert F.lib.fkv_page_select_workspace(ref(wide), ref(select_desc(F, q_heads=65535, n_tokens=1 << 30, max_kv=1 << 30,
+                                                                      max_pages=1 << 26))) == (1 << 64) - 1
+
+
+def test_select_of_too_many_rows(F):
+    desc = F.fkv_page_desc(8, 16, 2, 64, 0)
+    for kw in (dict(n_req=1 << 30), dict(n_req=1 << 20, max_new=1 << 20), dict(max_new=1 << 30)):
+        t = select_desc(F, **kw)
+        assert F.lib.fkv_page_select(ref(desc), ref(t), g, g, g, g, g, g, g, g, 1 << 40, None) == F.FKV_ERR_UNSUPPORTED, kw
+
+
+def attend_desc(F, **kw):
+    base = dict(n_req=2, n_tokens=4, max_new=2, max_kv=64, max_pages=4, q_stride_token=256, q_stride_head=64, o_stride_token=256,
+                o_stride_head=64, q_heads=4, type=0, scale=0.125, softcap=0.0, causal=1, window=0, sinks=0)
+    return F.fkv_attend_desc(**{**base, **kw})
+
+
+def test_attend_selected_arguments(F):
+    E = F.FKV_ERR_INVALID_ARG
+    desc = F.fkv_page_desc(8, 16, 2, 64, 0)
+
+    def attend(d=desc, ns=4, sel=g, kc=g, vc=g, sc=g, q=g, tab=g, kv=g, qs=g, slopes=None, prefix=None, first=None, out=g, lse=None,
+               ws=g, nws=1 << 30, **kw):
+        t = attend_desc(F, **kw)
+        return F.lib.fkv_page_attend_selected(ref(d), ref(t), ns, sel, kc, vc, sc, q, tab, kv, qs, slopes, prefix, first, out, lse, ws,
+                                              nws, None)
+
+    for kw in (dict(d=None), dict(ns=0), dict(ns=-1), dict(ns=(1 << 20) + 1), dict(sel=None), dict(sel=odd), dict(kc=None), dict(vc=half),
+               dict(sc=P(0x10004)), dict(q=None), dict(q=half), dict(out=None), dict(out=half), dict(tab=None), dict(kv=None), dict(qs=odd),
+               dict(slopes=odd), dict(prefix=odd), dict(first=odd), dict(lse=odd), dict(ws=half), dict(q_heads=3), dict(q_heads=0),
+               dict(type=2), dict(scale=float("nan")), dict(softcap=-1.0), dict(causal=2), dict(window=-1), dict(sinks=-1), dict(max_new=0),
+               dict(max_kv=-1), dict(max_pages=0), dict(n_req=-1), dict(n_tokens=-1), dict(q_stride_token=4), dict(o_stride_head=-8)):
+        assert attend(**kw) == E, kw
+    assert attend(n_req=0, q=None, out=None) == 0 and attend(n_tokens=0, q=None) == 0
+    for kw in (dict(n_req=1 << 30, max_new=1 << 30), dict(max_new=1 << 30, q_heads=65534), dict(n_req=1 << 30, q_heads=65534)):
+        assert attend(**kw) == F.FKV_ERR_UNSUPPORTED, kw
+
+
+def test_attend_selected_scratch(F):
+    """A call that splits the lists says how much scratch it takes and refuses less."""
+    desc = F.fkv_page_desc(4096, 64, 2, 64, 0)
+    t = attend_desc(F, n_req=1, n_tokens=1, max_new=1, max_kv=32768, max_pages=512)
+    need = F.lib.fkv_page_attend_selected_workspace(ref(desc), ref(t), 128)
+    assert need > 0
+    args = (ref(desc), ref(t), 128, g, g, g, g, g, g, g, g, None, None, None, g, None)
+    assert F.lib.fkv_page_attend_selected(*args, None, 0, None) == F.FKV_ERR_SCRATCH_TOO_SMALL
+    assert F.lib.fkv_page_attend_selected(*args, g, need - 1, None) == F.FKV_ERR_SCRATCH_TOO_SMALL
+    assert F.lib.fkv_page_attend_selected_workspace(ref(desc), ref(t), 1) == 0
+    assert F.lib.fkv_page_attend_selected_workspace(None, ref(t), 128) == 0
+    assert F.lib.fkv_page_attend_selected_workspace(ref(desc), ref(t), 0) == 0
