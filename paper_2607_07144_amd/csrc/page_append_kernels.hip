@@ -12,6 +12,8 @@
 // re-scaled box, and a box is brought up to date from itself and the new rows.
 #include "page_rows_device.h"
 
+#include <algorithm>
+
 namespace fkv {
 namespace {
 
@@ -80,173 +82,176 @@ __device__ __forceinline__ void turn(uint4 lo, uint4 hi, const float4 (&cs)[4], 
     }
 }
 
-// A wave writes a run of one head's keys, as store_run does, turned on the way.
-// Lane 16q + c has unit c % units of tokens 4q .. 4q+3 of every 16-token group whose
-// turn is c / units; kHeld turns (64 tokens of 128 channels) are held in registers
-// between the largest element and the codes.
-constexpr int kHeld = 2;
+// What a lane has of a run's key rows: one unit of every `slots`-th token from `first`.
+struct KeyLane {
+    Unit unit;
+    int u, slots, slot;
+    bool used;
+    __device__ __forceinline__ KeyLane(const AppendArgs& p, int units)
+    {
+        const int lane = threadIdx.x & 63;
+        slots = 64 / units;
+        slot = lane / units;
+        u = lane - slot * units;
+        used = slot < slots;
+        unit = unit_of(p, u);
+    }
+};
 
+// A wave writes a run of one head's keys, as store_run does, turned on the way.  It takes
+// 64 / units tokens T times over in a pass (16 tokens of 128 channels), which is held in
+// registers between the channels' smallest and largest values -- and with them the largest
+// of all -- and the codes; of a run of more the rows are read and turned a second time,
+// from the caches.
 template <bool E4M3, bool BF16>
 __device__ __forceinline__ void append_keys(const PageArgs& a, const AppendArgs& p, float* s_box, int64_t i, int h, int64_t page,
                                             int begin, int len)
 {
     constexpr float kLargest = E4M3 ? kLargestE4m3 : kLargestInt8;
-    const int lane = threadIdx.x & 63, c16 = lane & 15, tq = lane >> 4;
-    const int d = a.d, units = d >> 4, end = begin + len;
-    const int turns = 16 / units;                    // 16-token groups at a time
-    const int turn_of = c16 / units, u = c16 - turn_of * units;
-    const bool used = turn_of < turns;
-    const Unit unit = unit_of(p, u);
-    const int g0 = begin >> 4;
-    const int n_pass = (((end + 15) >> 4) - g0 + turns - 1) / turns;
+    constexpr int T = 2;
+    const int lane = threadIdx.x & 63;
+    const int d = a.d, units = d >> 4;
+    float* sp = (float*)&a.scales[page * a.heads + h];
+    uint8_t* codes = a.k_codes + (page * a.heads + h) * (int64_t)a.page * d;
+    const float was = begin ? *sp : 0.0f;
+    OldCodes<E4M3> before(codes, d, false, begin);
+    const KeyLane mine(p, units);
     const RowsFrom from(p.k, i, h);
-    auto first_token = [&](int pass) { return (g0 + pass * turns + turn_of) * 16 + tq * 4; };
-    auto load = [&](int pass, float (&f)[4][16]) {
-        const int o0 = first_token(pass);
-        uint4 lo[4], hi[4];
-        int row[4];
+    const int per_pass = mine.slots * T;
+    const int n_pass = (len + per_pass - 1) / per_pass;
+    auto token = [&](int pass, int j) { return pass * per_pass + j * mine.slots + mine.slot; };   // of the run
+    auto there = [&](int k) { return mine.used && k < len; };
+    float held[T][16];
+    auto load = [&](int pass) {
+        uint4 lo[T], hi[T];
+        int row[T];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < T; ++j) {
             lo[j] = hi[j] = make_uint4(0, 0, 0, 0);
             row[j] = 0;
-            if (used && o0 + j >= begin && o0 + j < end) {
-                const int64_t k = o0 + j - begin;
-                const uint8_t* at = from.row(p.k, (int)k);
-                lo[j] = *(const uint4*)(at + 16 * unit.c0);
-                hi[j] = *(const uint4*)(at + 16 * unit.c1);
-                if (unit.turned) row[j] = table_row(p, i + k);
+            const int k = token(pass, j);
+            if (there(k)) {
+                const uint8_t* at = from.row(p.k, k);
+                lo[j] = *(const uint4*)(at + 16 * mine.unit.c0);
+                hi[j] = *(const uint4*)(at + 16 * mine.unit.c1);
+                if (mine.unit.turned) row[j] = table_row(p, i + k);
             }
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < T; ++j) {
             float4 cs[4];
-            if (unit.turned) {
-                const float4* t = p.table + (int64_t)row[j] * (p.rot >> 2) + 4 * u;
+            if (mine.unit.turned) {
+                const float4* at = p.table + (int64_t)row[j] * (p.rot >> 2) + 4 * mine.u;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) cs[e] = t[e];
+                for (int e = 0; e < 4; ++e) cs[e] = at[e];
             }
-            turn<BF16>(lo[j], hi[j], cs, unit.turned, p.pairs, f[j]);
+            turn<BF16>(lo[j], hi[j], cs, mine.unit.turned, p.pairs, held[j]);
         }
     };
-    float held[kHeld][4][16];
-    // the largest of the values' bits without the sign, which are in the order of the numbers, and of the finite ones'
-    uint32_t most = 0;
-    auto look = [&](bool finite) {
-        for (int p0 = 0; p0 < n_pass; p0 += kHeld) {
+    auto passes = [&](bool again, auto each) {   // token by token, the rows loaded where they are not held
+        for (int k = 0; k < n_pass; ++k) {
+            if (again) load(k);
 #pragma unroll
-            for (int t = 0; t < kHeld; ++t) {
-                if (p0 + t >= n_pass) break;
-                load(p0 + t, held[t]);
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const uint32_t b = __float_as_uint(held[t][j][e]) & 0x7fffffffu;
-                        most = max(most, finite && b >= 0x7f800000u ? 0u : b);
-                    }
-            }
+            for (int j = 0; j < T; ++j) each(token(k, j), held[j]);
         }
-#pragma unroll
-        for (int k = 1; k < 64; k <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, k, 64));
     };
-    look(false);
-    const bool special = most >= 0x7f800000u;
-    if (special) {
-        most = 0;
-        look(true);
+    // smallest and largest of each channel; `strange` is a NaN once a value is none or infinite
+    float low[16], high[16], strange = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) low[e] = kInf, high[e] = -kInf;
+    passes(true, [&](int k, float (&f)[16]) {
+        if (!there(k)) return;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            low[e] = fminf(low[e], f[e]);
+            high[e] = fmaxf(high[e], f[e]);
+            strange = __builtin_fmaf(f[e], 0.0f, strange);
+        }
+    });
+    // the largest value, of the run's finite ones
+    float largest = 0.0f;
+    auto over_all = [&](float x) {
+#pragma unroll
+        for (int k = 1; k < 64; k <<= 1) x = fmaxf(x, __shfl_xor(x, k, 64));
+        return x;
+    };
+#pragma unroll
+    for (int e = 0; e < 16; ++e) largest = fmaxf(largest, fmaxf(-low[e], high[e]));   // (-infinity where no token is)
+    largest = over_all(strange != strange ? kInf : largest);
+    const bool special = largest == kInf;
+    if (special) {   // again: a NaN as 0, infinities beyond every finite value
+        largest = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) low[e] = kInf, high[e] = -kInf;
+        passes(true, [&](int k, float (&f)[16]) {
+            if (!there(k)) return;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const float x = f[e] != f[e] ? 0.0f : f[e];
+                low[e] = fminf(low[e], x);
+                high[e] = fmaxf(high[e], x);
+                largest = fmaxf(largest, fabsf(x) < kInf ? fabsf(x) : 0.0f);
+            }
+        });
+        largest = over_all(largest);
     }
-    const float largest = __uint_as_float(most);
-    float* sp = (float*)&a.scales[page * a.heads + h];
     float s = largest < 0x1p-90f ? 0.0f : largest * (1.0f / kLargest);
-    uint8_t* codes = a.k_codes + (page * a.heads + h) * (int64_t)a.page * d;
     float grow = 1.0f;
     if (begin) {
-        const float was = *sp;
         s = fmaxf(s, was);
         if (s > was) {
             grow = was / s;
-            rescale_before<E4M3>(codes, d, false, begin, grow);
+            before.rescale(grow);
         }
     }
     wave_sync();   // every lane has read the scale
     if (lane == 0) *sp = s;
     const float inv = s > 0.0f ? 1.0f / s : 0.0f;
-    float low[16], high[16];
+    auto scaled = [&](float x) {
+        const float y = x * inv;
+        return !special || fabsf(x) < kInf ? y : x != x ? 0.0f : copysignf(kLargest, x);
+    };
+    passes(n_pass > 1, [&](int k, float (&f)[16]) {
+        uint32_t w[4];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) low[e] = kInf, high[e] = -kInf;
-    for (int p0 = 0; p0 < n_pass; p0 += kHeld) {
-#pragma unroll
-        for (int t = 0; t < kHeld; ++t) {
-            if (p0 + t >= n_pass) break;
-            if (n_pass > kHeld) load(p0 + t, held[t]);
-            const int o0 = first_token(p0 + t);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float (&f)[16] = held[t][j];
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const float x = f[e];
-                    f[e] = x * inv;
-                    if (special) f[e] = fabsf(x) < kInf ? f[e] : x != x ? 0.0f : copysignf(kLargest, x);
-                }
-                const bool there = used && o0 + j >= begin && o0 + j < end;
-                if (p.boxes) {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        low[e] = fminf(low[e], there ? f[e] : kInf);
-                        high[e] = fmaxf(high[e], there ? f[e] : -kInf);
-                    }
-                }
-                uint32_t w[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float four[4] = {f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]};
-                    w[k] = near_codes<E4M3>(four);
-                }
-                if (there) {
-                    uint8_t* at = codes + (o0 + j) * d;
-                    *(uint2*)(at + 8 * unit.c0) = make_uint2(w[0], w[1]);
-                    *(uint2*)(at + 8 * unit.c1) = make_uint2(w[2], w[3]);
-                }
-            }
+        for (int q = 0; q < 4; ++q) {
+            const float four[4] = {scaled(f[4 * q]), scaled(f[4 * q + 1]), scaled(f[4 * q + 2]), scaled(f[4 * q + 3])};
+            w[q] = near_codes<E4M3>(four);
         }
-    }
+        if (!there(k)) return;
+        uint8_t* at = codes + (begin + k) * d;
+        *(uint2*)(at + 8 * mine.unit.c0) = make_uint2(w[0], w[1]);
+        *(uint2*)(at + 8 * mine.unit.c1) = make_uint2(w[2], w[3]);
+    });
     if (!p.boxes) return;
-    // The lanes of a unit together, and with the page's box before the run: a lane four channels.
-    wave_sync();   // (of the run before)
+    // The lanes of a unit together, and with the page's box before the run: a lane an end of a channel's range at a time.
+    // (A lane without a token has infinity on either side.)
+    wave_sync();   // (the box of the run before is read)
 #pragma unroll
     for (int e = 0; e < 16; ++e) s_box[e * 64 + lane] = low[e], s_box[(16 + e) * 64 + lane] = high[e];
     wave_sync();
-    if (4 * lane >= d) return;
-    const int chunk = lane >> 1, half = p.rot >> 4;
-    const bool apart = !p.pairs && chunk < 2 * half;
-    const int of = apart ? (chunk >= half ? chunk - half : chunk) : chunk >> 1;
-    const int e0 = 8 * (apart ? chunk >= half : chunk & 1) + 4 * (lane & 1);
-    uint32_t* box = (uint32_t*)(p.boxes + (page * a.heads + h) * 2 * (int64_t)d) + lane;
-    float lo[4], hi[4];
-    if (begin) {
-        codes_to_f32<E4M3>(box[0], lo);
-        codes_to_f32<E4M3>(box[d / 4], hi);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) lo[e] *= grow, hi[e] *= grow;
-        codes_to_f32<E4M3>(f32_to_codes<E4M3>(lo), lo);
-        codes_to_f32<E4M3>(f32_to_codes<E4M3>(hi), hi);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) lo[e] = kInf, hi[e] = -kInf;
-    }
-    for (int t = 0; t < turns; ++t)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int from_lane = 16 * q + t * units + of;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                lo[e] = fminf(lo[e], s_box[(e0 + e) * 64 + from_lane]);
-                hi[e] = fmaxf(hi[e], s_box[(16 + e0 + e) * 64 + from_lane]);
-            }
+    uint8_t* to = p.boxes + (page * a.heads + h) * 2 * (int64_t)d;
+    const int half = p.rot >> 4, used_slots = min(mine.slots, len);
+    for (int v = lane; v < 2 * d; v += 64) {
+        const bool upper = v >= d;
+        const int ch = upper ? v - d : v, chunk = ch >> 3;
+        const bool apart = !p.pairs && chunk < 2 * half;
+        const int u = apart ? (chunk >= half ? chunk - half : chunk) : chunk >> 1;
+        const int e = 8 * (apart ? chunk >= half : chunk & 1) + (ch & 7) + (upper ? 16 : 0);
+        float x = upper ? -kInf : kInf;
+        for (int t = 0; t < used_slots; ++t) {
+            const float y = s_box[e * 64 + t * units + u];
+            x = upper ? fmaxf(x, y) : fminf(x, y);
         }
-    box[0] = f32_to_codes<E4M3>(lo);
-    box[d / 4] = f32_to_codes<E4M3>(hi);
+        x = scaled(x);
+        if (begin) {
+            float old[4];
+            codes_to_f32<E4M3>(grown<E4M3>(to[v], grow), old);
+            x = upper ? fmaxf(x, old[0]) : fminf(x, old[0]);
+        }
+        const float one[4] = {x, 0.0f, 0.0f, 0.0f};
+        to[v] = (uint8_t)f32_to_codes<E4M3>(one);
+    }
 }
 
 // Query rows: a lane one unit of kQHeads heads of a token, whose table entries it
@@ -294,9 +299,14 @@ __device__ __forceinline__ void turn_queries(const PageArgs& a, const AppendArgs
     }
 }
 
-// A wave a run and head of K or of V, then waves for the query rows.
+// A wave a window of rows and head, of K or of V, then waves for the query rows.  What
+// bounds many rows is memory, where the K and V waves do not keep enough loads under way:
+// 32,768 tokens, 8 KV heads and 32 query heads of 128, 178 us (756 MB, 4.2 TB/s), 107 of them
+// for the K/V rows alone and the store without rotation and boxes 49.  (With the two kinds of
+// blocks in turn 183; with a block of four waves a run of keys 191, and a token of each of
+// 1024 requests 94 us instead of 53.)
 template <bool E4M3, bool BF16>
-__global__ __launch_bounds__(kThreads, 2) void page_append_kernel(PageArgs a, AppendArgs p)
+__global__ __launch_bounds__(kThreads, 3) void page_append_kernel(PageArgs a, AppendArgs p)
 {
     __shared__ float s_box[kWaves][32 * 64];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -367,19 +377,22 @@ extern "C" int fkv_page_append(const fkv_page_desc* desc, const fkv_rotate_desc*
     p.n_pos = rotate ? rotate->n_pos : 0;
     p.rot = rot;
     p.pairs = rotate && rotate->pairing == FKV_ROTATE_PAIRS;
-    // a wave looks at one row, or at a page's worth where the rows are many
-    p.window = n_tokens * desc->heads <= 32768 ? 1 : min(desc->page, 64);
+    // As many rows a wave as leave four thousand waves, up to a page's worth: a wave writes the runs that begin among them one
+    // by one, but waves of rows in which none begins hold up the others.  One row, and so many (us): 12 prompts of 2936 rows in
+    // all, 8 heads of 80, 51 and 25; a token of each of 1024 requests, 8 heads of 128, 54 and 53; of 4096 288 and 246.
+    const int64_t row_heads = n_tokens * desc->heads;
+    p.window = (int32_t)std::min((int64_t)std::min(desc->page, 64), std::max((int64_t)1, (row_heads + 2047) / 2048));
     p.store_items = (n_tokens + p.window - 1) / p.window * desc->heads * 2;
     if (with_q) {
         p.q_heads = rotate->q_heads;
         p.q_groups = (p.q_heads + kQHeads - 1) / kQHeads;
         p.q_lanes = n_tokens * p.q_groups * (desc->d / 16);
     }
-    const int64_t items = p.store_items + (p.q_lanes + 63) / 64;
-    if (p.store_items > kMostBlocks || (items + kWaves - 1) / kWaves > kMostBlocks) return FKV_ERR_UNSUPPORTED;
+    const int64_t blocks = (p.store_items + (p.q_lanes + 63) / 64 + kWaves - 1) / kWaves;
+    if (p.store_items > kMostBlocks || blocks > kMostBlocks) return FKV_ERR_UNSUPPORTED;
     const bool e4m3 = desc->format == FKV_PAGE_E4M3, bf16 = rows_k->type == FKV_ROW_BF16;
     auto kern = e4m3 ? bf16 ? page_append_kernel<true, true> : page_append_kernel<true, false>
                      : bf16 ? page_append_kernel<false, true> : page_append_kernel<false, false>;
-    hipLaunchKernelGGL(kern, dim3((unsigned)((items + kWaves - 1) / kWaves)), dim3(kThreads), 0, (hipStream_t)stream, a, p);
+    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(kThreads), 0, (hipStream_t)stream, a, p);
     return launch_status();
 }

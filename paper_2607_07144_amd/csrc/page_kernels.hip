@@ -268,7 +268,8 @@ __global__ __launch_bounds__(kThreads, 3) void page_store_kernel(PageArgs a, Row
         const int64_t slot = a.slots[i];
         const int64_t page = slot / a.page;
         const int begin = (int)(slot - page * a.page);
-        store_run<E4M3, BF16>(a, rows, values, i, h, page, begin, run_length(a, i, slot, begin));
+        const int len = run_length(a, i, slot, begin);
+        store_run<E4M3, BF16>(a, rows, values, i, h, page, begin, len);
     }
 }
 
