@@ -82,69 +82,89 @@ __device__ __forceinline__ float lanes_max(float v, int log)
     return v;
 }
 
-// Sixteen rows -- a few tokens' heads of one KV head, or 16 of one token's -- as whole
-// numbers: the right operand of the product, positive and negative parts.
-template <int NC>
-struct RowTile {
-    int4_t plus[NC], minus[NC];
-    float mul;   // 2^-e
+// Rows of q as whole numbers, a tile of 16 -- a few tokens' heads of one KV head, or
+// up to 16 of one token's -- in LDS: positive and negative parts, and 2^-e.  A wave
+// rounds four rows at a time, 16 lanes a row and 8 channels a lane.
+template <int NC, int R>
+struct RowsLds {
+    static constexpr int kDepth = NC * 64, kRow = 2 * kDepth + 16;   // bytes (16 more: rows begin in banks of their own)
+    uint8_t part[R * 16 * kRow];
+    float mul[R * 16];
 };
 
 template <int NC>
-__device__ __forceinline__ RowTile<NC> row_tile(const SelectArgs& a, const Request& rq, int tok, int head)
+__device__ __forceinline__ void round_row(const SelectArgs& a, const uint8_t* qp, uint8_t* to, float* mul_to)
 {
-    const int g = (threadIdx.x & 63) >> 4;
-    const uint8_t* qp = a.q + 2 * ((int64_t)(rq.start + tok) * a.q_token + head * a.q_head);
-    uint4 w[NC][2];
-    float most = 0.0f;
+    constexpr int kParts = NC <= 2 ? 1 : 2;   // of 128 channels
+    const int c16 = threadIdx.x & 15;
+    uint4 w[kParts];
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-        const int e = c * 64 + g * 16;
-        w[c][0] = w[c][1] = make_uint4(0, 0, 0, 0);
-        if (e < a.d) w[c][0] = *(const uint4*)(qp + 2 * e), w[c][1] = *(const uint4*)(qp + 2 * e + 16);
+    for (int k = 0; k < kParts; ++k) {
+        const int ch = k * 128 + c16 * 8;
+        w[k] = make_uint4(0, 0, 0, 0);
+        if (ch < a.d) w[k] = *(const uint4*)(qp + 2 * ch);
     }
-    auto each = [&](auto f) {
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                const uint4 u = w[c][k >> 3];
-                const uint32_t pair[4] = {u.x, u.y, u.z, u.w};
-                f(c, k, row_to_f32(pair[(k >> 1) & 3], k & 1, a.bf16));
-            }
+    auto element = [&](int k, int e) {
+        const uint32_t pair[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+        return row_to_f32(pair[e >> 1], e & 1, a.bf16);
     };
-    each([&](int, int, float x) { most = fmaxf(most, fabsf(x) < __builtin_inff() ? fabsf(x) : 0.0f); });
-    most = rows_max(most);
-    const int ex = (int)(__float_as_uint(most) >> 23);
-    const int e = ex == 0 ? 0 : min(133 - ex, 126);
-    const float mul = pow2(e);
-    RowTile<NC> t;
-    t.mul = pow2(-e);
-    uint32_t plus[NC][4], minus[NC][4];
+    // the row's largest; `strange` is a NaN once an element is none or infinite
+    float most = 0.0f, strange = 0.0f;
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
+    for (int k = 0; k < kParts; ++k)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) plus[c][k] = minus[c][k] = 0;
-    each([&](int c, int k, float x) {
-        const float y = rintf(fminf(fmaxf(x == x ? x * mul : 0.0f, -127.0f), 127.0f));
-        const int v = (int)y;
-        plus[c][k >> 2] |= (uint32_t)max(v, 0) << (8 * (k & 3));
-        minus[c][k >> 2] |= (uint32_t)(min(v, 0) & 0xff) << (8 * (k & 3));
-    });
+        for (int e = 0; e < 8; ++e) {
+            most = fmaxf(most, fabsf(element(k, e)));
+            strange = __builtin_fmaf(element(k, e), 0.0f, strange);
+        }
+    const bool special = __any(strange != strange);
+    if (special) {
+        most = 0.0f;
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-        t.plus[c] = int4_t{(int)plus[c][0], (int)plus[c][1], (int)plus[c][2], (int)plus[c][3]};
-        t.minus[c] = int4_t{(int)minus[c][0], (int)minus[c][1], (int)minus[c][2], (int)minus[c][3]};
+        for (int k = 0; k < kParts; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(element(k, e)) < __builtin_inff() ? fabsf(element(k, e)) : 0.0f);
     }
-    return t;
+    most = lanes_max(most, 4);
+    const int ex = (int)(__float_as_uint(most) >> 23);
+    const int e2 = ex == 0 ? 0 : min(133 - ex, 126);
+    const float mul = pow2(e2), most_whole = 127.0f * pow2(-e2);
+    if (c16 == 0) *mul_to = pow2(-e2);
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {
+        const int ch = k * 128 + c16 * 8;
+        uint32_t plus[2], minus[2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            uint32_t u[4];   // x * mul + 1.5 2^23 has the whole number, rounded to nearest with ties to even, in its low bits
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float x = element(k, 4 * q + e);
+                if (special) x = x == x ? x : 0.0f;
+                u[e] = __float_as_uint(__builtin_fmaf(__builtin_amdgcn_fmed3f(x, -most_whole, most_whole), mul, 12582912.0f));
+            }
+            const uint32_t lo = __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(u[3], u[2], 0x0c0c0400u);
+            const uint32_t four = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+            const uint32_t negative = ((four >> 7) & 0x01010101u) * 0xffu;   // the bytes of negative numbers
+            plus[q] = four & ~negative;
+            minus[q] = four & negative;
+        }
+        if (ch < NC * 64) {   // (zeros beyond d)
+            *(uint2*)(to + ch) = make_uint2(plus[0], plus[1]);
+            *(uint2*)(to + NC * 64 + ch) = make_uint2(minus[0], minus[1]);
+        }
+    }
 }
 
-// A wave: R tiles of 16 rows of one KV head of a request against wave_tiles tiles of
-// 16 pages.  The left operand takes a page's box as one of its rows, so that lane
-// 16g + c ends up with row c's sums of pages 4g .. 4g+3.
+// A block: R tiles of 16 rows of one KV head of a request, a wave of it every fourth of
+// the block's tiles of 16 pages.  The left operand takes a page's box as one of its rows,
+// so that lane 16g + c ends up with row c's sums of pages 4g .. 4g+3.  Of KV heads of
+// more than 16 rows a block has one token, and R tiles of its rows at a time.
 template <bool E4M3, int NC, int R>
-__global__ __launch_bounds__(kThreads) void page_score_kernel(SelectArgs a)
+__global__ __launch_bounds__(kThreads, NC <= 2 ? 4 : 3) void page_score_kernel(SelectArgs a)
 {
+    typedef RowsLds<NC, R> Lds;
+    __shared__ __align__(16) Lds sh;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c16 = lane & 15, g = lane >> 4;
     uint32_t b = blockIdx.x;
@@ -155,16 +175,18 @@ __global__ __launch_bounds__(kThreads) void page_score_kernel(SelectArgs a)
     const int64_t r = b / (uint32_t)a.row_groups;
     const int rg = (int)(b - (uint32_t)r * (uint32_t)a.row_groups);
     const Request rq = request_of(a, r);
-    // tokens of a tile, of the wave, and this lane's in its first tile
-    const int per_tile = 16 >> a.lanes_log;
-    const int tok0 = rg * R * per_tile;
+    const int chunks = (a.group + 15) >> 4;              // of a token's heads, 16 a tile
+    const int per_tile = 16 >> a.lanes_log;              // tokens of a tile,
+    const int tokens = chunks > 1 ? 1 : R * per_tile;    // and of the block
+    const int tok0 = rg * tokens;
     if (tok0 >= rq.rows) return;
-    const int most_seen = pages_seen(a, rq, min(tok0 + R * per_tile, rq.rows) - 1);   // (later tokens see no fewer)
+    const int most_seen = pages_seen(a, rq, min(tok0 + tokens, rq.rows) - 1);   // (later tokens see no fewer)
     if (most_seen <= a.n_select) return;   // every page of theirs is selected
     const int tiles = (most_seen + 15) >> 4;
-    const int first = chunk * a.wave_tiles * kWaves + wave;
-    if (first >= tiles) return;
-    const int n_tiles = min(a.wave_tiles, (tiles - first + kWaves - 1) / kWaves);
+    const int first_of_block = chunk * a.wave_tiles * kWaves;
+    if (first_of_block >= tiles) return;
+    const int first = first_of_block + wave;
+    const int n_tiles = first < tiles ? min(a.wave_tiles, (tiles - first + kWaves - 1) / kWaves) : 0;
 
     const int32_t* table = a.tables + r * a.max_pages;
     int kc[NC];   // channels beyond d are taken from the last ones: q is zero there
@@ -185,55 +207,64 @@ __global__ __launch_bounds__(kThreads) void page_score_kernel(SelectArgs a)
         for (int c = 0; c < NC; ++c) p.lo[c] = *(const uint4*)(box + kc[c]), p.hi[c] = *(const uint4*)(box + a.d + kc[c]);
         return p;
     };
-    int id1 = id_of(min(1, n_tiles - 1));
-    Pages next = load(id_of(0));
-    const int chunks = (a.group + 15) >> 4;   // of a token's heads, 16 a tile
-    auto tile_at = [&](int t, int c) {
-        const int tok = min(tok0 + t * per_tile + (c16 >> a.lanes_log), rq.rows - 1);
-        const int in_group = min(c * 16 + (c16 & ((1 << a.lanes_log) - 1)), a.group - 1);
-        return row_tile<NC>(a, rq, tok, h * a.group + in_group);
-    };
-    RowTile<NC> rows[R];
-#pragma unroll
-    for (int t = 0; t < R; ++t) rows[t] = tile_at(t, 0);
-    for (int k = 0; k < n_tiles; ++k) {
-        const Pages now = next;
-        if (k + 1 < n_tiles) {
-            next = load(id1);
-            id1 = id_of(min(k + 2, n_tiles - 1));
+    const int lanes = 1 << a.lanes_log;
+    for (int c0 = 0; c0 < chunks; c0 += R) {
+        const int n_rows_tiles = chunks > 1 ? min(R, chunks - c0) : R;
+        int id1 = id_of(min(1, max(n_tiles - 1, 0)));
+        Pages next = load(id_of(0));   // (of a wave without a tile: the last page, for nothing)
+        if (c0) __syncthreads();
+        // rows 4 (wave + 4k) + g of the block's tiles
+        for (int k = wave * 4; k < n_rows_tiles * 16; k += kWaves * 4) {
+            const int row = k + g, t = row >> 4, in_tile = row & 15;
+            const int tok = min(chunks > 1 ? tok0 : tok0 + t * per_tile + (in_tile >> a.lanes_log), rq.rows - 1);
+            const int in_group = min(chunks > 1 ? (c0 + t) * 16 + in_tile : in_tile & (lanes - 1), a.group - 1);
+            round_row<NC>(a, a.q + 2 * ((int64_t)(rq.start + tok) * a.q_token + (h * a.group + in_group) * a.q_head),
+                          sh.part + row * Lds::kRow, sh.mul + row);
         }
-        int4_t lo[NC], hi[NC];
+        __syncthreads();
+        for (int k = 0; k < n_tiles; ++k) {
+            const Pages now = next;
+            if (k + 1 < n_tiles) {
+                next = load(id1);
+                id1 = id_of(min(k + 2, n_tiles - 1));
+            }
+            int4_t lo[NC], hi[NC];
 #pragma unroll
-        for (int c = 0; c < NC; ++c) lo[c] = whole16<E4M3, false>(now.lo[c]), hi[c] = whole16<E4M3, true>(now.hi[c]);
-        float scale[4];
+            for (int c = 0; c < NC; ++c) lo[c] = whole16<E4M3, false>(now.lo[c]), hi[c] = whole16<E4M3, true>(now.hi[c]);
+            float scale[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) scale[i] = __shfl(now.scale, 4 * g + i, 64);
-        const int tile = first + k * kWaves;
-#pragma unroll
-        for (int t = 0; t < R; ++t) {
+            for (int i = 0; i < 4; ++i) scale[i] = __shfl(now.scale, 4 * g + i, 64);
             float x[4];
-            auto score = [&](const RowTile<NC>& row, bool again) {
+            for (int t = 0; t < n_rows_tiles; ++t) {
+                const uint8_t* rows = sh.part + (t * 16 + c16) * Lds::kRow + g * 16;
                 int4_t sum = {0, 0, 0, 0};
 #pragma unroll
                 for (int c = 0; c < NC; ++c) {
-                    sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(hi[c], row.plus[c], sum, 0, 0, 0);
-                    sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(lo[c], row.minus[c], sum, 0, 0, 0);
+                    sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(hi[c], *(const int4_t*)(rows + c * 64), sum, 0, 0, 0);
+                    sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(lo[c], *(const int4_t*)(rows + Lds::kDepth + c * 64), sum, 0, 0, 0);
                 }
+                const float mul = sh.mul[t * 16 + c16];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float y = ((float)sum[i] * scale[i]) * row.mul;
-                    const float z = y == y ? y : -__builtin_inff();
-                    x[i] = again ? fmaxf(x[i], z) : z;
+                    // (the larger of a NaN and another number is the other)
+                    const float y = fmaxf(((float)sum[i] * scale[i]) * mul, -__builtin_inff());
+                    x[i] = chunks > 1 && t ? fmaxf(x[i], y) : y;
                 }
-            };
-            score(rows[t], false);
-            for (int c = 1; c < chunks; ++c) score(tile_at(t, c), true);
+                if (chunks > 1 && t + 1 < n_rows_tiles) continue;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = lanes_max(x[i], a.lanes_log);
-            const int tok = tok0 + t * per_tile + (c16 >> a.lanes_log);
-            if ((c16 & ((1 << a.lanes_log) - 1)) == 0 && tok < rq.rows)
-                *(float4_t*)(a.scores + ((rq.start + tok) * (int64_t)a.heads + h) * a.score_stride + tile * 16 + g * 4) =
-                    float4_t{x[0], x[1], x[2], x[3]};
+                for (int i = 0; i < 4; ++i) x[i] = lanes_max(x[i], a.lanes_log);
+                const int tok = chunks > 1 ? tok0 : tok0 + t * per_tile + (c16 >> a.lanes_log);
+                if ((c16 & (lanes - 1)) == 0 && tok < rq.rows) {
+                    float4_t* to = (float4_t*)(a.scores + ((rq.start + tok) * (int64_t)a.heads + h) * a.score_stride + (first + k * kWaves) * 16 + g * 4);
+                    float4_t y = {x[0], x[1], x[2], x[3]};
+                    if (c0) {   // with the heads before
+                        const float4_t before = *to;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) y[i] = fmaxf(y[i], before[i]);
+                    }
+                    *to = y;
+                }
+            }
         }
     }
 }
@@ -254,14 +285,14 @@ struct SelectRow {
     bool any;
 };
 
-__device__ __forceinline__ SelectRow select_row(const SelectArgs& a, int64_t item)
+__device__ __forceinline__ SelectRow select_row(const SelectArgs& a, uint32_t item)   // (below 2^31)
 {
     SelectRow s = {0, 0, false};
-    if (item >= a.n_req * a.max_new * a.heads) return s;
-    const int h = (int)(item % a.heads);
-    const int64_t ri = item / a.heads;
-    const int64_t r = ri / a.max_new;
-    const int i = (int)(ri - r * a.max_new);
+    if (item >= (uint32_t)(a.n_req * a.max_new * a.heads)) return s;
+    const uint32_t ri = item / (uint32_t)a.heads;
+    const int h = (int)(item - ri * (uint32_t)a.heads);
+    const uint32_t r = ri / (uint32_t)a.max_new;
+    const int i = (int)(ri - r * (uint32_t)a.max_new);
     const Request rq = request_of(a, r);
     if (i >= rq.rows) return s;
     s.at = (rq.start + i) * (int64_t)a.heads + h;
@@ -270,30 +301,33 @@ __device__ __forceinline__ SelectRow select_row(const SelectArgs& a, int64_t ite
     return s;
 }
 
-// A wave a row, its scores in registers: page 64 n + lane in key[n].  The smallest
-// score selected is found bit by bit from the first that the scores differ in; each
-// step counts those above by ballots, and the search ends when the count fits.
-template <int N>
-__global__ __launch_bounds__(kThreads) void page_select_kernel(SelectArgs a)
+// W waves a row, its scores in registers: page 64 (N wave + n) + lane in key[n].  The
+// smallest score selected is found bit by bit from the first that the scores differ in;
+// each step counts those above by ballots, and the search ends when the count fits.
+template <int N, int W>
+__global__ __launch_bounds__(W > kWaves ? 64 * W : kThreads) void page_select_kernel(SelectArgs a)
 {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const SelectRow row = select_row(a, (int64_t)blockIdx.x * kWaves + wave);
+    __shared__ uint32_t s_top[W], s_low[W];
+    __shared__ int s_count[2][W], s_same[W];
+    const int lane = threadIdx.x & 63, wave_of_block = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = W == 1 ? 0 : wave_of_block, thread = W == 1 ? lane : (int)threadIdx.x;
+    const SelectRow row = select_row(a, W == 1 ? blockIdx.x * kWaves + wave_of_block : blockIdx.x);
     if (!row.any) return;
     int32_t* out = a.selected + row.at * a.n_select;
     if (row.seen <= a.n_select) {
-        for (int j = lane; j < a.n_select; j += 64) out[j] = j < row.seen ? j : -1;
+        for (int j = thread; j < a.n_select; j += 64 * W) out[j] = j < row.seen ? j : -1;
         return;
     }
     // (more pages than are selected: those always kept are apart from each other)
     const int from = a.keep_first, to = row.seen - a.keep_last, want = a.n_select - a.keep_first - a.keep_last;
     const float* scores = a.scores + row.at * a.score_stride;
+    const int page0 = wave * N * 64 + lane;
     uint32_t key[N];
+    float score[N];
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-        const int p = 64 * n + lane;
-        key[n] = 0;
-        if (p >= from && p < to) key[n] = order_of(scores[p]);
-    }
+    for (int n = 0; n < N; ++n) score[n] = scores[min(page0 + 64 * n, row.seen - 1)];   // (without a condition: all on their way at once)
+#pragma unroll
+    for (int n = 0; n < N; ++n) key[n] = page0 + 64 * n >= from && page0 + 64 * n < to ? order_of(score[n]) : 0u;
     uint32_t top = 0, low = 0xffffffffu;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
@@ -305,15 +339,34 @@ __global__ __launch_bounds__(kThreads) void page_select_kernel(SelectArgs a)
         top = max(top, (uint32_t)__shfl_xor((int)top, k, 64));
         low = min(low, (uint32_t)__shfl_xor((int)low, k, 64));
     }
+    if (W > 1) {
+        if (lane == 0) s_top[wave] = top, s_low[wave] = low;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < W; ++w) top = max(top, s_top[w]), low = min(low, s_low[w]);
+    }
+    top = __builtin_amdgcn_readfirstlane(top);
+    low = __builtin_amdgcn_readfirstlane(low);
+    int turn = 0;
+    auto over_row = [&](int c) {   // a count of the wave's, over the row's waves
+        if (W == 1) return c;
+        turn ^= 1;
+        if (lane == 0) s_count[turn][wave] = c;
+        __syncthreads();
+        c = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) c += s_count[turn][w];
+        return (int)__builtin_amdgcn_readfirstlane(c);
+    };
     auto count = [&](uint32_t least) {
         int c = 0;
 #pragma unroll
         for (int n = 0; n < N; ++n) c += __builtin_popcountll(__ballot(key[n] >= least));
         return c;
     };
-    // the largest t of which `want` scores or more are not below
+    // the largest t of which `want` scores or more are not below; of those equal to it the first `ties` are taken
     uint32_t t = 0xffffffffu;
-    int ties = 0;   // of those equal to t so many are taken, the first ones
+    int ties = 0;
     if (want) {
         const uint32_t differ = top ^ low;
         int bit = differ ? 31 - __builtin_clz(differ) : -1;
@@ -321,21 +374,38 @@ __global__ __launch_bounds__(kThreads) void page_select_kernel(SelectArgs a)
         bool fits = false;
         for (; bit >= 0 && !fits; --bit) {
             const uint32_t c = t | 1u << bit;
-            const int n = count(c);
+            const int n = over_row(count(c));
             if (n >= want) t = c;
             fits = n == want;
         }
-        ties = fits ? 0x7fffffff : want - (t == 0xffffffffu ? 0 : count(t + 1));
+        ties = fits ? 0x7fffffff : want - over_row(count(t + 1));   // (no score is 2^32 - 1)
     }
-    int at = 0;
     const unsigned long long below = (1ull << lane) - 1;
+    auto kept = [&](int p) { return p < row.seen && (p < from || p >= to); };
+    int at = 0;
+    if (W > 1) {   // what the waves before take
+        int taken = 0, same = 0;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            same += __builtin_popcountll(__ballot(want && key[n] == t));
+            taken += __builtin_popcountll(__ballot(kept(page0 + 64 * n) || (want && key[n] > t)));
+        }
+        turn ^= 1;
+        if (lane == 0) s_count[turn][wave] = taken, s_same[wave] = same;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+            if (w < wave) {
+                at += s_count[turn][w] + min(ties, s_same[w]);
+                ties -= min(ties, s_same[w]);
+            }
+    }
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-        const int p = 64 * n + lane;
-        if (64 * n >= row.seen) break;
+        const int p = page0 + 64 * n;
+        if (p - lane >= row.seen) break;
         const unsigned long long same = __ballot(want && key[n] == t);
-        const bool kept = p < row.seen && (p < from || p >= to);
-        const bool take = kept || (want && key[n] > t) || (want && key[n] == t && __builtin_popcountll(same & below) < ties);
+        const bool take = kept(p) || (want && key[n] > t) || (want && key[n] == t && __builtin_popcountll(same & below) < ties);
         ties -= min(ties, (int)__builtin_popcountll(same));
         const unsigned long long m = __ballot(take);
         if (take) out[at + __builtin_popcountll(m & below)] = p;
@@ -589,7 +659,7 @@ size_t bytes_or_most(size_t a, size_t b)
     return __builtin_mul_overflow(a, b, &n) ? ~(size_t)0 : n;
 }
 
-constexpr int kHeldPages = 2048;   // that a wave of the selection holds
+constexpr int kHeldPages = 16384;   // that the waves of a row hold at the most: 16 of 16 x 64
 
 // How the splits of an item's list are chosen: see fkv_page_attend_selected.
 struct ListedShape {
@@ -666,12 +736,12 @@ extern "C" int fkv_page_select(const fkv_page_desc* desc, const fkv_select_desc*
         a.lanes_log = 0;
         while (a.lanes_log < 4 && (1 << a.lanes_log) < a.group) ++a.lanes_log;
         const int64_t row_tiles = (a.max_new + (16 >> a.lanes_log) - 1) / (16 >> a.lanes_log);
-        const bool many = row_tiles >= 4 && a.d <= 128;   // four row tiles a wave
-        a.row_groups = many ? (row_tiles + 3) / 4 : row_tiles;
+        const bool many = a.group > 16 || row_tiles >= 4;   // four row tiles a block
+        a.row_groups = a.group > 16 || !many ? row_tiles : (row_tiles + 3) / 4;
         const int64_t tiles = (pages + 15) / 16;
-        // as many page tiles a wave as leave the chip two thousand waves
-        int64_t wave_tiles = std::min(tiles * a.row_groups, (int64_t)1 << 30) * std::min(a.n_req * a.heads, (int64_t)1 << 30) / 2048;
-        wave_tiles = std::min((int64_t)8, std::max((int64_t)1, wave_tiles));
+        // as many page tiles a wave as leave the chip eight thousand waves
+        int64_t wave_tiles = std::min(tiles * a.row_groups, (int64_t)1 << 30) * std::min(a.n_req * a.heads, (int64_t)1 << 30) / 8192;
+        wave_tiles = std::min((int64_t)16, std::max((int64_t)1, wave_tiles));
         a.wave_tiles = (int32_t)wave_tiles;
         a.tile_chunks = (int32_t)((tiles + wave_tiles * kWaves - 1) / (wave_tiles * kWaves));
         const int64_t blocks = a.n_req * a.heads * a.row_groups;   // (row groups are no more than max_new)
@@ -682,21 +752,38 @@ extern "C" int fkv_page_select(const fkv_page_desc* desc, const fkv_select_desc*
         };
         auto of_width = [&](auto nc) {
             constexpr int NC = decltype(nc)::value;
-            if constexpr (NC <= 2) {
-                if (many) return e4m3 ? go(page_score_kernel<true, NC, 4>) : go(page_score_kernel<false, NC, 4>);
-            }
+            if (many) return e4m3 ? go(page_score_kernel<true, NC, 4>) : go(page_score_kernel<false, NC, 4>);
             e4m3 ? go(page_score_kernel<true, NC, 1>) : go(page_score_kernel<false, NC, 1>);
         };
         if (a.d <= 64) of_width(std::integral_constant<int, 1>{});
         else if (a.d <= 128) of_width(std::integral_constant<int, 2>{});
         else of_width(std::integral_constant<int, 4>{});
     }
-    if (need && pages > kHeldPages) {
+    // a wave a row where the rows are many, four where they leave the chip idle, 16 for more pages
+    auto held = [&](auto n, auto w) {
+        constexpr int N = decltype(n)::value, W = decltype(w)::value;
+        const int64_t blocks = W == 1 ? (rows + kWaves - 1) / kWaves : rows;
+        hipLaunchKernelGGL((page_select_kernel<N, W>), dim3((unsigned)blocks), dim3(W == 1 ? kThreads : 64 * W), 0, st, a);
+    };
+    auto of_pages = [&](auto w) {
+        constexpr int W = decltype(w)::value;
+        const int64_t n = (pages + 64 * W - 1) / (64 * W);
+        if (!need || n <= 2) return held(std::integral_constant<int, 2>{}, w);
+        if (n <= 4) return held(std::integral_constant<int, 4>{}, w);
+        if (W == 4 || n <= 8) return held(std::integral_constant<int, 8>{}, w);
+        if constexpr (W != 4) {
+            if (W == 16 || n <= 16) return held(std::integral_constant<int, 16>{}, w);
+        }
+        if constexpr (W == 1) held(std::integral_constant<int, 32>{}, w);
+    };
+    if (need && pages > kHeldPages)
         hipLaunchKernelGGL(page_select_wide_kernel, dim3((unsigned)rows), dim3(kWideThreads), 0, st, a);
-    } else {
-        auto kern = !need || pages <= 256 ? page_select_kernel<4> : pages <= 512 ? page_select_kernel<8> : pages <= 1024 ? page_select_kernel<16> : page_select_kernel<32>;
-        hipLaunchKernelGGL(kern, dim3((unsigned)((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, st, a);
-    }
+    else if (need && pages > 64 * 32)
+        of_pages(std::integral_constant<int, 16>{});
+    else if (need && rows < 4096 && pages > 64)
+        of_pages(std::integral_constant<int, 4>{});
+    else
+        of_pages(std::integral_constant<int, 1>{});
     return launch_status();
 }
 
