@@ -20,7 +20,7 @@ typedef int int4_t __attribute__((ext_vector_type(4)));
 
 struct SelectArgs : AttendArgs {
     const uint8_t* boxes;
-    float* scores;      // [token][KV head][score_stride]
+    int32_t* scores;    // [token][KV head][score_stride], as ordered() gives them
     int32_t* selected;  // [token][KV head][n_select]
     int64_t score_stride;
     int64_t row_groups;   // of the scoring kernel: row tiles of a request, R a wave
@@ -67,19 +67,26 @@ __device__ __forceinline__ int4_t whole16(uint4 w)
     return int4_t{(int)whole4<E4M3, HIGH>(w.x), (int)whole4<E4M3, HIGH>(w.y), (int)whole4<E4M3, HIGH>(w.z), (int)whole4<E4M3, HIGH>(w.w)};
 }
 
-// The largest of the lanes that share all bits of their number but the lowest `log`
-// (up to four).
-__device__ __forceinline__ float lanes_max(float v, int log)
+// A score as a whole number, in the order of the scores; one that is a NaN as -infinity.
+__device__ __forceinline__ int ordered(float x)
+{
+    const int u = __builtin_bit_cast(int, fmaxf(x, -__builtin_inff()));   // (the larger of a NaN and another number is the other)
+    return u ^ (int)((uint32_t)(u >> 31) >> 1);
+}
+
+// The largest of the lanes that share all bits of their number but the lowest `log` (up
+// to four), of N values at once.
+template <int N>
+__device__ __forceinline__ void lanes_max(int (&v)[N], int log)
 {
     auto with = [&](auto ctrl) {
-        const int u = __builtin_bit_cast(int, v);
-        v = fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(u, u, decltype(ctrl)::value, 0xf, 0xf, false)));
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = max(v[i], __builtin_amdgcn_update_dpp(v[i], v[i], decltype(ctrl)::value, 0xf, 0xf, false));
     };
     if (log > 0) with(std::integral_constant<int, 0xb1>{});    // with the neighbour,
     if (log > 1) with(std::integral_constant<int, 0x4e>{});    // the other pair of four,
     if (log > 2) with(std::integral_constant<int, 0x141>{});   // the other four of eight,
     if (log > 3) with(std::integral_constant<int, 0x140>{});   // the other eight
-    return v;
 }
 
 // Rows of q as whole numbers, a tile of 16 -- a few tokens' heads of one KV head, or
@@ -125,7 +132,9 @@ __device__ __forceinline__ void round_row(const SelectArgs& a, const uint8_t* qp
 #pragma unroll
             for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(element(k, e)) < __builtin_inff() ? fabsf(element(k, e)) : 0.0f);
     }
-    most = lanes_max(most, 4);
+    int all[1] = {__builtin_bit_cast(int, most)};   // (of numbers that are not negative the bits are in their order)
+    lanes_max(all, 4);
+    most = __builtin_bit_cast(float, all[0]);
     const int ex = (int)(__float_as_uint(most) >> 23);
     const int e2 = ex == 0 ? 0 : min(133 - ex, 126);
     const float mul = pow2(e2), most_whole = 127.0f * pow2(-e2);
@@ -156,12 +165,12 @@ __device__ __forceinline__ void round_row(const SelectArgs& a, const uint8_t* qp
     }
 }
 
-// A block: R tiles of 16 rows of one KV head of a request, a wave of it every fourth of
-// the block's tiles of 16 pages.  The left operand takes a page's box as one of its rows,
+// A block: R tiles of 16 rows of one KV head of a request, a wave of it a quarter of the
+// block's tiles of 16 pages.  The left operand takes a page's box as one of its rows,
 // so that lane 16g + c ends up with row c's sums of pages 4g .. 4g+3.  Of KV heads of
-// more than 16 rows a block has one token, and R tiles of its rows at a time.
-template <bool E4M3, int NC, int R>
-__global__ __launch_bounds__(kThreads, NC <= 2 ? 4 : 3) void page_score_kernel(SelectArgs a)
+// more than 16 rows (WIDE) a block has one token, and R tiles of its rows at a time.
+template <bool E4M3, int NC, int R, bool WIDE>
+__global__ __launch_bounds__(kThreads, R == 1 || NC == 1 ? 4 : NC == 2 ? 3 : 2) void page_score_kernel(SelectArgs a)
 {
     typedef RowsLds<NC, R> Lds;
     __shared__ __align__(16) Lds sh;
@@ -175,9 +184,9 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 4 : 3) void page_score_kernel(S
     const int64_t r = b / (uint32_t)a.row_groups;
     const int rg = (int)(b - (uint32_t)r * (uint32_t)a.row_groups);
     const Request rq = request_of(a, r);
-    const int chunks = (a.group + 15) >> 4;              // of a token's heads, 16 a tile
+    const int chunks = WIDE ? (a.group + 15) >> 4 : 1;   // of a token's heads, 16 a tile
     const int per_tile = 16 >> a.lanes_log;              // tokens of a tile,
-    const int tokens = chunks > 1 ? 1 : R * per_tile;    // and of the block
+    const int tokens = WIDE ? 1 : R * per_tile;          // and of the block
     const int tok0 = rg * tokens;
     if (tok0 >= rq.rows) return;
     const int most_seen = pages_seen(a, rq, min(tok0 + tokens, rq.rows) - 1);   // (later tokens see no fewer)
@@ -185,8 +194,8 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 4 : 3) void page_score_kernel(S
     const int tiles = (most_seen + 15) >> 4;
     const int first_of_block = chunk * a.wave_tiles * kWaves;
     if (first_of_block >= tiles) return;
-    const int first = first_of_block + wave;
-    const int n_tiles = first < tiles ? min(a.wave_tiles, (tiles - first + kWaves - 1) / kWaves) : 0;
+    const int first = first_of_block + wave * a.wave_tiles;
+    const int n_tiles = max(min(a.wave_tiles, tiles - first), 0);
 
     const int32_t* table = a.tables + r * a.max_pages;
     int kc[NC];   // channels beyond d are taken from the last ones: q is zero there
@@ -196,7 +205,7 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 4 : 3) void page_score_kernel(S
         uint4 lo[NC], hi[NC];
         float scale;   // of page c16; a NaN where there is none
     };
-    auto id_of = [&](int k) { return table[min((first + k * kWaves) * 16 + c16, most_seen - 1)]; };
+    auto id_of = [&](int k) { return table[min((first + k) * 16 + c16, most_seen - 1)]; };
     auto load = [&](int id) {
         Pages p;
         const bool here = (uint32_t)id < (uint64_t)a.n_pages;
@@ -209,15 +218,15 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 4 : 3) void page_score_kernel(S
     };
     const int lanes = 1 << a.lanes_log;
     for (int c0 = 0; c0 < chunks; c0 += R) {
-        const int n_rows_tiles = chunks > 1 ? min(R, chunks - c0) : R;
+        const int row_tiles = WIDE ? min(R, chunks - c0) : R;
         int id1 = id_of(min(1, max(n_tiles - 1, 0)));
         Pages next = load(id_of(0));   // (of a wave without a tile: the last page, for nothing)
         if (c0) __syncthreads();
         // rows 4 (wave + 4k) + g of the block's tiles
-        for (int k = wave * 4; k < n_rows_tiles * 16; k += kWaves * 4) {
+        for (int k = wave * 4; k < row_tiles * 16; k += kWaves * 4) {
             const int row = k + g, t = row >> 4, in_tile = row & 15;
-            const int tok = min(chunks > 1 ? tok0 : tok0 + t * per_tile + (in_tile >> a.lanes_log), rq.rows - 1);
-            const int in_group = min(chunks > 1 ? (c0 + t) * 16 + in_tile : in_tile & (lanes - 1), a.group - 1);
+            const int tok = min(WIDE ? tok0 : tok0 + t * per_tile + (in_tile >> a.lanes_log), rq.rows - 1);
+            const int in_group = min(WIDE ? (c0 + t) * 16 + in_tile : in_tile & (lanes - 1), a.group - 1);
             round_row<NC>(a, a.q + 2 * ((int64_t)(rq.start + tok) * a.q_token + (h * a.group + in_group) * a.q_head),
                           sh.part + row * Lds::kRow, sh.mul + row);
         }
@@ -234,8 +243,10 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 4 : 3) void page_score_kernel(S
             float scale[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) scale[i] = __shfl(now.scale, 4 * g + i, 64);
-            float x[4];
-            for (int t = 0; t < n_rows_tiles; ++t) {
+            int x[4];
+#pragma unroll
+            for (int t = 0; t < R; ++t) {
+                if (WIDE && t >= row_tiles) break;
                 const uint8_t* rows = sh.part + (t * 16 + c16) * Lds::kRow + g * 16;
                 int4_t sum = {0, 0, 0, 0};
 #pragma unroll
@@ -246,23 +257,20 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 4 : 3) void page_score_kernel(S
                 const float mul = sh.mul[t * 16 + c16];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    // (the larger of a NaN and another number is the other)
-                    const float y = fmaxf(((float)sum[i] * scale[i]) * mul, -__builtin_inff());
-                    x[i] = chunks > 1 && t ? fmaxf(x[i], y) : y;
+                    const int y = ordered(((float)sum[i] * scale[i]) * mul);
+                    x[i] = WIDE && t ? max(x[i], y) : y;
                 }
-                if (chunks > 1 && t + 1 < n_rows_tiles) continue;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = lanes_max(x[i], a.lanes_log);
-                const int tok = chunks > 1 ? tok0 : tok0 + t * per_tile + (c16 >> a.lanes_log);
+                if (WIDE && t + 1 < row_tiles) continue;
+                lanes_max(x, a.lanes_log);
+                const int tok = WIDE ? tok0 : tok0 + t * per_tile + (c16 >> a.lanes_log);
                 if ((c16 & (lanes - 1)) == 0 && tok < rq.rows) {
-                    float4_t* to = (float4_t*)(a.scores + ((rq.start + tok) * (int64_t)a.heads + h) * a.score_stride + (first + k * kWaves) * 16 + g * 4);
-                    float4_t y = {x[0], x[1], x[2], x[3]};
-                    if (c0) {   // with the heads before
-                        const float4_t before = *to;
+                    int4_t* to = (int4_t*)(a.scores + ((rq.start + tok) * (int64_t)a.heads + h) * a.score_stride + (first + k) * 16 + g * 4);
+                    if (WIDE && c0) {   // with the heads before
+                        const int4_t before = *to;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) y[i] = fmaxf(y[i], before[i]);
+                        for (int i = 0; i < 4; ++i) x[i] = max(x[i], before[i]);
                     }
-                    *to = y;
+                    *to = int4_t{x[0], x[1], x[2], x[3]};
                 }
             }
         }
@@ -271,11 +279,10 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 4 : 3) void page_score_kernel(S
 
 // ------------------------------------------------------------- selection --
 
-// Scores as whole numbers in their order, none of them 0.
-__device__ __forceinline__ uint32_t order_of(float x)
+// The scores' order without a sign, none of them 0.
+__device__ __forceinline__ uint32_t key_of_score(int x)
 {
-    const uint32_t u = __float_as_uint(x + 0.0f);   // (-0 is 0)
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
+    return (uint32_t)(x == -1 ? 0 : x) ^ 0x80000000u;   // (-0, in order -1, is 0)
 }
 
 // A row of the lists: token, KV head, and how many pages the token sees.
@@ -320,14 +327,14 @@ __global__ __launch_bounds__(W > kWaves ? 64 * W : kThreads) void page_select_ke
     }
     // (more pages than are selected: those always kept are apart from each other)
     const int from = a.keep_first, to = row.seen - a.keep_last, want = a.n_select - a.keep_first - a.keep_last;
-    const float* scores = a.scores + row.at * a.score_stride;
+    const int32_t* scores = a.scores + row.at * a.score_stride;
     const int page0 = wave * N * 64 + lane;
     uint32_t key[N];
-    float score[N];
+    int score[N];
 #pragma unroll
     for (int n = 0; n < N; ++n) score[n] = scores[min(page0 + 64 * n, row.seen - 1)];   // (without a condition: all on their way at once)
 #pragma unroll
-    for (int n = 0; n < N; ++n) key[n] = page0 + 64 * n >= from && page0 + 64 * n < to ? order_of(score[n]) : 0u;
+    for (int n = 0; n < N; ++n) key[n] = page0 + 64 * n >= from && page0 + 64 * n < to ? key_of_score(score[n]) : 0u;
     uint32_t top = 0, low = 0xffffffffu;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
@@ -434,8 +441,8 @@ __global__ __launch_bounds__(kWideThreads) void page_select_wide_kernel(SelectAr
         return;
     }
     const int from = a.keep_first, to = row.seen - a.keep_last, want = a.n_select - a.keep_first - a.keep_last;
-    const float* scores = a.scores + row.at * a.score_stride;
-    auto key_of = [&](int p) { return p >= from && p < to ? order_of(scores[p]) : 0u; };
+    const int32_t* scores = a.scores + row.at * a.score_stride;
+    auto key_of = [&](int p) { return p >= from && p < to ? key_of_score(scores[p]) : 0u; };
     uint32_t top = 0, low = 0xffffffffu;
     for (int p = tid; p < row.seen; p += kWideThreads) {
         const uint32_t k = key_of(p);
@@ -704,7 +711,7 @@ using namespace fkv;
 extern "C" size_t fkv_page_select_workspace(const fkv_page_desc* desc, const fkv_select_desc* select)
 {
     if (!select_ok(desc, select)) return 0;
-    return bytes_or_most((size_t)(select->n_tokens * desc->heads), (size_t)score_stride(desc, select) * sizeof(float));
+    return bytes_or_most((size_t)(select->n_tokens * desc->heads), (size_t)score_stride(desc, select) * sizeof(int32_t));
 }
 
 extern "C" int fkv_page_select(const fkv_page_desc* desc, const fkv_select_desc* select, const uint8_t* boxes, const float* scales,
@@ -725,7 +732,7 @@ extern "C" int fkv_page_select(const fkv_page_desc* desc, const fkv_select_desc*
     t.q_heads = select->q_heads, t.type = select->type, t.causal = select->causal;
     SelectArgs a = {};
     (AttendArgs&)a = attend_args(desc, &t, nullptr, nullptr, scales, q, tables, kv_len, q_start, nullptr, nullptr, nullptr, nullptr, nullptr);
-    a.boxes = boxes, a.scores = (float*)workspace, a.selected = selected;
+    a.boxes = boxes, a.scores = (int32_t*)workspace, a.selected = selected;
     a.score_stride = score_stride(desc, select);
     a.n_select = select->n_select, a.keep_first = select->keep_first, a.keep_last = select->keep_last;
     const int64_t pages = most_pages(desc, select);
@@ -739,9 +746,11 @@ extern "C" int fkv_page_select(const fkv_page_desc* desc, const fkv_select_desc*
         const bool many = a.group > 16 || row_tiles >= 4;   // four row tiles a block
         a.row_groups = a.group > 16 || !many ? row_tiles : (row_tiles + 3) / 4;
         const int64_t tiles = (pages + 15) / 16;
-        // as many page tiles a wave as leave the chip eight thousand waves
+        // as many page tiles a wave as leave the chip eight thousand waves, where rounding the rows is to be shared.  With 2
+        // and 8 a wave (us): a chunk of 4096 tokens over 512 pages 136 and 104, 512 tokens over 256 pages 20 and 23; few rows,
+        // 16 contexts of 2048 pages 28.7 and 28.1, 64 of up to 2048 pages 27 and 34, one of 16,384 pages 32 and 35.
         int64_t wave_tiles = std::min(tiles * a.row_groups, (int64_t)1 << 30) * std::min(a.n_req * a.heads, (int64_t)1 << 30) / 8192;
-        wave_tiles = std::min((int64_t)16, std::max((int64_t)1, wave_tiles));
+        wave_tiles = many ? std::min((int64_t)8, std::max((int64_t)2, wave_tiles)) : 2;
         a.wave_tiles = (int32_t)wave_tiles;
         a.tile_chunks = (int32_t)((tiles + wave_tiles * kWaves - 1) / (wave_tiles * kWaves));
         const int64_t blocks = a.n_req * a.heads * a.row_groups;   // (row groups are no more than max_new)
@@ -752,8 +761,9 @@ extern "C" int fkv_page_select(const fkv_page_desc* desc, const fkv_select_desc*
         };
         auto of_width = [&](auto nc) {
             constexpr int NC = decltype(nc)::value;
-            if (many) return e4m3 ? go(page_score_kernel<true, NC, 4>) : go(page_score_kernel<false, NC, 4>);
-            e4m3 ? go(page_score_kernel<true, NC, 1>) : go(page_score_kernel<false, NC, 1>);
+            if (a.group > 16) return e4m3 ? go(page_score_kernel<true, NC, 4, true>) : go(page_score_kernel<false, NC, 4, true>);
+            if (many) return e4m3 ? go(page_score_kernel<true, NC, 4, false>) : go(page_score_kernel<false, NC, 4, false>);
+            e4m3 ? go(page_score_kernel<true, NC, 1, false>) : go(page_score_kernel<false, NC, 1, false>);
         };
         if (a.d <= 64) of_width(std::integral_constant<int, 1>{});
         else if (a.d <= 128) of_width(std::integral_constant<int, 2>{});
