@@ -551,15 +551,18 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 2 : 1) void attend_listed_kerne
     const int d = a.d;
     const int64_t q_heads = (int64_t)a.heads * a.group;
     const int split = (int)(blockIdx.x % (uint32_t)a.n_splits);
-    const int64_t block = blockIdx.x / (uint32_t)a.n_splits;
-    const int64_t item = W == 1 ? block * kWaves + wave : block;
-    const int chunks = (a.group + kFewRows - 1) / kFewRows;
-    if (item >= a.n_req * a.max_new * chunks * a.heads) return;
-    const int h = (int)(item % a.heads);
-    const int64_t of_token = item / a.heads;
-    const int chunk = (int)(of_token % chunks);
-    const int64_t r = of_token / chunks / a.max_new;
-    const int i = (int)(of_token / chunks - r * a.max_new);
+    const uint32_t block = blockIdx.x / (uint32_t)a.n_splits;
+    const uint32_t chunks = (uint32_t)(a.group + kFewRows - 1) / kFewRows;
+    // (blocks of one head go to one part of the chip, where the heads are as many as its parts: a head's pages are read there
+    // more often.  A wave an item: neighbouring tokens of one head in a block)
+    const uint32_t of_head = block / (uint32_t)a.heads;
+    const int h = (int)(block - of_head * (uint32_t)a.heads);
+    const uint32_t of_chunk = of_head / chunks;
+    const int chunk = (int)(of_head - of_chunk * chunks);
+    const int64_t ri = W == 1 ? (int64_t)of_chunk * kWaves + wave : of_chunk;
+    if (ri >= a.n_req * a.max_new) return;
+    const uint32_t r = (uint32_t)ri / (uint32_t)a.max_new;
+    const int i = (int)((uint32_t)ri - r * (uint32_t)a.max_new);
     const Request rq = request_of(a, r);
     if (i >= rq.rows) return;
     const int64_t token = rq.start + i;
@@ -672,7 +675,7 @@ constexpr int kHeldPages = 16384;   // that the waves of a row hold at the most:
 struct ListedShape {
     int waves;       // of an item in a block
     int n_splits;
-    int64_t items;
+    int64_t blocks;  // times the splits
     bool join_blocks;
 };
 
@@ -681,12 +684,14 @@ ListedShape listed_shape(const fkv_page_desc* p, const fkv_attend_desc* t, int64
     ListedShape s;
     const int64_t group = t->q_heads / p->heads;
     const int64_t of_token = p->heads * ((group + kFewRows - 1) / kFewRows);
-    s.items = std::min(t->n_req * t->max_new, (int64_t)1 << 34) * of_token;   // (2^34 are too many, whatever the heads)
+    const int64_t tokens = std::min(t->n_req * t->max_new, (int64_t)1 << 34);   // (2^34 are too many, whatever the heads)
+    const int64_t items = tokens * of_token;
     const int64_t tiles = (n_listed * (p->page / 16) + 3) / 4;
     s.n_splits = 1;
-    s.waves = s.items >= 2048 || tiles <= 1 ? 1 : kWaves;
-    if (s.waves == kWaves && s.items < 256) {
-        const int64_t want = (512 + s.items - 1) / std::max((int64_t)1, s.items), most = std::max((int64_t)1, tiles / (2 * kWaves));
+    s.waves = items >= 2048 || tiles <= 1 ? 1 : kWaves;
+    s.blocks = s.waves == 1 ? (tokens + kWaves - 1) / kWaves * of_token : items;
+    if (s.waves == kWaves && items < 256) {
+        const int64_t want = (512 + items - 1) / std::max((int64_t)1, items), most = std::max((int64_t)1, tiles / (2 * kWaves));
         s.n_splits = (int)std::min(want, most);
     }
     s.join_blocks = s.n_splits >= kManySplits;
@@ -820,8 +825,7 @@ extern "C" int fkv_page_attend_selected(const fkv_page_desc* desc, const fkv_att
     const ListedShape s = listed_shape(desc, attend, n_selected);
     const Workspace ws = listed_workspace(desc, attend, s);
     if (ws.bytes && (!workspace || workspace_bytes < ws.bytes)) return FKV_ERR_SCRATCH_TOO_SMALL;
-    const int64_t blocks = s.waves == 1 ? (s.items + kWaves - 1) / kWaves : s.items;
-    if (blocks > kMostBlocks / s.n_splits) return FKV_ERR_UNSUPPORTED;
+    if (s.blocks > kMostBlocks / s.n_splits || attend->n_req * attend->max_new > kMostBlocks) return FKV_ERR_UNSUPPORTED;
     AttendArgs a = attend_args(desc, attend, k_codes, v_codes, scales, q, tables, kv_len, q_start, slopes, prefix, first, out, lse);
     a.listed = selected, a.n_listed = n_selected;
     a.part = (float*)workspace;
@@ -835,7 +839,7 @@ extern "C" int fkv_page_attend_selected(const fkv_page_desc* desc, const fkv_att
     auto of_width = [&](auto nc) {
         constexpr int NC = decltype(nc)::value;
         auto go = [&](auto kern, size_t shm) {
-            hipLaunchKernelGGL(kern, dim3((unsigned)(blocks * s.n_splits)), dim3(kThreads), shm, st, a);
+            hipLaunchKernelGGL(kern, dim3((unsigned)(s.blocks * s.n_splits)), dim3(kThreads), shm, st, a);
         };
         if (s.waves == 1) return e4m3 ? go(attend_listed_kernel<true, NC, 1>, 0) : go(attend_listed_kernel<false, NC, 1>, 0);
         const size_t shm = (2 * kWaves * kFewRows + (size_t)kWaves * kFewRows * (a.d + 4)) * sizeof(float);
