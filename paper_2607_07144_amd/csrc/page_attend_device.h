@@ -354,6 +354,124 @@ struct FewSums {
     }
 };
 
+// What a lane knows of its row: the right operand of S^T -- channels 64c + 16g .. + 15
+// -- and how its scores are formed.
+template <int NC>
+struct FewQuery {
+    half8_t qf[NC][2];
+    float mul, cap, cap2, slope2;
+    int pos;
+    bool large_cap, slopes;
+    __device__ __forceinline__ FewQuery(const AttendArgs& a, const Request& rq, const FewRow& fr)
+    {
+        const int g = (threadIdx.x & 63) >> 4;
+        const uint8_t* qp = a.q + 2 * ((int64_t)(rq.start + fr.tok) * a.q_token + fr.head * a.q_head);
+        int shift = 0;
+        uint4 w[NC][2];
+        float most = 0.0f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int e = c * 64 + g * 16;
+            w[c][0] = w[c][1] = make_uint4(0, 0, 0, 0);
+            if (e < a.d) w[c][0] = *(const uint4*)(qp + 2 * e), w[c][1] = *(const uint4*)(qp + 2 * e + 16);
+            if (a.bf16) most = fmaxf(most, fmaxf(abs_most8(w[c][0]), abs_most8(w[c][1])));
+        }
+        if (a.bf16) shift = row_shift(rows_max(most));
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            qf[c][0] = q8(w[c][0], a.bf16, pow2(shift));
+            qf[c][1] = q8(w[c][1], a.bf16, pow2(shift));
+        }
+        cap = a.softcap;
+        cap2 = a.softcap * kLog2e;
+        large_cap = a.softcap > kSmallCap;
+        mul = pow2(-shift) * (a.softcap > 0.0f && !large_cap ? a.scale * 2.0f * kLog2e / a.softcap : a.scale * kLog2e);
+        slopes = a.slopes != nullptr;
+        slope2 = slopes ? a.slopes[fr.head] * kLog2e : 0.0f;
+        pos = rq.pos0 + fr.tok;
+    }
+};
+
+// The products of a tile's keys with the row: of keys j0g .. j0g+15 in turn, before
+// their factors.
+template <bool E4M3, int NC>
+__device__ __forceinline__ void few_products(const uint4 (&kw)[4][NC], const FewQuery<NC>& q, float4_t (&s)[4])
+{
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        s[t] = float4_t{0, 0, 0, 0};
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(kw[t][c].x, kw[t][c].y), q.qf[c][0], s[t], 0, 0, 0);
+            s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(kw[t][c].z, kw[t][c].w), q.qf[c][1], s[t], 0, 0, 0);
+        }
+    }
+}
+
+// The tile's scores, weights and values into the sums.  sc: the scales of the lane's key
+// group, which is there (`here`) or not; vw: its values.
+template <bool E4M3, int NC>
+__device__ __forceinline__ void few_update(const AttendArgs& a, const Request& rq, const Seen& mine, const FewQuery<NC>& q, FewSums<NC>& st,
+                                           const float4_t (&s)[4], uint4 (&vw)[4 * NC], float2 sc, bool here, bool mask, int j0g)
+{
+    const float mulk = q.mul * sc.x;
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = s[i >> 2][i & 3] * mulk;
+    if (q.large_cap) {
+        const float inv = 1.0f / q.cap2;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = capped_large(x[i], q.cap2, inv);
+    } else if (q.cap > 0.0f) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = capped(x[i], q.cap2);
+    }
+    if (q.slopes) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] -= q.slope2 * fabsf((float)(j0g + i - q.pos));
+    }
+    if (mask) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (!here || !visible(a, mine, j0g + i)) x[i] = -__builtin_inff();
+        if (E4M3) {   // codes after the last key may be anything, a NaN among it
+            const int n = here ? rq.kv - j0g : 0;
+#pragma unroll
+            for (int t = 0; t < 4 * NC; ++t) vw[t] = first_bytes(vw[t], n);
+        }
+    }
+    float top = x[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+    const float vtop = top > -__builtin_inff() ? sc.y : 0.0f;   // of a group of which the row sees a key
+    top = rows_max(top);
+    if (__any(top > st.m + kSlack || vtop > st.vref)) {
+        const float vnew = rows_max(fmaxf(st.vref, vtop));
+        const float mnew = fmaxf(st.m, top);
+        const float shrink = mnew == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(st.m - mnew);
+        st.l *= shrink;
+        const float k = shrink * (st.vref / vnew);
+#pragma unroll
+        for (int t = 0; t < 4 * NC; ++t) st.acc[t] *= k;
+        st.m = mnew;
+        st.vref = vnew;
+    }
+    const float m0 = st.m == -__builtin_inff() ? 0.0f : st.m;
+    const float vs = fminf(sc.y * (kTop / st.vref), kTop);   // (beyond that only where all weights are 0)
+    half8_t p[2];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float w = __builtin_amdgcn_exp2f(x[i] - m0);
+        st.l += w;
+        p[i >> 3][i & 7] = (_Float16)(w * vs);
+    }
+#pragma unroll
+    for (int t = 0; t < 4 * NC; ++t) {
+        st.acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(vw[t].x, vw[t].y), p[0], st.acc[t], 0, 0, 0);
+        st.acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(vw[t].z, vw[t].w), p[1], st.acc[t], 0, 0, 0);
+    }
+}
+
 // A wave over tiles e0, e0 + step, .. below e1 (one at least).  LISTED: tiles of four
 // groups of the pages in `list`, `places` groups in all, and rows of one token; else
 // tiles of the request's keys.  A list's entries are read two tiles ahead, its pages'
@@ -364,9 +482,9 @@ __device__ __forceinline__ void few_keys(const AttendArgs& a, const Request& rq,
 {
     typedef std::conditional_t<LISTED, ListPlace, Place> At;
     const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
-    const int d = a.d, tok = fr.tok, head = fr.head;
+    const int d = a.d;
     const int64_t per_head = (int64_t)a.page * d;
-    const Seen mine = seen_of(a, rq, r, tok);
+    const Seen mine = seen_of(a, rq, r, fr.tok);
     const int32_t* table = a.tables + r * a.max_pages;
     const int gk = c16 >> 2;   // the key group of this lane's left-operand rows
     // channels beyond d are loaded from the last ones: q is zero there, and their sums go nowhere
@@ -407,32 +525,7 @@ __device__ __forceinline__ void few_keys(const AttendArgs& a, const Request& rq,
     load_keys(pk);
     sc = scale_head[(int64_t)pv.id * a.heads];
 
-    // the right operand of S^T: channels 64c + 16g .. + 15 of the row
-    half8_t qf[NC][2];
-    int shift = 0;
-    {
-        const uint8_t* qp = a.q + 2 * ((int64_t)(rq.start + tok) * a.q_token + head * a.q_head);
-        uint4 w[NC][2];
-        float most = 0.0f;
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const int e = c * 64 + g * 16;
-            w[c][0] = w[c][1] = make_uint4(0, 0, 0, 0);
-            if (e < d) w[c][0] = *(const uint4*)(qp + 2 * e), w[c][1] = *(const uint4*)(qp + 2 * e + 16);
-            if (a.bf16) most = fmaxf(most, fmaxf(abs_most8(w[c][0]), abs_most8(w[c][1])));
-        }
-        if (a.bf16) shift = row_shift(rows_max(most));
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            qf[c][0] = q8(w[c][0], a.bf16, pow2(shift));
-            qf[c][1] = q8(w[c][1], a.bf16, pow2(shift));
-        }
-    }
-    const float cap2 = a.softcap * kLog2e;
-    const bool large_cap = a.softcap > kSmallCap;
-    const float mul = pow2(-shift) * (a.softcap > 0.0f && !large_cap ? a.scale * 2.0f * kLog2e / a.softcap : a.scale * kLog2e);
-    const float slope2 = a.slopes ? a.slopes[head] * kLog2e : 0.0f;
-    const int pos = rq.pos0 + tok;
+    const FewQuery<NC> query(a, rq, fr);
 
     for (int e = e0; e < e1; e += step) {
         // the tile's values, on their way while its scores are formed
@@ -451,17 +544,8 @@ __device__ __forceinline__ void few_keys(const AttendArgs& a, const Request& rq,
             mask = !tile_whole(a, tl, j0) || __any(!here);
         }
         if (!here) sc = make_float2(0.0f, 0.0f);
-        // scores of keys j0g .. j0g+15 in turn
         float4_t s[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            s[t] = float4_t{0, 0, 0, 0};
-#pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(kw[t][c].x, kw[t][c].y), qf[c][0], s[t], 0, 0, 0);
-                s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(kw[t][c].z, kw[t][c].w), qf[c][1], s[t], 0, 0, 0);
-            }
-        }
+        few_products<E4M3>(kw, query, s);
         // the next tile's keys, and the pages of the one after
         if (e + step < e1) {
             check_place(a, pk1);
@@ -482,62 +566,7 @@ __device__ __forceinline__ void few_keys(const AttendArgs& a, const Request& rq,
                 pv1 = place_of(a, table, rq.kv, (j1 >> 4) + g);
             }
         }
-        const float mulk = mul * sc.x;
-        float x[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = s[i >> 2][i & 3] * mulk;
-        if (large_cap) {
-            const float inv = 1.0f / cap2;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = capped_large(x[i], cap2, inv);
-        } else if (a.softcap > 0.0f) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = capped(x[i], cap2);
-        }
-        if (a.slopes) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] -= slope2 * fabsf((float)(j0g + i - pos));
-        }
-        if (mask) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (!here || !visible(a, mine, j0g + i)) x[i] = -__builtin_inff();
-            if (E4M3) {   // codes after the last key may be anything, a NaN among it
-                const int n = here ? rq.kv - j0g : 0;
-#pragma unroll
-                for (int t = 0; t < 4 * NC; ++t) vw[t] = first_bytes(vw[t], n);
-            }
-        }
-        float top = x[0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
-        const float vtop = top > -__builtin_inff() ? sc.y : 0.0f;   // of a group of which the row sees a key
-        top = rows_max(top);
-        if (__any(top > st.m + kSlack || vtop > st.vref)) {
-            const float vnew = rows_max(fmaxf(st.vref, vtop));
-            const float mnew = fmaxf(st.m, top);
-            const float shrink = mnew == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(st.m - mnew);
-            st.l *= shrink;
-            const float k = shrink * (st.vref / vnew);
-#pragma unroll
-            for (int t = 0; t < 4 * NC; ++t) st.acc[t] *= k;
-            st.m = mnew;
-            st.vref = vnew;
-        }
-        const float m0 = st.m == -__builtin_inff() ? 0.0f : st.m;
-        const float vs = fminf(sc.y * (kTop / st.vref), kTop);   // (beyond that only where all weights are 0)
-        half8_t p[2];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float w = __builtin_amdgcn_exp2f(x[i] - m0);
-            st.l += w;
-            p[i >> 3][i & 7] = (_Float16)(w * vs);
-        }
-#pragma unroll
-        for (int t = 0; t < 4 * NC; ++t) {
-            st.acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(vw[t].x, vw[t].y), p[0], st.acc[t], 0, 0, 0);
-            st.acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(vw[t].z, vw[t].w), p[1], st.acc[t], 0, 0, 0);
-        }
+        few_update<E4M3>(a, rq, mine, query, st, s, vw, sc, here, mask, j0g);
         sc = sc_next;
     }
     st.l = rows_sum(st.l);

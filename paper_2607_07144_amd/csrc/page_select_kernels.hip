@@ -539,11 +539,95 @@ __global__ __launch_bounds__(kWideThreads) void page_select_wide_kernel(SelectAr
 
 // ----------------------------------------------------- attention to lists --
 
+// few_keys over a list of pages of a multiple of 64 tokens: a tile lies in one page, so
+// that its place and scales are the same in all lanes; they are looked up in scalar
+// registers, and the loads of codes take their addresses from there and from offsets that
+// stay as they are.  The entries are read two tiles ahead, the pages' ids and scales one.
+template <bool E4M3, int NC>
+__device__ __forceinline__ void whole_tiles(const AttendArgs& a, const Request& rq, int64_t r, int h, const FewRow& fr, int e0, int step,
+                                            int e1, FewSums<NC>& st, const int32_t* list)
+{
+    const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
+    const int d = a.d;
+    const int64_t per_head = (int64_t)a.page * d;
+    Seen mine = seen_of(a, rq, r, fr.tok);   // (rows of one token: alike in all lanes)
+    mine.lo = __builtin_amdgcn_readfirstlane(mine.lo);
+    mine.hi = __builtin_amdgcn_readfirstlane(mine.hi);
+    mine.wlo = __builtin_amdgcn_readfirstlane(mine.wlo);
+    const int32_t* table = a.tables + r * a.max_pages;
+    const uint32_t columns = (uint32_t)pages_of(a, rq.kv);
+    // channels beyond d are loaded from the last ones: q is zero there, and their sums go nowhere
+    uint32_t kc[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) kc[c] = (c16 >> 2) * 16 * d + (c16 & 3) * d + min(c * 64 + g * 16, d - 16);
+    const uint32_t vc = g * 16 * d + c16 * 16;
+    struct Tile {
+        int id, pos, in_page;   // in_page: 16-token groups
+        bool here;
+    };
+    auto column = [&](int e) { return scalar_load(list + list_entry(a, 4 * min(e, e1 - 1))); };
+    auto place = [&](int e, int col) {
+        Tile t;
+        const int at = 4 * min(e, e1 - 1);
+        t.in_page = at - list_entry(a, at) * (int)a.per_page;
+        t.here = (uint32_t)col < columns;
+        col = t.here ? col : 0;
+        t.pos = (col * (int)a.per_page + t.in_page) * 16;
+        t.id = scalar_load(table + col);
+        return t;
+    };
+    auto check = [&](Tile& t) {
+        t.here = t.here && (uint32_t)t.id < (uint64_t)a.n_pages;
+        t.id = t.here ? t.id : 0;
+    };
+    uint4 kw[4][NC];
+    auto load_keys = [&](const Tile& t) {
+        const uint8_t* kp = a.k_codes + ((int64_t)t.id * a.heads + h) * per_head + t.in_page * 16 * d;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) kw[i][c] = *(const uint4*)(kp + i * 4 * d + kc[c]);
+    };
+    auto scales_of = [&](const Tile& t) {
+        const float2 sc = __builtin_bit_cast(float2, scalar_load((const uint64_t*)(a.scales + (int64_t)t.id * a.heads + h)));
+        return t.here ? sc : make_float2(0.0f, 0.0f);
+    };
+    const int c0 = column(e0), c1 = column(e0 + step);
+    int c2 = column(e0 + 2 * step);
+    Tile now = place(e0, c0), next = place(e0 + step, c1);
+    check(now);
+    load_keys(now);
+    float2 sc = scales_of(now);
+    const FewQuery<NC> query(a, rq, fr);
+    for (int e = e0; e < e1; e += step) {
+        uint4 vw[4 * NC];
+        const uint8_t* vp = a.v_codes + ((int64_t)now.id * a.heads + h) * per_head + now.in_page * 16 * d;
+#pragma unroll
+        for (int t = 0; t < 4 * NC; ++t) vw[t] = *(const uint4*)(vp + min(t * 16, d - 16) * 16 + vc);
+        const bool here = now.here;
+        const int j0 = now.pos;
+        const bool mask = !here || j0 < mine.lo || j0 + kTile > mine.hi || (a.window && j0 < mine.wlo && j0 + kTile > a.sinks);
+        float4_t s[4];
+        few_products<E4M3>(kw, query, s);
+        const float2 sc_now = sc;
+        if (e + step < e1) {
+            check(next);
+            load_keys(next);
+            sc = scales_of(next);
+            now = next;
+            next = place(e + 2 * step, c2);
+            c2 = column(e + 3 * step);
+        }
+        few_update<E4M3>(a, rq, mine, query, st, s, vw, sc_now, here, mask, j0 + g * 16);
+    }
+    st.l = rows_sum(st.l);
+}
+
 // W waves an item -- a token, a KV head and up to 16 of its query heads -- that take
 // the list's tiles in turn, with those of the item's other splits; their sums joined
 // in LDS, and the splits' by a second kernel.
-template <bool E4M3, int NC, int W>
-__global__ __launch_bounds__(kThreads, NC <= 2 ? 2 : 1) void attend_listed_kernel(AttendArgs a)
+template <bool E4M3, int NC, int W, bool WHOLE>
+__global__ __launch_bounds__(kThreads, NC == 2 && WHOLE ? 3 : NC <= 2 ? 2 : 1) void attend_listed_kernel(AttendArgs a)
 {
     extern __shared__ __align__(16) float lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -578,7 +662,10 @@ __global__ __launch_bounds__(kThreads, NC <= 2 ? 2 : 1) void attend_listed_kerne
     const FewRow fr = {min(c16, n_rows - 1), i, h * a.group + chunk * kFewRows + min(c16, n_rows - 1)};
     FewSums<NC> st;
     const int e0 = split * W + (W == 1 ? 0 : wave);
-    if (e0 < tiles) few_keys<E4M3, NC, true>(a, rq, r, h, Tiles{}, fr, e0, a.n_splits * W, tiles, st, list, places);
+    if (e0 < tiles) {
+        if constexpr (WHOLE) whole_tiles<E4M3, NC>(a, rq, r, h, fr, e0, a.n_splits * W, tiles, st, list);
+        else few_keys<E4M3, NC, true>(a, rq, r, h, Tiles{}, fr, e0, a.n_splits * W, tiles, st, list, places);
+    }
 
     if (W == 1) {
         if (c16 >= n_rows) return;
@@ -841,9 +928,14 @@ extern "C" int fkv_page_attend_selected(const fkv_page_desc* desc, const fkv_att
         auto go = [&](auto kern, size_t shm) {
             hipLaunchKernelGGL(kern, dim3((unsigned)(s.blocks * s.n_splits)), dim3(kThreads), shm, st, a);
         };
-        if (s.waves == 1) return e4m3 ? go(attend_listed_kernel<true, NC, 1>, 0) : go(attend_listed_kernel<false, NC, 1>, 0);
-        const size_t shm = (2 * kWaves * kFewRows + (size_t)kWaves * kFewRows * (a.d + 4)) * sizeof(float);
-        e4m3 ? go(attend_listed_kernel<true, NC, kWaves>, shm) : go(attend_listed_kernel<false, NC, kWaves>, shm);
+        const size_t shm = s.waves == 1 ? 0 : (2 * kWaves * kFewRows + (size_t)kWaves * kFewRows * (a.d + 4)) * sizeof(float);
+        auto of_pages = [&](auto whole) {
+            constexpr bool WHOLE = decltype(whole)::value;
+            if (s.waves == 1) return e4m3 ? go(attend_listed_kernel<true, NC, 1, WHOLE>, shm) : go(attend_listed_kernel<false, NC, 1, WHOLE>, shm);
+            e4m3 ? go(attend_listed_kernel<true, NC, kWaves, WHOLE>, shm) : go(attend_listed_kernel<false, NC, kWaves, WHOLE>, shm);
+        };
+        if (a.page % kTile == 0) of_pages(std::true_type{});
+        else of_pages(std::false_type{});
     };
     if (a.d <= 64) of_width(std::integral_constant<int, 1>{});
     else if (a.d <= 128) of_width(std::integral_constant<int, 2>{});
