@@ -169,31 +169,6 @@ __device__ __forceinline__ void check_place(const AttendArgs& a, Place& p)
     p.id = p.here ? p.id : 0;
 }
 
-// Likewise the 16-key group at place `at` of a list of pages, whose entry there is
-// known: `pos` is its first key.  Pages of entries that are no column of the request's
-// are not there.
-struct ListPlace : Place {
-    int pos;
-};
-
-__device__ __forceinline__ int list_entry(const AttendArgs& a, int at)   // the list's entry that holds place `at`
-{
-    return a.per_page_inv ? (int)__umulhi((uint32_t)at, a.per_page_inv) : at;
-}
-
-__device__ __forceinline__ ListPlace place_listed(const AttendArgs& a, const int32_t* table, int kv, int places, int at, int column)
-{
-    ListPlace p;
-    p.in_page = at - list_entry(a, at) * (int)a.per_page;
-    const int last = (kv - 1) >> 4;   // kv >= 1
-    const int columns = (int)((a.per_page_inv ? __umulhi((uint32_t)last, a.per_page_inv) : (uint32_t)last) + 1);
-    p.here = at < places && (uint32_t)column < (uint32_t)columns;
-    column = p.here ? column : 0;
-    p.pos = (column * (int)a.per_page + p.in_page) * 16;
-    p.id = table[column];
-    return p;
-}
-
 // 16 codes to binary16, exact.  An int8 code c becomes 1024 + (c + 128) by
 // placing the byte under the exponent of 1024, and 1152 less is c.
 template <bool E4M3>
@@ -472,15 +447,11 @@ __device__ __forceinline__ void few_update(const AttendArgs& a, const Request& r
     }
 }
 
-// A wave over tiles e0, e0 + step, .. below e1 (one at least).  LISTED: tiles of four
-// groups of the pages in `list`, `places` groups in all, and rows of one token; else
-// tiles of the request's keys.  A list's entries are read two tiles ahead, its pages'
-// ids one.
-template <bool E4M3, int NC, bool LISTED = false>
+// A wave over tiles e0, e0 + step, .. below e1 (one at least).
+template <bool E4M3, int NC>
 __device__ __forceinline__ void few_keys(const AttendArgs& a, const Request& rq, int64_t r, int h, const Tiles& tl, const FewRow& fr,
-                                         int e0, int step, int e1, FewSums<NC>& st, const int32_t* list = nullptr, int places = 0)
+                                         int e0, int step, int e1, FewSums<NC>& st)
 {
-    typedef std::conditional_t<LISTED, ListPlace, Place> At;
     const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
     const int d = a.d;
     const int64_t per_head = (int64_t)a.page * d;
@@ -504,22 +475,10 @@ __device__ __forceinline__ void few_keys(const AttendArgs& a, const Request& rq,
 #pragma unroll
             for (int c = 0; c < NC; ++c) kw[t][c] = *(const uint4*)(kp + kc[c] + t * 4 * d);
     };
-    int j0 = 0, j1 = 0;        // first keys of a tile and the next
-    int ck2 = 0, cv2 = 0;      // (LISTED) the entries of the one after that
-    At pk, pv, pk1, pv1;
-    if constexpr (LISTED) {
-        auto entry = [&](int e, int k) { return list[list_entry(a, min(4 * min(e, e1 - 1) + k, places - 1))]; };
-        const int ck0 = entry(e0, gk), cv0 = entry(e0, g), ck1 = entry(e0 + step, gk), cv1 = entry(e0 + step, g);
-        ck2 = entry(e0 + 2 * step, gk), cv2 = entry(e0 + 2 * step, g);
-        pk = place_listed(a, table, rq.kv, places, 4 * e0 + gk, ck0), pv = place_listed(a, table, rq.kv, places, 4 * e0 + g, cv0);
-        const int e = min(e0 + step, e1 - 1);
-        pk1 = place_listed(a, table, rq.kv, places, 4 * e + gk, ck1), pv1 = place_listed(a, table, rq.kv, places, 4 * e + g, cv1);
-    } else {
-        j0 = tl.tile(e0) * kTile;
-        pk = place_of(a, table, rq.kv, (j0 >> 4) + gk), pv = place_of(a, table, rq.kv, (j0 >> 4) + g);
-        j1 = tl.tile(min(e0 + step, e1 - 1)) * kTile;
-        pk1 = place_of(a, table, rq.kv, (j1 >> 4) + gk), pv1 = place_of(a, table, rq.kv, (j1 >> 4) + g);
-    }
+    int j0 = tl.tile(e0) * kTile;
+    Place pk = place_of(a, table, rq.kv, (j0 >> 4) + gk), pv = place_of(a, table, rq.kv, (j0 >> 4) + g);
+    int j1 = tl.tile(min(e0 + step, e1 - 1)) * kTile;
+    Place pk1 = place_of(a, table, rq.kv, (j1 >> 4) + gk), pv1 = place_of(a, table, rq.kv, (j1 >> 4) + g);
     check_place(a, pk);
     check_place(a, pv);
     load_keys(pk);
@@ -534,15 +493,8 @@ __device__ __forceinline__ void few_keys(const AttendArgs& a, const Request& rq,
 #pragma unroll
         for (int t = 0; t < 4 * NC; ++t) vw[t] = *(const uint4*)(vp + min(t * 16, d - 16) * 16);
         const bool here = pv.here;
-        bool mask;
-        int j0g;
-        if constexpr (LISTED) {
-            j0g = pv.pos;
-            mask = __any(!here || j0g < mine.lo || j0g + 16 > mine.hi || (a.window && j0g < mine.wlo && j0g + 16 > a.sinks));
-        } else {
-            j0g = j0 + g * 16;
-            mask = !tile_whole(a, tl, j0) || __any(!here);
-        }
+        const bool mask = !tile_whole(a, tl, j0) || __any(!here);
+        const int j0g = j0 + g * 16;
         if (!here) sc = make_float2(0.0f, 0.0f);
         float4_t s[4];
         few_products<E4M3>(kw, query, s);
@@ -552,19 +504,10 @@ __device__ __forceinline__ void few_keys(const AttendArgs& a, const Request& rq,
             check_place(a, pv1);
             load_keys(pk1);
             sc_next = scale_head[(int64_t)pv1.id * a.heads];
-            pv = pv1;
-            if constexpr (LISTED) {
-                const int n = min(e + 2 * step, e1 - 1), n1 = min(e + 3 * step, e1 - 1);
-                pk1 = place_listed(a, table, rq.kv, places, 4 * n + gk, ck2);
-                pv1 = place_listed(a, table, rq.kv, places, 4 * n + g, cv2);
-                ck2 = list[list_entry(a, min(4 * n1 + gk, places - 1))];
-                cv2 = list[list_entry(a, min(4 * n1 + g, places - 1))];
-            } else {
-                j0 = j1;
-                j1 = tl.tile(min(e + 2 * step, e1 - 1)) * kTile;
-                pk1 = place_of(a, table, rq.kv, (j1 >> 4) + gk);
-                pv1 = place_of(a, table, rq.kv, (j1 >> 4) + g);
-            }
+            j0 = j1, pv = pv1;
+            j1 = tl.tile(min(e + 2 * step, e1 - 1)) * kTile;
+            pk1 = place_of(a, table, rq.kv, (j1 >> 4) + gk);
+            pv1 = place_of(a, table, rq.kv, (j1 >> 4) + g);
         }
         few_update<E4M3>(a, rq, mine, query, st, s, vw, sc, here, mask, j0g);
         sc = sc_next;

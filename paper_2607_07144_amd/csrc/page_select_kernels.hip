@@ -539,11 +539,200 @@ __global__ __launch_bounds__(kWideThreads) void page_select_wide_kernel(SelectAr
 
 // ----------------------------------------------------- attention to lists --
 
-// few_keys over a list of pages of a multiple of 64 tokens: a tile lies in one page, so
+// A tile is four groups of 16 keys of the listed pages; its order of work is that of
+// few_keys.  Lists of pages that many tokens share come from the caches, and what bounds
+// them is the vector unit: so a weight with its value scale is one power of two,
+// 2^(s c - m + log2 v), as in the kernel for many rows: v = vs 2^8 / vr is held at 2^-40 from
+// below, and a sum over v is what l wants.
+template <int NC>
+struct ListedQuery : FewQuery<NC> {
+    __device__ __forceinline__ ListedQuery(const AttendArgs& a, const Request& rq, const FewRow& fr) : FewQuery<NC>(a, rq, fr)
+    {
+        // a negative scale's sign goes into the row, so that the factor of a score is not negative
+        const uint32_t sign = a.scale < 0.0f ? 0x80008000u : 0u;
+        this->mul = fabsf(this->mul);
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                uint4 u = __builtin_bit_cast(uint4, this->qf[c][k]);
+                u.x ^= sign, u.y ^= sign, u.z ^= sign, u.w ^= sign;
+                this->qf[c][k] = __builtin_bit_cast(half8_t, u);
+            }
+    }
+};
+
+// PLAIN: neither cap nor bias.
+template <bool E4M3, int NC, bool PLAIN>
+__device__ __forceinline__ void listed_update(const AttendArgs& a, const Request& rq, const Seen& mine, const ListedQuery<NC>& q,
+                                              FewSums<NC>& st, float4_t (&s)[4], uint4 (&vw)[4 * NC], float2 sc, bool here, bool mask, int j0g)
+{
+    float c = fmaxf(q.mul * sc.x, 0x1p-120f);   // a score's factor (never 0: hidden scores are infinite)
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = s[i >> 2][i & 3];
+    if (!PLAIN && (q.cap > 0.0f || q.slopes)) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] *= c;
+        if (q.large_cap) {
+            const float inv = 1.0f / q.cap2;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = capped_large(x[i], q.cap2, inv);
+        } else if (q.cap > 0.0f) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = capped(x[i], q.cap2);
+        }
+        if (q.slopes) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] -= q.slope2 * fabsf((float)(j0g + i - q.pos));
+        }
+        c = 1.0f;
+    }
+    if (mask) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (!here || !visible(a, mine, j0g + i)) x[i] = -__builtin_inff();
+        if (E4M3) {   // codes after the last key may be anything, a NaN among it
+            const int n = here ? rq.kv - j0g : 0;
+#pragma unroll
+            for (int t = 0; t < 4 * NC; ++t) vw[t] = first_bytes(vw[t], n);
+        }
+    }
+    float top = x[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = __builtin_elementwise_maximum(top, x[i]);
+    const float vtop = top > -__builtin_inff() ? sc.y : 0.0f;   // of a group of which the row sees a key
+    top = rows_max(top * c);
+    if (__any(top > st.m + kSlack || vtop > st.vref)) {
+        const float vnew = rows_max(fmaxf(st.vref, vtop));
+        const float mnew = fmaxf(st.m, top);
+        const float shrink = mnew == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(st.m - mnew);
+        st.l *= shrink;
+        const float k = shrink * (st.vref / vnew);
+#pragma unroll
+        for (int t = 0; t < 4 * NC; ++t) st.acc[t] *= k;
+        st.m = mnew;
+        st.vref = vnew;
+    }
+    const float m0 = st.m == -__builtin_inff() ? 0.0f : st.m;
+    const float v = __builtin_amdgcn_fmed3f(sc.y * (kTop * __builtin_amdgcn_rcpf(st.vref)), 0x1p-40f, kTop);   // (more only where all weights are 0)
+    const float vb = __builtin_amdgcn_logf(v) - m0;
+    half8_t p[2];
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, vb));
+        sum += w;
+        p[i >> 3][i & 7] = (_Float16)w;
+    }
+    st.l = __builtin_fmaf(sum, __builtin_amdgcn_rcpf(v), st.l);
+#pragma unroll
+    for (int t = 0; t < 4 * NC; ++t) {
+        st.acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(vw[t].x, vw[t].y), p[0], st.acc[t], 0, 0, 0);
+        st.acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(vw[t].z, vw[t].w), p[1], st.acc[t], 0, 0, 0);
+    }
+}
+
+// Where the 16-key group at place `at` of a list of pages lies, whose entry there is
+// known: `pos` is its first key.  Pages of entries that are no column of the request's
+// are not there.
+struct ListPlace : Place {
+    int pos;
+};
+
+__device__ __forceinline__ int list_entry(const AttendArgs& a, int at)   // the list's entry that holds place `at`
+{
+    return a.per_page_inv ? (int)__umulhi((uint32_t)at, a.per_page_inv) : at;
+}
+
+__device__ __forceinline__ ListPlace place_listed(const AttendArgs& a, const int32_t* table, int kv, int places, int at, int column)
+{
+    ListPlace p;
+    p.in_page = at - list_entry(a, at) * (int)a.per_page;
+    const int last = (kv - 1) >> 4;   // kv >= 1
+    const int columns = (int)((a.per_page_inv ? __umulhi((uint32_t)last, a.per_page_inv) : (uint32_t)last) + 1);
+    p.here = at < places && (uint32_t)column < (uint32_t)columns;
+    column = p.here ? column : 0;
+    p.pos = (column * (int)a.per_page + p.in_page) * 16;
+    p.id = table[column];
+    return p;
+}
+
+// A wave over the tiles e0, e0 + step, .. below e1 (one at least) of a list of `places`
+// groups, for rows of one token.  Any pages: a lane group looks up its own group's.  The
+// entries are read two tiles ahead, the pages' ids one.
+template <bool E4M3, int NC, bool PLAIN>
+__device__ __forceinline__ void listed_groups(const AttendArgs& a, const Request& rq, int64_t r, int h, const FewRow& fr, int e0, int step,
+                                              int e1, FewSums<NC>& st, const int32_t* list, int places)
+{
+    const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
+    const int d = a.d;
+    const int64_t per_head = (int64_t)a.page * d;
+    const Seen mine = seen_of(a, rq, r, fr.tok);
+    const int32_t* table = a.tables + r * a.max_pages;
+    const int gk = c16 >> 2;   // the key group of this lane's left-operand rows
+    // channels beyond d are loaded from the last ones: q is zero there, and their sums go nowhere
+    int kc[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) kc[c] = (c16 & 3) * d + min(c * 64 + g * 16, d - 16);
+    const uint8_t* k_head = a.k_codes + h * per_head;
+    const uint8_t* v_head = a.v_codes + h * per_head + c16 * 16;
+    const int64_t per_id = a.heads * per_head;
+    const float2* scale_head = a.scales + h;
+    uint4 kw[4][NC];
+    auto load_keys = [&](const Place& p) {
+        const uint8_t* kp = k_head + p.id * per_id + p.in_page * 16 * d;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) kw[t][c] = *(const uint4*)(kp + kc[c] + t * 4 * d);
+    };
+    auto entry = [&](int e, int k) { return list[list_entry(a, min(4 * min(e, e1 - 1) + k, places - 1))]; };
+    auto place = [&](int e, int k, int column) { return place_listed(a, table, rq.kv, places, 4 * min(e, e1 - 1) + k, column); };
+    const int ck0 = entry(e0, gk), cv0 = entry(e0, g), ck1 = entry(e0 + step, gk), cv1 = entry(e0 + step, g);
+    int ck2 = entry(e0 + 2 * step, gk), cv2 = entry(e0 + 2 * step, g);
+    ListPlace pk = place(e0, gk, ck0), pv = place(e0, g, cv0);
+    ListPlace pk1 = place(e0 + step, gk, ck1), pv1 = place(e0 + step, g, cv1);
+    check_place(a, pk);
+    check_place(a, pv);
+    load_keys(pk);
+    float2 sc = scale_head[(int64_t)pv.id * a.heads], sc_next = sc;
+    const ListedQuery<NC> query(a, rq, fr);
+    for (int e = e0; e < e1; e += step) {
+        // the tile's values, on their way while its scores are formed
+        uint4 vw[4 * NC];
+        const uint8_t* vp = v_head + pv.id * per_id + pv.in_page * 16 * d;
+#pragma unroll
+        for (int t = 0; t < 4 * NC; ++t) vw[t] = *(const uint4*)(vp + min(t * 16, d - 16) * 16);
+        const bool here = pv.here;
+        const int j0g = pv.pos;
+        const bool mask = __any(!here || j0g < mine.lo || j0g + 16 > mine.hi || (a.window && j0g < mine.wlo && j0g + 16 > a.sinks));
+        if (!here) sc = make_float2(0.0f, 0.0f);
+        float4_t s[4];
+        few_products<E4M3, NC>(kw, query, s);
+        // the next tile's keys, and the pages and entries of those after
+        if (e + step < e1) {
+            check_place(a, pk1);
+            check_place(a, pv1);
+            load_keys(pk1);
+            sc_next = scale_head[(int64_t)pv1.id * a.heads];
+            pv = pv1;
+            pk1 = place(e + 2 * step, gk, ck2);
+            pv1 = place(e + 2 * step, g, cv2);
+            ck2 = entry(e + 3 * step, gk);
+            cv2 = entry(e + 3 * step, g);
+        }
+        listed_update<E4M3, NC, PLAIN>(a, rq, mine, query, st, s, vw, sc, here, mask, j0g);
+        sc = sc_next;
+    }
+    st.l = rows_sum(st.l);
+}
+
+// The same of pages of a multiple of 64 tokens: a tile lies in one page, so
 // that its place and scales are the same in all lanes; they are looked up in scalar
 // registers, and the loads of codes take their addresses from there and from offsets that
 // stay as they are.  The entries are read two tiles ahead, the pages' ids and scales one.
-template <bool E4M3, int NC>
+template <bool E4M3, int NC, bool PLAIN>
 __device__ __forceinline__ void whole_tiles(const AttendArgs& a, const Request& rq, int64_t r, int h, const FewRow& fr, int e0, int step,
                                             int e1, FewSums<NC>& st, const int32_t* list)
 {
@@ -561,6 +750,12 @@ __device__ __forceinline__ void whole_tiles(const AttendArgs& a, const Request& 
 #pragma unroll
     for (int c = 0; c < NC; ++c) kc[c] = (c16 >> 2) * 16 * d + (c16 & 3) * d + min(c * 64 + g * 16, d - 16);
     const uint32_t vc = g * 16 * d + c16 * 16;
+    // (an offset of 32 bits beside an address in scalar registers, as loads take them; widened outside of the loop, each
+    // load would have an address of its own in vector registers)
+    auto here_of = [](uint32_t offset) {
+        asm("" : "+v"(offset));
+        return offset;
+    };
     struct Tile {
         int id, pos, in_page;   // in_page: 16-token groups
         bool here;
@@ -586,7 +781,7 @@ __device__ __forceinline__ void whole_tiles(const AttendArgs& a, const Request& 
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int c = 0; c < NC; ++c) kw[i][c] = *(const uint4*)(kp + i * 4 * d + kc[c]);
+            for (int c = 0; c < NC; ++c) kw[i][c] = *(const uint4*)(kp + i * 4 * d + here_of(kc[c]));
     };
     auto scales_of = [&](const Tile& t) {
         const float2 sc = __builtin_bit_cast(float2, scalar_load((const uint64_t*)(a.scales + (int64_t)t.id * a.heads + h)));
@@ -598,17 +793,17 @@ __device__ __forceinline__ void whole_tiles(const AttendArgs& a, const Request& 
     check(now);
     load_keys(now);
     float2 sc = scales_of(now);
-    const FewQuery<NC> query(a, rq, fr);
+    const ListedQuery<NC> query(a, rq, fr);
     for (int e = e0; e < e1; e += step) {
         uint4 vw[4 * NC];
         const uint8_t* vp = a.v_codes + ((int64_t)now.id * a.heads + h) * per_head + now.in_page * 16 * d;
 #pragma unroll
-        for (int t = 0; t < 4 * NC; ++t) vw[t] = *(const uint4*)(vp + min(t * 16, d - 16) * 16 + vc);
+        for (int t = 0; t < 4 * NC; ++t) vw[t] = *(const uint4*)(vp + min(t * 16, d - 16) * 16 + here_of(vc));
         const bool here = now.here;
         const int j0 = now.pos;
         const bool mask = !here || j0 < mine.lo || j0 + kTile > mine.hi || (a.window && j0 < mine.wlo && j0 + kTile > a.sinks);
         float4_t s[4];
-        few_products<E4M3>(kw, query, s);
+        few_products<E4M3, NC>(kw, query, s);
         const float2 sc_now = sc;
         if (e + step < e1) {
             check(next);
@@ -618,7 +813,7 @@ __device__ __forceinline__ void whole_tiles(const AttendArgs& a, const Request& 
             next = place(e + 2 * step, c2);
             c2 = column(e + 3 * step);
         }
-        few_update<E4M3>(a, rq, mine, query, st, s, vw, sc_now, here, mask, j0 + g * 16);
+        listed_update<E4M3, NC, PLAIN>(a, rq, mine, query, st, s, vw, sc_now, here, mask, j0 + g * 16);
     }
     st.l = rows_sum(st.l);
 }
@@ -626,7 +821,7 @@ __device__ __forceinline__ void whole_tiles(const AttendArgs& a, const Request& 
 // W waves an item -- a token, a KV head and up to 16 of its query heads -- that take
 // the list's tiles in turn, with those of the item's other splits; their sums joined
 // in LDS, and the splits' by a second kernel.
-template <bool E4M3, int NC, int W, bool WHOLE>
+template <bool E4M3, int NC, int W, bool WHOLE, bool PLAIN>
 __global__ __launch_bounds__(kThreads, NC == 2 && WHOLE ? 3 : NC <= 2 ? 2 : 1) void attend_listed_kernel(AttendArgs a)
 {
     extern __shared__ __align__(16) float lds[];
@@ -663,8 +858,8 @@ __global__ __launch_bounds__(kThreads, NC == 2 && WHOLE ? 3 : NC <= 2 ? 2 : 1) v
     FewSums<NC> st;
     const int e0 = split * W + (W == 1 ? 0 : wave);
     if (e0 < tiles) {
-        if constexpr (WHOLE) whole_tiles<E4M3, NC>(a, rq, r, h, fr, e0, a.n_splits * W, tiles, st, list);
-        else few_keys<E4M3, NC, true>(a, rq, r, h, Tiles{}, fr, e0, a.n_splits * W, tiles, st, list, places);
+        if constexpr (WHOLE) whole_tiles<E4M3, NC, PLAIN>(a, rq, r, h, fr, e0, a.n_splits * W, tiles, st, list);
+        else listed_groups<E4M3, NC, PLAIN>(a, rq, r, h, fr, e0, a.n_splits * W, tiles, st, list, places);
     }
 
     if (W == 1) {
@@ -929,13 +1124,14 @@ extern "C" int fkv_page_attend_selected(const fkv_page_desc* desc, const fkv_att
             hipLaunchKernelGGL(kern, dim3((unsigned)(s.blocks * s.n_splits)), dim3(kThreads), shm, st, a);
         };
         const size_t shm = s.waves == 1 ? 0 : (2 * kWaves * kFewRows + (size_t)kWaves * kFewRows * (a.d + 4)) * sizeof(float);
-        auto of_pages = [&](auto whole) {
-            constexpr bool WHOLE = decltype(whole)::value;
-            if (s.waves == 1) return e4m3 ? go(attend_listed_kernel<true, NC, 1, WHOLE>, shm) : go(attend_listed_kernel<false, NC, 1, WHOLE>, shm);
-            e4m3 ? go(attend_listed_kernel<true, NC, kWaves, WHOLE>, shm) : go(attend_listed_kernel<false, NC, kWaves, WHOLE>, shm);
+        auto of_form = [&](auto whole, auto plain) {
+            constexpr bool WHOLE = decltype(whole)::value, PLAIN = decltype(plain)::value;
+            if (s.waves == 1) return e4m3 ? go(attend_listed_kernel<true, NC, 1, WHOLE, PLAIN>, shm) : go(attend_listed_kernel<false, NC, 1, WHOLE, PLAIN>, shm);
+            e4m3 ? go(attend_listed_kernel<true, NC, kWaves, WHOLE, PLAIN>, shm) : go(attend_listed_kernel<false, NC, kWaves, WHOLE, PLAIN>, shm);
         };
-        if (a.page % kTile == 0) of_pages(std::true_type{});
-        else of_pages(std::false_type{});
+        const bool plain = a.softcap == 0.0f && !a.slopes;
+        if (a.page % kTile == 0) plain ? of_form(std::true_type{}, std::true_type{}) : of_form(std::true_type{}, std::false_type{});
+        else plain ? of_form(std::false_type{}, std::true_type{}) : of_form(std::false_type{}, std::false_type{});
     };
     if (a.d <= 64) of_width(std::integral_constant<int, 1>{});
     else if (a.d <= 128) of_width(std::integral_constant<int, 2>{});
