@@ -165,38 +165,21 @@ __device__ __forceinline__ void round_row(const SelectArgs& a, const uint8_t* qp
     }
 }
 
-// A block: R tiles of 16 rows of one KV head of a request, a wave of it a quarter of the
-// block's tiles of 16 pages.  The left operand takes a page's box as one of its rows,
-// so that lane 16g + c ends up with row c's sums of pages 4g .. 4g+3.  Of KV heads of
-// more than 16 rows (WIDE) a block has one token, and R tiles of its rows at a time.
-template <bool E4M3, int NC, int R, bool WIDE>
-__global__ __launch_bounds__(kThreads, R == 1 || NC == 1 ? 4 : NC == 2 ? 3 : 2) void page_score_kernel(SelectArgs a)
+// The WAVES waves of a block form the scores of R tiles of 16 rows of one KV head of a
+// request, from token tok0 on, this wave of n_tiles tiles of 16 pages: `first`, first +
+// step, ..  The left operand takes a page's box as one of its rows, so that lane 16g + c
+// ends up with row c's sums of pages 4g .. 4g+3.  Of KV heads of more than 16 rows (WIDE) a
+// block has one token, and R tiles of its rows at a time.  put(token, page, scores, c0) gets
+// four pages' scores; c0: the heads are not the first ones.
+template <bool E4M3, int NC, int R, bool WIDE, int WAVES, typename Put>
+__device__ __forceinline__ void score_block(const SelectArgs& a, const Request& rq, int64_t r, int h, int tok0, int most_seen, int first,
+                                            int step, int n_tiles, RowsLds<NC, R>& sh, Put put)
 {
     typedef RowsLds<NC, R> Lds;
-    __shared__ __align__(16) Lds sh;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c16 = lane & 15, g = lane >> 4;
-    uint32_t b = blockIdx.x;
-    const int h = (int)(b % (uint32_t)a.heads);
-    b /= (uint32_t)a.heads;
-    const int chunk = (int)(b % (uint32_t)a.tile_chunks);
-    b /= (uint32_t)a.tile_chunks;
-    const int64_t r = b / (uint32_t)a.row_groups;
-    const int rg = (int)(b - (uint32_t)r * (uint32_t)a.row_groups);
-    const Request rq = request_of(a, r);
     const int chunks = WIDE ? (a.group + 15) >> 4 : 1;   // of a token's heads, 16 a tile
-    const int per_tile = 16 >> a.lanes_log;              // tokens of a tile,
-    const int tokens = WIDE ? 1 : R * per_tile;          // and of the block
-    const int tok0 = rg * tokens;
-    if (tok0 >= rq.rows) return;
-    const int most_seen = pages_seen(a, rq, min(tok0 + tokens, rq.rows) - 1);   // (later tokens see no fewer)
-    if (most_seen <= a.n_select) return;   // every page of theirs is selected
-    const int tiles = (most_seen + 15) >> 4;
-    const int first_of_block = chunk * a.wave_tiles * kWaves;
-    if (first_of_block >= tiles) return;
-    const int first = first_of_block + wave * a.wave_tiles;
-    const int n_tiles = max(min(a.wave_tiles, tiles - first), 0);
-
+    const int per_tile = 16 >> a.lanes_log;              // tokens of a tile
     const int32_t* table = a.tables + r * a.max_pages;
     int kc[NC];   // channels beyond d are taken from the last ones: q is zero there
 #pragma unroll
@@ -205,7 +188,7 @@ __global__ __launch_bounds__(kThreads, R == 1 || NC == 1 ? 4 : NC == 2 ? 3 : 2) 
         uint4 lo[NC], hi[NC];
         float scale;   // of page c16; a NaN where there is none
     };
-    auto id_of = [&](int k) { return table[min((first + k) * 16 + c16, most_seen - 1)]; };
+    auto id_of = [&](int k) { return table[min((first + k * step) * 16 + c16, most_seen - 1)]; };
     auto load = [&](int id) {
         Pages p;
         const bool here = (uint32_t)id < (uint64_t)a.n_pages;
@@ -218,12 +201,13 @@ __global__ __launch_bounds__(kThreads, R == 1 || NC == 1 ? 4 : NC == 2 ? 3 : 2) 
     };
     const int lanes = 1 << a.lanes_log;
     for (int c0 = 0; c0 < chunks; c0 += R) {
-        const int row_tiles = WIDE ? min(R, chunks - c0) : R;
+        // (tiles of no token are left out)
+        const int row_tiles = WIDE ? min(R, chunks - c0) : min(R, (rq.rows - tok0 + per_tile - 1) / per_tile);
         int id1 = id_of(min(1, max(n_tiles - 1, 0)));
         Pages next = load(id_of(0));   // (of a wave without a tile: the last page, for nothing)
         if (c0) __syncthreads();
-        // rows 4 (wave + 4k) + g of the block's tiles
-        for (int k = wave * 4; k < row_tiles * 16; k += kWaves * 4) {
+        // rows 4 (wave + WAVES k) + g of the block's tiles
+        for (int k = wave * 4; k < row_tiles * 16; k += WAVES * 4) {
             const int row = k + g, t = row >> 4, in_tile = row & 15;
             const int tok = min(WIDE ? tok0 : tok0 + t * per_tile + (in_tile >> a.lanes_log), rq.rows - 1);
             const int in_group = min(WIDE ? (c0 + t) * 16 + in_tile : in_tile & (lanes - 1), a.group - 1);
@@ -232,6 +216,7 @@ __global__ __launch_bounds__(kThreads, R == 1 || NC == 1 ? 4 : NC == 2 ? 3 : 2) 
         }
         __syncthreads();
         for (int k = 0; k < n_tiles; ++k) {
+            if (WAVES > kWaves) asm volatile("" ::: "memory");   // (the rows' operands stay in LDS: a block of many waves has no registers for them)
             const Pages now = next;
             if (k + 1 < n_tiles) {
                 next = load(id1);
@@ -246,7 +231,7 @@ __global__ __launch_bounds__(kThreads, R == 1 || NC == 1 ? 4 : NC == 2 ? 3 : 2) 
             int x[4];
 #pragma unroll
             for (int t = 0; t < R; ++t) {
-                if (WIDE && t >= row_tiles) break;
+                if (t && t >= row_tiles) break;
                 const uint8_t* rows = sh.part + (t * 16 + c16) * Lds::kRow + g * 16;
                 int4_t sum = {0, 0, 0, 0};
 #pragma unroll
@@ -263,18 +248,46 @@ __global__ __launch_bounds__(kThreads, R == 1 || NC == 1 ? 4 : NC == 2 ? 3 : 2) 
                 if (WIDE && t + 1 < row_tiles) continue;
                 lanes_max(x, a.lanes_log);
                 const int tok = WIDE ? tok0 : tok0 + t * per_tile + (c16 >> a.lanes_log);
-                if ((c16 & (lanes - 1)) == 0 && tok < rq.rows) {
-                    int4_t* to = (int4_t*)(a.scores + ((rq.start + tok) * (int64_t)a.heads + h) * a.score_stride + (first + k) * 16 + g * 4);
-                    if (WIDE && c0) {   // with the heads before
-                        const int4_t before = *to;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) x[i] = max(x[i], before[i]);
-                    }
-                    *to = int4_t{x[0], x[1], x[2], x[3]};
-                }
+                if ((c16 & (lanes - 1)) == 0 && tok < rq.rows) put(tok, (first + k * step) * 16 + g * 4, int4_t{x[0], x[1], x[2], x[3]}, WIDE && c0);
             }
         }
     }
+}
+
+// Many rows or many pages: the scores go to the workspace.  A block R row tiles, a wave of it
+// a quarter of the block's page tiles.
+template <bool E4M3, int NC, int R, bool WIDE>
+__global__ __launch_bounds__(kThreads, R == 1 || NC == 1 ? 4 : NC == 2 ? 3 : 2) void page_score_kernel(SelectArgs a)
+{
+    __shared__ __align__(16) RowsLds<NC, R> sh;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    uint32_t b = blockIdx.x;
+    const int h = (int)(b % (uint32_t)a.heads);
+    b /= (uint32_t)a.heads;
+    const int chunk = (int)(b % (uint32_t)a.tile_chunks);
+    b /= (uint32_t)a.tile_chunks;
+    const int64_t r = b / (uint32_t)a.row_groups;
+    const int rg = (int)(b - (uint32_t)r * (uint32_t)a.row_groups);
+    const Request rq = request_of(a, r);
+    const int tokens = WIDE ? 1 : R * (16 >> a.lanes_log);   // of the block
+    const int tok0 = rg * tokens;
+    if (tok0 >= rq.rows) return;
+    const int most_seen = pages_seen(a, rq, min(tok0 + tokens, rq.rows) - 1);   // (later tokens see no fewer)
+    if (most_seen <= a.n_select) return;   // every page of theirs is selected
+    const int tiles = (most_seen + 15) >> 4;
+    const int first_of_block = chunk * a.wave_tiles * kWaves;
+    if (first_of_block >= tiles) return;
+    const int first = first_of_block + wave * a.wave_tiles;
+    score_block<E4M3, NC, R, WIDE, kWaves>(a, rq, r, h, tok0, most_seen, first, 1, max(min(a.wave_tiles, tiles - first), 0), sh,
+                                           [&](int tok, int page, int4_t x, bool again) {
+        int4_t* to = (int4_t*)(a.scores + ((rq.start + tok) * (int64_t)a.heads + h) * a.score_stride + page);
+        if (again) {   // with the heads before
+            const int4_t before = *to;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = max(x[i], before[i]);
+        }
+        *to = x;
+    });
 }
 
 // ------------------------------------------------------------- selection --
@@ -308,31 +321,31 @@ __device__ __forceinline__ SelectRow select_row(const SelectArgs& a, uint32_t it
     return s;
 }
 
-// W waves a row, its scores in registers: page 64 (N wave + n) + lane in key[n].  The
-// smallest score selected is found bit by bit from the first that the scores differ in;
-// each step counts those above by ballots, and the search ends when the count fits.
+// The W waves of a row write its list, its scores in registers: page 64 (N wave + n) +
+// lane in key[n].  The smallest score selected is found bit by bit from the first that the
+// scores differ in; each step counts those above by ballots, and the search ends when the
+// count fits.
+template <int W>
+struct PickLds {
+    uint32_t top[W], low[W];
+    int count[2][W], same[W];
+};
+
 template <int N, int W>
-__global__ __launch_bounds__(W > kWaves ? 64 * W : kThreads) void page_select_kernel(SelectArgs a)
+__device__ __forceinline__ void pick_pages(const SelectArgs& a, int seen, const int32_t* scores, int32_t* out, int wave, PickLds<W>& sh)
 {
-    __shared__ uint32_t s_top[W], s_low[W];
-    __shared__ int s_count[2][W], s_same[W];
-    const int lane = threadIdx.x & 63, wave_of_block = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wave = W == 1 ? 0 : wave_of_block, thread = W == 1 ? lane : (int)threadIdx.x;
-    const SelectRow row = select_row(a, W == 1 ? blockIdx.x * kWaves + wave_of_block : blockIdx.x);
-    if (!row.any) return;
-    int32_t* out = a.selected + row.at * a.n_select;
-    if (row.seen <= a.n_select) {
-        for (int j = thread; j < a.n_select; j += 64 * W) out[j] = j < row.seen ? j : -1;
+    const int lane = threadIdx.x & 63, thread = wave * 64 + lane;
+    if (seen <= a.n_select) {
+        for (int j = thread; j < a.n_select; j += 64 * W) out[j] = j < seen ? j : -1;
         return;
     }
     // (more pages than are selected: those always kept are apart from each other)
-    const int from = a.keep_first, to = row.seen - a.keep_last, want = a.n_select - a.keep_first - a.keep_last;
-    const int32_t* scores = a.scores + row.at * a.score_stride;
+    const int from = a.keep_first, to = seen - a.keep_last, want = a.n_select - a.keep_first - a.keep_last;
     const int page0 = wave * N * 64 + lane;
     uint32_t key[N];
     int score[N];
 #pragma unroll
-    for (int n = 0; n < N; ++n) score[n] = scores[min(page0 + 64 * n, row.seen - 1)];   // (without a condition: all on their way at once)
+    for (int n = 0; n < N; ++n) score[n] = scores[min(page0 + 64 * n, seen - 1)];   // (without a condition: all on their way at once)
 #pragma unroll
     for (int n = 0; n < N; ++n) key[n] = page0 + 64 * n >= from && page0 + 64 * n < to ? key_of_score(score[n]) : 0u;
     uint32_t top = 0, low = 0xffffffffu;
@@ -347,10 +360,10 @@ __global__ __launch_bounds__(W > kWaves ? 64 * W : kThreads) void page_select_ke
         low = min(low, (uint32_t)__shfl_xor((int)low, k, 64));
     }
     if (W > 1) {
-        if (lane == 0) s_top[wave] = top, s_low[wave] = low;
+        if (lane == 0) sh.top[wave] = top, sh.low[wave] = low;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < W; ++w) top = max(top, s_top[w]), low = min(low, s_low[w]);
+        for (int w = 0; w < W; ++w) top = max(top, sh.top[w]), low = min(low, sh.low[w]);
     }
     top = __builtin_amdgcn_readfirstlane(top);
     low = __builtin_amdgcn_readfirstlane(low);
@@ -358,11 +371,11 @@ __global__ __launch_bounds__(W > kWaves ? 64 * W : kThreads) void page_select_ke
     auto over_row = [&](int c) {   // a count of the wave's, over the row's waves
         if (W == 1) return c;
         turn ^= 1;
-        if (lane == 0) s_count[turn][wave] = c;
+        if (lane == 0) sh.count[turn][wave] = c;
         __syncthreads();
         c = 0;
 #pragma unroll
-        for (int w = 0; w < W; ++w) c += s_count[turn][w];
+        for (int w = 0; w < W; ++w) c += sh.count[turn][w];
         return (int)__builtin_amdgcn_readfirstlane(c);
     };
     auto count = [&](uint32_t least) {
@@ -388,7 +401,7 @@ __global__ __launch_bounds__(W > kWaves ? 64 * W : kThreads) void page_select_ke
         ties = fits ? 0x7fffffff : want - over_row(count(t + 1));   // (no score is 2^32 - 1)
     }
     const unsigned long long below = (1ull << lane) - 1;
-    auto kept = [&](int p) { return p < row.seen && (p < from || p >= to); };
+    auto kept = [&](int p) { return p < seen && (p < from || p >= to); };
     int at = 0;
     if (W > 1) {   // what the waves before take
         int taken = 0, same = 0;
@@ -398,19 +411,19 @@ __global__ __launch_bounds__(W > kWaves ? 64 * W : kThreads) void page_select_ke
             taken += __builtin_popcountll(__ballot(kept(page0 + 64 * n) || (want && key[n] > t)));
         }
         turn ^= 1;
-        if (lane == 0) s_count[turn][wave] = taken, s_same[wave] = same;
+        if (lane == 0) sh.count[turn][wave] = taken, sh.same[wave] = same;
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < W; ++w)
             if (w < wave) {
-                at += s_count[turn][w] + min(ties, s_same[w]);
-                ties -= min(ties, s_same[w]);
+                at += sh.count[turn][w] + min(ties, sh.same[w]);
+                ties -= min(ties, sh.same[w]);
             }
     }
 #pragma unroll
     for (int n = 0; n < N; ++n) {
         const int p = page0 + 64 * n;
-        if (p - lane >= row.seen) break;
+        if (p - lane >= seen) break;
         const unsigned long long same = __ballot(want && key[n] == t);
         const bool take = kept(p) || (want && key[n] > t) || (want && key[n] == t && __builtin_popcountll(same & below) < ties);
         ties -= min(ties, (int)__builtin_popcountll(same));
@@ -418,6 +431,46 @@ __global__ __launch_bounds__(W > kWaves ? 64 * W : kThreads) void page_select_ke
         if (take) out[at + __builtin_popcountll(m & below)] = p;
         at += __builtin_popcountll(m);
     }
+}
+
+template <int N, int W>
+__global__ __launch_bounds__(W > kWaves ? 64 * W : kThreads) void page_select_kernel(SelectArgs a)
+{
+    __shared__ PickLds<W> sh;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const SelectRow row = select_row(a, W == 1 ? blockIdx.x * kWaves + wave : blockIdx.x);
+    if (!row.any) return;
+    pick_pages<N, W>(a, row.seen, a.scores + row.at * a.score_stride, a.selected + row.at * a.n_select, W == 1 ? 0 : wave, sh);
+}
+
+// Small calls: a block a request and KV head forms the scores of its rows, of no more than
+// four tiles, in LDS, and a wave of it a row's list, so that there is one launch and no way
+// through memory.
+constexpr int kPickWaves = 16;
+constexpr int kPickPages = 512;
+constexpr int64_t kPickBlocks = 256;   // (of more, each compute unit would have several blocks in turn)
+
+template <bool E4M3, int NC, int R>
+__global__ __launch_bounds__(64 * kPickWaves) void page_pick_kernel(SelectArgs a)
+{
+    extern __shared__ __align__(16) int32_t s_scores[];   // [token][score_stride]
+    __shared__ __align__(16) RowsLds<NC, R> sh;
+    __shared__ PickLds<1> pick;   // (a wave has no use for it)
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t r = blockIdx.x / (uint32_t)a.heads;
+    const int h = (int)(blockIdx.x - (uint32_t)r * (uint32_t)a.heads);
+    const Request rq = request_of(a, r);
+    if (rq.rows == 0) return;
+    const int most_seen = pages_seen(a, rq, rq.rows - 1);   // (later tokens see no fewer)
+    if (most_seen > a.n_select) {
+        const int tiles = (most_seen + 15) >> 4;
+        score_block<E4M3, NC, R, false, kPickWaves>(a, rq, r, h, 0, most_seen, wave, kPickWaves, max((tiles - wave + kPickWaves - 1) / kPickWaves, 0),
+                                                    sh, [&](int tok, int page, int4_t x, bool) { *(int4_t*)(s_scores + tok * a.score_stride + page) = x; });
+        __syncthreads();
+    }
+    int32_t* out = a.selected + (rq.start * (int64_t)a.heads + h) * a.n_select;
+    for (int tok = wave; tok < rq.rows; tok += kPickWaves)
+        pick_pages<kPickPages / 64, 1>(a, pages_seen(a, rq, tok), s_scores + tok * a.score_stride, out + (int64_t)tok * a.heads * a.n_select, 0, pick);
 }
 
 // A block a row, for more pages than a wave holds: digits of 8 bits from the first
@@ -951,6 +1004,23 @@ size_t bytes_or_most(size_t a, size_t b)
     return __builtin_mul_overflow(a, b, &n) ? ~(size_t)0 : n;
 }
 
+int lanes_log(int64_t group)
+{
+    int n = 0;
+    while (n < 4 && (1 << n) < group) ++n;
+    return n;
+}
+
+// Whether page_pick_kernel does a call.  Without and with it (us a call, with the host's part): a token over 512 pages, 8 KV heads
+// of 128 16.0 and 11.8, 16 such requests 16.8 and 12.4, 8 of four tokens each 16.2 and 11.9.  Of 2048 pages it takes 31 in
+// place of 28, and 512 requests of 128 pages 157 in place of 42.
+bool picked_at_once(const fkv_page_desc* p, const fkv_select_desc* t)
+{
+    const int64_t group = t->q_heads / p->heads;
+    return score_stride(p, t) && group <= 16 && p->d <= 128 && t->max_new <= 4 * (16 >> lanes_log(group)) && most_pages(p, t) <= kPickPages &&
+           t->n_req * p->heads <= kPickBlocks;
+}
+
 constexpr int kHeldPages = 16384;   // that the waves of a row hold at the most: 16 of 16 x 64
 
 // How the splits of an item's list are chosen: see fkv_page_attend_selected.
@@ -997,7 +1067,7 @@ using namespace fkv;
 
 extern "C" size_t fkv_page_select_workspace(const fkv_page_desc* desc, const fkv_select_desc* select)
 {
-    if (!select_ok(desc, select)) return 0;
+    if (!select_ok(desc, select) || picked_at_once(desc, select)) return 0;
     return bytes_or_most((size_t)(select->n_tokens * desc->heads), (size_t)score_stride(desc, select) * sizeof(int32_t));
 }
 
@@ -1026,9 +1096,22 @@ extern "C" int fkv_page_select(const fkv_page_desc* desc, const fkv_select_desc*
     const hipStream_t st = (hipStream_t)stream;
     if (a.n_req > kMostBlocks / a.max_new || a.n_req * a.max_new > kMostBlocks / a.heads) return FKV_ERR_UNSUPPORTED;
     const int64_t rows = a.n_req * a.max_new * a.heads;
+    const bool e4m3 = desc->format == FKV_PAGE_E4M3;
+    a.lanes_log = lanes_log(a.group);
+    if (picked_at_once(desc, select)) {
+        auto go = [&](auto kern) {
+            hipLaunchKernelGGL(kern, dim3((unsigned)(a.n_req * a.heads)), dim3(64 * kPickWaves), (size_t)(a.max_new * a.score_stride) * sizeof(int32_t), st, a);
+        };
+        auto of_width = [&](auto nc) {
+            constexpr int NC = decltype(nc)::value;
+            if (a.max_new <= 16 >> a.lanes_log) return e4m3 ? go(page_pick_kernel<true, NC, 1>) : go(page_pick_kernel<false, NC, 1>);
+            e4m3 ? go(page_pick_kernel<true, NC, 4>) : go(page_pick_kernel<false, NC, 4>);
+        };
+        if (a.d <= 64) of_width(std::integral_constant<int, 1>{});
+        else of_width(std::integral_constant<int, 2>{});
+        return launch_status();
+    }
     if (need) {
-        a.lanes_log = 0;
-        while (a.lanes_log < 4 && (1 << a.lanes_log) < a.group) ++a.lanes_log;
         const int64_t row_tiles = (a.max_new + (16 >> a.lanes_log) - 1) / (16 >> a.lanes_log);
         const bool many = a.group > 16 || row_tiles >= 4;   // four row tiles a block
         a.row_groups = a.group > 16 || !many ? row_tiles : (row_tiles + 3) / 4;
@@ -1042,7 +1125,6 @@ extern "C" int fkv_page_select(const fkv_page_desc* desc, const fkv_select_desc*
         a.tile_chunks = (int32_t)((tiles + wave_tiles * kWaves - 1) / (wave_tiles * kWaves));
         const int64_t blocks = a.n_req * a.heads * a.row_groups;   // (row groups are no more than max_new)
         if (blocks > kMostBlocks / a.tile_chunks) return FKV_ERR_UNSUPPORTED;
-        const bool e4m3 = desc->format == FKV_PAGE_E4M3;
         auto go = [&](auto kern) {
             hipLaunchKernelGGL(kern, dim3((unsigned)(blocks * a.tile_chunks)), dim3(kThreads), 0, st, a);
         };

@@ -82,6 +82,12 @@ SELECTS = [
     (16, 2, 1, 16, INT8, F16, [(16 * 2048, 1)], 33, 1, 1),
     (16, 2, 1, 16, INT8, F16, [(16 * 2049, 2), (40, 1), (16 * 2049 - 17, 1)], 33, 1, 1),   # a block a row
     (16, 1, 2, 32, E4M3, BF16, [(16 * 5000 + 3, 1)], 1500, 0, 0),
+    (16, 2, 7, 96, E4M3, F16, [(16 * 300, 4), (16 * 90, 8), (50, 8)], 40, 2, 1),          # several tiles of few rows, at once
+    (16, 1, 1, 64, INT8, BF16, [(16 * 200, 64), (16 * 100, 17), (30, 30)], 20, 0, 2),
+    (16, 2, 16, 128, INT8, F16, [(16 * 1000, 4), (16 * 2048, 3)], 64, 1, 1),
+    (16, 64, 1, 16, INT8, F16, [(16 * 2100, 1), (16 * 3000 - 3, 1), (20, 1)], 30, 1, 1),  # all of a block's waves a row
+    (16, 128, 1, 16, E4M3, F16, [(16 * 16384 - 9, 1)], 100, 1, 1),
+    (16, 2, 4, 128, INT8, F16, [(16 * 900, 17), (16 * 2200, 1)], 100, 1, 1),
 ]
 
 

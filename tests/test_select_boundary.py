@@ -71,17 +71,21 @@ def test_select_arguments(F):
         assert select(**kw) == E, kw
     assert select(n_req=0, q=None, sel=None) == 0 and select(n_tokens=0, q=None) == 0
     assert F.lib.fkv_page_select(ref(desc), None, g, g, g, g, g, g, g, g, 1 << 20, None) == E
-    assert select(ws=None) == select(nws=2 * 4 * 16 * 4 - 1) == F.FKV_ERR_SCRATCH_TOO_SMALL
+    many = dict(n_tokens=200, max_new=100)      # (few rows need no scratch)
+    assert select(ws=None, **many) == select(nws=2 * 200 * 16 * 4 - 1, **many) == F.FKV_ERR_SCRATCH_TOO_SMALL
 
 
 def test_select_scratch(F):
-    """A score a row, KV head and page, rows of 16 pages; none where all pages are selected."""
+    """A score a row, KV head and page, rows of 16 pages; none where all pages are selected, nor for few rows."""
     desc = F.fkv_page_desc(8, 16, 2, 64, 0)
-    need = lambda **kw: F.lib.fkv_page_select_workspace(ref(desc), ref(select_desc(F, **kw)))     # noqa: E731
-    assert need() == 2 * 4 * 16 * 4
-    assert need(max_kv=300, max_pages=40) == 2 * 4 * 32 * 4
+    need = lambda **kw: F.lib.fkv_page_select_workspace(ref(desc), ref(select_desc(F, **{**dict(n_tokens=200, max_new=100), **kw})))     # noqa: E731
+    assert need() == 2 * 200 * 16 * 4
+    assert need(max_kv=300, max_pages=40) == 2 * 200 * 32 * 4
     assert need(n_select=4) == 0 and need(max_kv=32) == 0 and need(max_pages=2) == 0
     assert need(n_select=0) == 0 and F.lib.fkv_page_select_workspace(None, ref(select_desc(F))) == 0
+    assert need(max_new=2) == 0 and need(max_new=32) == 0 and need(max_new=33) > 0
+    assert need(max_new=1, max_kv=16 * 512, max_pages=512) == 0 and need(max_new=1, max_kv=16 * 513, max_pages=513) > 0
+    assert need(max_new=1, n_req=128) == 0 and need(max_new=1, n_req=129) > 0
     wide = F.fkv_page_desc(8, 16, 65535, 64, 0)
     assert F.lib.fkv_page_select_workspace(ref(wide), ref(select_desc(F, q_heads=65535, n_tokens=1 << 30, max_kv=1 << 30,
                                                                       max_pages=1 << 26))) == (1 << 64) - 1
