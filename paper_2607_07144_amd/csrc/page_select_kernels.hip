@@ -875,7 +875,7 @@ __device__ __forceinline__ void whole_tiles(const AttendArgs& a, const Request& 
 // the list's tiles in turn, with those of the item's other splits; their sums joined
 // in LDS, and the splits' by a second kernel.
 template <bool E4M3, int NC, int W, bool WHOLE, bool PLAIN>
-__global__ __launch_bounds__(kThreads, NC == 2 && WHOLE ? 3 : NC <= 2 ? 2 : 1) void attend_listed_kernel(AttendArgs a)
+__global__ __launch_bounds__(W > kWaves ? 64 * W : kThreads, NC == 2 && WHOLE && W <= kWaves ? 3 : NC <= 2 ? 2 : 1) void attend_listed_kernel(AttendArgs a)
 {
     extern __shared__ __align__(16) float lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1039,10 +1039,17 @@ ListedShape listed_shape(const fkv_page_desc* p, const fkv_attend_desc* t, int64
     const int64_t tokens = std::min(t->n_req * t->max_new, (int64_t)1 << 34);   // (2^34 are too many, whatever the heads)
     const int64_t items = tokens * of_token;
     const int64_t tiles = (n_listed * (p->page / 16) + 3) / 4;
+    // A wave an item where the items fill the chip, else four.  Of few items with up to 32 tiles eight waves have up to four tiles
+    // each and no second launch; longer lists are split, two tiles a wave at the least.  Measured with four waves, eight, and
+    // four splits of four (us a call, with the host's part), 8 KV heads of 128: one token, 16 tiles 14.6, 14.5 and 19.1, 32 tiles
+    // 18.2, 17.0 and 19.0, 64 tiles 30, 27 and 19.3; 16 tokens, 32 tiles 21.2, 19.6 and 21.0, 64 tiles 38, 33 and 31; 32 tokens,
+    // 32 tiles 26.3, 26.5 and 33.1; 64 tokens 54, 58 and 63.
     s.n_splits = 1;
     s.waves = items >= 2048 || tiles <= 1 ? 1 : kWaves;
     s.blocks = s.waves == 1 ? (tokens + kWaves - 1) / kWaves * of_token : items;
-    if (s.waves == kWaves && items < 256) {
+    if (items < 256 && tiles > 16 && tiles <= 32 && p->d <= 128) {
+        s.waves = 8;
+    } else if (items < 256 && tiles > 16) {
         const int64_t want = (512 + items - 1) / std::max((int64_t)1, items), most = std::max((int64_t)1, tiles / (2 * kWaves));
         s.n_splits = (int)std::min(want, most);
     }
@@ -1203,12 +1210,15 @@ extern "C" int fkv_page_attend_selected(const fkv_page_desc* desc, const fkv_att
     auto of_width = [&](auto nc) {
         constexpr int NC = decltype(nc)::value;
         auto go = [&](auto kern, size_t shm) {
-            hipLaunchKernelGGL(kern, dim3((unsigned)(s.blocks * s.n_splits)), dim3(kThreads), shm, st, a);
+            hipLaunchKernelGGL(kern, dim3((unsigned)(s.blocks * s.n_splits)), dim3(s.waves == 1 ? kThreads : 64 * s.waves), shm, st, a);
         };
-        const size_t shm = s.waves == 1 ? 0 : (2 * kWaves * kFewRows + (size_t)kWaves * kFewRows * (a.d + 4)) * sizeof(float);
+        const size_t shm = s.waves == 1 ? 0 : (2 * s.waves * kFewRows + (size_t)s.waves * kFewRows * (a.d + 4)) * sizeof(float);
         auto of_form = [&](auto whole, auto plain) {
             constexpr bool WHOLE = decltype(whole)::value, PLAIN = decltype(plain)::value;
             if (s.waves == 1) return e4m3 ? go(attend_listed_kernel<true, NC, 1, WHOLE, PLAIN>, shm) : go(attend_listed_kernel<false, NC, 1, WHOLE, PLAIN>, shm);
+            if constexpr (NC <= 2) {
+                if (s.waves == 8) return e4m3 ? go(attend_listed_kernel<true, NC, 8, WHOLE, PLAIN>, shm) : go(attend_listed_kernel<false, NC, 8, WHOLE, PLAIN>, shm);
+            }
             e4m3 ? go(attend_listed_kernel<true, NC, kWaves, WHOLE, PLAIN>, shm) : go(attend_listed_kernel<false, NC, kWaves, WHOLE, PLAIN>, shm);
         };
         const bool plain = a.softcap == 0.0f && !a.slopes;

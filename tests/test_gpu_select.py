@@ -241,6 +241,9 @@ ATTENDS = [
     (16, 2, 5, 144, E4M3, F16, [(300, 4)], 11),
     (64, 2, 4, 128, INT8, BF16, [(64 * 140, 1)], 130),           # split
     (16, 1, 3, 64, E4M3, F16, [(16 * 300, 1), (100, 1)], 260),
+    (64, 2, 4, 128, INT8, BF16, [(64 * 60, 1), (500, 1)], 30),   # eight waves a block
+    (16, 2, 3, 80, E4M3, F16, [(16 * 200, 1), (33, 2)], 100),
+    (128, 1, 9, 64, E4M3, BF16, [(128 * 20, 2)], 13),
     (16, 4, 2, 64, INT8, F16, [(400, 300)], 4),                 # a wave an item
     (64, 4, 4, 128, INT8, BF16, [(700, 450), (300, 300)], 3),
 ]
