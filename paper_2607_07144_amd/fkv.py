@@ -176,6 +176,15 @@ def _need(t, dtype, name):
     raise TypeError("%s must be a contiguous CUDA tensor of %s" % (name, dtype))
 
 
+def _here(*tensors) -> None:
+    """Refuses tensors of another device than the current one, whose stream and scratch a call takes."""
+    torch = _TORCH or _torch()
+    device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError("tensor on device %d, the current device is %d" % (t.get_device(), device))
+
+
 # ------------------------------------------------------------------ codec
 
 class Codec:
@@ -607,9 +616,11 @@ def _page_desc(pages) -> fkv_page_desc:
         kind = FKV_PAGE_E4M3
     else:
         raise TypeError("pages hold int8 or float8_e4m3fn codes")
-    _need(k, code, "pages.k")
-    _need(v, code, "pages.v")
-    _need(scales, torch.float32, "pages.scales")
+    if not (k.is_cuda and k.is_contiguous() and v.is_cuda and v.dtype is code and v.is_contiguous() and scales.is_cuda
+            and scales.dtype is torch.float32 and scales.is_contiguous()):
+        _need(k, code, "pages.k")
+        _need(v, code, "pages.v")
+        _need(scales, torch.float32, "pages.scales")
     if k.dim() != 4:
         raise ValueError("pages.k must be [n_pages][heads][page][d]")
     n, heads, page, d = k.shape
@@ -755,6 +766,7 @@ def fkv_page_append(pages, k, v, slots, positions=None, table=None, q=None, q_ou
         raise TypeError("q_out without q")
     if boxes is not None:
         _need_boxes(boxes, pages)
+    _here(*pages, k, v, slots, positions, table, q, q_out, boxes, n_bad)
     ref = ctypes.byref
     if rot or rq is not None:
         rotate = ref(fkv_rotate_desc(n_pos, rot, FKV_ROTATE_PAIRS if pairs else FKV_ROTATE_HALVES, q_heads))
@@ -789,13 +801,17 @@ def fkv_page_load(pages, slots, dtype=None, k=None, v=None, stream=None):
                              _ptr(k), _ptr(v), _stream(stream)), "fkv_page_load")
     return k, v
 
+
 def _q_rows(pages, q, tables, kv_len, q_start):
-    """The checks that calls over requests' query rows share: (page desc, row type, requests, columns of a table)."""
+    """The checks that the calls for long contexts share over requests' query rows (fkv_page_attend makes them in place: a
+    small call's time is these lines, and helpers cost it 0.6 of 11.5 us): (page desc, row type, requests, columns of a table,
+    q's shape and strides)."""
     torch = _TORCH or _torch()
     desc = _page_desc(pages)
     if not isinstance(q, torch.Tensor) or not q.is_cuda or q.dim() != 3:
         raise TypeError("q must be a CUDA tensor [n_tokens][q_heads][d]")
-    if q.shape[2] != desc.d or q.stride(2) != 1:
+    shape, stride = q.shape, q.stride()
+    if shape[2] != desc.d or stride[2] != 1:
         raise TypeError("q must have rows of %d contiguous elements" % desc.d)
     i32, kind = torch.int32, _row_type(q.dtype, "q")
     _need(tables, i32, "tables")
@@ -804,52 +820,33 @@ def _q_rows(pages, q, tables, kv_len, q_start):
     n_req, width = kv_len.numel(), tables.shape
     if len(width) != 2 or width[0] != n_req or q_start.numel() != n_req + 1:
         raise ValueError("shape mismatch between tables, kv_len and q_start")
-    return desc, kind, n_req, width[1]
+    return desc, kind, n_req, width[1], shape, stride
 
 
 def _scratch(need: int, device, stream):
-    """uint8 scratch from torch's allocator, of the stream that the call runs on; None for none."""
+    """uint8 scratch from torch's allocator, of the stream that the call runs on."""
     torch = _TORCH or _torch()
-    if not need:
-        return None
     if stream is None:
         return torch.empty(need, dtype=torch.uint8, device=device)
     with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device)):
         return torch.empty(need, dtype=torch.uint8, device=device)
 
 
-def _attention(desc, kind: int, n_req: int, width: int, q, max_new: int, max_kv: int, scale, softcap: float, causal: bool,
-               window: int, sinks: int, slopes, prefix, first, out, lse, want_lse: bool):
-    """The further arguments of the attention calls checked: (attend desc, out, lse)."""
+def _masks(n: int, q_heads: int, n_req: int, slopes, prefix, first) -> None:
+    """Checks of the attention calls' optional tensors."""
     torch = _TORCH or _torch()
-    (n, q_heads, d), q_stride, i32 = q.shape, q.stride(), torch.int32
     if prefix is not None:
-        _need(prefix, i32, "prefix")
+        _need(prefix, torch.int32, "prefix")
         if prefix.numel() != n_req:
             raise ValueError("prefix must have one entry per request")
     if first is not None:
-        _need(first, i32, "first")
+        _need(first, torch.int32, "first")
         if first.numel() != n:
             raise ValueError("first must have one entry per row of q")
     if slopes is not None:
         _need(slopes, torch.float32, "slopes")
         if slopes.numel() != q_heads:
             raise ValueError("slopes must have one entry per query head")
-    if out is None:
-        out = torch.empty((n, q_heads, d), dtype=q.dtype, device=q.device)
-        o_stride = (q_heads * d, d)
-    else:
-        if not out.is_cuda or out.shape != q.shape or out.dtype is not q.dtype or out.stride(2) != 1:
-            raise TypeError("out must be a CUDA tensor of q's shape and type, contiguous in d")
-        o_stride = out.stride()
-    if lse is not None:
-        _need(lse, torch.float32, "lse")
-        if lse.numel() != n * q_heads:
-            raise ValueError("lse has the wrong size")
-    elif want_lse:
-        lse = torch.empty((n, q_heads), dtype=torch.float32, device=q.device)
-    return fkv_attend_desc(n_req, n, max_new, max_kv, width, q_stride[0], q_stride[1], o_stride[0], o_stride[1], q_heads, kind,
-                           d ** -0.5 if scale is None else scale, softcap, 1 if causal else 0, window, sinks), out, lse
 
 
 def fkv_page_select(pages, boxes, q, tables, kv_len, q_start, max_new: int, max_kv: int, n_select: int, keep_first: int = 1,
@@ -861,9 +858,9 @@ def fkv_page_select(pages, boxes, q, tables, kv_len, q_start, max_new: int, max_
     the last; rows of no request are left as they were.  workspace: uint8 scratch of fkv_page_select_workspace bytes, for
     callers that keep one."""
     torch = _TORCH or _torch()
-    desc, kind, n_req, width = _q_rows(pages, q, tables, kv_len, q_start)
+    desc, kind, n_req, width, shape, q_stride = _q_rows(pages, q, tables, kv_len, q_start)
     _need_boxes(boxes, pages)
-    (n, q_heads, _), q_stride = q.shape, q.stride()
+    n, q_heads, _ = shape
     sel = fkv_select_desc(n_req, n, max_new, max_kv, width, q_stride[0], q_stride[1], q_heads, kind, 1 if causal else 0,
                           n_select, keep_first, keep_last)
     if selected is None:
@@ -872,11 +869,14 @@ def fkv_page_select(pages, boxes, q, tables, kv_len, q_start, max_new: int, max_
         _need(selected, torch.int32, "selected")
         if selected.shape != (n, desc.heads, n_select):
             raise ValueError("selected must be [n_tokens][heads][n_select]")
+    _here(*pages, boxes, q, tables, kv_len, q_start, selected, workspace)
     ref = ctypes.byref
     if workspace is not None:
         _need(workspace, torch.uint8, "workspace")
     else:
-        workspace = _scratch(lib.fkv_page_select_workspace(ref(desc), ref(sel)), q.device, stream)
+        need = lib.fkv_page_select_workspace(ref(desc), ref(sel))
+        if need:
+            workspace = _scratch(need, q.device, stream)
     _check(lib.fkv_page_select(ref(desc), ref(sel), boxes.data_ptr(), pages[2].data_ptr(), q.data_ptr(), tables.data_ptr(),
                                kv_len.data_ptr(), q_start.data_ptr(), selected.data_ptr(), _ptr(workspace),
                                0 if workspace is None else workspace.numel(), _stream(stream)), "fkv_page_select")
@@ -899,18 +899,37 @@ def fkv_page_attend_selected(pages, q, tables, kv_len, q_start, selected, max_ne
     (fkv_page_select's result; columns of the token's row of tables in any order, an entry that is none lists nothing).
     Returns (out, lse or None).  workspace: uint8 scratch of fkv_page_attend_selected_workspace bytes."""
     torch = _TORCH or _torch()
-    desc, kind, n_req, width = _q_rows(pages, q, tables, kv_len, q_start)
+    desc, kind, n_req, width, shape, q_stride = _q_rows(pages, q, tables, kv_len, q_start)
     _need(selected, torch.int32, "selected")
     at = selected.shape
-    if len(at) != 3 or at[0] != q.shape[0] or at[1] != desc.heads:
+    if len(at) != 3 or at[0] != shape[0] or at[1] != desc.heads:
         raise ValueError("selected must be [n_tokens][heads][n]")
-    att, out, lse = _attention(desc, kind, n_req, width, q, max_new, max_kv, scale, softcap, causal, window, sinks, slopes,
-                               prefix, first, out, lse, want_lse)
+    n, q_heads, d = shape
+    if slopes is not None or prefix is not None or first is not None:
+        _masks(n, q_heads, n_req, slopes, prefix, first)
+    if out is None:
+        out = torch.empty(shape, dtype=q.dtype, device=q.device)
+        o_stride = (q_heads * d, d)
+    else:
+        if not out.is_cuda or out.shape != shape or out.dtype is not q.dtype or out.stride(2) != 1:
+            raise TypeError("out must be a CUDA tensor of q's shape and type, contiguous in d")
+        o_stride = out.stride()
+    if lse is not None:
+        _need(lse, torch.float32, "lse")
+        if lse.numel() != n * q_heads:
+            raise ValueError("lse has the wrong size")
+    elif want_lse:
+        lse = torch.empty((n, q_heads), dtype=torch.float32, device=q.device)
+    _here(*pages, q, tables, kv_len, q_start, selected, slopes, prefix, first, out, lse, workspace)
+    att = fkv_attend_desc(n_req, n, max_new, max_kv, width, q_stride[0], q_stride[1], o_stride[0], o_stride[1], q_heads, kind,
+                          d ** -0.5 if scale is None else scale, softcap, 1 if causal else 0, window, sinks)
     ref = ctypes.byref
     if workspace is not None:
         _need(workspace, torch.uint8, "workspace")
     else:
-        workspace = _scratch(lib.fkv_page_attend_selected_workspace(ref(desc), ref(att), at[2]), q.device, stream)
+        need = lib.fkv_page_attend_selected_workspace(ref(desc), ref(att), at[2])
+        if need:
+            workspace = _scratch(need, q.device, stream)
     _check(lib.fkv_page_attend_selected(ref(desc), ref(att), at[2], selected.data_ptr(), pages[0].data_ptr(),
                                         pages[1].data_ptr(), pages[2].data_ptr(), q.data_ptr(), tables.data_ptr(),
                                         kv_len.data_ptr(), q_start.data_ptr(), _ptr(slopes), _ptr(prefix), _ptr(first),
@@ -938,14 +957,43 @@ def fkv_page_attend(pages, q, tables, kv_len, q_start, max_new: int, max_kv: int
     (out, lse or None).  workspace: uint8 scratch of fkv_page_attend_workspace bytes, for callers that keep one;
     without it the call takes its scratch from torch's allocator, on the stream it runs on."""
     torch = _TORCH or _torch()
-    desc, kind, n_req, width = _q_rows(pages, q, tables, kv_len, q_start)
-    att, out, lse = _attention(desc, kind, n_req, width, q, max_new, max_kv, scale, softcap, causal, window, sinks, slopes,
-                               prefix, first, out, lse, want_lse)
+    desc = _page_desc(pages)
+    if not isinstance(q, torch.Tensor) or not q.is_cuda or q.dim() != 3:
+        raise TypeError("q must be a CUDA tensor [n_tokens][q_heads][d]")
+    (n, q_heads, d), q_stride = q.shape, q.stride()
+    if d != desc.d or q_stride[2] != 1:
+        raise TypeError("q must have rows of %d contiguous elements" % desc.d)
+    i32, kind = torch.int32, _row_type(q.dtype, "q")
+    _need(tables, i32, "tables")
+    _need(kv_len, i32, "kv_len")
+    _need(q_start, i32, "q_start")
+    n_req, width = kv_len.numel(), tables.shape
+    if len(width) != 2 or width[0] != n_req or q_start.numel() != n_req + 1:
+        raise ValueError("shape mismatch between tables, kv_len and q_start")
+    if slopes is not None or prefix is not None or first is not None:
+        _masks(n, q_heads, n_req, slopes, prefix, first)
+    if out is None:
+        out = torch.empty((n, q_heads, d), dtype=q.dtype, device=q.device)
+        o_stride = (q_heads * d, d)
+    else:
+        if not out.is_cuda or out.shape != q.shape or out.dtype is not q.dtype or out.stride(2) != 1:
+            raise TypeError("out must be a CUDA tensor of q's shape and type, contiguous in d")
+        o_stride = out.stride()
+    if lse is not None:
+        _need(lse, torch.float32, "lse")
+        if lse.numel() != n * q_heads:
+            raise ValueError("lse has the wrong size")
+    elif want_lse:
+        lse = torch.empty((n, q_heads), dtype=torch.float32, device=q.device)
+    att = fkv_attend_desc(n_req, n, max_new, max_kv, width[1], q_stride[0], q_stride[1], o_stride[0], o_stride[1], q_heads, kind,
+                          d ** -0.5 if scale is None else scale, softcap, 1 if causal else 0, window, sinks)
     ref = ctypes.byref
     if workspace is not None:
         _need(workspace, torch.uint8, "workspace")
     else:
-        workspace = _scratch(lib.fkv_page_attend_workspace(ref(desc), ref(att)), q.device, stream)
+        need = lib.fkv_page_attend_workspace(ref(desc), ref(att))
+        if need:
+            workspace = _scratch(need, q.device, stream)
     _check(lib.fkv_page_attend(ref(desc), ref(att), pages[0].data_ptr(), pages[1].data_ptr(), pages[2].data_ptr(),
                                q.data_ptr(), tables.data_ptr(), kv_len.data_ptr(), q_start.data_ptr(), _ptr(slopes),
                                _ptr(prefix), _ptr(first), out.data_ptr(), _ptr(lse), _ptr(workspace),

@@ -137,3 +137,14 @@ def test_attend_selected_scratch(F):
     assert F.lib.fkv_page_attend_selected_workspace(ref(desc), ref(t), 1) == 0
     assert F.lib.fkv_page_attend_selected_workspace(None, ref(t), 128) == 0
     assert F.lib.fkv_page_attend_selected_workspace(ref(desc), ref(t), 0) == 0
+
+
+def test_tensors_of_another_device(F, monkeypatch):
+    """A call runs on the current device's stream: tensors of another device are refused before it."""
+    from types import SimpleNamespace
+    monkeypatch.setattr(F, "_TORCH", SimpleNamespace(_C=SimpleNamespace(_cuda_getDevice=lambda: 1), cuda=SimpleNamespace(current_device=None)))
+    t = [SimpleNamespace(get_device=lambda i=i: i) for i in range(2)]
+    F._here(t[1], None, t[1])
+    for bad in ((t[0],), (t[1], t[0]), (t[1], None, t[0])):
+        with pytest.raises(ValueError):
+            F._here(*bad)
