@@ -589,7 +589,8 @@ int fkv_page_attend(const fkv_page_desc* desc, const fkv_attend_desc* attend, co
  *   workspace  device scratch of fkv_page_select_workspace() bytes, 16-byte aligned;
  *              null when that is 0.  Calls that may run at the same time need one each
  * n_select: 1 .. 2^20, keep_first + keep_last at most n_select.  FKV_ERR_UNSUPPORTED
- * for more blocks than a launch holds (n_req * max_new * heads beyond 2^31). */
+ * for more blocks than a launch holds (the fewer of 2 n_tokens and n_req * max_new,
+ * times heads, beyond 2^31). */
 typedef struct {
     int64_t n_req;
     int64_t n_tokens;
@@ -620,8 +621,8 @@ int fkv_page_select(const fkv_page_desc* desc, const fkv_select_desc* select, co
  *   n_selected  1 .. 2^20
  *   workspace   of fkv_page_attend_selected_workspace() bytes
  * The other arguments, accuracy and errors are fkv_page_attend's, but for its limits
- * on rows: FKV_ERR_UNSUPPORTED for more blocks than a launch holds (n_req * max_new *
- * heads beyond 2^31). */
+ * on rows: FKV_ERR_UNSUPPORTED for more blocks than a launch holds, as of
+ * fkv_page_select, with q_heads in place of heads where they are more than 16 a head. */
 size_t fkv_page_attend_selected_workspace(const fkv_page_desc* desc, const fkv_attend_desc* attend, int64_t n_selected);
 
 int fkv_page_attend_selected(const fkv_page_desc* desc, const fkv_attend_desc* attend, int64_t n_selected,

@@ -49,6 +49,7 @@ struct AttendArgs {
     int32_t n_splits, split_tiles;
     const int32_t* listed;   // [token][KV head][n_listed] columns of the token's block table, of attention to listed pages
     int64_t n_listed;
+    int64_t searched;      // rows of q whose requests the kernels for lists look up (0: max_new places a request)
     int32_t piece_rows;    // of a KV head: max_new x group
     uint32_t per_page;     // 16-key groups of a page
     uint32_t per_page_inv; // and their reciprocal, 2^32 / per_page rounded up (0: one)

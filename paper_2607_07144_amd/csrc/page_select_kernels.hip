@@ -23,7 +23,8 @@ struct SelectArgs : AttendArgs {
     int32_t* scores;    // [token][KV head][score_stride], as ordered() gives them
     int32_t* selected;  // [token][KV head][n_select]
     int64_t score_stride;
-    int64_t row_groups;   // of the scoring kernel: row tiles of a request, R a wave
+    int64_t row_groups;   // of the scoring kernel: row tiles of a request, R a block
+    int64_t searched_groups;   // or of all requests, which the kernel looks up (0: row_groups a request)
     int32_t n_select, keep_first, keep_last;
     int32_t tile_chunks;  // and its blocks along the pages, of wave_tiles tiles of 16 pages a wave
     int32_t wave_tiles;
@@ -42,6 +43,45 @@ __device__ __forceinline__ int pages_seen(const AttendArgs& a, const Request& rq
 {
     const int end = a.causal ? min(rq.pos0 + i + 1, rq.kv) : rq.kv;
     return pages_of(a, max(end, 0));
+}
+
+// Prompts and single tokens in one call leave most of n_req x max_new places empty.  Then
+// a launch has a place for each row of q, and finds its request: the last whose rows
+// begin at `index` or before.  PER rows a place: of a request's rows the places
+// start / PER + r on, which are enough for any rows before the next request's.  -1: none.
+// (A step of 30 single tokens, 2048 of a chunk and 33 more, 8 heads of 128: selection 208 -> 73 us, attention to lists
+// 987 -> 640.)
+__device__ __forceinline__ int64_t first_place(const AttendArgs& a, int64_t r, int per)
+{
+    const uint32_t start = (uint32_t)min(max((int64_t)a.q_start[r], (int64_t)0), a.n_tokens);
+    return per == 1 ? start : start / (uint32_t)per + r;
+}
+
+__device__ __forceinline__ int64_t request_at(const AttendArgs& a, int64_t index, int per)
+{
+    const int lane = threadIdx.x & 63;
+    int64_t lo = 0, end = a.n_req;   // the requests not settled; but for the first round lo's rows begin early enough
+    for (;;) {
+        const int64_t step = (end - lo + 63) >> 6, j = lo + lane * step;
+        const int n = __builtin_popcountll(__ballot(j < end && first_place(a, min(j, end - 1), per) <= index));
+        if (n == 0) return -1;
+        lo += (n - 1) * step;
+        if (step == 1) return lo;
+        end = min(end, lo + step);
+    }
+}
+
+// The request and row of a launch's place for a token; r -1: of none, i -1: to be told from the request's first row.
+struct TokenPlace {
+    int64_t r;
+    int i;
+};
+
+__device__ __forceinline__ TokenPlace token_place(const AttendArgs& a, uint32_t place)
+{
+    if (a.searched) return TokenPlace{request_at(a, place, 1), -1};
+    const uint32_t r = place / (uint32_t)a.max_new;
+    return TokenPlace{r, (int)(place - r * (uint32_t)a.max_new)};
 }
 
 // ---------------------------------------------------------------- scores --
@@ -266,12 +306,20 @@ __global__ __launch_bounds__(kThreads, R == 1 || NC == 1 ? 4 : NC == 2 ? 3 : 2) 
     b /= (uint32_t)a.heads;
     const int chunk = (int)(b % (uint32_t)a.tile_chunks);
     b /= (uint32_t)a.tile_chunks;
-    const int64_t r = b / (uint32_t)a.row_groups;
-    const int rg = (int)(b - (uint32_t)r * (uint32_t)a.row_groups);
-    const Request rq = request_of(a, r);
     const int tokens = WIDE ? 1 : R * (16 >> a.lanes_log);   // of the block
+    int64_t r;
+    int rg;
+    if (a.searched_groups) {
+        r = request_at(a, b, tokens);
+        if (r < 0) return;
+        rg = (int)(b - first_place(a, r, tokens));
+    } else {
+        r = b / (uint32_t)a.row_groups;
+        rg = (int)(b - (uint32_t)r * (uint32_t)a.row_groups);
+    }
+    const Request rq = request_of(a, r);
+    if (rg < 0 || (int64_t)rg * tokens >= rq.rows) return;   // (negative: of starts out of order)
     const int tok0 = rg * tokens;
-    if (tok0 >= rq.rows) return;
     const int most_seen = pages_seen(a, rq, min(tok0 + tokens, rq.rows) - 1);   // (later tokens see no fewer)
     if (most_seen <= a.n_select) return;   // every page of theirs is selected
     const int tiles = (most_seen + 15) >> 4;
@@ -308,13 +356,14 @@ struct SelectRow {
 __device__ __forceinline__ SelectRow select_row(const SelectArgs& a, uint32_t item)   // (below 2^31)
 {
     SelectRow s = {0, 0, false};
-    if (item >= (uint32_t)(a.n_req * a.max_new * a.heads)) return s;
+    if (item >= (uint32_t)((a.searched ? a.searched : a.n_req * a.max_new) * a.heads)) return s;
     const uint32_t ri = item / (uint32_t)a.heads;
     const int h = (int)(item - ri * (uint32_t)a.heads);
-    const uint32_t r = ri / (uint32_t)a.max_new;
-    const int i = (int)(ri - r * (uint32_t)a.max_new);
-    const Request rq = request_of(a, r);
-    if (i >= rq.rows) return s;
+    const TokenPlace at = token_place(a, ri);
+    if (at.r < 0) return s;
+    const Request rq = request_of(a, at.r);
+    const int i = at.i < 0 ? (int)ri - rq.start : at.i;
+    if ((uint32_t)i >= (uint32_t)rq.rows) return s;   // (negative: of starts out of order)
     s.at = (rq.start + i) * (int64_t)a.heads + h;
     s.seen = pages_seen(a, rq, i);
     s.any = true;
@@ -892,11 +941,13 @@ __global__ __launch_bounds__(W > kWaves ? 64 * W : kThreads, NC == 2 && WHOLE &&
     const uint32_t of_chunk = of_head / chunks;
     const int chunk = (int)(of_head - of_chunk * chunks);
     const int64_t ri = W == 1 ? (int64_t)of_chunk * kWaves + wave : of_chunk;
-    if (ri >= a.n_req * a.max_new) return;
-    const uint32_t r = (uint32_t)ri / (uint32_t)a.max_new;
-    const int i = (int)((uint32_t)ri - r * (uint32_t)a.max_new);
+    if (ri >= (a.searched ? a.searched : a.n_req * a.max_new)) return;
+    const TokenPlace at = token_place(a, (uint32_t)ri);
+    if (at.r < 0) return;
+    const int64_t r = at.r;
     const Request rq = request_of(a, r);
-    if (i >= rq.rows) return;
+    const int i = at.i < 0 ? (int)ri - rq.start : at.i;
+    if ((uint32_t)i >= (uint32_t)rq.rows) return;   // (negative: of starts out of order)
     const int64_t token = rq.start + i;
     const int32_t* list = a.listed + (token * a.heads + h) * a.n_listed;
     int n = 0;   // entries up to the last that names a page
@@ -1023,11 +1074,18 @@ bool picked_at_once(const fkv_page_desc* p, const fkv_select_desc* t)
 
 constexpr int kHeldPages = 16384;   // that the waves of a row hold at the most: 16 of 16 x 64
 
-// How the splits of an item's list are chosen: see fkv_page_attend_selected.
+// Places for tokens in a launch, and whether their requests are looked up: where that spares half of them.
+int64_t searched_rows(int64_t n_req, int64_t max_new, int64_t n_tokens)
+{
+    n_tokens = std::max(n_tokens, (int64_t)1);
+    return n_req * max_new >= 2 * n_tokens ? n_tokens : 0;
+}
+
 struct ListedShape {
     int waves;       // of an item in a block
     int n_splits;
     int64_t blocks;  // times the splits
+    int64_t searched;
     bool join_blocks;
 };
 
@@ -1036,7 +1094,8 @@ ListedShape listed_shape(const fkv_page_desc* p, const fkv_attend_desc* t, int64
     ListedShape s;
     const int64_t group = t->q_heads / p->heads;
     const int64_t of_token = p->heads * ((group + kFewRows - 1) / kFewRows);
-    const int64_t tokens = std::min(t->n_req * t->max_new, (int64_t)1 << 34);   // (2^34 are too many, whatever the heads)
+    s.searched = searched_rows(t->n_req, t->max_new, t->n_tokens);
+    const int64_t tokens = s.searched ? s.searched : t->n_req * t->max_new;   // below 2^31
     const int64_t items = tokens * of_token;
     const int64_t tiles = (n_listed * (p->page / 16) + 3) / 4;
     // A wave an item where the items fill the chip, else four.  Of few items with up to 32 tiles eight waves have up to four tiles
@@ -1101,8 +1160,10 @@ extern "C" int fkv_page_select(const fkv_page_desc* desc, const fkv_select_desc*
     a.n_select = select->n_select, a.keep_first = select->keep_first, a.keep_last = select->keep_last;
     const int64_t pages = most_pages(desc, select);
     const hipStream_t st = (hipStream_t)stream;
-    if (a.n_req > kMostBlocks / a.max_new || a.n_req * a.max_new > kMostBlocks / a.heads) return FKV_ERR_UNSUPPORTED;
-    const int64_t rows = a.n_req * a.max_new * a.heads;
+    a.searched = searched_rows(a.n_req, a.max_new, a.n_tokens);
+    const int64_t tokens = a.searched ? a.searched : a.n_req * a.max_new;   // below 2^31
+    if (tokens > kMostBlocks / a.heads) return FKV_ERR_UNSUPPORTED;
+    const int64_t rows = tokens * a.heads;
     const bool e4m3 = desc->format == FKV_PAGE_E4M3;
     a.lanes_log = lanes_log(a.group);
     if (picked_at_once(desc, select)) {
@@ -1122,15 +1183,19 @@ extern "C" int fkv_page_select(const fkv_page_desc* desc, const fkv_select_desc*
         const int64_t row_tiles = (a.max_new + (16 >> a.lanes_log) - 1) / (16 >> a.lanes_log);
         const bool many = a.group > 16 || row_tiles >= 4;   // four row tiles a block
         a.row_groups = a.group > 16 || !many ? row_tiles : (row_tiles + 3) / 4;
+        const int64_t per = a.group > 16 ? 1 : (many ? 4 : 1) * (16 >> a.lanes_log);   // tokens of a group
+        const int64_t found = a.n_tokens / per + (per > 1 ? a.n_req : 0), in_order = a.n_req * a.row_groups;
+        a.searched_groups = in_order >= 2 * found ? found : 0;
+        const int64_t groups = a.searched_groups ? found : in_order;   // below 2^32
         const int64_t tiles = (pages + 15) / 16;
         // as many page tiles a wave as leave the chip eight thousand waves, where rounding the rows is to be shared.  With 2
         // and 8 a wave (us): a chunk of 4096 tokens over 512 pages 136 and 104, 512 tokens over 256 pages 20 and 23; few rows,
         // 16 contexts of 2048 pages 28.7 and 28.1, 64 of up to 2048 pages 27 and 34, one of 16,384 pages 32 and 35.
-        int64_t wave_tiles = std::min(tiles * a.row_groups, (int64_t)1 << 30) * std::min(a.n_req * a.heads, (int64_t)1 << 30) / 8192;
+        int64_t wave_tiles = std::min(groups * a.heads, (int64_t)1 << 40) * tiles / 8192;
         wave_tiles = many ? std::min((int64_t)8, std::max((int64_t)2, wave_tiles)) : 2;
         a.wave_tiles = (int32_t)wave_tiles;
         a.tile_chunks = (int32_t)((tiles + wave_tiles * kWaves - 1) / (wave_tiles * kWaves));
-        const int64_t blocks = a.n_req * a.heads * a.row_groups;   // (row groups are no more than max_new)
+        const int64_t blocks = groups * a.heads;
         if (blocks > kMostBlocks / a.tile_chunks) return FKV_ERR_UNSUPPORTED;
         auto go = [&](auto kern) {
             hipLaunchKernelGGL(kern, dim3((unsigned)(blocks * a.tile_chunks)), dim3(kThreads), 0, st, a);
@@ -1196,9 +1261,9 @@ extern "C" int fkv_page_attend_selected(const fkv_page_desc* desc, const fkv_att
     const ListedShape s = listed_shape(desc, attend, n_selected);
     const Workspace ws = listed_workspace(desc, attend, s);
     if (ws.bytes && (!workspace || workspace_bytes < ws.bytes)) return FKV_ERR_SCRATCH_TOO_SMALL;
-    if (s.blocks > kMostBlocks / s.n_splits || attend->n_req * attend->max_new > kMostBlocks) return FKV_ERR_UNSUPPORTED;
+    if (s.blocks > kMostBlocks / s.n_splits) return FKV_ERR_UNSUPPORTED;
     AttendArgs a = attend_args(desc, attend, k_codes, v_codes, scales, q, tables, kv_len, q_start, slopes, prefix, first, out, lse);
-    a.listed = selected, a.n_listed = n_selected;
+    a.listed = selected, a.n_listed = n_selected, a.searched = s.searched;
     a.part = (float*)workspace;
     a.stat = (float2*)((uint8_t*)workspace + ws.stat);
     a.n_splits = s.n_splits;

@@ -88,6 +88,8 @@ SELECTS = [
     (16, 64, 1, 16, INT8, F16, [(16 * 2100, 1), (16 * 3000 - 3, 1), (20, 1)], 30, 1, 1),  # all of a block's waves a row
     (16, 128, 1, 16, E4M3, F16, [(16 * 16384 - 9, 1)], 100, 1, 1),
     (16, 2, 4, 128, INT8, F16, [(16 * 900, 17), (16 * 2200, 1)], 100, 1, 1),
+    (16, 1, 1, 128, INT8, F16, [(16 * 512, 64)], 20, 1, 1),                               # the most of a block's LDS
+    (16, 2, 4, 64, E4M3, BF16, [(16 * 90, 1), (16 * 40, 130), (700, 1), (0, 0), (16 * 33, 2)], 12, 1, 1),   # few rows and many
 ]
 
 
@@ -246,6 +248,7 @@ ATTENDS = [
     (128, 1, 9, 64, E4M3, BF16, [(128 * 20, 2)], 13),
     (16, 4, 2, 64, INT8, F16, [(400, 300)], 4),                 # a wave an item
     (64, 4, 4, 128, INT8, BF16, [(700, 450), (300, 300)], 3),
+    (64, 2, 4, 64, INT8, BF16, [(700, 1), (300, 200), (0, 0), (64, 1), (500, 3)], 4),   # few rows and many
 ]
 
 

@@ -94,7 +94,7 @@ def test_select_scratch(F):
 def test_select_of_too_many_rows(F):
     desc = F.fkv_page_desc(8, 16, 2, 64, 0)
     for kw in (dict(n_req=1 << 30), dict(n_req=1 << 20, max_new=1 << 20), dict(max_new=1 << 30)):
-        t = select_desc(F, **kw)
+        t = select_desc(F, **{**dict(n_tokens=1 << 30), **kw})
         assert F.lib.fkv_page_select(ref(desc), ref(t), g, g, g, g, g, g, g, g, 1 << 40, None) == F.FKV_ERR_UNSUPPORTED, kw
 
 
@@ -121,7 +121,8 @@ def test_attend_selected_arguments(F):
                dict(max_kv=-1), dict(max_pages=0), dict(n_req=-1), dict(n_tokens=-1), dict(q_stride_token=4), dict(o_stride_head=-8)):
         assert attend(**kw) == E, kw
     assert attend(n_req=0, q=None, out=None) == 0 and attend(n_tokens=0, q=None) == 0
-    for kw in (dict(n_req=1 << 30, max_new=1 << 30), dict(max_new=1 << 30, q_heads=65534), dict(n_req=1 << 30, q_heads=65534)):
+    for kw in (dict(n_req=1 << 30, max_new=1 << 30, q_heads=65534), dict(max_new=1 << 30, q_heads=65534), dict(n_req=1 << 30, q_heads=65534)):
+        kw = {**dict(n_tokens=1 << 30), **kw}
         assert attend(**kw) == F.FKV_ERR_UNSUPPORTED, kw
 
 
