@@ -90,6 +90,8 @@ SELECTS = [
     (16, 2, 4, 128, INT8, F16, [(16 * 900, 17), (16 * 2200, 1)], 100, 1, 1),
     (16, 1, 1, 128, INT8, F16, [(16 * 512, 64)], 20, 1, 1),                               # the most of a block's LDS
     (16, 2, 4, 64, E4M3, BF16, [(16 * 90, 1), (16 * 40, 130), (700, 1), (0, 0), (16 * 33, 2)], 12, 1, 1),   # few rows and many
+    (16, 2, 2, 32, INT8, F16, [(33, 0)] * 70 + [(160, 9)] + [(17, 0)] * 64 + [(100, 1), (100, 1)] + [(0, 0)] * 200 + [(90, 40)], 3, 1, 1),
+    (16, 1, 20, 16, E4M3, F16, [(90, 0)] * 4100 + [(120, 3), (20, 0), (99, 1)] + [(1, 0)] * 40 + [(80, 1)], 2, 0, 1),
 ]
 
 
@@ -249,6 +251,8 @@ ATTENDS = [
     (16, 4, 2, 64, INT8, F16, [(400, 300)], 4),                 # a wave an item
     (64, 4, 4, 128, INT8, BF16, [(700, 450), (300, 300)], 3),
     (64, 2, 4, 64, INT8, BF16, [(700, 1), (300, 200), (0, 0), (64, 1), (500, 3)], 4),   # few rows and many
+    (16, 2, 2, 32, INT8, F16, [(33, 0)] * 70 + [(160, 9)] + [(17, 0)] * 64 + [(100, 1), (100, 1)] + [(0, 0)] * 200 + [(90, 40)], 3),
+    (16, 1, 20, 16, E4M3, F16, [(90, 0)] * 4100 + [(120, 3), (20, 0), (99, 1)] + [(1, 0)] * 40 + [(80, 1)], 5),
 ]
 
 
