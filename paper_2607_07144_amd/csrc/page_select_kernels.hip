@@ -664,36 +664,45 @@ struct ListedQuery : FewQuery<NC> {
     }
 };
 
-// PLAIN: neither cap nor bias.
-template <bool E4M3, int NC, bool PLAIN>
+// PLAIN: neither cap nor bias.  U: of few rows the operands' 16 columns hold each U times
+// over, and column u of a row's takes the u-th part of every 16 keys, as a wave of its own
+// would: its weights are 0 elsewhere.
+template <bool E4M3, int NC, bool PLAIN, int U>
 __device__ __forceinline__ void listed_update(const AttendArgs& a, const Request& rq, const Seen& mine, const ListedQuery<NC>& q,
                                               FewSums<NC>& st, float4_t (&s)[4], uint4 (&vw)[4 * NC], float2 sc, bool here, bool mask, int j0g)
 {
+    constexpr int N = 16 / U;   // keys
+    const int u = (threadIdx.x & 15) / N;
+    const int j0 = j0g + u * N;
     float c = fmaxf(q.mul * sc.x, 0x1p-120f);   // a score's factor (never 0: hidden scores are infinite)
-    float x[16];
+    float x[N];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = s[i >> 2][i & 3];
+    for (int i = 0; i < N; ++i) {
+        x[i] = s[i >> 2][i & 3];
+#pragma unroll
+        for (int k = 1; k < U; ++k) x[i] = u == k ? s[(k * N + i) >> 2][i & 3] : x[i];
+    }
     if (!PLAIN && (q.cap > 0.0f || q.slopes)) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] *= c;
+        for (int i = 0; i < N; ++i) x[i] *= c;
         if (q.large_cap) {
             const float inv = 1.0f / q.cap2;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = capped_large(x[i], q.cap2, inv);
+            for (int i = 0; i < N; ++i) x[i] = capped_large(x[i], q.cap2, inv);
         } else if (q.cap > 0.0f) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = capped(x[i], q.cap2);
+            for (int i = 0; i < N; ++i) x[i] = capped(x[i], q.cap2);
         }
         if (q.slopes) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] -= q.slope2 * fabsf((float)(j0g + i - q.pos));
+            for (int i = 0; i < N; ++i) x[i] -= q.slope2 * fabsf((float)(j0 + i - q.pos));
         }
         c = 1.0f;
     }
     if (mask) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if (!here || !visible(a, mine, j0g + i)) x[i] = -__builtin_inff();
+        for (int i = 0; i < N; ++i)
+            if (!here || !visible(a, mine, j0 + i)) x[i] = -__builtin_inff();
         if (E4M3) {   // codes after the last key may be anything, a NaN among it
             const int n = here ? rq.kv - j0g : 0;
 #pragma unroll
@@ -702,8 +711,8 @@ __device__ __forceinline__ void listed_update(const AttendArgs& a, const Request
     }
     float top = x[0];
 #pragma unroll
-    for (int i = 1; i < 16; ++i) top = __builtin_elementwise_maximum(top, x[i]);
-    const float vtop = top > -__builtin_inff() ? sc.y : 0.0f;   // of a group of which the row sees a key
+    for (int i = 1; i < N; ++i) top = __builtin_elementwise_maximum(top, x[i]);
+    const float vtop = top > -__builtin_inff() ? sc.y : 0.0f;   // of a group of which the column sees a key
     top = rows_max(top * c);
     if (__any(top > st.m + kSlack || vtop > st.vref)) {
         const float vnew = rows_max(fmaxf(st.vref, vtop));
@@ -719,19 +728,24 @@ __device__ __forceinline__ void listed_update(const AttendArgs& a, const Request
     const float m0 = st.m == -__builtin_inff() ? 0.0f : st.m;
     const float v = __builtin_amdgcn_fmed3f(sc.y * (kTop * __builtin_amdgcn_rcpf(st.vref)), 0x1p-40f, kTop);   // (more only where all weights are 0)
     const float vb = __builtin_amdgcn_logf(v) - m0;
-    half8_t p[2];
+    uint32_t p[8];   // the 16 keys' weights
     float sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, vb));
-        sum += w;
-        p[i >> 3][i & 7] = (_Float16)w;
+    for (int i = 0; i < N; i += 2) {
+        const float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, vb)), w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i + 1], c, vb));
+        sum += w0;
+        sum += w1;
+        const half2_t two = {(_Float16)w0, (_Float16)w1};
+#pragma unroll
+        for (int k = 0; k < U; ++k) p[(k * N + i) / 2] = U == 1 || u == k ? __builtin_bit_cast(uint32_t, two) : 0u;
     }
     st.l = __builtin_fmaf(sum, __builtin_amdgcn_rcpf(v), st.l);
+    const half8_t p0 = __builtin_bit_cast(half8_t, make_uint4(p[0], p[1], p[2], p[3]));
+    const half8_t p1 = __builtin_bit_cast(half8_t, make_uint4(p[4], p[5], p[6], p[7]));
 #pragma unroll
     for (int t = 0; t < 4 * NC; ++t) {
-        st.acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(vw[t].x, vw[t].y), p[0], st.acc[t], 0, 0, 0);
-        st.acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(vw[t].z, vw[t].w), p[1], st.acc[t], 0, 0, 0);
+        st.acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(vw[t].x, vw[t].y), p0, st.acc[t], 0, 0, 0);
+        st.acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(vw[t].z, vw[t].w), p1, st.acc[t], 0, 0, 0);
     }
 }
 
@@ -763,7 +777,7 @@ __device__ __forceinline__ ListPlace place_listed(const AttendArgs& a, const int
 // A wave over the tiles e0, e0 + step, .. below e1 (one at least) of a list of `places`
 // groups, for rows of one token.  Any pages: a lane group looks up its own group's.  The
 // entries are read two tiles ahead, the pages' ids one.
-template <bool E4M3, int NC, bool PLAIN>
+template <bool E4M3, int NC, bool PLAIN, int U>
 __device__ __forceinline__ void listed_groups(const AttendArgs& a, const Request& rq, int64_t r, int h, const FewRow& fr, int e0, int step,
                                               int e1, FewSums<NC>& st, const int32_t* list, int places)
 {
@@ -824,19 +838,78 @@ __device__ __forceinline__ void listed_groups(const AttendArgs& a, const Request
             ck2 = entry(e + 3 * step, gk);
             cv2 = entry(e + 3 * step, g);
         }
-        listed_update<E4M3, NC, PLAIN>(a, rq, mine, query, st, s, vw, sc, here, mask, j0g);
+        listed_update<E4M3, NC, PLAIN, U>(a, rq, mine, query, st, s, vw, sc, here, mask, j0g);
         sc = sc_next;
     }
     st.l = rows_sum(st.l);
 }
 
+template <int NC> constexpr int kKeyBytes = 4 * NC * 1024;   // of a wave's LDS
+
+// A tile's keys in LDS, 64 rows of d / 16 16-byte chunks, on their way there without registers: a left operand takes 16 rows
+// at a time, of which no two lie in a line, and read from memory so a load holds the cache's address unit for 64 cycles, not 16
+// (a chunk of 4096 tokens with lists of 16 pages of 64 x 128, 8 heads: the unit 93% busy and 620 us, so XX).  A row's chunks are
+// turned by a number of places so that 16 rows' reads fall into different banks.
+template <int NC>
+struct KeyTile {
+    uint8_t* lds;
+    uint32_t from[4 * NC];   // where in the tile this lane's 16 bytes of a load lie
+    uint32_t at[NC];         // its first operand's chunk in LDS
+    uint32_t chunks;
+    __device__ __forceinline__ KeyTile(uint8_t* lds_, int d) : lds(lds_), chunks(d >> 4)
+    {
+        const uint32_t lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
+        auto places = [&](uint32_t row) {
+            const uint32_t n = NC == 1 ? row >> 4 : NC == 2 ? (row >> 1 & 1) + 2 * (row >> 4) : (row & 3) + 4 * (row >> 4);
+            return n < chunks ? n : 0;
+        };
+        uint32_t to_row = lane / chunks, to = lane - to_row * chunks;
+        const uint32_t rows = 64 / chunks, rest = 64 - rows * chunks;
+#pragma unroll
+        for (int i = 0; i < 4 * NC; ++i) {
+            const uint32_t source = min(to_row, 63u), n = places(source);   // (rows of fewer than 4 NC chunks: some loads for nothing)
+            from[i] = (source * chunks + (to >= n ? to - n : to + chunks - n)) * 16;
+            to_row += rows;
+            to += rest;
+            if (to >= chunks) to -= chunks, ++to_row;
+        }
+        const uint32_t row = (c16 >> 2) * 16 + (c16 & 3), n = places(row);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const uint32_t chunk = min(4 * c + g, chunks - 1) + n;   // channels beyond d are taken from the last ones: q is zero there
+            at[c] = (row * chunks + (chunk >= chunks ? chunk - chunks : chunk)) * 16;
+        }
+    }
+    __device__ __forceinline__ void fetch(const uint8_t* keys) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4 * NC; ++i) {
+            uint32_t offset = from[i];
+            asm("" : "+v"(offset));   // (32 bits beside an address in scalar registers)
+            __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1)))*)(keys + offset),
+                                             (void __attribute__((address_space(3)))*)(lds + i * 1024), 16, 0, 0);
+        }
+    }
+    __device__ __forceinline__ void read(uint4 (&kw)[4][NC]) const
+    {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // fetched
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) kw[t][c] = *(const uint4*)(lds + at[c] + t * 64 * chunks);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // and read: the next ones may come
+    }
+};
+
 // The same of pages of a multiple of 64 tokens: a tile lies in one page, so
 // that its place and scales are the same in all lanes; they are looked up in scalar
 // registers, and the loads of codes take their addresses from there and from offsets that
 // stay as they are.  The entries are read two tiles ahead, the pages' ids and scales one.
-template <bool E4M3, int NC, bool PLAIN>
+// THROUGH: the keys go through LDS; where few items wait for their tiles in turn the way
+// there is longer than it is worth (16 requests with 32 pages each, 8 heads: 34.2 us, 32.9).
+template <bool E4M3, int NC, bool PLAIN, int U, bool THROUGH>
 __device__ __forceinline__ void whole_tiles(const AttendArgs& a, const Request& rq, int64_t r, int h, const FewRow& fr, int e0, int step,
-                                            int e1, FewSums<NC>& st, const int32_t* list)
+                                            int e1, FewSums<NC>& st, const int32_t* list, uint8_t* lds)
 {
     const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
     const int d = a.d;
@@ -847,11 +920,6 @@ __device__ __forceinline__ void whole_tiles(const AttendArgs& a, const Request& 
     mine.wlo = __builtin_amdgcn_readfirstlane(mine.wlo);
     const int32_t* table = a.tables + r * a.max_pages;
     const uint32_t columns = (uint32_t)pages_of(a, rq.kv);
-    // channels beyond d are loaded from the last ones: q is zero there, and their sums go nowhere
-    uint32_t kc[NC];
-#pragma unroll
-    for (int c = 0; c < NC; ++c) kc[c] = (c16 >> 2) * 16 * d + (c16 & 3) * d + min(c * 64 + g * 16, d - 16);
-    const uint32_t vc = g * 16 * d + c16 * 16;
     // (an offset of 32 bits beside an address in scalar registers, as loads take them; widened outside of the loop, each
     // load would have an address of its own in vector registers)
     auto here_of = [](uint32_t offset) {
@@ -859,63 +927,87 @@ __device__ __forceinline__ void whole_tiles(const AttendArgs& a, const Request& 
         return offset;
     };
     struct Tile {
+        int64_t at;   // its codes, of keys as of values
+        float2 scales;
+        int pos;
+        bool here;
+    };
+    struct Place {
         int id, pos, in_page;   // in_page: 16-token groups
         bool here;
     };
     auto column = [&](int e) { return scalar_load(list + list_entry(a, 4 * min(e, e1 - 1))); };
     auto place = [&](int e, int col) {
-        Tile t;
+        Place p;
         const int at = 4 * min(e, e1 - 1);
-        t.in_page = at - list_entry(a, at) * (int)a.per_page;
-        t.here = (uint32_t)col < columns;
-        col = t.here ? col : 0;
-        t.pos = (col * (int)a.per_page + t.in_page) * 16;
-        t.id = scalar_load(table + col);
+        p.in_page = at - list_entry(a, at) * (int)a.per_page;
+        p.here = (uint32_t)col < columns;
+        col = p.here ? col : 0;
+        p.pos = (col * (int)a.per_page + p.in_page) * 16;
+        p.id = scalar_load(table + col);
+        return p;
+    };
+    auto tile_of = [&](const Place& p) {
+        Tile t;
+        t.here = p.here && (uint32_t)p.id < (uint64_t)a.n_pages;
+        const int64_t of_head = (t.here ? p.id : 0) * (int64_t)a.heads + h;
+        t.at = of_head * per_head + p.in_page * 16 * d;
+        t.scales = __builtin_bit_cast(float2, scalar_load((const uint64_t*)(a.scales + of_head)));
+        t.pos = p.pos;
         return t;
     };
-    auto check = [&](Tile& t) {
-        t.here = t.here && (uint32_t)t.id < (uint64_t)a.n_pages;
-        t.id = t.here ? t.id : 0;
-    };
-    uint4 kw[4][NC];
+    // channels beyond d are loaded from the last ones: q is zero there, and their sums go nowhere
+    uint32_t kc[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) kc[c] = (c16 >> 2) * 16 * d + (c16 & 3) * d + min(c * 64 + g * 16, d - 16);
+    const uint32_t vc = g * 16 * d + c16 * 16;
+    const KeyTile<NC> keys(lds, d);
+    uint4 kw[4][NC], vw[4 * NC];
     auto load_keys = [&](const Tile& t) {
-        const uint8_t* kp = a.k_codes + ((int64_t)t.id * a.heads + h) * per_head + t.in_page * 16 * d;
+        const uint8_t* kp = a.k_codes + t.at;
+        if constexpr (THROUGH) {
+            keys.fetch(kp);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int c = 0; c < NC; ++c) kw[i][c] = *(const uint4*)(kp + i * 4 * d + here_of(kc[c]));
+                for (int c = 0; c < NC; ++c) kw[i][c] = *(const uint4*)(kp + i * 4 * d + here_of(kc[c]));
+        }
     };
-    auto scales_of = [&](const Tile& t) {
-        const float2 sc = __builtin_bit_cast(float2, scalar_load((const uint64_t*)(a.scales + (int64_t)t.id * a.heads + h)));
-        return t.here ? sc : make_float2(0.0f, 0.0f);
+    auto load_values = [&](const Tile& t) {
+        const uint8_t* vp = a.v_codes + t.at;
+#pragma unroll
+        for (int i = 0; i < 4 * NC; ++i) vw[i] = *(const uint4*)(vp + min(i * 16, d - 16) * 16 + here_of(vc));
     };
     const int c0 = column(e0), c1 = column(e0 + step);
     int c2 = column(e0 + 2 * step);
-    Tile now = place(e0, c0), next = place(e0 + step, c1);
-    check(now);
+    const Place p0 = place(e0, c0);
+    Place next = place(e0 + step, c1);
+    Tile now = tile_of(p0);
     load_keys(now);
-    float2 sc = scales_of(now);
     const ListedQuery<NC> query(a, rq, fr);
     for (int e = e0; e < e1; e += step) {
-        uint4 vw[4 * NC];
-        const uint8_t* vp = a.v_codes + ((int64_t)now.id * a.heads + h) * per_head + now.in_page * 16 * d;
-#pragma unroll
-        for (int t = 0; t < 4 * NC; ++t) vw[t] = *(const uint4*)(vp + min(t * 16, d - 16) * 16 + here_of(vc));
-        const bool here = now.here;
-        const int j0 = now.pos;
-        const bool mask = !here || j0 < mine.lo || j0 + kTile > mine.hi || (a.window && j0 < mine.wlo && j0 + kTile > a.sinks);
-        float4_t s[4];
-        few_products<E4M3, NC>(kw, query, s);
-        const float2 sc_now = sc;
-        if (e + step < e1) {
-            check(next);
-            load_keys(next);
-            sc = scales_of(next);
-            now = next;
+        const Tile tile = now;
+        auto advance = [&] {
+            now = tile_of(next);   // (behind the last tile that one again, but its keys)
+            if (e + step < e1) load_keys(now);
             next = place(e + 2 * step, c2);
             c2 = column(e + 3 * step);
+        };
+        float4_t s[4];
+        if constexpr (THROUGH) {   // (loads arrive in their order: the next tile's keys first, and with the values they are there)
+            keys.read(kw);
+            advance();
+            load_values(tile);
+            few_products<E4M3, NC>(kw, query, s);
+        } else {
+            load_values(tile);
+            few_products<E4M3, NC>(kw, query, s);
+            advance();
         }
-        listed_update<E4M3, NC, PLAIN>(a, rq, mine, query, st, s, vw, sc_now, here, mask, j0 + g * 16);
+        const bool mask = !tile.here || tile.pos < mine.lo || tile.pos + kTile > mine.hi || (tile.pos < mine.wlo && tile.pos + kTile > a.sinks);
+        const float2 sc = tile.here ? tile.scales : make_float2(0.0f, 0.0f);
+        listed_update<E4M3, NC, PLAIN, U>(a, rq, mine, query, st, s, vw, sc, tile.here, mask, tile.pos + g * 16);
     }
     st.l = rows_sum(st.l);
 }
@@ -923,13 +1015,14 @@ __device__ __forceinline__ void whole_tiles(const AttendArgs& a, const Request& 
 // W waves an item -- a token, a KV head and up to 16 of its query heads -- that take
 // the list's tiles in turn, with those of the item's other splits; their sums joined
 // in LDS, and the splits' by a second kernel.
-template <bool E4M3, int NC, int W, bool WHOLE, bool PLAIN>
+template <bool E4M3, int NC, int W, bool WHOLE, bool PLAIN, int U>
 __global__ __launch_bounds__(W > kWaves ? 64 * W : kThreads, NC == 2 && WHOLE && W <= kWaves ? 3 : NC <= 2 ? 2 : 1) void attend_listed_kernel(AttendArgs a)
 {
     extern __shared__ __align__(16) float lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c16 = lane & 15, g = lane >> 4;
-    const int d = a.d;
+    constexpr int kColumns = kFewRows / U;   // that hold the rows once
+    const int d = a.d, row = c16 & (kColumns - 1);
     const int64_t q_heads = (int64_t)a.heads * a.group;
     const int split = (int)(blockIdx.x % (uint32_t)a.n_splits);
     const uint32_t block = blockIdx.x / (uint32_t)a.n_splits;
@@ -958,15 +1051,34 @@ __global__ __launch_bounds__(W > kWaves ? 64 * W : kThreads, NC == 2 && WHOLE &&
         }
     const int places = n * (int)a.per_page, tiles = (places + 3) >> 2;
     const int n_rows = min(a.group - chunk * kFewRows, kFewRows);
-    const FewRow fr = {min(c16, n_rows - 1), i, h * a.group + chunk * kFewRows + min(c16, n_rows - 1)};
+    const FewRow fr = {min(row, n_rows - 1), i, h * a.group + chunk * kFewRows + min(row, n_rows - 1)};
     FewSums<NC> st;
     const int e0 = split * W + (W == 1 ? 0 : wave);
     if (e0 < tiles) {
-        if constexpr (WHOLE) whole_tiles<E4M3, NC, PLAIN>(a, rq, r, h, fr, e0, a.n_splits * W, tiles, st, list);
-        else listed_groups<E4M3, NC, PLAIN>(a, rq, r, h, fr, e0, a.n_splits * W, tiles, st, list, places);
+        if constexpr (WHOLE) whole_tiles<E4M3, NC, PLAIN, U, W == 1>(a, rq, r, h, fr, e0, a.n_splits * W, tiles, st, list, (uint8_t*)lds + wave * kKeyBytes<NC>);
+        else listed_groups<E4M3, NC, PLAIN, U>(a, rq, r, h, fr, e0, a.n_splits * W, tiles, st, list, places);
     }
 
     if (W == 1) {
+        if (U > 1) {   // a row's columns together
+            auto over_columns = [](float x, auto join) {
+                x = join(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x128, 0xf, 0xf, false)));   // 8 lanes on
+                if (U > 2) x = join(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x124, 0xf, 0xf, false)));
+                return x;
+            };
+            auto sum = [](float x, float y) { return x + y; };
+            auto most = [](float x, float y) { return fmaxf(x, y); };
+            const float m = over_columns(st.m, most), vref = over_columns(st.vref, most);
+            const float k = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(st.m - m);
+            st.l = over_columns(st.l * k, sum);
+            const float kv = k * (st.vref / vref);
+#pragma unroll
+            for (int t = 0; t < 4 * NC; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) st.acc[t][e] = over_columns(st.acc[t][e] * kv, sum);
+            st.m = m;
+            st.vref = vref;
+        }
         if (c16 >= n_rows) return;
         const float inv = st.l == 0.0f ? 0.0f : st.vref * (1.0f / kTop) / st.l;
 #pragma unroll
@@ -1277,14 +1389,20 @@ extern "C" int fkv_page_attend_selected(const fkv_page_desc* desc, const fkv_att
         auto go = [&](auto kern, size_t shm) {
             hipLaunchKernelGGL(kern, dim3((unsigned)(s.blocks * s.n_splits)), dim3(s.waves == 1 ? kThreads : 64 * s.waves), shm, st, a);
         };
-        const size_t shm = s.waves == 1 ? 0 : (2 * s.waves * kFewRows + (size_t)s.waves * kFewRows * (a.d + 4)) * sizeof(float);
+        const size_t shm = s.waves == 1 ? a.page % kTile ? 0 : (size_t)kWaves * kKeyBytes<NC>
+                                        : (2 * s.waves * kFewRows + (size_t)s.waves * kFewRows * (a.d + 4)) * sizeof(float);
         auto of_form = [&](auto whole, auto plain) {
             constexpr bool WHOLE = decltype(whole)::value, PLAIN = decltype(plain)::value;
-            if (s.waves == 1) return e4m3 ? go(attend_listed_kernel<true, NC, 1, WHOLE, PLAIN>, shm) : go(attend_listed_kernel<false, NC, 1, WHOLE, PLAIN>, shm);
+            auto of_waves = [&](auto w, auto u) {
+                constexpr int W = decltype(w)::value, U = decltype(u)::value;
+                e4m3 ? go(attend_listed_kernel<true, NC, W, WHOLE, PLAIN, U>, shm) : go(attend_listed_kernel<false, NC, W, WHOLE, PLAIN, U>, shm);
+            };
+            const std::integral_constant<int, 1> one;
+            if (s.waves == 1) return a.group <= 4 ? of_waves(one, std::integral_constant<int, 4>{}) : of_waves(one, one);
             if constexpr (NC <= 2) {
-                if (s.waves == 8) return e4m3 ? go(attend_listed_kernel<true, NC, 8, WHOLE, PLAIN>, shm) : go(attend_listed_kernel<false, NC, 8, WHOLE, PLAIN>, shm);
+                if (s.waves == 8) return of_waves(std::integral_constant<int, 8>{}, one);
             }
-            e4m3 ? go(attend_listed_kernel<true, NC, kWaves, WHOLE, PLAIN>, shm) : go(attend_listed_kernel<false, NC, kWaves, WHOLE, PLAIN>, shm);
+            of_waves(std::integral_constant<int, kWaves>{}, one);
         };
         const bool plain = a.softcap == 0.0f && !a.slopes;
         if (a.page % kTile == 0) plain ? of_form(std::true_type{}, std::true_type{}) : of_form(std::true_type{}, std::false_type{});
