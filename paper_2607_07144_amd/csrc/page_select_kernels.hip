@@ -294,7 +294,9 @@ __device__ __forceinline__ void score_block(const SelectArgs& a, const Request& 
     }
 }
 
-// Many rows or many pages: the scores go to the workspace.  A block R row tiles, a wave of it
+// Many rows or many pages: the scores go to the workspace (16 contexts of 2048 pages, 8 heads
+// of 128: 67 MB of boxes, 17.5 us, 3.8 TB/s; a chunk's rows over 512 pages: 52 us, the vector
+// unit's, that turns sums to scores and joins the heads).  A block R row tiles, a wave of it
 // a quarter of the block's page tiles.
 template <bool E4M3, int NC, int R, bool WIDE>
 __global__ __launch_bounds__(kThreads, R == 1 || NC == 1 ? 4 : NC == 2 ? 3 : 2) void page_score_kernel(SelectArgs a)
@@ -642,8 +644,11 @@ __global__ __launch_bounds__(kWideThreads) void page_select_wide_kernel(SelectAr
 // ----------------------------------------------------- attention to lists --
 
 // A tile is four groups of 16 keys of the listed pages; its order of work is that of
-// few_keys.  Lists of pages that many tokens share come from the caches, and what bounds
-// them is the vector unit: so a weight with its value scale is one power of two,
+// few_keys.  Single tokens' lists come from memory (16 requests with 32 pages of 64 x 128, 8
+// heads: 135 MB in 30 us, 4.5 TB/s).  Lists that many tokens share come from the caches, and
+// what bounds them is the vector unit (a chunk of 4096 tokens with 16 pages each: 0.12 PFLOP/s,
+// the unit 85% busy; 320 of a tile's 420 instructions widen int8 codes to binary16, once for
+// each token: lists differ): so a weight with its value scale is one power of two,
 // 2^(s c - m + log2 v), as in the kernel for many rows: v = vs 2^8 / vr is held at 2^-40 from
 // below, and a sum over v is what l wants.
 template <int NC>
@@ -666,7 +671,8 @@ struct ListedQuery : FewQuery<NC> {
 
 // PLAIN: neither cap nor bias.  U: of few rows the operands' 16 columns hold each U times
 // over, and column u of a row's takes the u-th part of every 16 keys, as a wave of its own
-// would: its weights are 0 elsewhere.
+// would: its weights are 0 elsewhere.  (Of groups of four the chunk took 632 us without and 619 with it; where a block's waves
+// are joined in LDS, four times the parts cost one token over 32 pages 1 of 16 us.)
 template <bool E4M3, int NC, bool PLAIN, int U>
 __device__ __forceinline__ void listed_update(const AttendArgs& a, const Request& rq, const Seen& mine, const ListedQuery<NC>& q,
                                               FewSums<NC>& st, float4_t (&s)[4], uint4 (&vw)[4 * NC], float2 sc, bool here, bool mask, int j0g)
@@ -848,7 +854,7 @@ template <int NC> constexpr int kKeyBytes = 4 * NC * 1024;   // of a wave's LDS
 
 // A tile's keys in LDS, 64 rows of d / 16 16-byte chunks, on their way there without registers: a left operand takes 16 rows
 // at a time, of which no two lie in a line, and read from memory so a load holds the cache's address unit for 64 cycles, not 16
-// (a chunk of 4096 tokens with lists of 16 pages of 64 x 128, 8 heads: the unit 93% busy and 620 us, so XX).  A row's chunks are
+// (a chunk of 4096 tokens with lists of 16 pages of 64 x 128, 8 heads: the unit 93% busy and 620 us, so 570).  A row's chunks are
 // turned by a number of places so that 16 rows' reads fall into different banks.
 template <int NC>
 struct KeyTile {
