@@ -644,7 +644,7 @@ __global__ __launch_bounds__(kWideThreads) void page_select_wide_kernel(SelectAr
 // ----------------------------------------------------- attention to lists --
 
 // A tile is four groups of 16 keys of the listed pages; its order of work is that of
-// few_keys.  Single tokens' lists come from memory (16 requests with 32 pages of 64 x 128, 8
+// few_keys.  Single tokens' lists come from memory (16 requests with 64 pages of 64 x 128, 8
 // heads: 135 MB in 30 us, 4.5 TB/s).  Lists that many tokens share come from the caches, and
 // what bounds them is the vector unit (a chunk of 4096 tokens with 16 pages each: 0.12 PFLOP/s,
 // the unit 85% busy; 320 of a tile's 420 instructions widen int8 codes to binary16, once for
@@ -912,7 +912,7 @@ struct KeyTile {
 // registers, and the loads of codes take their addresses from there and from offsets that
 // stay as they are.  The entries are read two tiles ahead, the pages' ids and scales one.
 // THROUGH: the keys go through LDS; where few items wait for their tiles in turn the way
-// there is longer than it is worth (16 requests with 32 pages each, 8 heads: 34.2 us, 32.9).
+// there is longer than it is worth (16 requests with 64 pages each, 8 heads: 34.2 us, 32.9).
 template <bool E4M3, int NC, bool PLAIN, int U, bool THROUGH>
 __device__ __forceinline__ void whole_tiles(const AttendArgs& a, const Request& rq, int64_t r, int h, const FewRow& fr, int e0, int step,
                                             int e1, FewSums<NC>& st, const int32_t* list, uint8_t* lds)
