@@ -277,6 +277,45 @@ def test_attend_selected_masks(fkv, codes, rows, how, n):
     check_attend(fkv, 16, 2, 3, 64, codes, rows, LENGTHS, n, "picked", seed=4, **how)
 
 
+HOWS = {
+    "all": dict(causal=False), "cap": dict(softcap=20.0), "large cap": dict(softcap=500.0), "bias": dict(slopes=(0.01, 0.5)),
+    "window": dict(window=70, sinks=9), "window and cap": dict(window=5, sinks=40, softcap=30.0), "prefix": dict(prefix=200),
+    "first": dict(first=90), "negative": dict(scale=-0.2), "window of all": dict(causal=False, window=60, slopes=(0.5, 0.01)),
+    "bad pages": dict(bad_pages=True), "strides": dict(strided=True), "more rows": dict(extra_rows=5)}
+
+
+@pytest.mark.parametrize("codes,rows", [(INT8, F16), (E4M3, BF16)])
+@pytest.mark.parametrize("name", HOWS)
+@pytest.mark.parametrize("heads,group,d,lengths", [(2, 3, 64, LENGTHS), (16, 3, 64, [(330, 128), (70, 2)]), (16, 5, 80, [(270, 129)])])
+def test_attend_selected_masks_of_whole_tiles(fkv, codes, rows, name, heads, group, d, lengths):
+    """Pages of 64 tokens: of few items, and of so many that a wave has one."""
+    how, n, g = dict(HOWS[name]), sum(m for _, m in lengths), torch.Generator().manual_seed(d)
+    if "slopes" in how:
+        how["slopes"] = torch.linspace(*how["slopes"], heads * group)
+    if "prefix" in how:
+        how["prefix"] = torch.randint(0, how["prefix"], (len(lengths),), generator=g, dtype=torch.int32)
+    if "first" in how:
+        how["first"] = torch.randint(-3, how["first"], (n,), generator=g, dtype=torch.int32)
+    check_attend(fkv, 64, heads, group, d, codes, rows, lengths, 6, "any", seed=d, **how)
+
+
+@pytest.mark.parametrize("kind", ["picked", "any"])
+@pytest.mark.parametrize("page,heads,group,d,codes,rows,lengths,n", [
+    (64, 16, 3, 80, E4M3, F16, [(500, 130)], 4),
+    (128, 16, 1, 48, INT8, BF16, [(700, 130)], 3),
+    (64, 16, 8, 144, INT8, F16, [(300, 129)], 3),
+    (192, 16, 4, 256, E4M3, BF16, [(800, 128)], 2),
+    (64, 32, 2, 16, INT8, F16, [(200, 70)], 3),
+    (64, 16, 4, 96, INT8, F16, [(64 * 9, 130)], 9),
+    (256, 16, 2, 112, E4M3, F16, [(900, 129)], 3),
+    (48, 16, 2, 112, INT8, BF16, [(400, 129)], 5),
+    (64, 3, 4, 240, E4M3, F16, [(60, 9), (130, 1)], 1),
+    (64, 2, 4, 128, INT8, BF16, [(64 * 140, 1), (300, 0), (200, 3), (64 * 90, 1)], 130),   # few rows of many places, split
+])
+def test_attend_selected_of_many(fkv, page, heads, group, d, codes, rows, lengths, n, kind):
+    check_attend(fkv, page, heads, group, d, codes, rows, lengths, n, kind, seed=d + page)
+
+
 def test_attend_of_all_pages_is_attend(fkv):
     page, heads, group, d, lengths = 32, 2, 4, 64, [(1000, 3), (33, 2), (400, 1)]
     n_pages = sum(-(-kv // page) for kv, _ in lengths) + 3
