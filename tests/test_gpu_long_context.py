@@ -249,3 +249,26 @@ def test_binding_refuses(fkv):
             fkv.fkv_page_attend_selected(pool, **{**dict(q=q, tables=t, kv_len=kv, q_start=qs, selected=lists, max_new=8, max_kv=8), **kw})
     assert fkv.fkv_page_select(pool, boxes, q[:0], t, kv, qs, 8, 8, 2).shape == (0, 2, 2)
     assert fkv.fkv_page_attend_selected(pool, q[:0], t, kv, qs, lists[:0], 8, 8)[0].shape == (0, 4, 64)
+
+
+@pytest.mark.parametrize("new", [3, 70])
+def test_pages_beyond_32_bits(fkv, new):
+    """The last pages of a pool of more than 2^32 bytes of keys give what the same pages of a small one give."""
+    page, heads, group, d, kv = 256, 16, 2, 256, 900
+    n = 4500                          # 4.7 GB of keys, as much of values
+    results = []
+    for n_pages, ids in ((n, [n - 1, n - 3, n - 2, n - 4]), (4, [3, 1, 2, 0])):
+        pool = fkv.fkv_pages(n_pages, page, heads, d)
+        boxes, table = fkv.fkv_boxes(pool), fkv.fkv_rotation_table(1024, d)
+        tables = dev([ids])
+        for start, rows in ((0, kv), (kv, new)):
+            at = torch.arange(start, start + rows)
+            slots = (torch.tensor(ids)[at // page] * page + at % page).cuda()
+            k, v, q = some(rows, heads, d, BF16, start), some(rows, heads, d, BF16, start + 1), some(rows, heads * group, d, BF16, start + 2)
+            q = fkv.fkv_page_append(pool, k, v, slots, at.int().cuda(), table, q=q, boxes=boxes)
+        lists = fkv.fkv_page_select(pool, boxes, q, tables, dev([kv + new]), dev([0, new]), new, kv + new, 2)
+        out, lse = fkv.fkv_page_attend_selected(pool, q, tables, dev([kv + new]), dev([0, new]), lists, new, kv + new, want_lse=True)
+        ids = torch.tensor(ids).cuda()
+        results.append([bits(x) for x in (pool.k[ids], pool.v[ids], pool.scales[ids], boxes[ids], q, lists, out, lse)])
+        del pool
+    assert all(torch.equal(a, b) for a, b in zip(*results))
