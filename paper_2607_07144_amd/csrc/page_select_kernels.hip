@@ -646,14 +646,35 @@ __global__ __launch_bounds__(kWideThreads) void page_select_wide_kernel(SelectAr
 // A tile is four groups of 16 keys of the listed pages; its order of work is that of
 // few_keys.  Single tokens' lists come from memory (16 requests with 64 pages of 64 x 128, 8
 // heads: 135 MB in 30 us, 4.5 TB/s).  Lists that many tokens share come from the caches, and
-// what bounds them is the vector unit (a chunk of 4096 tokens with 16 pages each: 0.12 PFLOP/s,
-// the unit 85% busy; 320 of a tile's 420 instructions widen int8 codes to binary16, once for
-// each token: lists differ): so a weight with its value scale is one power of two,
+// what bounds them is the vector unit (a chunk of 4096 tokens with 16 pages each: 480 us, 0.14
+// PFLOP/s, the unit 85% busy; 192 of a tile's 290 instructions widen int8 codes to binary16, once for each token:
+// lists differ): so a weight with its value scale is one power of two,
 // 2^(s c - m + log2 v), as in the kernel for many rows: v = vs 2^8 / vr is held at 2^-40 from
 // below, and a sum over v is what l wants.
-template <int NC>
+//
+// SHIFTED, of int8 codes where the vector unit is what a call waits for: codes are taken as 2^-24 (c + 128), a byte each as a
+// subnormal binary16 number, three instructions for four codes in place of five (the chunk 555 -> 476 us).  What the 128 add is
+// taken out of the sums: of a score's by where it begins, of the values' by 128 times the sum of the weights as they were
+// rounded.  The fp32 sums are then of terms up to 255 units where they had |c|: three bits of 24 for codes of 30 on average, and
+// errors of 2^-16 of a code's step, which itself stands for anything within half a step.
+__device__ __forceinline__ half8_t shifted8(uint32_t a, uint32_t b)
+{
+    const uint32_t x = a ^ 0x80808080u, y = b ^ 0x80808080u;
+    return __builtin_bit_cast(half8_t, make_uint4(__builtin_amdgcn_perm(0, x, 0x0c010c00u), __builtin_amdgcn_perm(0, x, 0x0c030c02u),
+                                                  __builtin_amdgcn_perm(0, y, 0x0c010c00u), __builtin_amdgcn_perm(0, y, 0x0c030c02u)));
+}
+
+template <bool E4M3, bool SHIFTED>
+__device__ __forceinline__ half8_t listed8(uint32_t a, uint32_t b)
+{
+    if constexpr (SHIFTED) return shifted8(a, b);
+    else return codes8<E4M3>(a, b);
+}
+
+template <int NC, bool SHIFTED>
 struct ListedQuery : FewQuery<NC> {
-    __device__ __forceinline__ ListedQuery(const AttendArgs& a, const Request& rq, const FewRow& fr) : FewQuery<NC>(a, rq, fr)
+    float4_t base;   // of a row's products
+    __device__ __forceinline__ ListedQuery(const AttendArgs& a, const Request& rq, const FewRow& fr) : FewQuery<NC>(a, rq, fr), base{0, 0, 0, 0}
     {
         // a negative scale's sign goes into the row, so that the factor of a score is not negative
         const uint32_t sign = a.scale < 0.0f ? 0x80008000u : 0u;
@@ -666,16 +687,47 @@ struct ListedQuery : FewQuery<NC> {
                 u.x ^= sign, u.y ^= sign, u.z ^= sign, u.w ^= sign;
                 this->qf[c][k] = __builtin_bit_cast(half8_t, u);
             }
+        if constexpr (SHIFTED) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum += (float)this->qf[c][k][e];
+            sum = rows_sum(sum) * -0x1p-17f;   // 128 x 2^-24
+            base = float4_t{sum, sum, sum, sum};
+            this->mul *= 0x1p24f;
+        }
     }
 };
+
+template <int NC>
+struct ListedSums : FewSums<NC> {
+    float4_t weights = {0, 0, 0, 0};   // SHIFTED: the column's weights as they were rounded, in each part
+};
+
+template <bool E4M3, int NC, bool SHIFTED>
+__device__ __forceinline__ void listed_products(const uint4 (&kw)[4][NC], const ListedQuery<NC, SHIFTED>& q, float4_t (&s)[4])
+{
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        s[t] = q.base;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(listed8<E4M3, SHIFTED>(kw[t][c].x, kw[t][c].y), q.qf[c][0], s[t], 0, 0, 0);
+            s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(listed8<E4M3, SHIFTED>(kw[t][c].z, kw[t][c].w), q.qf[c][1], s[t], 0, 0, 0);
+        }
+    }
+}
 
 // PLAIN: neither cap nor bias.  U: of few rows the operands' 16 columns hold each U times
 // over, and column u of a row's takes the u-th part of every 16 keys, as a wave of its own
 // would: its weights are 0 elsewhere.  (Of groups of four the chunk took 632 us without and 619 with it; where a block's waves
 // are joined in LDS, four times the parts cost one token over 32 pages 1 of 16 us.)
-template <bool E4M3, int NC, bool PLAIN, int U>
-__device__ __forceinline__ void listed_update(const AttendArgs& a, const Request& rq, const Seen& mine, const ListedQuery<NC>& q,
-                                              FewSums<NC>& st, float4_t (&s)[4], uint4 (&vw)[4 * NC], float2 sc, bool here, bool mask, int j0g)
+template <bool E4M3, int NC, bool PLAIN, int U, bool SHIFTED>
+__device__ __forceinline__ void listed_update(const AttendArgs& a, const Request& rq, const Seen& mine, const ListedQuery<NC, SHIFTED>& q,
+                                              ListedSums<NC>& st, float4_t (&s)[4], uint4 (&vw)[4 * NC], float2 sc, bool here, bool mask, int j0g)
 {
     constexpr int N = 16 / U;   // keys
     const int u = (threadIdx.x & 15) / N;
@@ -728,6 +780,7 @@ __device__ __forceinline__ void listed_update(const AttendArgs& a, const Request
         const float k = shrink * (st.vref / vnew);
 #pragma unroll
         for (int t = 0; t < 4 * NC; ++t) st.acc[t] *= k;
+        if (SHIFTED) st.weights *= k;
         st.m = mnew;
         st.vref = vnew;
     }
@@ -750,8 +803,13 @@ __device__ __forceinline__ void listed_update(const AttendArgs& a, const Request
     const half8_t p1 = __builtin_bit_cast(half8_t, make_uint4(p[4], p[5], p[6], p[7]));
 #pragma unroll
     for (int t = 0; t < 4 * NC; ++t) {
-        st.acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(vw[t].x, vw[t].y), p0, st.acc[t], 0, 0, 0);
-        st.acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<E4M3>(vw[t].z, vw[t].w), p1, st.acc[t], 0, 0, 0);
+        st.acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(listed8<E4M3, SHIFTED>(vw[t].x, vw[t].y), p0, st.acc[t], 0, 0, 0);
+        st.acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(listed8<E4M3, SHIFTED>(vw[t].z, vw[t].w), p1, st.acc[t], 0, 0, 0);
+    }
+    if constexpr (SHIFTED) {
+        const half8_t ones = {1, 1, 1, 1, 1, 1, 1, 1};
+        st.weights = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, p0, st.weights, 0, 0, 0);
+        st.weights = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, p1, st.weights, 0, 0, 0);
     }
 }
 
@@ -783,9 +841,9 @@ __device__ __forceinline__ ListPlace place_listed(const AttendArgs& a, const int
 // A wave over the tiles e0, e0 + step, .. below e1 (one at least) of a list of `places`
 // groups, for rows of one token.  Any pages: a lane group looks up its own group's.  The
 // entries are read two tiles ahead, the pages' ids one.
-template <bool E4M3, int NC, bool PLAIN, int U>
+template <bool E4M3, int NC, bool PLAIN, int U, bool SHIFTED>
 __device__ __forceinline__ void listed_groups(const AttendArgs& a, const Request& rq, int64_t r, int h, const FewRow& fr, int e0, int step,
-                                              int e1, FewSums<NC>& st, const int32_t* list, int places)
+                                              int e1, ListedSums<NC>& st, const int32_t* list, int places)
 {
     const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
     const int d = a.d;
@@ -819,7 +877,7 @@ __device__ __forceinline__ void listed_groups(const AttendArgs& a, const Request
     check_place(a, pv);
     load_keys(pk);
     float2 sc = scale_head[(int64_t)pv.id * a.heads], sc_next = sc;
-    const ListedQuery<NC> query(a, rq, fr);
+    const ListedQuery<NC, SHIFTED> query(a, rq, fr);
     for (int e = e0; e < e1; e += step) {
         // the tile's values, on their way while its scores are formed
         uint4 vw[4 * NC];
@@ -831,7 +889,7 @@ __device__ __forceinline__ void listed_groups(const AttendArgs& a, const Request
         const bool mask = __any(!here || j0g < mine.lo || j0g + 16 > mine.hi || (a.window && j0g < mine.wlo && j0g + 16 > a.sinks));
         if (!here) sc = make_float2(0.0f, 0.0f);
         float4_t s[4];
-        few_products<E4M3, NC>(kw, query, s);
+        listed_products<E4M3, NC>(kw, query, s);
         // the next tile's keys, and the pages and entries of those after
         if (e + step < e1) {
             check_place(a, pk1);
@@ -844,7 +902,7 @@ __device__ __forceinline__ void listed_groups(const AttendArgs& a, const Request
             ck2 = entry(e + 3 * step, gk);
             cv2 = entry(e + 3 * step, g);
         }
-        listed_update<E4M3, NC, PLAIN, U>(a, rq, mine, query, st, s, vw, sc, here, mask, j0g);
+        listed_update<E4M3, NC, PLAIN, U, SHIFTED>(a, rq, mine, query, st, s, vw, sc, here, mask, j0g);
         sc = sc_next;
     }
     st.l = rows_sum(st.l);
@@ -913,9 +971,9 @@ struct KeyTile {
 // stay as they are.  The entries are read two tiles ahead, the pages' ids and scales one.
 // THROUGH: the keys go through LDS; where few items wait for their tiles in turn the way
 // there is longer than it is worth (16 requests with 64 pages each, 8 heads: 34.2 us, 32.9).
-template <bool E4M3, int NC, bool PLAIN, int U, bool THROUGH>
+template <bool E4M3, int NC, bool PLAIN, int U, bool THROUGH, bool SHIFTED>
 __device__ __forceinline__ void whole_tiles(const AttendArgs& a, const Request& rq, int64_t r, int h, const FewRow& fr, int e0, int step,
-                                            int e1, FewSums<NC>& st, const int32_t* list, uint8_t* lds)
+                                            int e1, ListedSums<NC>& st, const int32_t* list, uint8_t* lds)
 {
     const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
     const int d = a.d;
@@ -991,7 +1049,7 @@ __device__ __forceinline__ void whole_tiles(const AttendArgs& a, const Request& 
     Place next = place(e0 + step, c1);
     Tile now = tile_of(p0);
     load_keys(now);
-    const ListedQuery<NC> query(a, rq, fr);
+    const ListedQuery<NC, SHIFTED> query(a, rq, fr);
     for (int e = e0; e < e1; e += step) {
         const Tile tile = now;
         auto advance = [&] {
@@ -1005,15 +1063,15 @@ __device__ __forceinline__ void whole_tiles(const AttendArgs& a, const Request& 
             keys.read(kw);
             advance();
             load_values(tile);
-            few_products<E4M3, NC>(kw, query, s);
+            listed_products<E4M3, NC>(kw, query, s);
         } else {
             load_values(tile);
-            few_products<E4M3, NC>(kw, query, s);
+            listed_products<E4M3, NC>(kw, query, s);
             advance();
         }
         const bool mask = !tile.here || tile.pos < mine.lo || tile.pos + kTile > mine.hi || (tile.pos < mine.wlo && tile.pos + kTile > a.sinks);
         const float2 sc = tile.here ? tile.scales : make_float2(0.0f, 0.0f);
-        listed_update<E4M3, NC, PLAIN, U>(a, rq, mine, query, st, s, vw, sc, tile.here, mask, tile.pos + g * 16);
+        listed_update<E4M3, NC, PLAIN, U, SHIFTED>(a, rq, mine, query, st, s, vw, sc, tile.here, mask, tile.pos + g * 16);
     }
     st.l = rows_sum(st.l);
 }
@@ -1058,13 +1116,18 @@ __global__ __launch_bounds__(W > kWaves ? 64 * W : kThreads, NC == 2 && WHOLE &&
     const int places = n * (int)a.per_page, tiles = (places + 3) >> 2;
     const int n_rows = min(a.group - chunk * kFewRows, kFewRows);
     const FewRow fr = {min(row, n_rows - 1), i, h * a.group + chunk * kFewRows + min(row, n_rows - 1)};
-    FewSums<NC> st;
+    constexpr bool kShifted = !E4M3 && W == 1;
+    ListedSums<NC> st;
     const int e0 = split * W + (W == 1 ? 0 : wave);
     if (e0 < tiles) {
-        if constexpr (WHOLE) whole_tiles<E4M3, NC, PLAIN, U, W == 1>(a, rq, r, h, fr, e0, a.n_splits * W, tiles, st, list, (uint8_t*)lds + wave * kKeyBytes<NC>);
-        else listed_groups<E4M3, NC, PLAIN, U>(a, rq, r, h, fr, e0, a.n_splits * W, tiles, st, list, places);
+        if constexpr (WHOLE) whole_tiles<E4M3, NC, PLAIN, U, W == 1, kShifted>(a, rq, r, h, fr, e0, a.n_splits * W, tiles, st, list, (uint8_t*)lds + wave * kKeyBytes<NC>);
+        else listed_groups<E4M3, NC, PLAIN, U, kShifted>(a, rq, r, h, fr, e0, a.n_splits * W, tiles, st, list, places);
     }
 
+    if (kShifted) {
+#pragma unroll
+        for (int t = 0; t < 4 * NC; ++t) st.acc[t] = st.acc[t] * 0x1p24f - st.weights * 128.0f;
+    }
     if (W == 1) {
         if (U > 1) {   // a row's columns together
             auto over_columns = [](float x, auto join) {

@@ -115,8 +115,12 @@ def select(boxes, scales, q, tables, kv_len, q_start, page, n_select, keep_first
 # ---------------------------------------------------------------- attention to lists
 
 def attend_selected(k, v, scales, q, tables, kv_len, q_start, selected, scale, softcap=0.0, causal=True, window=0, sinks=0,
-                    slopes=None, prefix=None, first=None):
-    """As pages_reference.attend, whose bounds hold here too, over the listed pages' keys, each as often as listed."""
+                    slopes=None, prefix=None, first=None, shifted=0):
+    """As pages_reference.attend, whose bounds hold here too, over the listed pages' keys, each as often as listed.
+
+    shifted: tiles of 64 keys of a list whose int8 codes are summed as c + 128, at most 255, and 128 times the other factors'
+    sum taken off.  A score's d + 8 roundings are then of sums up to 255 scale sum |q|; those of the values, 64 a tile and 16
+    at the end, of sums up to 255 of the weights times value scales, and as many of 128 times those."""
     n_pages, heads, page, d = k.shape
     kk, vv = pages.values(k, v, scales)
     n, q_heads, _ = q.shape
@@ -149,6 +153,9 @@ def attend_selected(k, v, scales, q, tables, kv_len, q_start, selected, scale, s
                     x = q[i, hq].double()
                     z = ks @ x * scale
                     err = (ks.abs() @ x.abs()) * abs(scale) * (d + 8) * 2.0 ** -24
+                    if shifted:
+                        both = scales[ids, h].double().repeat_interleave(page, 0)[see]
+                        err = both[:, 0] * x.abs().sum() * 255 * abs(scale) * (d + 8) * 2.0 ** -24
                     if softcap:
                         z = softcap * torch.tanh(z / softcap)
                         err = err + softcap * 2.0 ** -21
@@ -166,5 +173,7 @@ def attend_selected(k, v, scales, q, tables, kv_len, q_start, selected, scale, s
                     big = torch.where(w > 2.0 ** -30, err, 0.0).max()
                     assert big < 0.25
                     off[i, hq] = (2.0 ** -11 + 4 * big + 2.0 ** -18) * (w @ vs.abs())
+                    if shifted:
+                        off[i, hq] += (64 * shifted + 16) * 2.0 ** -24 * (255 + 128) * (w @ both[:, 1])
                     loff[i, hq] = 2 * big + lse[i, hq].abs() * 2.0 ** -20 + 2.0 ** -18
     return out, lse, off, loff

@@ -84,7 +84,8 @@ def test_prompts_and_tokens_in_turn(fkv, page, heads, group, d, codes, kind, pai
         want = torch.full((len(q), heads, 4), -9, dtype=torch.int32)
         ref.select(box.to(codes), cpu[2], want_q, tables, ends, starts, page, 4, 1, 1, True, want)
         assert torch.equal(lists.cpu(), want)
-        exact, elog, off, loff = ref.attend_selected(*cpu, want_q, tables, ends, starts, want, d ** -0.5)
+        exact, elog, off, loff = ref.attend_selected(*cpu, want_q, tables, ends, starts, want, d ** -0.5,
+                                                     shifted=int(codes == INT8 and page == 16))
         half = torch.finfo(kind).eps / 2
         assert ((out.cpu().double() - exact).abs() <= off + half * (exact.abs() + off) + 2.0 ** -25).all()
         assert ((lse.cpu().double() - elog).abs() <= loff).all()

@@ -219,7 +219,11 @@ def check_attend(fkv, page, heads, group, d, codes, rows, lengths, n_selected, k
     torch.cuda.synchronize()
     scale = d ** -0.5 if scale is None else scale
     sane = (torch.nan_to_num(pool[0].float()).to(codes), torch.nan_to_num(pool[1].float()).to(codes), pool[2])
-    want, wlse, off, loff = ref.attend_selected(*sane, q, tables, kv, starts, selected, scale, causal=causal, **how)
+    # int8 codes are shifted where a wave has an item: of one tile, or of 2048 items
+    rows_of_q, tiles = len(lengths) * max_new, -(-n_selected * (page // 16) // 4)
+    items = (n if rows_of_q >= 2 * n else rows_of_q) * heads * -(-group // 16)
+    shifted = tiles if codes == INT8 and (items >= 2048 or tiles == 1) else 0
+    want, wlse, off, loff = ref.attend_selected(*sane, q, tables, kv, starts, selected, scale, causal=causal, shifted=shifted, **how)
     used = int(starts[-1])
     got, glse = out.cpu().double(), lse.cpu().double()
     assert torch.equal(torch.isinf(glse[:used]), torch.isinf(wlse[:used]))
