@@ -470,8 +470,9 @@ int fkv_page_store(const fkv_page_desc* desc, const fkv_row_desc* rows_k, const 
  *   boxes           device [n_pages][heads][2][d] codes in the pages' format,
  *                   16-byte aligned, nullable: of each page that a row is written
  *                   to, the smallest and the largest code of every key channel over
- *                   its tokens up to the row.  A page is to have been written with
- *                   its boxes from its first token on
+ *                   its tokens up to the row, formed of the codes: neither what the
+ *                   box was nor which call wrote the tokens before matters, and
+ *                   tokens that are written over leave nothing in it
  *   n_bad           device u32 counter, += rows whose slot lies beyond the pool or
  *                   whose position lies outside the table; nullable
  * The other arguments, and what they may hold, are fkv_page_store's. */

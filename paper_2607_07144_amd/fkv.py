@@ -733,7 +733,7 @@ def fkv_page_append(pages, k, v, slots, positions=None, table=None, q=None, q_ou
     """Writes rows into the pages' slots as fkv_page_store does, the key rows turned by their positions on the way, and
     turns the query rows: k, v, q f16 or bf16 [n][heads][d] for slots i64 [n] and positions i32 [n], or [b][heads][t][d]
     for [b][t]; table f32 [n_pos][rot // 2][2] (fkv_rotation_table), None for no rotation; channels (i, i + rot // 2) are
-    turned together, or (2i, 2i + 1) with pairs.  boxes (fkv_boxes) of the pages written are kept up to date.  Returns
+    turned together, or (2i, 2i + 1) with pairs.  boxes (fkv_boxes) of the pages written are formed of the codes that they then hold.  Returns
     the query rows (q_out, which may be q; by default new ones), or None without q."""
     torch = _TORCH or _torch()
     desc = _page_desc(pages)
