@@ -697,7 +697,6 @@ struct ListedQuery : FewQuery<NC> {
                     for (int e = 0; e < 8; ++e) sum += (float)this->qf[c][k][e];
             sum = rows_sum(sum) * -0x1p-17f;   // 128 x 2^-24
             base = float4_t{sum, sum, sum, sum};
-            this->mul *= 0x1p24f;
         }
     }
 };
@@ -732,7 +731,7 @@ __device__ __forceinline__ void listed_update(const AttendArgs& a, const Request
     constexpr int N = 16 / U;   // keys
     const int u = (threadIdx.x & 15) / N;
     const int j0 = j0g + u * N;
-    float c = fmaxf(q.mul * sc.x, 0x1p-120f);   // a score's factor (never 0: hidden scores are infinite)
+    float c = q.mul * sc.x;   // a score's factor
     float x[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -740,6 +739,15 @@ __device__ __forceinline__ void listed_update(const AttendArgs& a, const Request
 #pragma unroll
         for (int k = 1; k < U; ++k) x[i] = u == k ? s[(k * N + i) >> 2][i & 3] : x[i];
     }
+    if (SHIFTED) {   // the codes' 2^24 goes into the factor, or into the products where that would be beyond fp32's end
+        if (__any(c > 0x1p100f)) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i] *= 0x1p24f;
+        } else {
+            c *= 0x1p24f;
+        }
+    }
+    c = fmaxf(c, 0x1p-120f);   // (never 0: hidden scores are infinite)
     if (!PLAIN && (q.cap > 0.0f || q.slopes)) {
 #pragma unroll
         for (int i = 0; i < N; ++i) x[i] *= c;
