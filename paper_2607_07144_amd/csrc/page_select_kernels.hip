@@ -794,7 +794,15 @@ __device__ __forceinline__ void listed_update(const AttendArgs& a, const Request
     }
     const float m0 = st.m == -__builtin_inff() ? 0.0f : st.m;
     const float v = __builtin_amdgcn_fmed3f(sc.y * (kTop * __builtin_amdgcn_rcpf(st.vref)), 0x1p-40f, kTop);   // (more only where all weights are 0)
-    const float vb = __builtin_amdgcn_logf(v) - m0;
+    const float log_v = __builtin_amdgcn_logf(v);
+    float vb = log_v - m0;
+    // the product of a large score is rounded before the maximum is taken off, as it was for that: exact, it may be far above
+    if (__any(fabsf(m0) > 0x1p20f)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = x[i] * c - m0;
+        c = 1.0f;
+        vb = log_v;
+    }
     uint32_t p[8];   // the 16 keys' weights
     float sum = 0.0f;
 #pragma unroll

@@ -50,3 +50,55 @@ def test_bfloat16_rows_near_the_types_ends(fkv, codes, page, group, d, lengths, 
     half = torch.finfo(BF16).eps / 2
     assert ((lse - wlse).abs() <= loff).all()
     assert ((got - want).abs() <= off + half * (want.abs() + off) + 2.0 ** -25).all()
+
+
+@pytest.mark.parametrize("codes", [INT8, E4M3])
+@pytest.mark.parametrize("page,group,d", [(64, 3, 128), (64, 8, 64), (16, 4, 80)])
+@pytest.mark.parametrize("lengths", [FEW, MANY])
+@pytest.mark.parametrize("how", [{}, dict(slopes=0.01), dict(softcap=1e36)])
+def test_keys_near_the_types_ends(fkv, codes, page, group, d, lengths, how):
+    """Keys of up to 2^117 and binary16 rows: scores are finite and so far apart that a row's best key has all the weight."""
+    heads, n = 16, 4
+    pool, tables, kv, starts, q, selected = inputs(page, heads, group, d, codes, F16, lengths, n, d + page)
+    pool[2][:, :, 0] *= 2.0 ** 111
+    q = torch.where(q.abs() < 2.0 ** -5, 2.0 ** -5, q).to(F16)
+    got, lse = call(fkv, pool, tables, kv, starts, q, selected, lengths, scale=2.0 ** -3,
+                    **{k: torch.full((heads * group,), x, device="cuda") if k == "slopes" else x for k, x in how.items()})
+    assert torch.isfinite(got).all()
+    want, top, err, sure = best(pool, tables, kv, starts, q, selected, 2.0 ** -3)
+    # the best key is taken where the next is further off than both scores' errors, (d + 8) 2^-24 of the sum of 255 units of a
+    # scale; a cap keeps their order and takes t^2 / 3 of them, less than 2^-13 of scores of up to 0.018 of it
+    assert sure.float().mean() > 0.9
+    half = torch.finfo(F16).eps / 2
+    # (a weight of 1 times its value scale is rounded to 11 bits)
+    assert ((got - want).abs() <= (half + 2.0 ** -11 + 2.0 ** -18) * want.abs() + 383 * 2.0 ** -19 * pool[2][:, :, 1].max() + 2.0 ** -25)[sure].all()
+    assert top.max() < 1.8e34 and ((lse - top).abs() <= err + top.abs() * 2.0 ** -13)[sure].all()
+
+
+def best(pool, tables, kv, starts, q, selected, scale):
+    """The value row of each row's best key, its score and that one's error, and whether the next one is far enough below."""
+    import pages_reference as pages
+    n_pages, heads, page, d = pool[0].shape
+    kk, vv = pages.values(*pool)
+    n, q_heads, _ = q.shape
+    group = q_heads // heads
+    want, sure = torch.zeros((n, q_heads, d), dtype=torch.float64), torch.zeros((n, q_heads), dtype=torch.bool)
+    top, off = torch.zeros((2, n, q_heads), dtype=torch.float64)
+    for r in range(len(kv)):
+        b, e = int(starts[r]), int(starts[r + 1])
+        for i in range(b, e):
+            pos = int(kv[r]) - (e - b) + (i - b)
+            for h in range(heads):
+                column = selected[i, h].long()
+                column = column[column >= 0]
+                ids, j = tables[r, column].long(), (column[:, None] * page + torch.arange(page)).flatten()
+                see = j <= pos
+                ks, vs, sc = kk[ids, h].reshape(-1, d)[see], vv[ids, h].reshape(-1, d)[see], pool[2][ids, h, 0].double().repeat_interleave(page)[see]
+                for hq in range(h * group, (h + 1) * group):
+                    x = q[i, hq].double()
+                    z = ks @ x * scale
+                    err = sc * 255 * x.abs().sum() * scale * (d + 8) * 2.0 ** -24 + z.abs() * 2.0 ** -20
+                    o = z.argsort(descending=True)
+                    want[i, hq], top[i, hq], off[i, hq] = vs[o[0]], z[o[0]], err[o[0]]
+                    sure[i, hq] = len(o) == 1 or bool((z[o[0]] - z[o[1:]] > err[o[0]] + err[o[1:]] + 2.0 ** 20).all())
+    return want, top, off, sure
