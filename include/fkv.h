@@ -621,10 +621,13 @@ int fkv_page_select(const fkv_page_desc* desc, const fkv_select_desc* select, co
  *               more than once count as often
  *   n_selected  1 .. 2^20
  *   workspace   of fkv_page_attend_selected_workspace() bytes
- * The other arguments, accuracy and errors are fkv_page_attend's, but that sums over
- * int8 codes may be formed of c + 128 (errors of 2^-24 of sums of 255 units of a scale
- * where fkv_page_attend's are of |c|), and for its limits on rows: FKV_ERR_UNSUPPORTED for more blocks than a launch holds, as of
- * fkv_page_select, with q_heads in place of heads where they are more than 16 a head. */
+ * The other arguments, accuracy and errors are fkv_page_attend's, but that int8 codes
+ * may be summed as c + 128, the 128 taken out of a score's sum where it begins and of
+ * the values' after each 64 keys: a score's roundings are of sums of up to 255 units of a
+ * scale where fkv_page_attend's are of |c|, and the values' further error is within
+ * 2^-14 of a unit of their largest scale, however long the list; and for its limits on
+ * rows: FKV_ERR_UNSUPPORTED for more blocks than a launch holds, as of fkv_page_select,
+ * with q_heads in place of heads where they are more than 16 a head. */
 size_t fkv_page_attend_selected_workspace(const fkv_page_desc* desc, const fkv_attend_desc* attend, int64_t n_selected);
 
 int fkv_page_attend_selected(const fkv_page_desc* desc, const fkv_attend_desc* attend, int64_t n_selected,

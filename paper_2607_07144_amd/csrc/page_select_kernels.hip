@@ -653,10 +653,13 @@ __global__ __launch_bounds__(kWideThreads) void page_select_wide_kernel(SelectAr
 // below, and a sum over v is what l wants.
 //
 // SHIFTED, of int8 codes where the vector unit is what a call waits for: codes are taken as 2^-24 (c + 128), a byte each as a
-// subnormal binary16 number, three instructions for four codes in place of five (the chunk 555 -> 476 us).  What the 128 add is
-// taken out of the sums: of a score's by where it begins, of the values' by 128 times the sum of the weights as they were
-// rounded.  The fp32 sums are then of terms up to 255 units where they had |c|: three bits of 24 for codes of 30 on average, and
-// errors of 2^-16 of a code's step, which itself stands for anything within half a step.
+// subnormal binary16 number, three instructions for four codes in place of five (the chunk 580 -> 513 us).  What the 128 add is
+// taken out of the sums: of a score's by where it begins, of the values' tile by tile, by 128 times the sum of the tile's weights
+// as they were rounded.  (Once at the end it is 499 us, but the sums then grow with the list, and with them their roundings: an
+// error of 2^-15 of a code's step at 16 tiles, 2^-12 at 512.)  So a score's roundings are of sums of up to 255 units where they
+// had |c|, and the values' are, beside those of the sums themselves, four a tile of up to 255 units of that tile's weights: one
+// rounding a product, 2^-14 of a step at most over a list of any length, 2^-18 as emulated, and a step stands for anything within
+// half of it.
 __device__ __forceinline__ half8_t shifted8(uint32_t a, uint32_t b)
 {
     const uint32_t x = a ^ 0x80808080u, y = b ^ 0x80808080u;
@@ -701,11 +704,6 @@ struct ListedQuery : FewQuery<NC> {
     }
 };
 
-template <int NC>
-struct ListedSums : FewSums<NC> {
-    float4_t weights = {0, 0, 0, 0};   // SHIFTED: the column's weights as they were rounded, in each part
-};
-
 template <bool E4M3, int NC, bool SHIFTED>
 __device__ __forceinline__ void listed_products(const uint4 (&kw)[4][NC], const ListedQuery<NC, SHIFTED>& q, float4_t (&s)[4])
 {
@@ -726,7 +724,7 @@ __device__ __forceinline__ void listed_products(const uint4 (&kw)[4][NC], const 
 // are joined in LDS, four times the parts cost one token over 32 pages 1 of 16 us.)
 template <bool E4M3, int NC, bool PLAIN, int U, bool SHIFTED>
 __device__ __forceinline__ void listed_update(const AttendArgs& a, const Request& rq, const Seen& mine, const ListedQuery<NC, SHIFTED>& q,
-                                              ListedSums<NC>& st, float4_t (&s)[4], uint4 (&vw)[4 * NC], float2 sc, bool here, bool mask, int j0g)
+                                              FewSums<NC>& st, float4_t (&s)[4], uint4 (&vw)[4 * NC], float2 sc, bool here, bool mask, int j0g)
 {
     constexpr int N = 16 / U;   // keys
     const int u = (threadIdx.x & 15) / N;
@@ -788,7 +786,6 @@ __device__ __forceinline__ void listed_update(const AttendArgs& a, const Request
         const float k = shrink * (st.vref / vnew);
 #pragma unroll
         for (int t = 0; t < 4 * NC; ++t) st.acc[t] *= k;
-        if (SHIFTED) st.weights *= k;
         st.m = mnew;
         st.vref = vnew;
     }
@@ -817,15 +814,20 @@ __device__ __forceinline__ void listed_update(const AttendArgs& a, const Request
     st.l = __builtin_fmaf(sum, __builtin_amdgcn_rcpf(v), st.l);
     const half8_t p0 = __builtin_bit_cast(half8_t, make_uint4(p[0], p[1], p[2], p[3]));
     const half8_t p1 = __builtin_bit_cast(half8_t, make_uint4(p[4], p[5], p[6], p[7]));
+    if constexpr (SHIFTED) {   // the tile's 128 out of the sums: 2^-24 x 128 times the weights as they were rounded
+        const half8_t ones = {1, 1, 1, 1, 1, 1, 1, 1};
+        float4_t weights = {0, 0, 0, 0};
+        weights = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, p0, weights, 0, 0, 0);
+        weights = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, p1, weights, 0, 0, 0);
+#pragma unroll
+        for (int t = 0; t < 4 * NC; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) st.acc[t][e] = __builtin_fmaf(weights[e], -0x1p-17f, st.acc[t][e]);
+    }
 #pragma unroll
     for (int t = 0; t < 4 * NC; ++t) {
         st.acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(listed8<E4M3, SHIFTED>(vw[t].x, vw[t].y), p0, st.acc[t], 0, 0, 0);
         st.acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(listed8<E4M3, SHIFTED>(vw[t].z, vw[t].w), p1, st.acc[t], 0, 0, 0);
-    }
-    if constexpr (SHIFTED) {
-        const half8_t ones = {1, 1, 1, 1, 1, 1, 1, 1};
-        st.weights = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, p0, st.weights, 0, 0, 0);
-        st.weights = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, p1, st.weights, 0, 0, 0);
     }
 }
 
@@ -859,7 +861,7 @@ __device__ __forceinline__ ListPlace place_listed(const AttendArgs& a, const int
 // entries are read two tiles ahead, the pages' ids one.
 template <bool E4M3, int NC, bool PLAIN, int U, bool SHIFTED>
 __device__ __forceinline__ void listed_groups(const AttendArgs& a, const Request& rq, int64_t r, int h, const FewRow& fr, int e0, int step,
-                                              int e1, ListedSums<NC>& st, const int32_t* list, int places)
+                                              int e1, FewSums<NC>& st, const int32_t* list, int places)
 {
     const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
     const int d = a.d;
@@ -989,7 +991,7 @@ struct KeyTile {
 // there is longer than it is worth (16 requests with 64 pages each, 8 heads: 34.2 us, 32.9).
 template <bool E4M3, int NC, bool PLAIN, int U, bool THROUGH, bool SHIFTED>
 __device__ __forceinline__ void whole_tiles(const AttendArgs& a, const Request& rq, int64_t r, int h, const FewRow& fr, int e0, int step,
-                                            int e1, ListedSums<NC>& st, const int32_t* list, uint8_t* lds)
+                                            int e1, FewSums<NC>& st, const int32_t* list, uint8_t* lds)
 {
     const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
     const int d = a.d;
@@ -1133,7 +1135,7 @@ __global__ __launch_bounds__(W > kWaves ? 64 * W : kThreads, NC == 2 && WHOLE &&
     const int n_rows = min(a.group - chunk * kFewRows, kFewRows);
     const FewRow fr = {min(row, n_rows - 1), i, h * a.group + chunk * kFewRows + min(row, n_rows - 1)};
     constexpr bool kShifted = !E4M3 && W == 1;
-    ListedSums<NC> st;
+    FewSums<NC> st;
     const int e0 = split * W + (W == 1 ? 0 : wave);
     if (e0 < tiles) {
         if constexpr (WHOLE) whole_tiles<E4M3, NC, PLAIN, U, W == 1, kShifted>(a, rq, r, h, fr, e0, a.n_splits * W, tiles, st, list, (uint8_t*)lds + wave * kKeyBytes<NC>);
@@ -1142,7 +1144,7 @@ __global__ __launch_bounds__(W > kWaves ? 64 * W : kThreads, NC == 2 && WHOLE &&
 
     if (kShifted) {
 #pragma unroll
-        for (int t = 0; t < 4 * NC; ++t) st.acc[t] = st.acc[t] * 0x1p24f - st.weights * 128.0f;
+        for (int t = 0; t < 4 * NC; ++t) st.acc[t] *= 0x1p24f;
     }
     if (W == 1) {
         if (U > 1) {   // a row's columns together
