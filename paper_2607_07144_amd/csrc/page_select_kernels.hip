@@ -45,32 +45,6 @@ __device__ __forceinline__ int pages_seen(const AttendArgs& a, const Request& rq
     return pages_of(a, max(end, 0));
 }
 
-// Prompts and single tokens in one call leave most of n_req x max_new places empty.  Then
-// a launch has a place for each row of q, and finds its request: the last whose rows
-// begin at `index` or before.  PER rows a place: of a request's rows the places
-// start / PER + r on, which are enough for any rows before the next request's.  -1: none.
-// (A step of 30 single tokens, 2048 of a chunk and 33 more, 8 heads of 128: selection 208 -> 73 us, attention to lists
-// 987 -> 640.)
-__device__ __forceinline__ int64_t first_place(const AttendArgs& a, int64_t r, int per)
-{
-    const uint32_t start = (uint32_t)min(max((int64_t)a.q_start[r], (int64_t)0), a.n_tokens);
-    return per == 1 ? start : start / (uint32_t)per + r;
-}
-
-__device__ __forceinline__ int64_t request_at(const AttendArgs& a, int64_t index, int per)
-{
-    const int lane = threadIdx.x & 63;
-    int64_t lo = 0, end = a.n_req;   // the requests not settled; but for the first round lo's rows begin early enough
-    for (;;) {
-        const int64_t step = (end - lo + 63) >> 6, j = lo + lane * step;
-        const int n = __builtin_popcountll(__ballot(j < end && first_place(a, min(j, end - 1), per) <= index));
-        if (n == 0) return -1;
-        lo += (n - 1) * step;
-        if (step == 1) return lo;
-        end = min(end, lo + step);
-    }
-}
-
 // The request and row of a launch's place for a token; r -1: of none, i -1: to be told from the request's first row.
 struct TokenPlace {
     int64_t r;
@@ -1466,9 +1440,6 @@ extern "C" int fkv_page_attend_selected(const fkv_page_desc* desc, const fkv_att
     a.part = (float*)workspace;
     a.stat = (float2*)((uint8_t*)workspace + ws.stat);
     a.n_splits = s.n_splits;
-    const int64_t items = s.n_splits > 1 ? a.n_req * a.max_new * a.heads * a.group : 0;   // rows to be joined
-    const int64_t joins = s.join_blocks ? items : (items + kWaves - 1) / kWaves;
-    if (joins > kMostBlocks) return FKV_ERR_UNSUPPORTED;
     const hipStream_t st = (hipStream_t)stream;
     const bool e4m3 = desc->format == FKV_PAGE_E4M3;
     auto of_width = [&](auto nc) {
@@ -1498,7 +1469,10 @@ extern "C" int fkv_page_attend_selected(const fkv_page_desc* desc, const fkv_att
     if (a.d <= 64) of_width(std::integral_constant<int, 1>{});
     else if (a.d <= 128) of_width(std::integral_constant<int, 2>{});
     else of_width(std::integral_constant<int, 4>{});
-    if (a.n_splits > 1)
+    if (a.n_splits > 1) {
+        const int64_t rows = (a.searched ? a.searched : a.n_req * a.max_new) * a.heads * a.group;   // (fewer than 256 items')
+        const int64_t joins = s.join_blocks ? rows : (rows + kWaves - 1) / kWaves;
         hipLaunchKernelGGL(s.join_blocks ? attend_join_kernel<kWaves> : attend_join_kernel<1>, dim3((unsigned)joins), dim3(kThreads), 0, st, a);
+    }
     return launch_status();
 }

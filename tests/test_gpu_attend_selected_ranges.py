@@ -139,3 +139,27 @@ def test_long_lists_of_many_items(fkv, codes, page, group, d, tiles):
     assert ((got - want).abs() <= room + torch.finfo(F16).eps / 2 * (want + room) + 2.0 ** -25).all(), float(((got - want).abs() / room).max())
     exact = as_rows(torch.logsumexp(z, -1)[..., None] + math.log(tiles * 64 / kv))
     assert ((lse[..., None] - exact).abs() <= 2 * big + (tiles * 64 + 64) * 2.0 ** -24 + exact.abs() * 2.0 ** -20).all()
+
+
+@pytest.mark.parametrize("entries", [70, 512, 4096])
+@pytest.mark.parametrize("n_req,max_new", [(1 << 20, 4096), (512, 2048), (4, 1)])
+def test_split_lists_of_few_rows_in_many_places(fkv, entries, n_req, max_new):
+    """Long lists of four rows of four requests, among many requests without rows and with a loose bound on a request's rows: the
+    same as of those four alone."""
+    page, heads, group, d, width = 64, 2, 2, 64, 8
+    pool = up(ref.pool(40, heads, page, d, INT8, 1))
+    g = torch.Generator().manual_seed(entries)
+    q = torch.randn((4, heads * group, d), generator=g).half().cuda()
+    tables = torch.randint(0, 40, (n_req, width), generator=g, dtype=torch.int32)
+    kv, new = torch.full((n_req,), 17, dtype=torch.int32), torch.zeros(n_req, dtype=torch.int64)
+    at = [n_req * i // 4 for i in range(4)]
+    kv[at], new[at] = torch.tensor([512, 300, 77, 1], dtype=torch.int32), 1
+    starts = torch.cat((torch.zeros(1, dtype=torch.int64), new.cumsum(0))).int()
+    selected = torch.randint(-1, width, (4, heads, entries), generator=g, dtype=torch.int32).cuda()
+    got = fkv.fkv_page_attend_selected(pool, q, tables.cuda(), kv.cuda(), starts.cuda(), selected, max_new, 512, want_lse=True)
+    alone = fkv.fkv_page_attend_selected(pool, q, tables[at].cuda(), kv[at].cuda(), torch.arange(5, dtype=torch.int32, device="cuda"), selected,
+                                         1, 512, want_lse=True)
+    assert all(torch.equal(a, b) for a, b in zip(got, alone))
+    want, wlse, off, loff = ref.attend_selected(*(t.cpu() for t in pool), q.cpu(), tables[at], kv[at], torch.arange(5), selected.cpu(), d ** -0.5)
+    assert ((got[0].cpu().double() - want).abs() <= off + torch.finfo(F16).eps / 2 * (want.abs() + off) + 2.0 ** -25).all()
+    assert ((got[1].cpu().double() - wlse).abs() <= loff).all()
