@@ -2,7 +2,9 @@
 
 Argument marshalling only: every step of the archive path runs in the HIP
 kernels of libfkv.so.  PyTorch provides device memory and the current HIP
-stream.  Importing this module loads the library and raises ImportError when
+stream; what a call makes itself (results, scratch) lies in the memory of the
+stream that it runs on, the current one or that of `stream=`, a raw handle.
+Importing this module loads the library and raises ImportError when
 it has not been built -- there is no fallback path.
 """
 from __future__ import annotations
@@ -185,6 +187,29 @@ def _here(*tensors) -> None:
             raise ValueError("tensor on device %d, the current device is %d" % (t.get_device(), device))
 
 
+def _new(shape, dtype, device, stream, zero=False):
+    """A tensor that a call makes, from the memory of the stream that it runs on, as its kernels write it there: of another
+    stream's memory, that one's work on what it held before might not be done.  (What reads a result on a third stream
+    waits for it, and keeps it until it is done, as with torch.cuda.stream.  The attention calls make theirs in place where no
+    stream is given: a small call's time is such lines.)"""
+    torch = _TORCH or _torch()
+    make = torch.zeros if zero else torch.empty
+    if stream is None:
+        return make(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=device)):
+        return make(shape, dtype=dtype, device=device)
+
+
+def _clear(t, stream) -> None:
+    """Zeros, on the stream that the call runs on."""
+    torch = _TORCH or _torch()
+    if stream is None:
+        t.zero_()
+        return
+    with torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=t.device)):
+        t.zero_()
+
+
 # ------------------------------------------------------------------ codec
 
 class Codec:
@@ -239,12 +264,12 @@ def fkv_rvq_assign(x, books, stream_book, t_begin: int, t_end: int, symbols=None
         raise ValueError("shape mismatch between x, books and stream_book")
     Ta = t_end - t_begin
     if symbols is None:
-        symbols = torch.empty((ns, Ta * S), dtype=torch.uint8, device=x.device)
+        symbols = _new((ns, Ta * S), torch.uint8, x.device, stream)
     _need(symbols, torch.uint8, "symbols")
     if symbols.numel() != ns * Ta * S:
         raise ValueError("symbols has the wrong size")
     if residual is None and want_residual:
-        residual = torch.empty((ns, Ta, d), dtype=torch.float32, device=x.device)
+        residual = _new((ns, Ta, d), torch.float32, x.device, stream)
     if residual is not None:
         _need(residual, torch.float32, "residual")
         if residual.numel() != ns * Ta * d:
@@ -292,12 +317,12 @@ def fkv_rvq_assign_groups(x, books, stream_book, groups, t_begin: int, t_end: in
         raise ValueError("shape mismatch between x, books, stream_book and groups")
     Ta = t_end - t_begin
     if symbols is None:
-        symbols = torch.empty((ns, Ta * S), dtype=torch.uint8, device=x.device)
+        symbols = _new((ns, Ta * S), torch.uint8, x.device, stream)
     _need(symbols, torch.uint8, "symbols")
     if symbols.numel() != ns * Ta * S:
         raise ValueError("symbols has the wrong size")
     if residual is None and want_residual:
-        residual = torch.empty((ns, Ta, d), dtype=torch.float32, device=x.device)
+        residual = _new((ns, Ta, d), torch.float32, x.device, stream)
     if residual is not None:
         _need(residual, torch.float32, "residual")
         if residual.numel() != ns * Ta * d:
@@ -338,18 +363,18 @@ def fkv_rvq_assign_encode(codec: Codec, x, books, stream_book, t_begin: int, t_e
         raise ValueError("shape mismatch between x, books and stream_book")
     Ta = t_end - t_begin
     if symbols is None:
-        symbols = torch.empty((ns, Ta * S), dtype=torch.uint8, device=x.device)
+        symbols = _new((ns, Ta * S), torch.uint8, x.device, stream)
     _need(symbols, torch.uint8, "symbols")
     if symbols.numel() != ns * Ta * S:
         raise ValueError("symbols has the wrong size")
     n_spans = codec.n_spans(Ta * S)
     if points is None:
-        points = torch.empty((ns, n_spans, 2), dtype=torch.float64, device=x.device)
+        points = _new((ns, n_spans, 2), torch.float64, x.device, stream)
     _need(points, torch.float64, "points")
     if points.numel() != ns * n_spans * 2:
         raise ValueError("points has the wrong size")
     if residual is None and want_residual:
-        residual = torch.empty((ns, Ta, d), dtype=torch.float32, device=x.device)
+        residual = _new((ns, Ta, d), torch.float32, x.device, stream)
     if residual is not None:
         _need(residual, torch.float32, "residual")
     if n_bad is not None:
@@ -370,7 +395,7 @@ def fkv_cgr_encode_spans(codec: Codec, symbols, points=None, stream=None):
     _need(symbols, torch.uint8, "symbols")
     ns, n_sym = symbols.shape
     if points is None:
-        points = torch.empty((ns, codec.n_spans(n_sym), 2), dtype=torch.float64, device=symbols.device)
+        points = _new((ns, codec.n_spans(n_sym), 2), torch.float64, symbols.device, stream)
     _need(points, torch.float64, "points")
     if points.numel() != ns * codec.n_spans(n_sym) * 2:
         raise ValueError("points has the wrong size")
@@ -390,7 +415,7 @@ def fkv_cgr_decode_spans(codec: Codec, points, n_sym: int, symbols=None, span_ok
     if points.numel() != ns * codec.n_spans(n_sym) * 2:
         raise ValueError("points does not match n_sym")
     if symbols is None:
-        symbols = torch.empty((ns, n_sym), dtype=torch.uint8, device=points.device)
+        symbols = _new((ns, n_sym), torch.uint8, points.device, stream)
     _need(symbols, torch.uint8, "symbols")
     if span_ok is not None:
         _need(span_ok, torch.uint8, "span_ok")
@@ -415,7 +440,7 @@ def fkv_span_lookup(codec: Codec, points, n_sym: int, S: int, q_stream, q_token,
     if q_token.numel() != nq:
         raise ValueError("q_stream and q_token differ in length")
     if out is None:
-        out = torch.empty((nq, S), dtype=torch.uint8, device=points.device)
+        out = _new((nq, S), torch.uint8, points.device, stream)
     _need(out, torch.uint8, "out")
     if q_status is not None:
         _need(q_status, torch.uint8, "q_status")
@@ -447,7 +472,7 @@ def fkv_rehydrate(codec: Codec, points, n_sym: int, S: int, books, stream_book, 
     if q_token.numel() != nq:
         raise ValueError("q_stream and q_token differ in length")
     if out is None:
-        out = torch.empty((nq, d), dtype=torch.float16, device=points.device)
+        out = _new((nq, d), torch.float16, points.device, stream)
     _need(out, torch.float16, "out")
     if q_status is not None:
         _need(q_status, torch.uint8, "q_status")
@@ -485,7 +510,7 @@ def fkv_trajectory(codec: Codec, symbols, W: int = 0, traj=None, stream=None):
     ns, n = symbols.shape
     W = W or codec.L
     if traj is None:
-        traj = torch.empty((ns, n, 2), dtype=torch.float64, device=symbols.device)
+        traj = _new((ns, n, 2), torch.float64, symbols.device, stream)
     _need(traj, torch.float64, "traj")
     _check(lib.fkv_trajectory(ctypes.byref(codec.c), _ptr(codec.table(symbols.device)), _ptr(symbols), ns, n, W,
                               _ptr(traj), _stream(stream)), "fkv_trajectory")
@@ -501,12 +526,12 @@ def fkv_suffix_search(codec: Codec, traj, query, verify: bool = True, max_hits: 
     _need(query, torch.uint8, "query")
     ns, n = traj.shape[0], traj.shape[1]
     if hits is None:
-        hits = torch.empty((max(max_hits, 1), 2), dtype=torch.int32, device=traj.device)
+        hits = _new((max(max_hits, 1), 2), torch.int32, traj.device, stream)
     _need(hits, torch.int32, "hits")
     if n_hits is None:
-        n_hits = torch.zeros(1, dtype=torch.int32, device=traj.device)
+        n_hits = _new(1, torch.int32, traj.device, stream, zero=True)
     if n_candidates is None:
-        n_candidates = torch.zeros(1, dtype=torch.int32, device=traj.device)
+        n_candidates = _new(1, torch.int32, traj.device, stream, zero=True)
     _check(lib.fkv_suffix_search(ctypes.byref(codec.c), _ptr(codec.table(traj.device)), _ptr(traj), ns, n,
                                  _ptr(query), query.numel(), 1 if verify else 0, _ptr(hits), max_hits,
                                  _ptr(n_hits), _ptr(n_candidates), _stream(stream)), "fkv_suffix_search")
@@ -530,13 +555,13 @@ def fkv_kmeans_step(x, books, stream_book, t_begin: int, t_end: int, symbols, st
     if d2 != d or stream_book.shape != (ns,) or symbols.numel() != ns * (t_end - t_begin) * S:
         raise ValueError("shape mismatch")
     if sums is None:
-        sums = torch.zeros((nb, K, d), dtype=torch.int64, device=x.device)
+        sums = _new((nb, K, d), torch.int64, x.device, stream, zero=True)
     else:
-        sums.zero_()
+        _clear(sums, stream)
     if counts is None:
-        counts = torch.zeros((nb, K), dtype=torch.int32, device=x.device)
+        counts = _new((nb, K), torch.int32, x.device, stream, zero=True)
     else:
-        counts.zero_()
+        _clear(counts, stream)
     desc = fkv_rvq_desc(ns, T, t_begin, t_end, d, S, K, nb)
     st = _stream(stream)
     _check(lib.fkv_kmeans_accumulate(ctypes.byref(desc), _ptr(x), _ptr(books), _ptr(stream_book), _ptr(symbols),
@@ -672,7 +697,7 @@ def fkv_page_plan(page: int, kv_len, new_len, free_pages, head, tables, n_tokens
     # the call as offsets, and the tensors are made while the kernel runs
     r4 = (n_req + 3) // 4
     sizes = (2 * n_tokens, n_tokens, n_req + 1, n_req, 1, 1, r4)
-    buf = torch.empty(3 * n_tokens + 2 * n_req + 3 + r4, dtype=i32, device=kv_len.device)
+    buf = _new(3 * n_tokens + 2 * n_req + 3 + r4, i32, kv_len.device, stream)
     at = buf.data_ptr()
     rows = at + 12 * n_tokens          # q_start
     ends = rows + 4 * n_req + 4        # kv_end
@@ -733,8 +758,8 @@ def fkv_page_append(pages, k, v, slots, positions=None, table=None, q=None, q_ou
     """Writes rows into the pages' slots as fkv_page_store does, the key rows turned by their positions on the way, and
     turns the query rows: k, v, q f16 or bf16 [n][heads][d] for slots i64 [n] and positions i32 [n], or [b][heads][t][d]
     for [b][t]; table f32 [n_pos][rot // 2][2] (fkv_rotation_table), None for no rotation; channels (i, i + rot // 2) are
-    turned together, or (2i, 2i + 1) with pairs.  boxes (fkv_boxes) of the pages written are formed of the codes that they then hold.  Returns
-    the query rows (q_out, which may be q; by default new ones), or None without q."""
+    turned together, or (2i, 2i + 1) with pairs.  boxes (fkv_boxes) of the pages written are formed of the codes that they then
+    hold.  Returns the query rows (q_out, which may be q; by default new ones), or None without q."""
     torch = _TORCH or _torch()
     desc = _page_desc(pages)
     _need(slots, torch.int64, "slots")
@@ -760,7 +785,7 @@ def fkv_page_append(pages, k, v, slots, positions=None, table=None, q=None, q_ou
         q_heads = q.shape[1]
         rq = _rows(q, slots, q_heads, d, "q")
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if stream is None else _new(q.shape, q.dtype, q.device, stream)
         ro = _rows(q_out, slots, q_heads, d, "q_out")
     elif q_out is not None:
         raise TypeError("q_out without q")
@@ -789,8 +814,8 @@ def fkv_page_load(pages, slots, dtype=None, k=None, v=None, stream=None):
         at = slots.shape
         shape = (at[0], heads, d) if len(at) == 1 else (at[0], heads, at[1], d)
         dtype = dtype or torch.float16
-        k = torch.empty(shape, dtype=dtype, device=slots.device)
-        v = torch.empty(shape, dtype=dtype, device=slots.device)
+        k = _new(shape, dtype, slots.device, stream)
+        v = _new(shape, dtype, slots.device, stream)
         rk = rv = _rows(k, slots, heads, d, "k")
     else:
         rk = _rows(k, slots, heads, d, "k") if k is not None else None
@@ -821,15 +846,6 @@ def _q_rows(pages, q, tables, kv_len, q_start):
     if len(width) != 2 or width[0] != n_req or q_start.numel() != n_req + 1:
         raise ValueError("shape mismatch between tables, kv_len and q_start")
     return desc, kind, n_req, width[1], shape, stride
-
-
-def _scratch(need: int, device, stream):
-    """uint8 scratch from torch's allocator, of the stream that the call runs on."""
-    torch = _TORCH or _torch()
-    if stream is None:
-        return torch.empty(need, dtype=torch.uint8, device=device)
-    with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device)):
-        return torch.empty(need, dtype=torch.uint8, device=device)
 
 
 def _masks(n: int, q_heads: int, n_req: int, slopes, prefix, first) -> None:
@@ -864,7 +880,7 @@ def fkv_page_select(pages, boxes, q, tables, kv_len, q_start, max_new: int, max_
     sel = fkv_select_desc(n_req, n, max_new, max_kv, width, q_stride[0], q_stride[1], q_heads, kind, 1 if causal else 0,
                           n_select, keep_first, keep_last)
     if selected is None:
-        selected = torch.empty((n, desc.heads, max(n_select, 1)), dtype=torch.int32, device=q.device)
+        selected = _new((n, desc.heads, max(n_select, 1)), torch.int32, q.device, stream)
     else:
         _need(selected, torch.int32, "selected")
         if selected.shape != (n, desc.heads, n_select):
@@ -876,7 +892,7 @@ def fkv_page_select(pages, boxes, q, tables, kv_len, q_start, max_new: int, max_
     else:
         need = lib.fkv_page_select_workspace(ref(desc), ref(sel))
         if need:
-            workspace = _scratch(need, q.device, stream)
+            workspace = _new(need, torch.uint8, q.device, stream)
     _check(lib.fkv_page_select(ref(desc), ref(sel), boxes.data_ptr(), pages[2].data_ptr(), q.data_ptr(), tables.data_ptr(),
                                kv_len.data_ptr(), q_start.data_ptr(), selected.data_ptr(), _ptr(workspace),
                                0 if workspace is None else workspace.numel(), _stream(stream)), "fkv_page_select")
@@ -908,7 +924,7 @@ def fkv_page_attend_selected(pages, q, tables, kv_len, q_start, selected, max_ne
     if slopes is not None or prefix is not None or first is not None:
         _masks(n, q_heads, n_req, slopes, prefix, first)
     if out is None:
-        out = torch.empty(shape, dtype=q.dtype, device=q.device)
+        out = torch.empty(shape, dtype=q.dtype, device=q.device) if stream is None else _new(shape, q.dtype, q.device, stream)
         o_stride = (q_heads * d, d)
     else:
         if not out.is_cuda or out.shape != shape or out.dtype is not q.dtype or out.stride(2) != 1:
@@ -919,7 +935,7 @@ def fkv_page_attend_selected(pages, q, tables, kv_len, q_start, selected, max_ne
         if lse.numel() != n * q_heads:
             raise ValueError("lse has the wrong size")
     elif want_lse:
-        lse = torch.empty((n, q_heads), dtype=torch.float32, device=q.device)
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if stream is None else _new(q.shape[:2], torch.float32, q.device, stream)
     _here(*pages, q, tables, kv_len, q_start, selected, slopes, prefix, first, out, lse, workspace)
     att = fkv_attend_desc(n_req, n, max_new, max_kv, width, q_stride[0], q_stride[1], o_stride[0], o_stride[1], q_heads, kind,
                           d ** -0.5 if scale is None else scale, softcap, 1 if causal else 0, window, sinks)
@@ -929,7 +945,7 @@ def fkv_page_attend_selected(pages, q, tables, kv_len, q_start, selected, max_ne
     else:
         need = lib.fkv_page_attend_selected_workspace(ref(desc), ref(att), at[2])
         if need:
-            workspace = _scratch(need, q.device, stream)
+            workspace = _new(need, torch.uint8, q.device, stream)
     _check(lib.fkv_page_attend_selected(ref(desc), ref(att), at[2], selected.data_ptr(), pages[0].data_ptr(),
                                         pages[1].data_ptr(), pages[2].data_ptr(), q.data_ptr(), tables.data_ptr(),
                                         kv_len.data_ptr(), q_start.data_ptr(), _ptr(slopes), _ptr(prefix), _ptr(first),
@@ -973,7 +989,7 @@ def fkv_page_attend(pages, q, tables, kv_len, q_start, max_new: int, max_kv: int
     if slopes is not None or prefix is not None or first is not None:
         _masks(n, q_heads, n_req, slopes, prefix, first)
     if out is None:
-        out = torch.empty((n, q_heads, d), dtype=q.dtype, device=q.device)
+        out = torch.empty((n, q_heads, d), dtype=q.dtype, device=q.device) if stream is None else _new(q.shape, q.dtype, q.device, stream)
         o_stride = (q_heads * d, d)
     else:
         if not out.is_cuda or out.shape != q.shape or out.dtype is not q.dtype or out.stride(2) != 1:
@@ -984,7 +1000,7 @@ def fkv_page_attend(pages, q, tables, kv_len, q_start, max_new: int, max_kv: int
         if lse.numel() != n * q_heads:
             raise ValueError("lse has the wrong size")
     elif want_lse:
-        lse = torch.empty((n, q_heads), dtype=torch.float32, device=q.device)
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if stream is None else _new(q.shape[:2], torch.float32, q.device, stream)
     att = fkv_attend_desc(n_req, n, max_new, max_kv, width[1], q_stride[0], q_stride[1], o_stride[0], o_stride[1], q_heads, kind,
                           d ** -0.5 if scale is None else scale, softcap, 1 if causal else 0, window, sinks)
     ref = ctypes.byref
@@ -993,7 +1009,7 @@ def fkv_page_attend(pages, q, tables, kv_len, q_start, max_new: int, max_kv: int
     else:
         need = lib.fkv_page_attend_workspace(ref(desc), ref(att))
         if need:
-            workspace = _scratch(need, q.device, stream)
+            workspace = _new(need, torch.uint8, q.device, stream)
     _check(lib.fkv_page_attend(ref(desc), ref(att), pages[0].data_ptr(), pages[1].data_ptr(), pages[2].data_ptr(),
                                q.data_ptr(), tables.data_ptr(), kv_len.data_ptr(), q_start.data_ptr(), _ptr(slopes),
                                _ptr(prefix), _ptr(first), out.data_ptr(), _ptr(lse), _ptr(workspace),
@@ -1019,7 +1035,7 @@ def fkv_diag_mfma_loop(n_blocks: int, iters: int, out=None, random_operands: boo
     pseudo-random operand sets per lane, as real data would."""
     torch = _torch()
     if out is None:
-        out = torch.empty(1, dtype=torch.float32, device="cuda")
+        out = _new(1, torch.float32, "cuda", stream)
     _need(out, torch.float32, "out")
     _check(lib.fkv_diag_mfma_loop(n_blocks, iters, 1 if random_operands else 0, a, b, _ptr(out), _stream(stream)),
            "fkv_diag_mfma_loop")
