@@ -102,19 +102,21 @@ struct KeyLane {
 };
 
 // The codes of a page's keys before `begin`, as the lanes have the new rows: a lane its unit
-// of every `slots`-th token, kTurns tokens in flight, the first ones read before the new
-// scale is known.  (Reading them for each box, not only where the scale grows: a token of each
-// of 64 requests with half full pages of 64 x 128, 8 heads, 8.0 -> 9.3 us, of 4096 requests
-// 185 -> 208; 12 ragged prompts the same within 1%.)
+// of every `slots`-th token, kTurns tokens in flight, for a box the first ones read before
+// the new scale is known.  (Reading them for each box, not only where the scale grows: a token of each
+// of 64 requests with half full pages of 64 x 128, 8 heads, 8.0 -> 9.4 us, of 4096 requests
+// 185 -> 196; 12 ragged prompts 45.5 -> 47.1.)
 template <bool E4M3>
 struct OldKeys {
     static constexpr int kTurns = 4;
     uint8_t* codes;
     int d, begin;
+    bool ahead;
     uint2 lo[kTurns], hi[kTurns];
-    __device__ __forceinline__ OldKeys(uint8_t* codes_, int d_, int begin_, const KeyLane& mine) : codes(codes_), d(d_), begin(begin_)
+    __device__ __forceinline__ OldKeys(uint8_t* codes_, int d_, int begin_, bool ahead_, const KeyLane& mine)
+        : codes(codes_), d(d_), begin(begin_), ahead(ahead_)
     {
-        if (begin) fetch(0, mine);
+        if (begin && ahead) fetch(0, mine);
     }
     __device__ __forceinline__ void fetch(int k0, const KeyLane& mine)
     {
@@ -131,7 +133,7 @@ struct OldKeys {
     __device__ __forceinline__ void rescale(float grow, const KeyLane& mine, F each)
     {
         for (int k0 = 0; k0 < begin; k0 += kTurns * mine.slots) {
-            if (k0) fetch(k0, mine);
+            if (k0 || !ahead) fetch(k0, mine);
             uint32_t w[kTurns][4];
 #pragma unroll
             for (int t = 0; t < kTurns; ++t) w[t][0] = lo[t].x, w[t][1] = lo[t].y, w[t][2] = hi[t].x, w[t][3] = hi[t].y;
@@ -169,7 +171,7 @@ __device__ __forceinline__ void append_keys(const PageArgs& a, const AppendArgs&
     uint8_t* codes = a.k_codes + (page * a.heads + h) * (int64_t)a.page * d;
     const float was = begin ? *sp : 0.0f;
     const KeyLane mine(p, units);
-    OldKeys<E4M3> before(codes, d, begin, mine);
+    OldKeys<E4M3> before(codes, d, begin, p.boxes != nullptr, mine);
     const RowsFrom from(p.k, i, h);
     const int per_pass = mine.slots * T;
     const int n_pass = (len + per_pass - 1) / per_pass;

@@ -114,11 +114,6 @@ __device__ __forceinline__ int run_length(const PageArgs& a, int64_t i, int64_t 
     return len;
 }
 
-// The codes that a page holds before `begin`, as a wave brings them to a new scale: 16
-// bytes a lane and turn -- of the keys' rows as they lie, of the values 16 tokens of a
-// channel -- kOldTurns turns in flight, the first ones read before the new scale is known.
-// (One word a lane and turn, each turn waiting for its load: appending a token to each of
-// 64 pages of 64 tokens x 128 channels and 8 heads took 19.3 us, so 11.7.)
 template <bool E4M3>
 __device__ __forceinline__ uint32_t grown(uint32_t w, float grow)   // four codes
 {
@@ -129,54 +124,47 @@ __device__ __forceinline__ uint32_t grown(uint32_t w, float grow)   // four code
     return f32_to_codes<E4M3>(f);
 }
 
+// A wave brings the codes that a page holds before `begin` to a new scale, times `grow`: 16 bytes
+// a lane and turn -- of the keys' rows as they lie, of the values 16 tokens of a channel --
+// kOldTurns turns in flight.  (One word a lane and turn, each turn waiting for its load: a token
+// stored to each of 64 requests' pages of 64 tokens x 128 channels, 8 heads, whose scales grow
+// took 17.6 us with the launch that set them back, so 12.0; of 4096 requests 407, so 232.  With the
+// first ones read before the new scale is known 12.0 and 228, but where scales do not grow, as most
+// do not, 8192 requests then take 309 us in place of 282.)
+constexpr int kOldTurns = 4;
+
 template <bool E4M3>
-struct OldCodes {
-    static constexpr int kOldTurns = 4;
-    uint8_t* codes;
-    int d, begin, n, first;   // n: 16-byte parts; first: this lane's
-    bool values;
-    uint4 held[kOldTurns];
-    __device__ __forceinline__ OldCodes(uint8_t* codes_, int d_, bool values_, int begin_)
-        : codes(codes_), d(d_), begin(begin_), n(values_ ? (begin_ + 15) / 16 * d_ : begin_ * (d_ / 16)),
-          first(threadIdx.x & 63), values(values_)
-    {
-        if (n) fetch(0);
-    }
-    __device__ __forceinline__ void fetch(int t0)
-    {
+__device__ __forceinline__ void rescale_codes(uint8_t* codes, int d, bool values, int begin, float grow)
+{
+    const int n = values ? (begin + 15) / 16 * d : begin * (d / 16);   // 16-byte parts
+    for (int t0 = threadIdx.x & 63; t0 < n; t0 += kOldTurns * 64) {
+        uint4 held[kOldTurns];
 #pragma unroll
-        for (int t = 0; t < kOldTurns; ++t) held[t] = ((const uint4*)codes)[min(t0 + t * 64 + first, n - 1)];
-    }
-    // all of them times `grow`, back to where they were; of the value tokens that `begin` lies among, only those before it
-    __device__ __forceinline__ void rescale(float grow)
-    {
-        for (int t0 = 0; t0 < n; t0 += kOldTurns * 64) {
-            if (t0) fetch(t0);
+        for (int t = 0; t < kOldTurns; ++t) held[t] = ((const uint4*)codes)[min(t0 + t * 64, n - 1)];
 #pragma unroll
-            for (int t = 0; t < kOldTurns; ++t) {
-                const int at = t0 + t * 64 + first;
-                if (at >= n) break;
-                const uint4 w = make_uint4(grown<E4M3>(held[t].x, grow), grown<E4M3>(held[t].y, grow), grown<E4M3>(held[t].z, grow),
-                                           grown<E4M3>(held[t].w, grow));
-                uint8_t* to = codes + (int64_t)at * 16;
-                const int keep = values ? begin - at / d * 16 : 16;
-                if (keep >= 16) {
-                    *(uint4*)to = w;
-                    continue;
-                }
-                const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+        for (int t = 0; t < kOldTurns; ++t) {
+            const int at = t0 + t * 64;
+            if (at >= n) break;
+            const uint4 w = make_uint4(grown<E4M3>(held[t].x, grow), grown<E4M3>(held[t].y, grow), grown<E4M3>(held[t].z, grow),
+                                       grown<E4M3>(held[t].w, grow));
+            uint8_t* to = codes + (int64_t)at * 16;
+            const int keep = values ? begin - at / d * 16 : 16;   // of the value tokens that `begin` lies among, only those before it
+            if (keep >= 16) {
+                *(uint4*)to = w;
+                continue;
+            }
+            const uint32_t words[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    if (keep >= 4 * q + 4) *(uint32_t*)(to + 4 * q) = words[q];
-                    else
+            for (int q = 0; q < 4; ++q) {
+                if (keep >= 4 * q + 4) *(uint32_t*)(to + 4 * q) = words[q];
+                else
 #pragma unroll
-                        for (int e = 0; e < 3; ++e)
-                            if (keep > 4 * q + e) to[4 * q + e] = (uint8_t)(words[q] >> (8 * e));
-                }
+                    for (int e = 0; e < 3; ++e)
+                        if (keep > 4 * q + e) to[4 * q + e] = (uint8_t)(words[q] >> (8 * e));
             }
         }
     }
-};
+}
 
 // A wave writes a run of one head's keys or values: len rows from row i on, to the
 // tokens begin .. of a page.  Up to 64 columns of it (a page of 64 tokens x 128
@@ -203,7 +191,6 @@ __device__ __forceinline__ void store_run(const PageArgs& a, const Rows& rows, b
     float* sp = (float*)&a.scales[page * a.heads + h] + (values ? 1 : 0);
     uint8_t* codes = (values ? a.v_codes : a.k_codes) + (page * a.heads + h) * (int64_t)a.page * a.d;
     const float was = begin ? *sp : 0.0f;
-    OldCodes<E4M3> before(codes, a.d, values, begin);
     // this lane's tokens of a column: offsets first .. first+3 in the page
     auto place = [&](int col, int& grp, int& chunk) {
         grp = g0 + (int)((uint32_t)col / chunks);
@@ -264,7 +251,7 @@ __device__ __forceinline__ void store_run(const PageArgs& a, const Rows& rows, b
     float s = largest < 0x1p-90f ? 0.0f : largest * (1.0f / kLargest);
     if (begin) {
         s = fmaxf(s, was);
-        if (s > was) before.rescale(was / s);
+        if (s > was) rescale_codes<E4M3>(codes, a.d, values, begin, was / s);
     }
     wave_sync();   // every lane has read the scale, and words of which others write bytes
     if (lane == 0) *sp = s;
