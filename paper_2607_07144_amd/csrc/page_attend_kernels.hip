@@ -587,6 +587,17 @@ __global__ __launch_bounds__(64 * W, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) void atte
                 vb[k] = __builtin_amdgcn_logf(v) - m0 + (SCORES == CAPPED ? cap2 : 0.0f);
                 vinv[k] = __builtin_amdgcn_rcpf(v);
             }
+            // the product of a large score is rounded before the maximum is taken off, as it was for that: exact, it may be far above
+            // (a capped one is no more than 2^8)
+            if (SCORES != CAPPED && __any(fabsf(m0) > 0x1p20f)) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    const int part = ONE ? 0 : i >> 3;
+                    x[i] = (SCORES == PLAIN ? x[i] * c[part] : x[i]) - m0;
+                }
+#pragma unroll
+                for (int k = 0; k < G; ++k) c[k] = 1.0f, vb[k] = -__builtin_amdgcn_logf(vinv[k]);
+            }
             auto weights = [&](int k) {   // of keys 16k .. 16k+15, this lane's half of them
                 const int part = ONE ? 0 : k;
                 float sum = 0.0f;

@@ -78,9 +78,8 @@ def test_keys_near_the_types_ends(fkv, codes, page, group, d, lengths, how):
     assert top.max() < 1.9e34 and ((lse - top).abs() <= err + top.abs() * 2.0 ** -13)[sure].all()
 
 
-def best(pool, tables, kv, starts, q, selected, scale):
+def best(pool, tables, kv, starts, q, selected, scale, gap=2.0 ** 20):
     """The value row of each row's best key, its score and that one's error, and whether the next one is far enough below."""
-
     n_pages, heads, page, d = pool[0].shape
     kk, vv = pages.values(*pool)
     n, q_heads, _ = q.shape
@@ -103,7 +102,7 @@ def best(pool, tables, kv, starts, q, selected, scale):
                     err = sc * 255 * x.abs().sum() * scale * (d + 8) * 2.0 ** -24 + z.abs() * 2.0 ** -20
                     o = z.argsort(descending=True)
                     want[i, hq], top[i, hq], off[i, hq] = vs[o[0]], z[o[0]], err[o[0]]
-                    sure[i, hq] = len(o) == 1 or bool((z[o[0]] - z[o[1:]] > err[o[0]] + err[o[1:]] + 2.0 ** 20).all())
+                    sure[i, hq] = len(o) == 1 or bool((z[o[0]] - z[o[1:]] > err[o[0]] + err[o[1:]] + gap).all())
     return want, top, off, sure
 
 
