@@ -344,7 +344,9 @@ int fkv_kmeans_update_noalloc(const fkv_rvq_desc* desc, const uint16_t* x_f16, u
  *       values  v_codes u8 [n_pages][heads][page/16][d][16]  (16-token groups,
  *               token minor, so that a value channel's tokens are contiguous)
  *       scales  f32 [n_pages][heads][2]: one for the keys, one for the values
- *               of that page and head; an element is code * scale
+ *               of that page and head; an element is code * scale.  They are finite
+ *               and not negative, as the calls write them; of others, what attention
+ *               gives rows that see a key of the page is undefined
  *     k_codes and v_codes 16-byte aligned, scales 8-byte aligned.
  *   - format: FKV_PAGE_INT8, codes -127..127 (largest code q = 127), or
  *     FKV_PAGE_E4M3, 8-bit floats with 4 exponent and 3 mantissa bits and no
@@ -581,7 +583,7 @@ int fkv_page_attend(const fkv_page_desc* desc, const fkv_attend_desc* attend, co
  * ceil(code / 4) (8-bit floats), and scale its key scale.  A product that is a NaN, and
  * any of a table entry that is no page of the pool, counts as -infinity.
  *   boxes      device [n_pages][heads][2][d] codes, 16-byte aligned, as
- *              fkv_page_append keeps them; scales: the pages'
+ *              fkv_page_append writes them; scales: the pages', of any value
  *   q          rows [n_tokens][q_heads][d] with the strides given, 16-byte aligned
  *   tables, kv_len, q_start, max_new, max_kv, max_pages   as for fkv_page_attend
  *   selected   device out int32 [n_tokens][heads][n_select]: columns of the token's
@@ -589,6 +591,8 @@ int fkv_page_attend(const fkv_page_desc* desc, const fkv_attend_desc* attend, co
  *              leaves unwritten are left as they were
  *   workspace  device scratch of fkv_page_select_workspace() bytes, 16-byte aligned;
  *              null when that is 0.  Calls that may run at the same time need one each
+ * A window, documents or a prefix of the attention that follows play no part: pages
+ * that they hide may be listed, and pages that only a prefix shows are not.
  * n_select: 1 .. 2^20, keep_first + keep_last at most n_select.  FKV_ERR_UNSUPPORTED
  * for more blocks than a launch holds (the fewer of 2 n_tokens and n_req * max_new,
  * times heads, beyond 2^31). */

@@ -376,10 +376,10 @@ __device__ __forceinline__ void turn_queries(const PageArgs& a, const AppendArgs
 
 // A wave a window of rows and head, of K or of V, then waves for the query rows.  What
 // bounds many rows is memory, where the K and V waves do not keep enough loads under way:
-// 32,768 tokens, 8 KV heads and 32 query heads of 128, 178 us (756 MB, 4.2 TB/s), 107 of them
-// for the K/V rows alone and the store without rotation and boxes 49.  (With the two kinds of
-// blocks in turn 183; with a block of four waves a run of keys 191, and a token of each of
-// 1024 requests 94 us instead of 53.)
+// 32,768 tokens, 8 KV heads and 32 query heads of 128, 182 us (756 MB, 4.2 TB/s), 106 of them
+// for the K/V rows alone and the store without rotation and boxes 49.  (Tried where it took 178:
+// the two kinds of blocks in turn 183; a block of four waves a run of keys 191, and a token of
+// each of 1024 requests 94 us instead of 53.)
 template <bool E4M3, bool BF16>
 __global__ __launch_bounds__(kThreads, 3) void page_append_kernel(PageArgs a, AppendArgs p)
 {
@@ -454,7 +454,7 @@ extern "C" int fkv_page_append(const fkv_page_desc* desc, const fkv_rotate_desc*
     p.pairs = rotate && rotate->pairing == FKV_ROTATE_PAIRS;
     // As many rows a wave as leave four thousand waves, up to a page's worth: a wave writes the runs that begin among them one
     // by one, but waves of rows in which none begins hold up the others.  One row, and so many (us): 12 prompts of 2936 rows in
-    // all, 8 heads of 80, 51 and 25; a token of each of 1024 requests, 8 heads of 128, 54 and 53; of 4096 288 and 246.
+    // all, 8 heads of 80, 51 and 29; a token of each of 1024 requests, 8 heads of 128, 59 and 60; of 64 requests 32 tokens 56 and 35.
     const int64_t row_heads = n_tokens * desc->heads;
     p.window = (int32_t)std::min((int64_t)std::min(desc->page, 64), std::max((int64_t)1, (row_heads + 2047) / 2048));
     p.store_items = (n_tokens + p.window - 1) / p.window * desc->heads * 2;

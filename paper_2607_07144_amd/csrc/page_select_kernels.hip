@@ -269,8 +269,8 @@ __device__ __forceinline__ void score_block(const SelectArgs& a, const Request& 
 }
 
 // Many rows or many pages: the scores go to the workspace (16 contexts of 2048 pages, 8 heads
-// of 128: 67 MB of boxes, 17.5 us, 3.8 TB/s; a chunk's rows over 512 pages: 52 us, the vector
-// unit's, that turns sums to scores and joins the heads).  A block R row tiles, a wave of it
+// of 128: 67 MB of boxes, 19.5 us, 3.4 TB/s; a chunk's rows over 512 pages: 57 us, the vector
+// unit 76% busy, that turns sums to scores and joins the heads, the matrix cores 13%).  A block R row tiles, a wave of it
 // a quarter of the block's page tiles.
 template <bool E4M3, int NC, int R, bool WIDE>
 __global__ __launch_bounds__(kThreads, R == 1 || NC == 1 ? 4 : NC == 2 ? 3 : 2) void page_score_kernel(SelectArgs a)
@@ -619,9 +619,9 @@ __global__ __launch_bounds__(kWideThreads) void page_select_wide_kernel(SelectAr
 
 // A tile is four groups of 16 keys of the listed pages; its order of work is that of
 // few_keys.  Single tokens' lists come from memory (16 requests with 64 pages of 64 x 128, 8
-// heads: 135 MB in 30 us, 4.5 TB/s).  Lists that many tokens share come from the caches, and
-// what bounds them is the vector unit (a chunk of 4096 tokens with 16 pages each: 480 us, 0.14
-// PFLOP/s, the unit 85% busy; 192 of a tile's 290 instructions widen int8 codes to binary16, once for each token:
+// heads: 135 MB in 26 us, 5.1 TB/s).  Lists that many tokens share come from the caches, and
+// what bounds them is the vector unit (a chunk of 4096 tokens with 16 pages each: 500 us, 0.14
+// PFLOP/s, the unit 89% busy; 192 of a tile's some 325 instructions widen int8 codes to binary16, once for each token:
 // lists differ): so a weight with its value scale is one power of two,
 // 2^(s c - m + log2 v), as in the kernel for many rows: v = vs 2^8 / vr is held at 2^-40 from
 // below, and a sum over v is what l wants.
