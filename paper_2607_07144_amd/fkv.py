@@ -187,6 +187,13 @@ def _here(*tensors) -> None:
             raise ValueError("tensor on device %d, the current device is %d" % (t.get_device(), device))
 
 
+def _on(stream, device):
+    """torch's stream of a raw handle, to be current while a call makes or clears tensors (torch takes the handle 0 of the
+    default stream for a new stream's)."""
+    cuda = (_TORCH or _torch()).cuda
+    return cuda.stream(cuda.ExternalStream(int(stream), device=device) if stream else cuda.default_stream(device))
+
+
 def _new(shape, dtype, device, stream, zero=False):
     """A tensor that a call makes, from the memory of the stream that it runs on, as its kernels write it there: of another
     stream's memory, that one's work on what it held before might not be done.  (What reads a result on a third stream
@@ -196,17 +203,16 @@ def _new(shape, dtype, device, stream, zero=False):
     make = torch.zeros if zero else torch.empty
     if stream is None:
         return make(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=device)):
+    with _on(stream, device):
         return make(shape, dtype=dtype, device=device)
 
 
 def _clear(t, stream) -> None:
     """Zeros, on the stream that the call runs on."""
-    torch = _TORCH or _torch()
     if stream is None:
         t.zero_()
         return
-    with torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=t.device)):
+    with _on(stream, t.device):
         t.zero_()
 
 

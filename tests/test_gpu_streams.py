@@ -103,3 +103,24 @@ def test_what_a_call_clears_it_clears_on_its_stream(fkv):
     assert hit(got[0]) == hit(hits.cpu())
     assert torch.equal(got[3], want.cpu()) and torch.equal(got[4], want.cpu())
     assert np.array_equal(got[5].view(torch.int16), one.cpu().view(torch.int16)) and np.array_equal(got[6].view(torch.int16), one.cpu().view(torch.int16))
+
+
+def test_the_default_streams_handle(fkv):
+    """0 is the default stream's handle, whatever stream is current."""
+    ns, T, d, S, K = 4, 300, 64, 3, 32
+    x, books, sb = rows(ns, T, d), rows(2, S, K, d, seed=1), dev([0, 1, 1, 0])
+    pool, slots = fkv.fkv_pages(2, 16, 2, 64), torch.arange(4, device="cuda")
+    side = torch.cuda.Stream()
+    sym, _ = fkv.fkv_rvq_assign(x, books, sb, 0, T)
+    one, two = books.clone(), books.clone()
+    _, want = fkv.fkv_kmeans_step(x, one, sb, 0, T, sym, 1)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        work = busy()
+        k, v = fkv.fkv_page_load(pool, slots, stream=0)
+        _, counts = fkv.fkv_kmeans_step(x, two, sb, 0, T, sym, 1, stream=torch.cuda.default_stream().cuda_stream)
+    torch.cuda.synchronize()
+    del work
+    assert torch.cuda.default_stream().cuda_stream == 0
+    assert stream_of(k) == stream_of(v) == stream_of(counts) == 0 != side.cuda_stream
+    assert torch.equal(counts, want) and torch.equal(one.view(torch.int16), two.view(torch.int16))
