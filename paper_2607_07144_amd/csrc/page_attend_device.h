@@ -20,7 +20,8 @@ constexpr int kFewRows = 16;       // rows of the kernel for few rows
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr float kTop = 256.0f;     // the weight of a key at the reference maximum, and
-constexpr float kSlack = 6.0f;     // how far scores may pass that before it moves: weights stay below 2^14
+constexpr float kSlack = 6.0f;     // how far scores may pass that before it moves: weights stay below 2^14 (of large scores the difference
+                                   // is exact, and the sum of both might be rounded up to the score)
 constexpr float kLeast = 0x1p-100f;
 // Sums of weights times values that are to be joined with others are kept times 2^-30: bfloat16 values may be near
 // fp32's end, where a sum of a few of them is beyond it and their mean is not (2^24 keys of weights up to 2^6).
@@ -447,7 +448,7 @@ __device__ __forceinline__ void few_update(const AttendArgs& a, const Request& r
     for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
     const float vtop = top > -__builtin_inff() ? sc.y : 0.0f;   // of a group of which the row sees a key
     top = rows_max(top);
-    if (__any(top > st.m + kSlack || vtop > st.vref)) {
+    if (__any(top - st.m > kSlack || vtop > st.vref)) {
         const float vnew = rows_max(fmaxf(st.vref, vtop));
         const float mnew = fmaxf(st.m, top);
         const float shrink = mnew == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(st.m - mnew);

@@ -568,7 +568,7 @@ __global__ __launch_bounds__(64 * W, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) void atte
                 for (int k = 0; k < G; ++k) vtop = fmaxf(vtop, tops[k] != kHidden ? sn[k].y : -1.0f);
                 vtop = halves_max(vtop);
             }
-            if (__any(top > m + kSlack || vtop > vref)) {
+            if (__any(top - m > kSlack || vtop > vref)) {
                 const float mnew = fmaxf(m, top), vnew = fmaxf(vref, vtop);
                 const float shrink = mnew == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m - mnew);
                 l *= shrink;

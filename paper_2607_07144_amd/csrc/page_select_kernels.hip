@@ -752,7 +752,7 @@ __device__ __forceinline__ void listed_update(const AttendArgs& a, const Request
     for (int i = 1; i < N; ++i) top = __builtin_elementwise_maximum(top, x[i]);
     const float vtop = top > -__builtin_inff() ? sc.y : 0.0f;   // of a group of which the column sees a key
     top = rows_max(top * c);
-    if (__any(top > st.m + kSlack || vtop > st.vref)) {
+    if (__any(top - st.m > kSlack || vtop > st.vref)) {
         const float vnew = rows_max(fmaxf(st.vref, vtop));
         const float mnew = fmaxf(st.m, top);
         const float shrink = mnew == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(st.m - mnew);

@@ -35,3 +35,32 @@ def test_large_scores(fkv, codes, page, heads, group, d, lengths, how, power):
     half = torch.finfo(F16).eps / 2
     assert ((got - want).abs() <= (half + 2.0 ** -11 + 2.0 ** -18) * want.abs() + 2.0 ** -25)[sure].all()
     assert ((lse - top).abs() <= err + top.abs() * 2.0 ** -12 + 30)[sure].all()
+
+
+@pytest.mark.parametrize("listed", [False, True])
+@pytest.mark.parametrize("heads,group,new", [(1, 2, 1), (2, 4, 40), (16, 3, 130), (16, 5, 130)])
+@pytest.mark.parametrize("codes", [INT8, E4M3])
+@pytest.mark.parametrize("level", [2.0 ** 24 * 1.5, 2.0 ** 25 * 1.5, 2.0 ** 26 * 1.5])
+def test_tiles_a_rounding_apart(fkv, listed, heads, group, new, codes, level):
+    """Scores of 2^24 and more, where fp32's steps are 2, 4 and 8, the second tile's 8 above the first's in base 2: all values
+    are alike, so the result is that value."""
+    page, d, kv = 64, 16, 320
+    k, v = torch.zeros((5, heads, page, d)), torch.full((5, heads, page // 16, d, 16), 96.0)
+    k[:, :, :, 0] = 96.0
+    k[1:, :, :, 1] = 1.0
+    scales = torch.tensor([32.0, 0.25]).repeat(5, heads, 1)
+    q = torch.zeros((new, heads * group, d))
+    q[:, :, 0], q[:, :, 1] = level / (96 * 32), 0.25
+    assert q.half().float().equal(q)
+    pool = (k.to(codes).cuda(), v.to(codes).cuda(), scales.cuda())
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")      # noqa: E731
+    args = (pool, q.half().cuda(), i32([[0, 1, 2, 3, 4]]), i32([kv]), i32([0, new]))
+    how = dict(scale=0.6931472, causal=False, want_lse=True)
+    if listed:
+        every = torch.arange(5, dtype=torch.int32, device="cuda").repeat(new, heads, 1)
+        out, lse = fkv.fkv_page_attend_selected(*args, every, new, kv, **how)
+    else:
+        out, lse = fkv.fkv_page_attend(*args, new, kv, **how)
+    # weights of 11 bits, their sums and what binary16 holds of 24
+    assert ((out.cpu().double() - 24).abs() <= 24 * (2.0 ** -11 + 2.0 ** -11 + 2.0 ** -16)).all()
+    assert torch.isfinite(lse).all()
