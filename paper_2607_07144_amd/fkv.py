@@ -197,7 +197,7 @@ def _on(stream, device):
 def _new(shape, dtype, device, stream, zero=False):
     """A tensor that a call makes, from the memory of the stream that it runs on, as its kernels write it there: of another
     stream's memory, that one's work on what it held before might not be done.  (What reads a result on a third stream
-    waits for it, and keeps it until it is done, as with torch.cuda.stream.  The attention calls make theirs in place where no
+    waits for it, and keeps it until it is done, as with torch.cuda.stream.  The paged calls make theirs in place where no
     stream is given: a small call's time is such lines.)"""
     torch = _TORCH or _torch()
     make = torch.zeros if zero else torch.empty
@@ -703,7 +703,8 @@ def fkv_page_plan(page: int, kv_len, new_len, free_pages, head, tables, n_tokens
     # the call as offsets, and the tensors are made while the kernel runs
     r4 = (n_req + 3) // 4
     sizes = (2 * n_tokens, n_tokens, n_req + 1, n_req, 1, 1, r4)
-    buf = _new(3 * n_tokens + 2 * n_req + 3 + r4, i32, kv_len.device, stream)
+    size = 3 * n_tokens + 2 * n_req + 3 + r4
+    buf = torch.empty(size, dtype=i32, device=kv_len.device) if stream is None else _new(size, i32, kv_len.device, stream)
     at = buf.data_ptr()
     rows = at + 12 * n_tokens          # q_start
     ends = rows + 4 * n_req + 4        # kv_end
@@ -820,8 +821,11 @@ def fkv_page_load(pages, slots, dtype=None, k=None, v=None, stream=None):
         at = slots.shape
         shape = (at[0], heads, d) if len(at) == 1 else (at[0], heads, at[1], d)
         dtype = dtype or torch.float16
-        k = _new(shape, dtype, slots.device, stream)
-        v = _new(shape, dtype, slots.device, stream)
+        if stream is None:
+            k = torch.empty(shape, dtype=dtype, device=slots.device)
+            v = torch.empty(shape, dtype=dtype, device=slots.device)
+        else:
+            k, v = (_new(shape, dtype, slots.device, stream) for _ in "kv")
         rk = rv = _rows(k, slots, heads, d, "k")
     else:
         rk = _rows(k, slots, heads, d, "k") if k is not None else None
@@ -941,7 +945,8 @@ def fkv_page_attend_selected(pages, q, tables, kv_len, q_start, selected, max_ne
         if lse.numel() != n * q_heads:
             raise ValueError("lse has the wrong size")
     elif want_lse:
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if stream is None else _new(q.shape[:2], torch.float32, q.device, stream)
+        size = (n, q_heads)   # (a slice of q's shape takes torch half a microsecond)
+        lse = torch.empty(size, dtype=torch.float32, device=q.device) if stream is None else _new(size, torch.float32, q.device, stream)
     _here(*pages, q, tables, kv_len, q_start, selected, slopes, prefix, first, out, lse, workspace)
     att = fkv_attend_desc(n_req, n, max_new, max_kv, width, q_stride[0], q_stride[1], o_stride[0], o_stride[1], q_heads, kind,
                           d ** -0.5 if scale is None else scale, softcap, 1 if causal else 0, window, sinks)
@@ -1006,7 +1011,8 @@ def fkv_page_attend(pages, q, tables, kv_len, q_start, max_new: int, max_kv: int
         if lse.numel() != n * q_heads:
             raise ValueError("lse has the wrong size")
     elif want_lse:
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if stream is None else _new(q.shape[:2], torch.float32, q.device, stream)
+        size = (n, q_heads)   # (a slice of q's shape takes torch half a microsecond)
+        lse = torch.empty(size, dtype=torch.float32, device=q.device) if stream is None else _new(size, torch.float32, q.device, stream)
     att = fkv_attend_desc(n_req, n, max_new, max_kv, width[1], q_stride[0], q_stride[1], o_stride[0], o_stride[1], q_heads, kind,
                           d ** -0.5 if scale is None else scale, softcap, 1 if causal else 0, window, sinks)
     ref = ctypes.byref
